@@ -313,6 +313,99 @@ carnator_status carnator_seed_expansion(const void* Q, const void* K, const floa
                                         void* ws, size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
+ * What stands around a layer's attention: layer norm with modulation, the projections' matrix product with its
+ * epilogue, and the gradients of both.  The paper has no counterpart for these calls; they are what a transformer
+ * layer does with its tokens between two attention calls, on the same conventions (strides, streams, errors).
+ *
+ * Layer norm, for every row (b, h, n) of C channels:
+ *   mu = sum x / C,  rstd = (sum (x - mu)^2 / C + eps)^-1/2,  xh = (x - mu) rstd,
+ *   y = (xh weight + bias) (1 + scale_b) + shift_b          statistics and sums in fp32
+ *   X, Y, dY, dX  device, of x_dtype (X, dX) and y_dtype (Y, dY), [B,H,N,C] with the strides of `shape` (H = 1: whole
+ *          token rows; H heads of C channels: the norm of Q and K before attention, read from and written to the
+ *          strided views of a fused projection's output).  Strides are multiples of 16 bytes, base pointers 16-byte
+ *          aligned; the channels are contiguous.  Inputs may have a stride of 0; rows of an output do not overlap.
+ *          Y may be X and dX may be X or dY (same type and strides).
+ *   weight, bias   device, [C] of weight_dtype, or NULL (1, 0);  shift, scale  device, [B,C] of mod_dtype with the batch
+ *          strides of `shape`, or NULL (0).  These are aligned to their type only.
+ *   mean, rstd     device, fp32 [B,H,N] contiguous; written by the forward call if given, read by the backward call
+ * carnator_layer_norm_backward: with a = weight (1 + scale_b), g = dy a:
+ *   dX = rstd (g - mean(g) - xh mean(g xh));  dweight = sum (1 + scale_b) dy xh,  dbias = sum (1 + scale_b) dy, over all rows;
+ *   dscale_b = sum dy (xh weight + bias),  dshift_b = sum dy, over the rows of entry b
+ *   dweight, dbias  device, fp32 [C];  dshift, dscale  device, fp32 [B,C] contiguous; any of them NULL: not wanted
+ *   ws     device workspace, 256-byte aligned, >= carnator_layer_norm_backward_workspace_bytes (partial sums)
+ * Limits: C <= 16384, B <= 65535, H N <= 2^30.
+ * ------------------------------------------------------------------------ */
+typedef struct carnator_norm_shape {
+    int32_t B, H, N, C;
+    int64_t x_stride[3], y_stride[3];       /* element strides of (batch, head, token) */
+    int64_t dy_stride[3], dx_stride[3];     /* used by the backward call only, which does not use y_stride */
+    int64_t shift_stride, scale_stride;     /* element strides of the batch axis; 0: one row for all entries */
+    int32_t x_dtype, y_dtype, weight_dtype, mod_dtype;     /* CARNATOR_DTYPE_* */
+    float   eps;                            /* >= 0 */
+} carnator_norm_shape;
+
+carnator_status carnator_layer_norm(const void* X, const void* weight, const void* bias, const void* shift, const void* scale,
+                                    const carnator_norm_shape* shape, void* Y, float* mean_opt, float* rstd_opt, void* stream);
+
+size_t carnator_layer_norm_backward_workspace_bytes(const carnator_norm_shape* shape);
+
+carnator_status carnator_layer_norm_backward(const void* dY, const void* X, const float* mean, const float* rstd,
+                                             const void* weight, const void* bias, const void* scale,
+                                             const carnator_norm_shape* shape, void* dX,
+                                             float* dweight_opt, float* dbias_opt, float* dshift_opt, float* dscale_opt,
+                                             void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Matrix product with bias, activation, gate and residual in its epilogue, for every row (b, n):
+ *   z = x W^T + bias,   y = residual + gate_b act(z)
+ *   X, W   device, bf16 [B,N,in_features] and [out_features,in_features];  W is a plain Linear weight, w_stride its row stride
+ *   bias   device, [out_features] of bias_dtype, or NULL;  gate  device, [B,out_features] of gate_dtype, or NULL (1)
+ *   residual   device, of y_dtype, [B,N,out_features], or NULL (0); may be Y (same strides)
+ *   Y      device, of y_dtype;  Z  device, bf16, or NULL: the pre-activation, which the backward call wants
+ *   ws     device workspace, 256-byte aligned, >= carnator_linear_workspace_bytes (the status header)
+ * Strides are multiples of 16 bytes, base pointers 16-byte aligned, features contiguous; bias and gate are aligned to
+ * their type only.  Any in_features and out_features: a row's features need not fill its stride, and nothing outside
+ * them is read or written.  The products are bf16 x bf16 with fp32 sums; bias, activation, gate and residual are applied
+ * to the unrounded sum and y is rounded once.
+ * carnator_linear_backward:  dz = dy gate_b act'(z);
+ *   dX = dz W,  dW = dz^T x  (bf16, dz rounded to bf16 as their operand);
+ *   dbias = sum of dz over all rows,  dgate_b = sum of dy act(z) over the rows of entry b  (fp32, from unrounded terms).
+ *   The residual's gradient is dy itself.
+ *   Z      may be NULL if the activation is CARNATOR_ACT_NONE and dgate is not wanted
+ *   dX     [B,N,in_features] with dx_stride, or NULL;  dW  [out_features,in_features] with row stride dw_stride, or NULL
+ *   dbias  fp32 [out_features] or NULL;  dgate  fp32 [B,out_features] contiguous or NULL (wants gate)
+ *   ws     device workspace, >= carnator_linear_backward_workspace_bytes (header, dz, partial sums)
+ * Up to 16 rows in all run on a kernel that streams W once through the registers of mma.sync; more rows on tcgen05 with
+ * bounded waits, whose status carnator_query_status(ws) returns.
+ * Limits: B N, in_features, out_features <= 2^30, B <= 65535.
+ * ------------------------------------------------------------------------ */
+enum { CARNATOR_ACT_NONE = 0, CARNATOR_ACT_GELU_TANH = 1, CARNATOR_ACT_GELU = 2, CARNATOR_ACT_SILU = 3 };
+
+typedef struct carnator_linear_shape {
+    int32_t B, N, in_features, out_features;
+    int64_t x_stride[2], y_stride[2];       /* element strides of (batch, token); y_stride is also dY's */
+    int64_t residual_stride[2], z_stride[2];
+    int64_t dx_stride[2];
+    int64_t w_stride, dw_stride;            /* row strides */
+    int64_t gate_stride;                    /* batch stride; 0: one row for all entries */
+    int32_t activation;                     /* CARNATOR_ACT_* */
+    int32_t y_dtype, bias_dtype, gate_dtype;       /* CARNATOR_DTYPE_*; y_dtype is also the residual's and dY's */
+} carnator_linear_shape;
+
+size_t carnator_linear_workspace_bytes(const carnator_linear_shape* shape);
+
+carnator_status carnator_linear(const void* X, const void* W, const void* bias, const void* gate, const void* residual,
+                                const carnator_linear_shape* shape, void* Y, void* Z_opt,
+                                void* ws, size_t ws_bytes, void* stream);
+
+size_t carnator_linear_backward_workspace_bytes(const carnator_linear_shape* shape);
+
+carnator_status carnator_linear_backward(const void* dY, const void* X, const void* W, const void* Z, const void* gate,
+                                         const carnator_linear_shape* shape, void* dX_opt, void* dW_opt,
+                                         float* dbias_opt, float* dgate_opt,
+                                         void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
  * Host-side scalars of the reuse-validity gate and of its offline risk certificate.  No GPU work; all
  * pointers are HOST pointers; invalid arguments give NaN (0 for the gate).
  *

@@ -10,7 +10,7 @@ from __future__ import annotations
 import ctypes
 import math
 import os
-from typing import Optional
+from typing import NamedTuple, Optional
 
 _PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG_DIR, "libcarnator.so")
@@ -31,6 +31,8 @@ EXPORTS = [
     "carnator_regions_workspace_bytes", "carnator_build_regions", "carnator_fuse_latents",
     "carnator_region_block_flags", "carnator_sparse_attn_region",
     "carnator_seed_workspace_bytes", "carnator_seed_expansion",
+    "carnator_layer_norm", "carnator_layer_norm_backward_workspace_bytes", "carnator_layer_norm_backward",
+    "carnator_linear_workspace_bytes", "carnator_linear", "carnator_linear_backward_workspace_bytes", "carnator_linear_backward",
     "carnator_delta_e00", "carnator_context_discrepancy", "carnator_size_discrepancy", "carnator_shape_discrepancy",
     "carnator_compatibility_gate", "carnator_clopper_pearson_upper",
     "carnator_query_status", "carnator_selftest_wait_timeout", "carnator_debug_set_builder_path", "carnator_status_string", "carnator_last_cuda_error",
@@ -64,6 +66,30 @@ class BuildParams(ctypes.Structure):
         ("mode", ctypes.c_int32), ("keep_ratio", ctypes.c_float), ("mass", ctypes.c_float),
         ("window_frames", ctypes.c_int32), ("text_dense", ctypes.c_int32),
         ("count_includes_forced", ctypes.c_int32),
+    ]
+
+
+class NormShape(ctypes.Structure):
+    """Mirror of carnator_norm_shape."""
+    _fields_ = [
+        ("B", ctypes.c_int32), ("H", ctypes.c_int32), ("N", ctypes.c_int32), ("C", ctypes.c_int32),
+        ("x_stride", ctypes.c_int64 * 3), ("y_stride", ctypes.c_int64 * 3),
+        ("dy_stride", ctypes.c_int64 * 3), ("dx_stride", ctypes.c_int64 * 3),
+        ("shift_stride", ctypes.c_int64), ("scale_stride", ctypes.c_int64),
+        ("x_dtype", ctypes.c_int32), ("y_dtype", ctypes.c_int32), ("weight_dtype", ctypes.c_int32), ("mod_dtype", ctypes.c_int32),
+        ("eps", ctypes.c_float),
+    ]
+
+
+class LinearShape(ctypes.Structure):
+    """Mirror of carnator_linear_shape."""
+    _fields_ = [
+        ("B", ctypes.c_int32), ("N", ctypes.c_int32), ("in_features", ctypes.c_int32), ("out_features", ctypes.c_int32),
+        ("x_stride", ctypes.c_int64 * 2), ("y_stride", ctypes.c_int64 * 2),
+        ("residual_stride", ctypes.c_int64 * 2), ("z_stride", ctypes.c_int64 * 2), ("dx_stride", ctypes.c_int64 * 2),
+        ("w_stride", ctypes.c_int64), ("dw_stride", ctypes.c_int64), ("gate_stride", ctypes.c_int64),
+        ("activation", ctypes.c_int32),
+        ("y_dtype", ctypes.c_int32), ("bias_dtype", ctypes.c_int32), ("gate_dtype", ctypes.c_int32),
     ]
 
 
@@ -136,6 +162,21 @@ def lib() -> ctypes.CDLL:
     L.carnator_seed_workspace_bytes.argtypes = [ps]
     L.carnator_seed_expansion.restype = ctypes.c_int
     L.carnator_seed_expansion.argtypes = [vp, vp, vp, vp, ctypes.c_int32, ctypes.c_int32, ps, vp, vp, vp, sz, vp]
+    pn, pl = ctypes.POINTER(NormShape), ctypes.POINTER(LinearShape)
+    L.carnator_layer_norm.restype = ctypes.c_int
+    L.carnator_layer_norm.argtypes = [vp, vp, vp, vp, vp, pn, vp, vp, vp, vp]
+    L.carnator_layer_norm_backward_workspace_bytes.restype = sz
+    L.carnator_layer_norm_backward_workspace_bytes.argtypes = [pn]
+    L.carnator_layer_norm_backward.restype = ctypes.c_int
+    L.carnator_layer_norm_backward.argtypes = [vp, vp, vp, vp, vp, vp, vp, pn, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.carnator_linear_workspace_bytes.restype = sz
+    L.carnator_linear_workspace_bytes.argtypes = [pl]
+    L.carnator_linear.restype = ctypes.c_int
+    L.carnator_linear.argtypes = [vp, vp, vp, vp, vp, pl, vp, vp, vp, sz, vp]
+    L.carnator_linear_backward_workspace_bytes.restype = sz
+    L.carnator_linear_backward_workspace_bytes.argtypes = [pl]
+    L.carnator_linear_backward.restype = ctypes.c_int
+    L.carnator_linear_backward.argtypes = [vp, vp, vp, vp, vp, pl, vp, vp, vp, vp, vp, sz, vp]
     dbl, pd = ctypes.c_double, ctypes.POINTER(ctypes.c_double)
     L.carnator_delta_e00.restype = dbl
     L.carnator_delta_e00.argtypes = [pd, pd]
@@ -455,6 +496,274 @@ def seed_expansion(Q, K, LSE, seeds, n_pos: int, n_neg: int, shape: Shape, per_h
                                        _ptr(per_head), _ptr(out), _ptr(ws), ws.numel(), _stream(stream))
     _check(st, "carnator_seed_expansion")
     return (out, ws) if return_ws else out
+
+
+# ---- around the attention: layer norm, projections, their gradients -----------------------------------
+ACT_NONE, ACT_GELU_TANH, ACT_GELU, ACT_SILU = 0, 1, 2, 3
+
+
+def _dtype_code(t, what: str) -> int:
+    import torch
+    if t.dtype == torch.float32:
+        return DTYPE_F32
+    if t.dtype == torch.bfloat16:
+        return DTYPE_BF16
+    raise ValueError(f"{what} must be float32 or bfloat16, not {t.dtype}")
+
+
+def _want(t, what: str, code: int, size, device) -> None:
+    """What the record says of a tensor, and what the call is about to do with it, have to agree."""
+    if t is None:
+        return
+    if _dtype_code(t, what) != code:
+        raise ValueError(f"{what} has another type than the shape record says")
+    if t.device != device:
+        raise ValueError(f"{what} is on {t.device}, not on {device}")
+    if tuple(t.shape) != size:
+        raise ValueError(f"{what} has shape {tuple(t.shape)}, not {size}")
+
+
+def _on_current_device(device) -> None:
+    """The kernels run on the current device, on its current stream; a machine without a GPU only checks arguments."""
+    import torch
+    if device.type == "cuda" and device.index != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on {device}, the current device is cuda:{torch.cuda.current_device()}")
+
+
+def _want_strides(t, what: str, recorded) -> None:
+    """The record was made for tensors laid out like this one (the stride of an axis of one entry does not matter)."""
+    if t is not None:
+        for i, (n, a, b) in enumerate(zip(t.shape, t.stride(), recorded)):
+            if n > 1 and a != b:
+                raise ValueError(f"{what} has stride {a} on axis {i}, the shape record says {b}")
+        if t.stride(-1) != 1 and t.shape[-1] > 1:
+            raise ValueError(f"{what}: the last axis must be contiguous")
+
+
+def _want_vector(t, what: str, code: int, size, device, stride: int = 0) -> None:
+    """A parameter vector [C], or one row per batch entry [B,C] with the record's batch stride."""
+    if t is None:
+        return
+    _want(t, what, code, size, device)
+    if size[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{what}: the last axis must be contiguous")
+    if len(size) == 2 and size[0] > 1 and t.stride(0) != stride:
+        raise ValueError(f"{what} has batch stride {t.stride(0)}, the shape record says {stride}")
+
+
+def _rows_of(stride, *tensors):
+    for t in tensors:
+        if t is not None:
+            return type(stride)(*t.stride()[:len(stride)])
+    return stride
+
+
+def _last_axis(t, what: str):
+    if t is not None and t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{what}: the last axis must be contiguous")
+
+
+def make_norm_shape(X, Y, weight=None, scale=None, shift=None, dX=None, eps: float = 1e-6) -> NormShape:
+    """Record of a layer norm over the last axis of X [B,H,N,C] (H = 1: whole token rows).  Y is the output of the forward
+    call or the gradient dY that the backward call gets; types and strides are taken from the tensors.  shift has the
+    batch stride of scale unless given."""
+    for t, what in ((X, "X"), (Y, "Y"), (dX, "dX")):
+        if t is not None and t.dim() != 4:
+            raise ValueError(f"{what} must be [B,H,N,C]")
+        _last_axis(t, what)
+    s = NormShape()
+    s.B, s.H, s.N, s.C = X.shape
+    s.x_stride, s.y_stride = _rows_of(s.x_stride, X), _rows_of(s.y_stride, Y)
+    s.dy_stride, s.dx_stride = _rows_of(s.dy_stride, Y), _rows_of(s.dx_stride, dX, X)
+    s.x_dtype, s.y_dtype = _dtype_code(X, "X"), _dtype_code(Y, "Y")
+    s.weight_dtype = DTYPE_F32 if weight is None else _dtype_code(weight, "weight")
+    mod = scale if scale is not None else shift
+    s.mod_dtype = DTYPE_F32 if mod is None else _dtype_code(mod, "scale")
+    s.scale_stride = 0 if mod is None else mod.stride(0)
+    s.shift_stride = s.scale_stride if shift is None else shift.stride(0)
+    s.eps = eps
+    return s
+
+
+def _dtype_of(code: int):
+    import torch
+    return torch.float32 if code == DTYPE_F32 else torch.bfloat16
+
+
+def layer_norm(X, shape: NormShape, weight=None, bias=None, shift=None, scale=None, Y=None, mean=None, rstd=None, stream=None):
+    """carnator_layer_norm.  Returns Y [B,H,N,C]; mean and rstd fp32 [B,H,N] (contiguous) are written if given."""
+    import torch
+    dev, size = X.device, (shape.B, shape.H, shape.N, shape.C)
+    if Y is None:
+        Y = torch.empty(size, dtype=_dtype_of(shape.y_dtype), device=dev)
+        shape.y_stride = _rows_of(shape.y_stride, Y)
+    _on_current_device(dev)
+    _want(X, "X", shape.x_dtype, size, dev)
+    _want(Y, "Y", shape.y_dtype, size, dev)
+    _want_strides(X, "X", shape.x_stride)
+    _want_strides(Y, "Y", shape.y_stride)
+    for t, what in ((weight, "weight"), (bias, "bias")):
+        _want_vector(t, what, shape.weight_dtype, size[3:], dev)
+    _want_vector(shift, "shift", shape.mod_dtype, (shape.B, shape.C), dev, shape.shift_stride)
+    _want_vector(scale, "scale", shape.mod_dtype, (shape.B, shape.C), dev, shape.scale_stride)
+    for t, what in ((mean, "mean"), (rstd, "rstd")):
+        _want(t, what, DTYPE_F32, size[:3], dev)
+        if t is not None and not t.is_contiguous():
+            raise ValueError(f"{what} must be contiguous")
+    st = lib().carnator_layer_norm(_ptr(X), _ptr(weight), _ptr(bias), _ptr(shift), _ptr(scale), ctypes.byref(shape), _ptr(Y),
+                                   _ptr(mean), _ptr(rstd), _stream(stream))
+    _check(st, "carnator_layer_norm")
+    return Y
+
+
+def layer_norm_backward_workspace_bytes(shape: NormShape) -> int:
+    return int(lib().carnator_layer_norm_backward_workspace_bytes(ctypes.byref(shape)))
+
+
+class NormGrads(NamedTuple):
+    """Gradients of a layer norm; those of vectors that the norm does not have, or that were not wanted, are None."""
+    dX: object
+    dweight: object
+    dbias: object
+    dshift: object
+    dscale: object
+
+
+def layer_norm_backward(dY, X, mean, rstd, shape: NormShape, weight=None, bias=None, scale=None, dX=None,
+                        want=("weight", "bias", "shift", "scale"), modulated=None, ws=None, stream=None) -> NormGrads:
+    """carnator_layer_norm_backward.  ``want`` names the vector gradients to compute: weight and bias (if the norm has a
+    weight), shift and scale (if it has a scale, or ``modulated`` says that it has a shift only)."""
+    import torch
+    dev, size = X.device, (shape.B, shape.H, shape.N, shape.C)
+    if dX is None:
+        dX = torch.empty(size, dtype=_dtype_of(shape.x_dtype), device=dev)
+        shape.dx_stride = _rows_of(shape.dx_stride, dX)
+    _on_current_device(dev)
+    _want(dY, "dY", shape.y_dtype, size, dev)
+    _want(X, "X", shape.x_dtype, size, dev)
+    _want(dX, "dX", shape.x_dtype, size, dev)
+    _want_strides(dY, "dY", shape.dy_stride)
+    _want_strides(X, "X", shape.x_stride)
+    _want_strides(dX, "dX", shape.dx_stride)
+    for t, what in ((weight, "weight"), (bias, "bias")):
+        _want_vector(t, what, shape.weight_dtype, size[3:], dev)
+    _want_vector(scale, "scale", shape.mod_dtype, (shape.B, shape.C), dev, shape.scale_stride)
+    for t, what in ((mean, "mean"), (rstd, "rstd")):
+        _want(t, what, DTYPE_F32, size[:3], dev)
+        if not t.is_contiguous():
+            raise ValueError(f"{what} must be contiguous")
+    if modulated is None:
+        modulated = scale is not None
+    new = lambda has, name, n: torch.empty(n, dtype=torch.float32, device=dev) if has and name in want else None  # noqa: E731
+    g = NormGrads(dX, new(weight is not None, "weight", size[3:]), new(weight is not None, "bias", size[3:]),
+                  new(modulated, "shift", (shape.B, shape.C)), new(modulated, "scale", (shape.B, shape.C)))
+    if ws is None:
+        ws = _new_ws(layer_norm_backward_workspace_bytes(shape), dev)
+    st = lib().carnator_layer_norm_backward(_ptr(dY), _ptr(X), _ptr(mean), _ptr(rstd), _ptr(weight), _ptr(bias), _ptr(scale),
+                                            ctypes.byref(shape), _ptr(dX), _ptr(g.dweight), _ptr(g.dbias), _ptr(g.dshift), _ptr(g.dscale),
+                                            _ptr(ws), ws.numel(), _stream(stream))
+    _check(st, "carnator_layer_norm_backward")
+    return g
+
+
+def make_linear_shape(X, W, Y, residual=None, Z=None, bias=None, gate=None, dX=None, dW=None, activation: int = ACT_NONE) -> LinearShape:
+    """Record of Y = residual + gate * act(X W^T + bias): X [B,N,in_features], W [out_features,in_features], Y (or the dY of
+    a backward call) [B,N,out_features]; types and strides are taken from the tensors."""
+    for t, what, dims in ((X, "X", 3), (W, "W", 2), (Y, "Y", 3), (residual, "residual", 3), (Z, "Z", 3), (dX, "dX", 3), (dW, "dW", 2)):
+        if t is not None and t.dim() != dims:
+            raise ValueError(f"{what} must have {dims} axes")
+        _last_axis(t, what)
+    s = LinearShape()
+    s.B, s.N, s.in_features = X.shape
+    s.out_features = W.shape[0]
+    if W.shape[1] != s.in_features or tuple(Y.shape) != (s.B, s.N, s.out_features):
+        raise ValueError(f"X {tuple(X.shape)}, W {tuple(W.shape)} and Y {tuple(Y.shape)} do not belong together")
+    s.x_stride, s.y_stride = _rows_of(s.x_stride, X), _rows_of(s.y_stride, Y)
+    s.residual_stride, s.z_stride = _rows_of(s.residual_stride, residual, Y), _rows_of(s.z_stride, Z)
+    s.dx_stride = _rows_of(s.dx_stride, dX)
+    s.w_stride = W.stride(0)
+    s.dw_stride = s.w_stride if dW is None else dW.stride(0)
+    s.gate_stride = 0 if gate is None else gate.stride(0)
+    s.activation = activation
+    s.y_dtype = _dtype_code(Y, "Y")
+    s.bias_dtype = DTYPE_F32 if bias is None else _dtype_code(bias, "bias")
+    s.gate_dtype = DTYPE_F32 if gate is None else _dtype_code(gate, "gate")
+    return s
+
+
+def linear_workspace_bytes(shape: LinearShape) -> int:
+    return int(lib().carnator_linear_workspace_bytes(ctypes.byref(shape)))
+
+
+def linear(X, W, shape: LinearShape, bias=None, gate=None, residual=None, Y=None, Z=None, ws=None, stream=None):
+    """carnator_linear.  Returns (Y [B,N,out_features], ws); Z (bf16, the pre-activation) is written if given."""
+    import torch
+    dev, B, N, K, M = X.device, shape.B, shape.N, shape.in_features, shape.out_features
+    if Y is None:
+        wide = -(-M // 8) * 8                      # rows on 16-byte boundaries
+        Y = torch.empty((B, N, wide), dtype=_dtype_of(shape.y_dtype), device=dev)[..., :M]
+        shape.y_stride = _rows_of(shape.y_stride, Y)
+    _on_current_device(dev)
+    _want(X, "X", DTYPE_BF16, (B, N, K), dev)
+    _want(W, "W", DTYPE_BF16, (M, K), dev)
+    _want(Y, "Y", shape.y_dtype, (B, N, M), dev)
+    _want(Z, "Z", DTYPE_BF16, (B, N, M), dev)
+    _want(residual, "residual", shape.y_dtype, (B, N, M), dev)
+    _want_strides(X, "X", shape.x_stride)
+    _want_strides(W, "W", (shape.w_stride,))
+    _want_strides(Y, "Y", shape.y_stride)
+    _want_strides(Z, "Z", shape.z_stride)
+    _want_strides(residual, "residual", shape.residual_stride)
+    _want_vector(bias, "bias", shape.bias_dtype, (M,), dev)
+    _want_vector(gate, "gate", shape.gate_dtype, (B, M), dev, shape.gate_stride)
+    if ws is None:
+        ws = _new_ws(linear_workspace_bytes(shape), dev)
+    st = lib().carnator_linear(_ptr(X), _ptr(W), _ptr(bias), _ptr(gate), _ptr(residual), ctypes.byref(shape), _ptr(Y), _ptr(Z),
+                               _ptr(ws), ws.numel(), _stream(stream))
+    _check(st, "carnator_linear")
+    return Y, ws
+
+
+def linear_backward_workspace_bytes(shape: LinearShape) -> int:
+    return int(lib().carnator_linear_backward_workspace_bytes(ctypes.byref(shape)))
+
+
+class LinearGrads(NamedTuple):
+    """Gradients of linear; the residual's is dY itself.  dX, dW and those not wanted are None where the call was given no room for them."""
+    dX: object
+    dW: object
+    dbias: object
+    dgate: object
+
+
+def linear_backward(dY, X, W, shape: LinearShape, Z=None, gate=None, dX=None, dW=None, want=("bias", "gate"), ws=None,
+                    stream=None) -> LinearGrads:
+    """carnator_linear_backward.  dX and dW are computed where given (bf16); ``want`` names the fp32 vector gradients: bias, gate
+    (if there is one).  Z is the pre-activation that the forward call wrote."""
+    import torch
+    dev, B, N, K, M = dY.device, shape.B, shape.N, shape.in_features, shape.out_features
+    _on_current_device(dev)
+    _want(dY, "dY", shape.y_dtype, (B, N, M), dev)
+    _want(X, "X", DTYPE_BF16, (B, N, K), dev)
+    _want(W, "W", DTYPE_BF16, (M, K), dev)
+    _want(Z, "Z", DTYPE_BF16, (B, N, M), dev)
+    _want(dX, "dX", DTYPE_BF16, (B, N, K), dev)
+    _want(dW, "dW", DTYPE_BF16, (M, K), dev)
+    _want_strides(dY, "dY", shape.y_stride)
+    _want_strides(X, "X", shape.x_stride)
+    _want_strides(W, "W", (shape.w_stride,))
+    _want_strides(Z, "Z", shape.z_stride)
+    _want_strides(dX, "dX", shape.dx_stride)
+    _want_strides(dW, "dW", (shape.dw_stride,))
+    _want_vector(gate, "gate", shape.gate_dtype, (B, M), dev, shape.gate_stride)
+    g = LinearGrads(dX, dW, torch.empty(M, dtype=torch.float32, device=dev) if "bias" in want else None,
+                    torch.empty((B, M), dtype=torch.float32, device=dev) if "gate" in want and gate is not None else None)
+    if ws is None:
+        ws = _new_ws(linear_backward_workspace_bytes(shape), dev)
+    st = lib().carnator_linear_backward(_ptr(dY), _ptr(X), _ptr(W), _ptr(Z), _ptr(gate), ctypes.byref(shape), _ptr(dX), _ptr(dW),
+                                        _ptr(g.dbias), _ptr(g.dgate), _ptr(ws), ws.numel(), _stream(stream))
+    _check(st, "carnator_linear_backward")
+    return g
 
 
 # ---- host-side scalars (no GPU) ---------------------------------------------------------------------

@@ -17,6 +17,10 @@
 #include "regions.cuh"
 #include "seed_expand.cuh"
 #include "seed_expand_tcgen05.cuh"
+#include "norm.cuh"
+#include "linear_tcgen05.cuh"
+#include "linear_rows.cuh"
+#include "linear_grad.cuh"
 #include "compat_host.inl"
 
 using namespace carnator;
@@ -970,6 +974,323 @@ extern "C" carnator_status carnator_seed_expansion(const void* Q, const void* K,
     const int64_t n = int64_t(s->B) * s->N;
     head_mean_kernel<<<unsigned((n + 255) / 256), 256, 0, stream>>>(a.per_head, s->B, s->H, s->N, contrast);
     LAUNCH_CHECK("head_mean_kernel");
+    return CARNATOR_OK;
+}
+
+// ------------------------------------------------------------------------------------------------
+// layer norm, matrix product with its epilogue, and their gradients
+// ------------------------------------------------------------------------------------------------
+namespace {
+bool dtype_ok(int32_t d) { return d == CARNATOR_DTYPE_F32 || d == CARNATOR_DTYPE_BF16; }
+int64_t dtype_bytes(int32_t d) { return d == CARNATOR_DTYPE_F32 ? 4 : 2; }
+int64_t dtype_unit(int32_t d) { return 16 / dtype_bytes(d); }       // elements in 16 bytes
+
+// Element strides of an operand with `n` axes in front of `row` contiguous elements: whole 16-byte steps and at most 2^38, not
+// negative.  For one that is written (or read through TMA, `positive`) no two rows may overlap (be the same).
+bool axes_ok(const int64_t* stride, const int64_t* size, int n, int64_t row, int32_t dtype, bool written, bool positive) {
+    int64_t st[3], sz[3];
+    int used = 0;
+    for (int i = 0; i < n; ++i) {
+        if (stride[i] < 0 || stride[i] % dtype_unit(dtype) || stride[i] > (int64_t(1) << 38)) return false;
+        if (size[i] > 1) { if (positive && stride[i] == 0) return false; st[used] = stride[i]; sz[used] = size[i]; ++used; }
+    }
+    if (!written) return true;
+    int64_t extent = row;
+    for (int k = 0; k < used; ++k) {                  // from the innermost axis out
+        int at = k;
+        for (int i = k + 1; i < used; ++i) if (st[i] < st[at]) at = i;
+        std::swap(st[k], st[at]); std::swap(sz[k], sz[at]);
+        if (st[k] < extent) return false;
+        extent += st[k] * (sz[k] - 1);
+    }
+    return true;
+}
+bool vec16(const void* p, int64_t stride, int32_t dtype) { return !p || (aligned(p, 16) && stride % dtype_unit(dtype) == 0); }
+
+carnator_status check_norm_shape(const carnator_norm_shape* s) {
+    if (!s || s->B <= 0 || s->H <= 0 || s->N <= 0 || s->C <= 0) return CARNATOR_ERR_INVALID_ARG;
+    if (!dtype_ok(s->x_dtype) || !dtype_ok(s->y_dtype) || !dtype_ok(s->weight_dtype) || !dtype_ok(s->mod_dtype)) return CARNATOR_ERR_INVALID_ARG;
+    if (!(s->eps >= 0.f) || std::isinf(s->eps)) return CARNATOR_ERR_INVALID_ARG;
+    if (s->shift_stride < 0 || s->scale_stride < 0) return CARNATOR_ERR_INVALID_ARG;
+    if (s->C > norm::kMaxChannels || s->B > 65535 || int64_t(s->H) * s->N > (int64_t(1) << 30)) return CARNATOR_ERR_UNSUPPORTED;
+    return CARNATOR_OK;
+}
+bool norm_axes_ok(const carnator_norm_shape* s, const int64_t st[3], int32_t dtype, bool written) {
+    const int64_t size[3] = {s->B, s->H, s->N};
+    return axes_ok(st, size, 3, s->C, dtype, written, false);
+}
+// The rows of an entry in the order of x's memory: the axis with the smaller stride inside.
+void norm_order(const carnator_norm_shape* s, norm::Args& a, const int64_t xs[3], const int64_t ys[3], const int64_t ds[3]) {
+    const bool heads_inside = s->H > 1 && (s->N == 1 || xs[1] < xs[2]);
+    const int o = heads_inside ? 2 : 1, i = heads_inside ? 1 : 2;
+    a.inner = heads_inside ? s->H : s->N;
+    a.rows = s->H * s->N;
+    a.xs[0] = xs[0]; a.xs[1] = xs[o]; a.xs[2] = xs[i];
+    a.ys[0] = ys[0]; a.ys[1] = ys[o]; a.ys[2] = ys[i];
+    a.ds[0] = ds[0]; a.ds[1] = ds[o]; a.ds[2] = ds[i];
+    const int64_t ss[3] = {int64_t(s->H) * s->N, s->N, 1};
+    a.ss[0] = ss[0]; a.ss[1] = ss[o]; a.ss[2] = ss[i];
+    a.C = s->C; a.eps = s->eps; a.inv_c = 1.0f / float(s->C);
+    a.shift_stride = s->shift_stride; a.scale_stride = s->scale_stride;
+    a.w_f32 = s->weight_dtype == CARNATOR_DTYPE_F32; a.mod_f32 = s->mod_dtype == CARNATOR_DTYPE_F32;
+}
+bool norm_params_aligned(const carnator_norm_shape* s, const void* weight, const void* bias, const void* shift, const void* scale) {
+    const size_t w = size_t(dtype_bytes(s->weight_dtype)), m = size_t(dtype_bytes(s->mod_dtype));
+    return (!weight || aligned(weight, w)) && (!bias || aligned(bias, w)) && (!shift || aligned(shift, m)) && (!scale || aligned(scale, m));
+}
+}  // namespace
+
+extern "C" carnator_status carnator_layer_norm(const void* X, const void* weight, const void* bias, const void* shift, const void* scale,
+                                               const carnator_norm_shape* s, void* Y, float* mean_opt, float* rstd_opt, void* stream_) {
+    carnator_status st = check_norm_shape(s);
+    if (st != CARNATOR_OK) return st;
+    if (!X || !Y || !aligned(X, 16) || !aligned(Y, 16) || (!mean_opt != !rstd_opt)) return CARNATOR_ERR_INVALID_ARG;
+    if (!aligned(mean_opt, 4) || !aligned(rstd_opt, 4) || !norm_params_aligned(s, weight, bias, shift, scale)) return CARNATOR_ERR_INVALID_ARG;
+    if (!norm_axes_ok(s, s->x_stride, s->x_dtype, false) || !norm_axes_ok(s, s->y_stride, s->y_dtype, true)) return CARNATOR_ERR_INVALID_ARG;
+    st = check_device();
+    if (st != CARNATOR_OK) return st;
+    norm::Args a = {};
+    a.x = X; a.y = Y; a.w = weight; a.beta = bias; a.shift = shift; a.scale = scale;
+    a.mean = mean_opt; a.rstd = rstd_opt;
+    norm_order(s, a, s->x_stride, s->y_stride, s->y_stride);
+    a.vec_ok = vec16(weight, 0, s->weight_dtype) && vec16(bias, 0, s->weight_dtype) && vec16(shift, s->shift_stride, s->mod_dtype) && vec16(scale, s->scale_stride, s->mod_dtype);
+    const norm::Form f = norm::form_of(s->C);
+    a.chunks = norm::chunks_of(f, s->B, a.rows, false);
+    const cudaError_t e = norm::launch<false>(a, s->B, f, s->x_dtype == CARNATOR_DTYPE_F32, s->y_dtype == CARNATOR_DTYPE_F32, static_cast<cudaStream_t>(stream_));
+    if (e != cudaSuccess) return cuda_fail(e, "norm_forward_kernel");
+    g_launches.fetch_add(1, std::memory_order_relaxed);
+    return CARNATOR_OK;
+}
+
+extern "C" size_t carnator_layer_norm_backward_workspace_bytes(const carnator_norm_shape* s) {
+    if (check_norm_shape(s) != CARNATOR_OK) return 0;
+    const int chunks = norm::chunks_of(norm::form_of(s->C), s->B, int64_t(s->H) * s->N, true);
+    return align256(size_t(s->B) * chunks * 2 * s->C * 4);
+}
+
+extern "C" carnator_status carnator_layer_norm_backward(const void* dY, const void* X, const float* mean, const float* rstd,
+                                                        const void* weight, const void* bias, const void* scale,
+                                                        const carnator_norm_shape* s, void* dX,
+                                                        float* dweight_opt, float* dbias_opt, float* dshift_opt, float* dscale_opt,
+                                                        void* ws, size_t ws_bytes, void* stream_) {
+    carnator_status st = check_norm_shape(s);
+    if (st != CARNATOR_OK) return st;
+    if (!dY || !X || !mean || !rstd || !dX) return CARNATOR_ERR_INVALID_ARG;
+    if (!aligned(dY, 16) || !aligned(X, 16) || !aligned(dX, 16) || !aligned(mean, 4) || !aligned(rstd, 4)) return CARNATOR_ERR_INVALID_ARG;
+    if (!aligned(dweight_opt, 4) || !aligned(dbias_opt, 4) || !aligned(dshift_opt, 4) || !aligned(dscale_opt, 4)) return CARNATOR_ERR_INVALID_ARG;
+    if (!norm_params_aligned(s, weight, bias, nullptr, scale)) return CARNATOR_ERR_INVALID_ARG;
+    if (!norm_axes_ok(s, s->x_stride, s->x_dtype, false) || !norm_axes_ok(s, s->dy_stride, s->y_dtype, false) ||
+        !norm_axes_ok(s, s->dx_stride, s->x_dtype, true)) return CARNATOR_ERR_INVALID_ARG;
+    if (!ws || !aligned(ws, 256) || ws_bytes < carnator_layer_norm_backward_workspace_bytes(s)) return CARNATOR_ERR_WORKSPACE;
+    st = check_device();
+    if (st != CARNATOR_OK) return st;
+    const bool sums = dweight_opt || dbias_opt || dshift_opt || dscale_opt;
+    norm::Args a = {};
+    a.x = X; a.dy = dY; a.y = dX; a.w = weight; a.scale = scale;
+    a.mean_in = mean; a.rstd_in = rstd;
+    a.part = sums ? static_cast<float*>(ws) : nullptr;
+    norm_order(s, a, s->x_stride, s->dx_stride, s->dy_stride);
+    a.vec_ok = vec16(weight, 0, s->weight_dtype) && vec16(scale, s->scale_stride, s->mod_dtype);
+    const norm::Form f = norm::form_of(s->C);
+    a.chunks = norm::chunks_of(f, s->B, a.rows, true);
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    cudaError_t e = norm::launch<true>(a, s->B, f, s->x_dtype == CARNATOR_DTYPE_F32, s->y_dtype == CARNATOR_DTYPE_F32, stream);
+    if (e != cudaSuccess) return cuda_fail(e, "norm_backward_kernel");
+    g_launches.fetch_add(1, std::memory_order_relaxed);
+    if (!sums) return CARNATOR_OK;
+    norm::ReduceArgs r = {};
+    r.part = a.part; r.w = weight; r.beta = bias; r.scale = scale;
+    r.dw = dweight_opt; r.dbeta = dbias_opt; r.dshift = dshift_opt; r.dscale = dscale_opt;
+    r.scale_stride = s->scale_stride;
+    r.B = s->B; r.chunks = a.chunks; r.C = s->C; r.w_f32 = a.w_f32; r.mod_f32 = a.mod_f32;
+    CUDA_TRY(launch_dependent(norm::norm_reduce_kernel, dim3(ceil_div(s->C, 32)), dim3(32 * norm::kReduceWarps), 0, stream, r));
+    g_launches.fetch_add(1, std::memory_order_relaxed);
+    return CARNATOR_OK;
+}
+
+namespace {
+carnator_status check_linear_shape(const carnator_linear_shape* s) {
+    if (!s || s->B <= 0 || s->N <= 0 || s->in_features <= 0 || s->out_features <= 0) return CARNATOR_ERR_INVALID_ARG;
+    if (s->activation < CARNATOR_ACT_NONE || s->activation > CARNATOR_ACT_SILU) return CARNATOR_ERR_INVALID_ARG;
+    if (!dtype_ok(s->y_dtype) || !dtype_ok(s->bias_dtype) || !dtype_ok(s->gate_dtype) || s->gate_stride < 0) return CARNATOR_ERR_INVALID_ARG;
+    const int64_t most = int64_t(1) << 30;
+    if (int64_t(s->B) * s->N > most || s->in_features > most || s->out_features > most || s->B > 65535) return CARNATOR_ERR_UNSUPPORTED;
+    return CARNATOR_OK;
+}
+bool linear_axes_ok(const carnator_linear_shape* s, const int64_t st[2], int64_t row, int32_t dtype, bool written) {
+    const int64_t size[2] = {s->B, s->N};
+    return axes_ok(st, size, 2, row, dtype, written, true) && (s->N == 1 || st[1] >= row);
+}
+bool matrix_ok(int64_t rows, int64_t cols, int64_t stride) {
+    return stride >= 0 && stride % 8 == 0 && stride <= (int64_t(1) << 38) && (rows == 1 || stride >= cols);
+}
+// Batch entries that follow each other evenly are one run of rows.
+bool runs_on(const carnator_linear_shape* s, const int64_t st[2]) { return s->B == 1 || s->N == 1 || st[0] == int64_t(s->N) * st[1]; }
+int64_t run_stride(const carnator_linear_shape* s, const int64_t st[2]) { return s->N == 1 && s->B > 1 ? st[0] : st[1]; }
+
+struct GradWs { __nv_bfloat16* dz; float* part_bias; float* part_gate; int64_t dz_stride; int chunks; size_t bytes; };
+// The partial sums are per batch entry, or over all rows as one where no gate's gradient is wanted: room for either.
+GradWs grad_ws_layout(void* base, const carnator_linear_shape* s) {
+    GradWs w;
+    char* p = static_cast<char*>(base);
+    size_t off = align256(sizeof(WsHeader));
+    w.dz_stride = (int64_t(s->out_features) + 7) / 8 * 8;
+    w.dz = reinterpret_cast<__nv_bfloat16*>(p + off);    off += align256(size_t(s->B) * s->N * w.dz_stride * 2);
+    w.chunks = lin::grad_chunks(s->B, s->N, s->out_features);
+    const size_t part = align256(size_t(std::max(s->B * w.chunks, lin::grad_chunks(1, int64_t(s->B) * s->N, s->out_features))) * s->out_features * 4);
+    w.part_bias = reinterpret_cast<float*>(p + off);     off += part;
+    w.part_gate = reinterpret_cast<float*>(p + off);     off += part;
+    w.bytes = off;
+    return w;
+}
+void plain_epilogue(lin::Epilogue& e, void* y, int64_t batch_stride, int64_t row_stride) {
+    e = {};
+    e.y = y; e.ys[0] = batch_stride; e.ys[1] = row_stride; e.rows_per_gate = 1;
+}
+}  // namespace
+
+extern "C" size_t carnator_linear_workspace_bytes(const carnator_linear_shape* s) {
+    return check_linear_shape(s) == CARNATOR_OK ? align256(sizeof(WsHeader)) : 0;
+}
+
+extern "C" carnator_status carnator_linear(const void* X, const void* W, const void* bias, const void* gate, const void* residual,
+                                           const carnator_linear_shape* s, void* Y, void* Z_opt, void* ws, size_t ws_bytes, void* stream_) {
+    carnator_status st = check_linear_shape(s);
+    if (st != CARNATOR_OK) return st;
+    if (!X || !W || !Y || !aligned(X, 16) || !aligned(W, 16) || !aligned(Y, 16) || !aligned(Z_opt, 16) || !aligned(residual, 16)) return CARNATOR_ERR_INVALID_ARG;
+    if (!aligned(bias, size_t(dtype_bytes(s->bias_dtype))) || !aligned(gate, size_t(dtype_bytes(s->gate_dtype)))) return CARNATOR_ERR_INVALID_ARG;
+    if (!linear_axes_ok(s, s->x_stride, s->in_features, CARNATOR_DTYPE_BF16, false) || !matrix_ok(s->out_features, s->in_features, s->w_stride) ||
+        !linear_axes_ok(s, s->y_stride, s->out_features, s->y_dtype, true) ||
+        (residual && !linear_axes_ok(s, s->residual_stride, s->out_features, s->y_dtype, false)) ||
+        (Z_opt && !linear_axes_ok(s, s->z_stride, s->out_features, CARNATOR_DTYPE_BF16, true))) return CARNATOR_ERR_INVALID_ARG;
+    if (!ws || !aligned(ws, 256) || ws_bytes < carnator_linear_workspace_bytes(s)) return CARNATOR_ERR_WORKSPACE;
+    st = check_device();
+    if (st != CARNATOR_OK) return st;
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    lin::Epilogue e = {};
+    e.y = Y; e.z = Z_opt; e.bias = bias; e.gate = gate; e.residual = residual;
+    for (int i = 0; i < 2; ++i) { e.ys[i] = s->y_stride[i]; e.zs[i] = s->z_stride[i]; e.rs[i] = s->residual_stride[i]; }
+    e.gate_stride = s->gate_stride;
+    e.act = s->activation; e.y_f32 = s->y_dtype == CARNATOR_DTYPE_F32;
+    e.bias_f32 = s->bias_dtype == CARNATOR_DTYPE_F32; e.gate_f32 = s->gate_dtype == CARNATOR_DTYPE_F32;
+    e.vec_ok = vec16(bias, 0, s->bias_dtype) && vec16(gate, s->gate_stride, s->gate_dtype);
+    e.rows_per_gate = s->N;
+    const int64_t rows = int64_t(s->B) * s->N;
+    if (rows <= lin::kRowsMost) {
+        lin::RowsArgs a;
+        a.e = e; a.x = static_cast<const __nv_bfloat16*>(X); a.w = static_cast<const __nv_bfloat16*>(W);
+        a.xs[0] = s->x_stride[0]; a.xs[1] = s->x_stride[1]; a.w_stride = s->w_stride;
+        a.hdr = static_cast<WsHeader*>(ws);
+        a.rows = int(rows); a.per_batch = s->N; a.K = s->in_features; a.cols = s->out_features;
+        const cudaError_t err = lin::launch_rows(a, stream);
+        if (err != cudaSuccess) return cuda_fail(err, "linear_rows_kernel");
+        g_launches.fetch_add(1, std::memory_order_relaxed);
+        return CARNATOR_OK;
+    }
+    lin::TcArgs a = {};
+    a.e = e;
+    a.hdr = static_cast<WsHeader*>(ws);
+    lin::Operand A = {X, s->B, s->N, s->in_features, s->x_stride[0], s->x_stride[1]};
+    a.batches = s->B; a.rows = s->N;
+    if (runs_on(s, s->x_stride) && runs_on(s, s->y_stride) && (!residual || runs_on(s, s->residual_stride)) && (!Z_opt || runs_on(s, s->z_stride))) {
+        a.batches = 1; a.rows = int(rows);
+        A.batches = 1; A.rows = rows; A.row_stride = run_stride(s, s->x_stride);
+        a.e.ys[1] = run_stride(s, s->y_stride); a.e.zs[1] = run_stride(s, s->z_stride); a.e.rs[1] = run_stride(s, s->residual_stride);
+    }
+    const lin::Operand Bo = {W, 1, s->out_features, s->in_features, 0, s->w_stride};
+    a.cols = s->out_features;
+    a.tiles_m = ceil_div(a.rows, lin::kTileM);
+    a.k_batches = 1; a.k_tiles = ceil_div(s->in_features, lin::kTileK);
+    st = lin::launch_tc_product<0, 0>(A, Bo, a, stream, g_cuda_error, sizeof(g_cuda_error));
+    if (st == CARNATOR_OK) g_launches.fetch_add(1, std::memory_order_relaxed);
+    return st;
+}
+
+extern "C" size_t carnator_linear_backward_workspace_bytes(const carnator_linear_shape* s) {
+    return check_linear_shape(s) == CARNATOR_OK ? grad_ws_layout(nullptr, s).bytes : 0;
+}
+
+extern "C" carnator_status carnator_linear_backward(const void* dY, const void* X, const void* W, const void* Z, const void* gate,
+                                                    const carnator_linear_shape* s, void* dX_opt, void* dW_opt,
+                                                    float* dbias_opt, float* dgate_opt, void* ws, size_t ws_bytes, void* stream_) {
+    carnator_status st = check_linear_shape(s);
+    if (st != CARNATOR_OK) return st;
+    if (!dY || !aligned(dY, 16) || !aligned(Z, 16) || !aligned(gate, size_t(dtype_bytes(s->gate_dtype)))) return CARNATOR_ERR_INVALID_ARG;
+    if (!linear_axes_ok(s, s->y_stride, s->out_features, s->y_dtype, false)) return CARNATOR_ERR_INVALID_ARG;
+    const bool use_z = s->activation != CARNATOR_ACT_NONE || dgate_opt;
+    if ((use_z && !Z) || (dgate_opt && !gate)) return CARNATOR_ERR_INVALID_ARG;
+    if (use_z && !linear_axes_ok(s, s->z_stride, s->out_features, CARNATOR_DTYPE_BF16, false)) return CARNATOR_ERR_INVALID_ARG;
+    if (dX_opt && (!W || !aligned(W, 16) || !aligned(dX_opt, 16) || !matrix_ok(s->out_features, s->in_features, s->w_stride) ||
+                   !linear_axes_ok(s, s->dx_stride, s->in_features, CARNATOR_DTYPE_BF16, true))) return CARNATOR_ERR_INVALID_ARG;
+    if (dW_opt && (!X || !aligned(X, 16) || !aligned(dW_opt, 16) || !matrix_ok(s->out_features, s->in_features, s->dw_stride) ||
+                   !linear_axes_ok(s, s->x_stride, s->in_features, CARNATOR_DTYPE_BF16, false))) return CARNATOR_ERR_INVALID_ARG;
+    if (!aligned(dbias_opt, 4) || !aligned(dgate_opt, 4)) return CARNATOR_ERR_INVALID_ARG;
+    if (!ws || !aligned(ws, 256)) return CARNATOR_ERR_WORKSPACE;
+    const GradWs w = grad_ws_layout(ws, s);
+    if (ws_bytes < w.bytes) return CARNATOR_ERR_WORKSPACE;
+    st = check_device();
+    if (st != CARNATOR_OK) return st;
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    const bool products = dX_opt || dW_opt;
+    const bool own_dz = products && (s->activation != CARNATOR_ACT_NONE || gate || s->y_dtype == CARNATOR_DTYPE_F32);
+    lin::Operand dz = {dY, s->B, s->N, s->out_features, s->y_stride[0], s->y_stride[1]};
+    if (own_dz) { dz.base = w.dz; dz.batch_stride = w.dz_stride * s->N; dz.row_stride = w.dz_stride; }
+    if (own_dz || dbias_opt || dgate_opt) {
+        lin::GradArgs a = {};
+        a.dy = dY; a.z = use_z ? static_cast<const __nv_bfloat16*>(Z) : nullptr; a.gate = gate;
+        a.dz = own_dz ? w.dz : nullptr;
+        a.part_bias = dbias_opt ? w.part_bias : nullptr; a.part_gate = dgate_opt ? w.part_gate : nullptr;
+        for (int i = 0; i < 2; ++i) { a.ds[i] = s->y_stride[i]; a.zs[i] = s->z_stride[i]; }
+        a.dzs[0] = w.dz_stride * s->N; a.dzs[1] = w.dz_stride;
+        a.gate_stride = s->gate_stride; a.gate_f32 = s->gate_dtype == CARNATOR_DTYPE_F32;
+        a.act = s->activation; a.dy_f32 = s->y_dtype == CARNATOR_DTYPE_F32;
+        a.rows = s->N; a.cols = s->out_features; a.chunks = w.chunks;
+        int batches = s->B;
+        if (!gate && runs_on(s, s->y_stride) && (!use_z || runs_on(s, s->z_stride))) {
+            batches = 1; a.rows = s->B * s->N;
+            a.ds[1] = run_stride(s, s->y_stride); a.zs[1] = run_stride(s, s->z_stride);
+            a.chunks = lin::grad_chunks(1, a.rows, a.cols);
+        }
+        cudaError_t e = lin::launch_grad(a, batches, stream);
+        if (e != cudaSuccess) return cuda_fail(e, "linear_grad_kernel");
+        g_launches.fetch_add(1, std::memory_order_relaxed);
+        if (dbias_opt || dgate_opt) {
+            const lin::GradReduceArgs r = {a.part_bias, a.part_gate, dbias_opt, dgate_opt, batches, a.chunks, a.cols};
+            CUDA_TRY(launch_dependent(lin::linear_grad_reduce_kernel, dim3(ceil_div(a.cols, 32)), dim3(32 * lin::kGradReduceWarps), 0, stream, r));
+            g_launches.fetch_add(1, std::memory_order_relaxed);
+        }
+    }
+    const bool dz_runs = own_dz || runs_on(s, s->y_stride);
+    const int64_t rows = int64_t(s->B) * s->N;
+    if (!products) CUDA_TRY(cudaMemsetAsync(ws, 0, 16, stream));       // no product clears the status word
+    for (int pass = 0; pass < 2; ++pass) {
+        if (pass == 0 ? !dX_opt : !dW_opt) continue;
+        lin::TcArgs a = {};
+        a.hdr = static_cast<WsHeader*>(ws);
+        a.cols = s->in_features;
+        lin::Operand A = dz;
+        const int64_t* other = pass == 0 ? s->dx_stride : s->x_stride;
+        const bool one_run = dz_runs && runs_on(s, other);
+        if (one_run) { A.batches = 1; A.rows = rows; A.row_stride = own_dz ? w.dz_stride : run_stride(s, s->y_stride); }
+        if (pass == 0) {
+            const lin::Operand Bo = {W, 1, s->out_features, s->in_features, 0, s->w_stride};
+            plain_epilogue(a.e, dX_opt, s->dx_stride[0], one_run ? run_stride(s, s->dx_stride) : s->dx_stride[1]);
+            a.batches = int(A.batches); a.rows = int(A.rows);
+            a.k_batches = 1; a.k_tiles = ceil_div(s->out_features, lin::kTileK);
+            a.tiles_m = ceil_div(a.rows, lin::kTileM);
+            st = lin::launch_tc_product<0, 1>(A, Bo, a, stream, g_cuda_error, sizeof(g_cuda_error));
+        } else {
+            lin::Operand Bo = {X, s->B, s->N, s->in_features, s->x_stride[0], s->x_stride[1]};
+            if (one_run) { Bo.batches = 1; Bo.rows = rows; Bo.row_stride = run_stride(s, s->x_stride); }
+            plain_epilogue(a.e, dW_opt, 0, s->dw_stride);
+            a.batches = 1; a.rows = s->out_features;
+            a.k_batches = int(A.batches); a.k_tiles = ceil_div(int(A.rows), lin::kTileK);
+            a.tiles_m = ceil_div(a.rows, lin::kTileM);
+            st = lin::launch_tc_product<1, 1>(A, Bo, a, stream, g_cuda_error, sizeof(g_cuda_error));
+        }
+        if (st != CARNATOR_OK) return st;
+        g_launches.fetch_add(1, std::memory_order_relaxed);
+    }
     return CARNATOR_OK;
 }
 

@@ -1,0 +1,154 @@
+// The elementwise half of a projection's gradients: from dy, the saved pre-activation z and the gate,
+//   dz = dy gate_b act'(z),   dbias = sum over rows of dz,   dgate_b = sum over the rows of entry b of dy act(z).
+// One pass over dy and z; dz is rounded to bf16 here, because the two products behind it take 16-bit operands (its rounding adds as much error to
+// dX and dW as their own does).  The sums are taken from the unrounded values: a thread keeps 8 columns over every eighth row of
+// its CTA's rows, a CTA leaves one partial row, a second kernel adds those in a fixed order.
+#pragma once
+#include "linear_tcgen05.cuh"
+
+namespace carnator {
+namespace lin {
+
+struct GradArgs {
+    const void* dy; const __nv_bfloat16* z; const void* gate;
+    __nv_bfloat16* dz;                   // [batches, rows, ...] or NULL: only the sums are wanted
+    float* part_bias; float* part_gate;  // [batches * chunks][cols] or NULL
+    int64_t ds[2], zs[2], dzs[2], gate_stride;
+    int act, dy_f32, gate_f32;
+    int rows, cols, chunks;              // rows and chunks of rows of a batch entry
+};
+
+constexpr int kGradCols = 256, kGradLanes = 8;       // columns and row lanes of a CTA
+
+// value and slope of the activation
+template <int ACT>
+__device__ __forceinline__ void act_and_slope(float z, float& f, float& s) {
+    if (ACT == kActSilu) {
+        const float g = __fdividef(1.f, 1.f + ex2_approx(-kLog2e * z));
+        f = z * g;
+        s = fmaf(f, 1.f - g, g);
+    } else if (ACT == kActGelu) {
+        const float c = 0.5f * (1.f + erff(z * 0.7071067811865476f));
+        f = z * c;
+        s = fmaf(z * 0.3989422804014327f, ex2_approx(-0.5f * kLog2e * z * z), c);
+    } else if (ACT == kActGeluTanh) {    // (1 + tanh u) / 2 = g, (1 - tanh^2 u) / 2 = 2 g (1 - g)
+        const float zz = z * z, e = ex2_approx((-2.f * kLog2e * kGeluA) * fmaf(kGeluB * zz, z, z));
+        const float g = __fdividef(1.f, 1.f + e);
+        f = z * g;
+        s = fmaf(2.f * f * (1.f - g), kGeluA * fmaf(3.f * kGeluB, zz, 1.f), g);
+    } else {
+        f = z; s = 1.f;
+    }
+}
+
+template <int ACT, bool DYF>
+__global__ void __launch_bounds__(32 * kGradLanes) linear_grad_kernel(const GradArgs a) {
+    __shared__ float sums[2][kGradLanes][kGradCols + 8];
+    grid_launch_dependents();
+    const int cv = threadIdx.x & 31, rl = threadIdx.x >> 5, b = blockIdx.z;
+    const int col = blockIdx.x * kGradCols + cv * 8, n = min(max(a.cols - col, 0), 8);
+    const int r0 = int(int64_t(blockIdx.y) * a.rows / a.chunks), r1 = int(int64_t(blockIdx.y + 1) * a.rows / a.chunks);
+    float sb[8], sg[8], gate[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { sb[i] = 0.f; sg[i] = 0.f; gate[i] = 1.f; }
+    if (a.gate) norm::load_param8(a.gate, b * a.gate_stride + col, a.gate_f32, 0, n, gate);
+    constexpr int U = 4;
+    if (n > 0)
+        for (int r = r0 + rl; r < r1; r += kGradLanes * U) {
+            norm::Raw8<DYF> dy[U];
+            norm::Raw8<false> zr[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int row = r + u * kGradLanes;
+                const int m = row < r1 ? n : 0;
+                dy[u] = norm::load_raw<DYF>(a.dy, b * a.ds[0] + row * a.ds[1] + col, m);
+                if (a.z) zr[u] = norm::load_raw<false>(a.z, b * a.zs[0] + row * a.zs[1] + col, m);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int row = r + u * kGradLanes;
+                if (row >= r1) break;
+                float d[8], z[8];
+                norm::to_float(dy[u], d);
+                if (a.z) norm::to_float(zr[u], z);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    float f = 0.f, s = 1.f;
+                    if (a.z) act_and_slope<ACT>(z[i], f, s);
+                    sg[i] = fmaf(d[i], f, sg[i]);
+                    d[i] *= gate[i] * s;
+                    sb[i] += d[i];
+                }
+                if (a.dz) norm::store8<false>(a.dz, b * a.dzs[0] + row * a.dzs[1] + col, d, n);
+            }
+        }
+    if (!a.part_bias && !a.part_gate) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { sums[0][rl][cv * 8 + i] = sb[i]; sums[1][rl][cv * 8 + i] = sg[i]; }
+    __syncthreads();
+    const int c = blockIdx.x * kGradCols + threadIdx.x;
+    if (c >= a.cols) return;
+    float tb = 0.f, tg = 0.f;
+#pragma unroll
+    for (int k = 0; k < kGradLanes; ++k) { tb += sums[0][k][threadIdx.x]; tg += sums[1][k][threadIdx.x]; }
+    const int64_t out = (int64_t(b) * a.chunks + blockIdx.y) * a.cols + c;
+    if (a.part_bias) a.part_bias[out] = tb;
+    if (a.part_gate) a.part_gate[out] = tg;
+}
+
+// dbias = sum over all partial rows, dgate of an entry over its own: 32 columns per CTA, as norm_reduce_kernel
+struct GradReduceArgs { const float* part_bias; const float* part_gate; float* dbias; float* dgate; int batches, chunks, cols; };
+constexpr int kGradReduceWarps = 16;
+__global__ void __launch_bounds__(32 * kGradReduceWarps) linear_grad_reduce_kernel(const GradReduceArgs a) {
+    __shared__ float sums[2][kGradReduceWarps][32];
+    grid_wait();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+    float total = 0.f;
+    for (int b = 0; b < a.batches; ++b) {
+        float p = 0.f, g = 0.f;
+        if (c < a.cols)
+#pragma unroll 4
+            for (int k = warp; k < a.chunks; k += kGradReduceWarps) {
+                const int64_t at = (int64_t(b) * a.chunks + k) * a.cols + c;
+                if (a.dbias) p += a.part_bias[at];
+                if (a.dgate) g += a.part_gate[at];
+            }
+        sums[0][warp][lane] = p;
+        sums[1][warp][lane] = g;
+        __syncthreads();
+        if (warp == 0 && c < a.cols) {
+            p = 0.f; g = 0.f;
+#pragma unroll
+            for (int k = 0; k < kGradReduceWarps; ++k) { p += sums[0][k][lane]; g += sums[1][k][lane]; }
+            total += p;
+            if (a.dgate) a.dgate[int64_t(b) * a.cols + c] = g;
+        }
+        __syncthreads();
+    }
+    if (warp == 0 && c < a.cols && a.dbias) a.dbias[c] = total;
+}
+
+// Chunks of rows per batch entry: about four CTAs an SM over the columns, none with fewer than 32 rows.
+inline int grad_chunks(int64_t batches, int64_t rows, int64_t cols) {
+    const int64_t strips = (cols + kGradCols - 1) / kGradCols, want = (148 * 4 + strips * batches - 1) / (strips * batches);
+    return int(std::max<int64_t>(1, std::min(want, rows / 32)));
+}
+
+template <int ACT>
+inline void launch_grad_act(const GradArgs& a, dim3 grid, cudaStream_t stream) {
+    if (a.dy_f32) linear_grad_kernel<ACT, true><<<grid, 32 * kGradLanes, 0, stream>>>(a);
+    else linear_grad_kernel<ACT, false><<<grid, 32 * kGradLanes, 0, stream>>>(a);
+}
+inline cudaError_t launch_grad(const GradArgs& a, int batches, cudaStream_t stream) {
+    const dim3 grid(ceil_div(a.cols, kGradCols), a.chunks, batches);
+    switch (a.act) {
+        case kActGeluTanh: launch_grad_act<kActGeluTanh>(a, grid, stream); break;
+        case kActGelu: launch_grad_act<kActGelu>(a, grid, stream); break;
+        case kActSilu: launch_grad_act<kActSilu>(a, grid, stream); break;
+        default: launch_grad_act<kActNone>(a, grid, stream); break;
+    }
+    return cudaGetLastError();
+}
+
+}  // namespace lin
+}  // namespace carnator

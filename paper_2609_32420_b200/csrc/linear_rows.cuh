@@ -1,0 +1,116 @@
+// The projection's product for a few rows (the conditioning of a denoising step: one row per batch entry):
+//   z = x W^T + bias,   y = residual + gate_b act(z),   up to 16 rows.
+// All it has to move is W, once.  A CTA takes 16 rows of W (output features); its warps share k, and a lane fetches W straight
+// into the registers of the matrix instruction: mma.m16n8k16 wants k = 2t, 2t+1, 2t+8, 2t+9 from lane t of a quad, but a sum over k may be taken
+// in any order, so lane t reads 8 consecutive k (16 bytes) of its row and gives them to two instructions, and the x operand is read the same way.
+// No shared memory and no barrier until the warps' partial sums are added, in the order of k.
+#pragma once
+#include "linear_tcgen05.cuh"
+
+namespace carnator {
+namespace lin {
+
+constexpr int kRowsMost = 16;            // rows of x per call that this kernel takes: two column tiles of the instruction
+constexpr int kRowsWarps = 8;
+
+struct RowsArgs {
+    Epilogue e;
+    const __nv_bfloat16* x; const __nv_bfloat16* w;
+    int64_t xs[2], w_stride;
+    WsHeader* hdr;
+    int rows, per_batch, K, cols;        // rows over all batch entries; rows of an entry
+};
+
+__device__ __forceinline__ uint4 load_k8(const __nv_bfloat16* row, int k, int K) {
+    if (k + 8 <= K) return __ldg(reinterpret_cast<const uint4*>(row + k));
+    uint32_t t[4] = {0, 0, 0, 0};        // the last k of a row: what lies behind them is not the row's
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (k + i < K) t[i / 2] |= uint32_t(reinterpret_cast<const uint16_t*>(row)[k + i]) << (16 * (i & 1));
+    return make_uint4(t[0], t[1], t[2], t[3]);
+}
+__device__ __forceinline__ void mma_16x8x16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+template <int NT>                        // column tiles of 8 rows of x
+__global__ void __launch_bounds__(32 * kRowsWarps) linear_rows_kernel(const RowsArgs a) {
+    __shared__ float sums[kRowsWarps][16][8 * NT + 1];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+    if (blockIdx.x == 0 && tid == 0) a.hdr->status = 0;
+    const int f0 = blockIdx.x * 16;
+    const bool on0 = f0 + g < a.cols, on1 = f0 + g + 8 < a.cols;
+    const __nv_bfloat16* w0 = a.w + int64_t(f0 + g) * a.w_stride;
+    const __nv_bfloat16* w1 = w0 + 8 * a.w_stride;
+    const __nv_bfloat16* xr[NT];
+    bool xon[NT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+        const int row = j * 8 + g;
+        xon[j] = row < a.rows;
+        const int b = xon[j] ? row / a.per_batch : 0;
+        xr[j] = a.x + b * a.xs[0] + (xon[j] ? row - b * a.per_batch : 0) * a.xs[1];
+    }
+    float d[NT][4];
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) d[j][i] = 0.f;
+    const uint4 zero = make_uint4(0, 0, 0, 0);
+    constexpr int U = 4;                 // pieces of 32 k in flight per warp
+    const int pieces = (a.K + 31) / 32;
+    for (int p = warp; p < pieces; p += kRowsWarps * U) {
+        uint4 u0[U], u1[U], xv[U][NT];
+#pragma unroll
+        for (int q = 0; q < U; ++q) {
+            const int k = (p + q * kRowsWarps) * 32 + t * 8;         // past the end: zero
+            u0[q] = on0 ? load_k8(w0, k, a.K) : zero;
+            u1[q] = on1 ? load_k8(w1, k, a.K) : zero;
+#pragma unroll
+            for (int j = 0; j < NT; ++j) xv[q][j] = xon[j] ? load_k8(xr[j], k, a.K) : zero;
+        }
+#pragma unroll
+        for (int q = 0; q < U; ++q)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                mma_16x8x16(d[j], u0[q].x, u1[q].x, u0[q].y, u1[q].y, xv[q][j].x, xv[q][j].y);
+                mma_16x8x16(d[j], u0[q].z, u1[q].z, u0[q].w, u1[q].w, xv[q][j].z, xv[q][j].w);
+            }
+    }
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {       // d0, d1: feature g, rows 2t and 2t + 1 of x; d2, d3: feature g + 8
+        sums[warp][g][j * 8 + 2 * t] = d[j][0];
+        sums[warp][g][j * 8 + 2 * t + 1] = d[j][1];
+        sums[warp][g + 8][j * 8 + 2 * t] = d[j][2];
+        sums[warp][g + 8][j * 8 + 2 * t + 1] = d[j][3];
+    }
+    __syncthreads();
+    const int f = tid & 15, col = f0 + f, row = tid >> 4;
+    if (row < 8 * NT && row < a.rows && col < a.cols) {
+        float z = 0.f;
+#pragma unroll
+        for (int k = 0; k < kRowsWarps; ++k) z += sums[k][f][row];
+        const int b = row / a.per_batch, r = row - b * a.per_batch;
+        auto param = [&](const void* p, int64_t i, int f32) { return f32 ? static_cast<const float*>(p)[i] : __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]); };
+        if (a.e.bias) z += param(a.e.bias, col, a.e.bias_f32);
+        if (a.e.z) static_cast<__nv_bfloat16*>(a.e.z)[b * a.e.zs[0] + r * a.e.zs[1] + col] = __float2bfloat16_rn(z);
+        float y = a.e.act == kActGeluTanh ? activation<kActGeluTanh>(z) : a.e.act == kActGelu ? activation<kActGelu>(z)
+                : a.e.act == kActSilu ? activation<kActSilu>(z) : z;
+        if (a.e.gate) y *= param(a.e.gate, b * a.e.gate_stride + col, a.e.gate_f32);
+        if (a.e.residual) y += param(a.e.residual, b * a.e.rs[0] + r * a.e.rs[1] + col, a.e.y_f32);
+        const int64_t off = b * a.e.ys[0] + r * a.e.ys[1] + col;
+        if (a.e.y_f32) static_cast<float*>(a.e.y)[off] = y;
+        else static_cast<__nv_bfloat16*>(a.e.y)[off] = __float2bfloat16_rn(y);
+    }
+}
+
+inline cudaError_t launch_rows(const RowsArgs& a, cudaStream_t stream) {
+    const int grid = ceil_div(a.cols, 16);
+    if (a.rows <= 8) linear_rows_kernel<1><<<grid, 32 * kRowsWarps, 0, stream>>>(a);
+    else linear_rows_kernel<2><<<grid, 32 * kRowsWarps, 0, stream>>>(a);
+    return cudaGetLastError();
+}
+
+}  // namespace lin
+}  // namespace carnator

@@ -1,0 +1,484 @@
+// Matrix products of a layer's projections on the 5th-generation tensor cores, with everything that follows the product in the
+// epilogue:   z = x W^T + bias,   y = residual + gate_b act(z)   (and z itself, for the backward pass),
+// and the two products of its gradients, dX = dz W and dW = dz^T x.
+//
+// One kernel, D[m,n] = sum_k A[m,k] B[n,k]; either operand may have its k axis contiguous (K-major: x, W and dz in the forward
+// product and dX) or its m / n axis (MN-major: W in dX, both in dW), which only changes the boxes that TMA fetches and the descriptors.
+// A pair of CTAs shares a tile of 256 x BN (tcgen05 cta_group::2): each loads 128 rows of A and half of the rows of B, and the product
+// of the pair reads both halves, so that an SM stages 32 KB per 64 columns of k where a CTA on its own would stage 48 KB for the same
+// flops.  Accumulators: 2 x 256 fp32 columns of tensor memory, so a tile's epilogue runs under the next tile's product.
+//
+// Warp roles (384 threads, one CTA per SM): warp 0 TMA producer; warp 1 (of the pair's first CTA) MMA issue; warp 2 tensor-memory
+// allocation; warps 4-11 epilogue.
+// The epilogue turns 32 x 32 pieces through shared memory, so that bias, gate and residual are read and y and z written as
+// whole 64- or 128-byte runs of a row.
+// Few tiles: 2 or 4 pairs of one cluster take a share of k each and add their partial tiles through distributed shared memory, in
+// the order of k: no workspace, no atomics, the same bits every time.
+// Every wait on an mbarrier is bounded, as in the attention kernel.
+#pragma once
+#include <cuda.h>
+
+#include "attn_tcgen05.cuh"
+#include "norm.cuh"
+
+namespace carnator {
+namespace lin {
+using namespace tc;
+
+constexpr int kThreadsTc = 384;
+constexpr int kEpiWarps = 8;
+constexpr int kTileM = 256;              // rows of a pair's tile
+constexpr int kTileK = 64;               // one 128-byte swizzle row of bf16
+constexpr int kMaxStages = 8;
+constexpr uint32_t kABytes = 128 * kTileK * 2;       // a CTA's share of A per stage
+constexpr int kPieceStride = 36;         // floats per row of a 32 x 32 piece: rows start 4 banks apart
+constexpr uint32_t kPieceBytes = 32 * kPieceStride * 4;
+constexpr uint32_t kStageBudget = 232448 - 256 - 1024 - 512 - kEpiWarps * kPieceBytes;     // of the 227 KB, less the static shared memory: ring of stages
+constexpr uint32_t kSmemTc = kStageBudget + 1024 + 512 + kEpiWarps * kPieceBytes;
+
+enum { kActNone = 0, kActGeluTanh = 1, kActGelu = 2, kActSilu = 3 };
+
+// What follows the product.
+struct Epilogue {
+    void* y; void* z;                    // z: bf16 or NULL
+    const void* bias; const void* gate; const void* residual;
+    int64_t ys[2], zs[2], rs[2], gate_stride;      // (batch, row)
+    int act, y_f32, bias_f32, gate_f32, vec_ok;
+    int rows_per_gate;                   // rows that share a gate row (batch entries that follow each other evenly are one)
+};
+
+struct TcArgs {
+    Epilogue e;
+    WsHeader* hdr;
+    int batches, rows, cols;             // D: rows per batch entry, columns
+    int tiles_m, tiles_n, tiles;         // per batch entry; columns; all of them
+    int group_m;                         // row tiles that are worked through together, column by column
+    int bn;                              // columns of a tile, a multiple of 32 (of 128 where B is MN-major)
+    int k_batches, k_tiles;              // k: batch entries (dW) x tiles of 64
+    int stages, splits;
+};
+
+__device__ __forceinline__ uint32_t cluster_ctarank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
+__device__ __forceinline__ uint32_t map_cta(uint32_t addr, uint32_t rank) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void arrive_remote(uint32_t cluster_bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+// the copy lands in this CTA and counts on the barrier of the pair's first CTA
+__device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap* map, uint32_t cluster_bar, int c0, int c1, int c2) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+        ::"r"(dst), "l"(map), "r"(cluster_bar), "r"(c0), "r"(c1), "r"(c2) : "memory");
+}
+__device__ __forceinline__ void mma_pair_el(uint32_t d_tmem, uint64_t da, uint64_t db, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p, e;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "elect.sync _|e, 0xffffffff;\n\t"
+        "@e tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "l"(da), "l"(db), "r"(idesc), "r"(accumulate) : "memory");
+}
+// arrives on the barrier at this offset in both CTAs of the pair once every product issued so far has completed
+__device__ __forceinline__ void commit_pair_el(uint32_t bar, uint16_t mask) {
+    asm volatile(
+        "{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
+        "@e tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n\t}"
+        ::"r"(bar), "h"(mask) : "memory");
+}
+
+// ---- activations ----------------------------------------------------------------------------------
+// gelu_tanh(z) = z (1 + tanh u) / 2 = z / (1 + exp(-2u)), u = sqrt(2/pi) (z + 0.044715 z^3): no cancellation where tanh is near -1
+constexpr float kGeluA = 0.7978845608028654f, kGeluB = 0.044715f;
+template <int ACT>
+__device__ __forceinline__ float activation(float z) {
+    if (ACT == kActSilu) return __fdividef(z, 1.f + ex2_approx(-kLog2e * z));
+    if (ACT == kActGelu) return 0.5f * z * (1.f + erff(z * 0.7071067811865476f));
+    if (ACT == kActGeluTanh) return __fdividef(z, 1.f + ex2_approx((-2.f * kLog2e * kGeluA) * fmaf(kGeluB * z * z, z, z)));
+    return z;
+}
+template <int ACT>
+__device__ __forceinline__ void activate8(float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = activation<ACT>(v[i]);
+}
+__device__ __forceinline__ void activate8(float (&v)[8], int act) {
+    switch (act) {
+        case kActGeluTanh: activate8<kActGeluTanh>(v); break;
+        case kActGelu: activate8<kActGelu>(v); break;
+        case kActSilu: activate8<kActSilu>(v); break;
+        default: break;
+    }
+}
+
+// ---- epilogue of 8 columns of one row ---------------------------------------------------------------
+struct Columns {                         // what 8 columns share over the rows of a piece
+    float bias[8], gate[8];
+    int gate_row;
+};
+__device__ __forceinline__ void columns_begin(const Epilogue& e, Columns& c, int col, int n) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { c.bias[i] = 0.f; c.gate[i] = 1.f; }
+    if (e.bias) norm::load_param8(e.bias, col, e.bias_f32, e.vec_ok, n, c.bias);
+    c.gate_row = -1;
+}
+__device__ __forceinline__ void load_residual(const Epilogue& e, int b, int row, int col, int n, norm::Raw8<true>& r) {
+    const int64_t off = b * e.rs[0] + row * e.rs[1] + col;
+    if (e.y_f32) r = norm::load_raw<true>(e.residual, off, n);
+    else r.q[0] = norm::load_raw<false>(e.residual, off, n).q[0];
+}
+__device__ __forceinline__ void finish(const Epilogue& e, Columns& c, int b, int row, int col, int n, float (&v)[8], const norm::Raw8<true>& res) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += c.bias[i];
+    if (e.z) norm::store8<false>(e.z, b * e.zs[0] + row * e.zs[1] + col, v, n);
+    activate8(v, e.act);
+    if (e.gate) {
+        const int g = b + row / e.rows_per_gate;
+        if (g != c.gate_row) { norm::load_param8(e.gate, g * e.gate_stride + col, e.gate_f32, e.vec_ok, n, c.gate); c.gate_row = g; }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] *= c.gate[i];
+    }
+    if (e.residual) {
+        float r[8];
+        if (e.y_f32) norm::to_float(res, r);
+        else { norm::Raw8<false> h; h.q[0] = res.q[0]; norm::to_float(h, r); }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += r[i];
+    }
+    const int64_t off = b * e.ys[0] + row * e.ys[1] + col;
+    if (e.y_f32) norm::store8<true>(e.y, off, v, n);
+    else norm::store8<false>(e.y, off, v, n);
+}
+
+// Tile t of the launch: group_m row tiles are worked through column by column, so that what runs at one time shares rows of A
+// and of B in L2.
+__device__ __forceinline__ void tile_at(const TcArgs& a, int t, int& b, int& m, int& n) {
+    const int all = a.batches * a.tiles_m, per_group = a.group_m * a.tiles_n;
+    const int g = t / per_group, r = t - g * per_group, first = g * a.group_m, size = min(a.group_m, all - first);
+    n = r / size;
+    const int mt = first + r - n * size;
+    b = mt / a.tiles_m;
+    m = mt - b * a.tiles_m;
+}
+
+template <int AMN, int BMN>
+__global__ void __launch_bounds__(kThreadsTc, 1)
+linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB, const TcArgs a) {
+    extern __shared__ unsigned char lin_smem[];
+    __shared__ uint32_t tmem_slot;
+    __shared__ int abort_flag;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t base = (smem_u32(lin_smem) + 1023u) & ~1023u;
+    const uint32_t pieces = base + kStageBudget, bars = pieces + kEpiWarps * kPieceBytes;
+    const uint32_t rank = cluster_ctarank(), half = rank & 1u, leader = rank & ~1u, split = rank >> 1;
+    const uint32_t b_bytes = uint32_t(a.bn / 2) * kTileK * 2, stage_bytes = kABytes + b_bytes;
+    auto bar_full = [&](int s) { return bars + 8 * s; };                       // used in the pair's first CTA: both CTAs' copies have landed
+    auto bar_empty = [&](int s) { return bars + 64 + 8 * s; };                 // the products that read stage s have completed
+    auto bar_done = [&](int u) { return bars + 128 + 8 * u; };                 // accumulator u holds a tile
+    auto bar_read = [&](int u) { return bars + 144 + 8 * u; };                 // first CTA: both CTAs have read accumulator u
+    volatile int* abortp = &abort_flag;
+    const unsigned long long limit = kDefaultWaitNs;
+    const uint16_t pair_mask = uint16_t(3u << leader);
+
+    if (tid == 0) {
+        abort_flag = 0;
+        for (int s = 0; s < kMaxStages; ++s) { mbar_init(bar_full(s), 1); mbar_init(bar_empty(s), 1); }
+        for (int u = 0; u < 2; ++u) { mbar_init(bar_done(u), 1); mbar_init(bar_read(u), 2 * kEpiWarps); }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        // the status word of the call: nothing sets it before its wait limit has passed, which is after this
+        if (blockIdx.x == 0) a.hdr->status = 0;
+    }
+    if (warp == 2) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    if (warp == 0 && lane == 0) { prefetch_tmap(&mapA); prefetch_tmap(&mapB); }
+    tc_fence_before();
+    __syncwarp();
+    cluster_sync();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot;
+
+    // the clusters take the tiles in turn; with splits > 1 there is one cluster per tile and a pair has its share of k
+    const int first = int(blockIdx.x / (2 * a.splits)), step = int(gridDim.x / (2 * a.splits));
+    const int k_all = a.k_batches * a.k_tiles;
+    const int k0 = int(int64_t(k_all) * split / a.splits), k1 = int(int64_t(k_all) * (split + 1) / a.splits);
+
+    if (warp == 0) {
+        // ================= TMA producer =================
+        if (lane == 0) {
+            const uint32_t full0 = map_cta(bar_full(0), leader);
+            int s = 0, issued = 0;
+            uint32_t phase = 0;
+            bool ok = true;
+            for (int t = first; t < a.tiles && ok; t += step) {
+                int b, m, n;
+                tile_at(a, t, b, m, n);
+                const int m0 = m * kTileM + int(half) * 128, n0 = n * a.bn + int(half) * (a.bn / 2);
+                int kb = k0 / a.k_tiles, kt = k0 - kb * a.k_tiles;
+                for (int k = k0; k < k1; ++k) {
+                    if (issued >= a.stages && !mbar_wait(bar_empty(s), phase ^ 1u, abortp, 0, limit)) {
+                        set_status(a.hdr, CARNATOR_ERR_DEVICE_TIMEOUT, 70, k, blockIdx.x); ok = false; break;
+                    }
+                    if (half == 0) mbar_expect_tx(bar_full(s), 2 * stage_bytes);
+                    const uint32_t sa = base + uint32_t(s) * stage_bytes, sb = sa + kABytes, bar = full0 + 8 * s;
+                    if (AMN) {           // 64 columns of m x 64 rows of k, twice
+                        tma_load_pair(sa, &mapA, bar, m0, kt * kTileK, kb);
+                        tma_load_pair(sa + kABytes / 2, &mapA, bar, m0 + 64, kt * kTileK, kb);
+                    } else {
+                        tma_load_pair(sa, &mapA, bar, kt * kTileK, m0, b);
+                    }
+                    if (BMN) {
+                        for (int c = 0; c < a.bn / 2; c += 64)
+                            tma_load_pair(sb + uint32_t(c) * 128, &mapB, bar, n0 + c, kt * kTileK, kb);
+                    } else {
+                        tma_load_pair(sb, &mapB, bar, kt * kTileK, n0, 0);
+                    }
+                    ++issued;
+                    if (++s == a.stages) { s = 0; phase ^= 1u; }
+                    if (++kt == a.k_tiles) { kt = 0; ++kb; }
+                }
+            }
+            // The last products' completion on every stage: no copy is in flight and no arrival on its way to this CTA afterwards.
+            const int used = min(issued, a.stages);
+            for (int i = 0; i < used; ++i) {
+                const int q = issued - used + i, sq = q % a.stages;
+                const uint32_t par = uint32_t(q / a.stages) & 1u;
+                if (*abortp ? !mbar_wait_drain(bar_empty(sq), par, 2000000ull) : !mbar_wait(bar_empty(sq), par, abortp, 0, limit))
+                    set_status(a.hdr, CARNATOR_ERR_DEVICE_TIMEOUT, 71, i, blockIdx.x);
+            }
+            if (*abortp) {               // given up: copies whose products were never issued land within microseconds
+                const unsigned long long t0 = global_ns();
+                for (int it = 0; it < 20000 && global_ns() - t0 < 1000000ull; ++it) __nanosleep(100);
+            }
+        }
+    } else if (warp == 1) {
+        // ================= MMA issuer (converged warp, one elected lane issues) =================
+        if (half == 0) {
+            const uint32_t idesc = instr_desc(kTileM, 0, BMN) | (uint32_t(a.bn >> 3) << 17) | (uint32_t(AMN) << 15);
+            // K-major: 8-row groups 1024 B apart, 16 columns of k = 32 B.  MN-major: 64-column slabs of 8 KB, 16 rows of k = 2 KB.
+            const uint64_t da0 = AMN ? smem_desc(base, kABytes / 2, 1024) : smem_desc(base, 16, 1024);
+            const uint64_t db0 = BMN ? smem_desc(base + kABytes, 8192, 1024) : smem_desc(base + kABytes, 16, 1024);
+            constexpr uint32_t step_a = (AMN ? 2048 : 32) >> 4, step_b = (BMN ? 2048 : 32) >> 4;
+            int s = 0, i = 0;
+            uint32_t phase = 0;
+            bool ok = true;
+            for (int t = first; t < a.tiles && ok; t += step, ++i) {
+                const int u = i & 1;
+                if (i >= 2) {
+                    ok = mbar_wait_warp(bar_read(u), uint32_t((i >> 1) - 1) & 1u, abortp, 0, limit);
+                    if (!ok) { if (lane == 0) set_status(a.hdr, CARNATOR_ERR_DEVICE_TIMEOUT, 72, i, blockIdx.x); break; }
+                    tc_fence_after();
+                }
+                const uint32_t d = tmem + uint32_t(u) * 256u;
+                for (int k = k0; k < k1; ++k) {
+                    ok = mbar_wait_warp(bar_full(s), phase, abortp, 0, limit);
+                    if (!ok) { if (lane == 0) set_status(a.hdr, CARNATOR_ERR_DEVICE_TIMEOUT, 73, k, blockIdx.x); break; }
+                    tc_fence_after();
+                    const uint32_t off = (uint32_t(s) * stage_bytes) >> 4;
+#pragma unroll
+                    for (int kk = 0; kk < kTileK / 16; ++kk)
+                        mma_pair_el(d, da0 + off + kk * step_a, db0 + off + kk * step_b, idesc, (k > k0 || kk > 0) ? 1u : 0u);
+                    commit_pair_el(bar_empty(s), pair_mask);
+                    if (++s == a.stages) { s = 0; phase ^= 1u; }
+                }
+                if (ok) commit_pair_el(bar_done(u), pair_mask);
+            }
+        }
+    } else if (warp >= 4) {
+        // ================= epilogue =================
+        const int w = warp - 4, quarter = warp & 3, side = w >> 2;         // rows 32 quarter .. of this CTA's 128; every other piece of 32 columns
+        const uint32_t lane_base = uint32_t(quarter * 32) << 16;
+        const uint32_t piece = pieces + uint32_t(w) * kPieceBytes;
+        const uint32_t read0 = map_cta(bar_read(0), leader);
+        const int sub_row = lane >> 2, sub_col = (lane & 3) * 8;
+        bool ok = true;
+        int i = 0;
+        if (a.splits == 1) {
+            for (int t = first; t < a.tiles && ok; t += step, ++i) {
+                const int u = i & 1;
+                int b, m, n;
+                tile_at(a, t, b, m, n);
+                const int row0 = m * kTileM + int(half) * 128 + quarter * 32, left = min(a.cols - n * a.bn, a.bn);
+                ok = mbar_wait_warp(bar_done(u), uint32_t(i >> 1) & 1u, abortp, 20, limit);
+                if (!ok) { if (lane == 0) set_status(a.hdr, CARNATOR_ERR_DEVICE_TIMEOUT, 74, i, blockIdx.x); break; }
+                tc_fence_after();
+                for (int c = side * 32; c < left; c += 64) {               // warp-uniform
+                    const int col = n * a.bn + c + sub_col, cn = min(max(a.cols - col, 0), 8);
+                    norm::Raw8<true> res[4];
+                    if (a.e.residual)
+#pragma unroll
+                        for (int p = 0; p < 4; ++p) {
+                            const int row = row0 + p * 8 + sub_row;
+                            load_residual(a.e, b, row, col, row < a.rows ? cn : 0, res[p]);
+                        }
+                    Columns cols;
+                    columns_begin(a.e, cols, col, cn);
+                    float v[32];
+                    tmem_ld32(tmem + lane_base + uint32_t(u * 256 + c), v);
+                    tmem_wait_ld(v);
+                    __syncwarp();
+#pragma unroll
+                    for (int q = 0; q < 8; ++q)
+                        asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(piece + uint32_t(lane * kPieceStride + 4 * q) * 4u),
+                                     "f"(v[4 * q]), "f"(v[4 * q + 1]), "f"(v[4 * q + 2]), "f"(v[4 * q + 3]) : "memory");
+                    __syncwarp();
+#pragma unroll
+                    for (int p = 0; p < 4; ++p) {
+                        const int r = p * 8 + sub_row, row = row0 + r;
+                        float f[8];
+#pragma unroll
+                        for (int q = 0; q < 2; ++q)
+                            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(f[4 * q]), "=f"(f[4 * q + 1]), "=f"(f[4 * q + 2]), "=f"(f[4 * q + 3])
+                                         : "r"(piece + uint32_t(r * kPieceStride + sub_col + 4 * q) * 4u) : "memory");
+                        if (row < a.rows && cn > 0) finish(a.e, cols, b, row, col, cn, f, res[p]);
+                    }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) arrive_remote(read0 + 8 * u);
+            }
+        } else {
+            // partial tile to shared memory (every stage has been read by now: bar_done follows the last product)
+            ok = mbar_wait_warp(bar_done(0), 0, abortp, 20, limit);
+            if (!ok) { if (lane == 0) set_status(a.hdr, CARNATOR_ERR_DEVICE_TIMEOUT, 75, 0, blockIdx.x); }
+            tc_fence_after();
+            const uint32_t pitch = uint32_t(a.bn + 4) * 4u;
+            if (ok)
+                for (int c = side * 32; c < a.bn; c += 64) {
+                    float v[32];
+                    tmem_ld32(tmem + lane_base + uint32_t(c), v);
+                    tmem_wait_ld(v);
+#pragma unroll
+                    for (int q = 0; q < 8; ++q)
+                        asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(base + uint32_t(quarter * 32 + lane) * pitch + uint32_t(c + 4 * q) * 4u),
+                                     "f"(v[4 * q]), "f"(v[4 * q + 1]), "f"(v[4 * q + 2]), "f"(v[4 * q + 3]) : "memory");
+                }
+            tc_fence_before();
+        }
+    }
+
+    if (a.splits > 1) {
+        // Every CTA of the cluster finishes a run of the columns: the partial tiles of the same rows, added in the order of k.
+        __syncwarp();
+        cluster_sync();
+        int b, m, n;
+        tile_at(a, first, b, m, n);
+        const uint32_t pitch = uint32_t(a.bn + 4) * 4u;
+        const int share = a.bn / a.splits, groups = share / 8, c0 = int(split) * share;
+        if (!*abortp)
+            for (int i = tid; i < 128 * groups; i += kThreadsTc) {
+                const int r = i / groups, c = c0 + (i - r * groups) * 8;
+                const int row = m * kTileM + int(half) * 128 + r, col = n * a.bn + c, cn = min(max(a.cols - col, 0), 8);
+                if (row >= a.rows || cn == 0) continue;
+                norm::Raw8<true> res;
+                if (a.e.residual) load_residual(a.e, b, row, col, cn, res);
+                Columns cols;
+                columns_begin(a.e, cols, col, cn);
+                float f[8];
+#pragma unroll
+                for (int q = 0; q < 8; ++q) f[q] = 0.f;
+                for (int sp = 0; sp < a.splits; ++sp) {
+                    const uint32_t src = map_cta(base + uint32_t(r) * pitch + uint32_t(c) * 4u, uint32_t(2 * sp) + half);
+                    float g[8];
+#pragma unroll
+                    for (int q = 0; q < 2; ++q)
+                        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(g[4 * q]), "=f"(g[4 * q + 1]), "=f"(g[4 * q + 2]), "=f"(g[4 * q + 3])
+                                     : "r"(src + 16u * q) : "memory");
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) f[q] += g[q];
+                }
+                finish(a.e, cols, b, row, col, cn, f, res);
+            }
+    }
+    tc_fence_before();
+    __syncwarp();
+    cluster_sync();                      // nothing of the cluster reads this CTA's memory or arrives on its barriers any more
+    if (warp == 2) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+    }
+}
+
+// ---- host side ------------------------------------------------------------------------------------
+// 3-D map over [batches, rows, cols] bf16 with the columns contiguous: box = 64 columns x box_rows x 1, 128-byte swizzle, what lies
+// outside reads as zero.
+inline bool make_map_3d(CUtensorMap* map, const void* base, int64_t batches, int64_t rows, int64_t cols, int64_t batch_stride, int64_t row_stride, int box_rows) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    cuuint64_t dims[3] = {cuuint64_t(cols), cuuint64_t(rows), cuuint64_t(batches)};
+    // the stride of an axis of one entry is never used, but has to be a valid value
+    const cuuint64_t row = rows > 1 ? cuuint64_t(row_stride) * 2 : cuuint64_t((cols + 7) / 8 * 16);
+    cuuint64_t strides[2] = {row, batches > 1 ? cuuint64_t(batch_stride) * 2 : row};
+    cuuint32_t box[3] = {64, cuuint32_t(box_rows), 1};
+    cuuint32_t estr[3] = {1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// A bf16 operand as [batches, rows, cols].
+struct Operand { const void* base; int64_t batches, rows, cols, batch_stride, row_stride; };
+
+// Columns of a tile and pairs that share one.  Time of a launch in units of one column of 256 rows: the turns that the pairs of 148 SMs take, times a tile's columns (a tile
+// narrower than 128 columns waits for shared memory instead: its A operand costs as much to read) times its share of k.
+struct Plan { int bn, splits; };
+inline Plan plan_of(int64_t m_tiles, int64_t cols, int64_t k_all, bool b_mn) {
+    Plan best = {256, 1};
+    double best_cost = 1e30;
+    for (int bn = 256; bn >= (b_mn ? 128 : 64); bn -= b_mn ? 128 : 32) {
+        const int64_t tiles = m_tiles * ((cols + bn - 1) / bn);
+        for (int splits = 1; splits <= 4; splits *= 2) {
+            if (splits > 1 && (tiles * splits > 72 || k_all < 4 * splits || bn % (8 * splits))) break;
+            const int64_t pairs = std::min<int64_t>(74, tiles * splits);
+            const double turns = double((tiles * splits + pairs - 1) / pairs);
+            // per tile of k: the product, and what an SM takes to fetch its operands from L2; per tile: filling and draining
+            const double cost = turns * ((double(k_all) / splits) * std::max(bn, 112) + (splits > 1 ? 500 + 2 * bn : 400 + bn));
+            if (cost < best_cost * 0.995) { best_cost = cost; best = {bn, splits}; }
+        }
+    }
+    return best;
+}
+
+template <int AMN, int BMN>
+inline carnator_status launch_tc_product(const Operand& A, const Operand& B, TcArgs a, cudaStream_t stream, char* err, size_t errlen) {
+    const Plan p = plan_of(int64_t(a.batches) * a.tiles_m, a.cols, int64_t(a.k_batches) * a.k_tiles, BMN);
+    a.bn = p.bn; a.splits = p.splits;
+    a.tiles_n = ceil_div(a.cols, a.bn);
+    const int64_t tiles = int64_t(a.batches) * a.tiles_m * a.tiles_n;
+    if (tiles > (int64_t(1) << 30)) return CARNATOR_ERR_UNSUPPORTED;
+    a.tiles = int(tiles);
+    a.group_m = 8;
+    const uint32_t stage = kABytes + uint32_t(a.bn / 2) * kTileK * 2;
+    a.stages = int(std::min<uint32_t>(kMaxStages, kStageBudget / stage));
+    CUtensorMap ma, mb;
+    if (!make_map_3d(&ma, A.base, A.batches, A.rows, A.cols, A.batch_stride, A.row_stride, AMN ? kTileK : 128) ||
+        !make_map_3d(&mb, B.base, B.batches, B.rows, B.cols, B.batch_stride, B.row_stride, BMN ? kTileK : a.bn / 2)) {
+        snprintf(err, errlen, "cuTensorMapEncodeTiled failed or is unavailable");
+        return CARNATOR_ERR_CUDA;
+    }
+    auto kern = linear_tc_kernel<AMN, BMN>;
+    static SmemAllowed allowed;
+    const unsigned long long ctx = context_id();
+    if (!allowed.has(ctx)) {
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kSmemTc));
+        if (e != cudaSuccess) return cuda_error(e, "cudaFuncSetAttribute(linear_tc_kernel)", err, errlen);
+        allowed.add(ctx);
+    }
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = unsigned(2 * a.splits); at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    const int clusters = a.splits > 1 ? a.tiles : std::min(a.tiles, 74);
+    cfg.gridDim = dim3(unsigned(clusters * 2 * a.splits)); cfg.blockDim = dim3(kThreadsTc); cfg.dynamicSmemBytes = kSmemTc; cfg.stream = stream;
+    cfg.attrs = at; cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, ma, mb, a);
+    if (e != cudaSuccess) return cuda_error(e, "linear_tc_kernel", err, errlen);
+    return CARNATOR_OK;
+}
+
+}  // namespace lin
+}  // namespace carnator

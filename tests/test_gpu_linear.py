@@ -1,0 +1,246 @@
+"""Matrix product with bias, activation, gate and residual, and its gradients, against the formulas in 64 bits."""
+import pytest
+import torch
+
+from paper_2609_32420_b200 import carnator as cn
+from tests.layer_util import (ACT_ERR, DTYPES, SLOPE_MOST, U16, U32, act64, canvas, check, half_step, linear_grad_ref, linear_ref, padded, untouched)
+
+pytestmark = pytest.mark.gpu
+
+ACTS = [cn.ACT_NONE, cn.ACT_GELU_TANH, cn.ACT_GELU, cn.ACT_SILU]
+
+
+def make(B, N, K, M, y="bf16", p="bf16", bias=True, gate=True, residual=True, seed=0, extra=1):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    t = dict(x=padded((B, N, K), torch.bfloat16, gen, extra=extra), w=padded((M, K), torch.bfloat16, gen, 1.5 / K ** 0.5),
+             dy=padded((B, N, M), DTYPES[y], gen, extra=extra))
+    vec = lambda *n: torch.randn(n, device="cuda", generator=gen)  # noqa: E731
+    t["bias"] = vec(M).to(DTYPES[p]) if bias else None
+    t["gate"] = vec(B, 6, M)[:, 2].to(DTYPES[p]) if gate else None
+    t["residual"] = padded((B, N, M), DTYPES[y], gen, extra=extra) if residual else None
+    return t
+
+
+def forward(t, act, keep=True, extra=1):
+    B, N, _ = t["x"].shape
+    M = t["w"].shape[0]
+    buf, y = canvas((B, N, M), t["dy"].dtype, extra=extra)
+    zbuf, z = canvas((B, N, M), torch.bfloat16, extra=extra)
+    s = cn.make_linear_shape(t["x"], t["w"], y, residual=t["residual"], Z=z, bias=t["bias"], gate=t["gate"], activation=act)
+    ws = torch.full((cn.linear_workspace_bytes(s),), 255, dtype=torch.uint8, device="cuda")
+    out, _ = cn.linear(t["x"], t["w"], s, bias=t["bias"], gate=t["gate"], residual=t["residual"], Y=y, Z=z if keep else None, ws=ws)
+    assert cn.query_status(ws) == cn.OK, cn.last_cuda_error()
+    assert untouched(buf, y) and (untouched(zbuf, z) if keep else bool((zbuf == 77.0).all()))
+    return out, z
+
+
+def check_forward(t, act, y, z=None):
+    ry, rz, ez, ey = linear_ref(t["x"], t["w"], t["bias"], t["gate"], t["residual"], act)
+    if z is not None:
+        check(z, rz, ez + U16 * rz.abs(), "z")
+    check(y, ry, ey + half_step(y.dtype) * (ry.abs() + ey), "y")
+
+
+def backward(t, z, act, need=("x", "w"), want=("bias", "gate"), extra=1):
+    bx, dx = canvas(t["x"].shape, torch.bfloat16, extra=extra)
+    bw, dw = canvas(t["w"].shape, torch.bfloat16)
+    s = cn.make_linear_shape(t["x"], t["w"], t["dy"], Z=z, gate=t["gate"], dX=dx, dW=dw, activation=act)
+    ws = torch.full((cn.linear_backward_workspace_bytes(s),), 255, dtype=torch.uint8, device="cuda")
+    g = cn.linear_backward(t["dy"], t["x"], t["w"], s, Z=z, gate=t["gate"], dX=dx if "x" in need else None, dW=dw if "w" in need else None, want=want, ws=ws)
+    assert cn.query_status(ws) == cn.OK, cn.last_cuda_error()
+    assert untouched(bx, dx) if "x" in need else bool((bx == 77.0).all())
+    assert untouched(bw, dw) if "w" in need else bool((bw == 77.0).all())
+    return g
+
+
+def check_backward(t, z, act, g):
+    ref = linear_grad_ref(t["dy"], t["x"], t["w"], z, t["gate"], act)
+    for name in ("dbias", "dgate", "dX", "dW"):
+        got = getattr(g, name)
+        if got is not None:
+            r, e = ref[name]
+            check(got, r, e + half_step(got.dtype) * (r.abs() + e), name)
+
+
+# rows, in, out: single rows, both sides of the few-row kernel's limit, tile borders (128, 256), odd everything, a long k with few tiles (split), many tiles (persistent)
+SIZES = [(1, 1, 1), (1, 1536, 1536), (2, 37, 19), (7, 1541, 333), (8, 4096, 16), (9, 64, 130), (16, 5120, 40), (17, 5120, 40), (33, 65, 257),
+         (64, 8, 8), (127, 1000, 129), (128, 128, 128), (129, 63, 300), (256, 256, 256), (257, 1541, 513), (300, 4099, 96), (513, 512, 1536), (700, 9000, 333),
+         (1100, 200, 5000), (5003, 100, 2100)]
+
+
+@pytest.mark.parametrize("N,K,M", SIZES)
+def test_every_size(N, K, M):
+    t = make(1, N, K, M, seed=N + K + M)
+    y, z = forward(t, cn.ACT_GELU_TANH)
+    check_forward(t, cn.ACT_GELU_TANH, y, z)
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("B,N", [(3, 1), (2, 6), (2, 150), (3, 301)])
+@pytest.mark.parametrize("y,p", [("bf16", "f32"), ("f32", "bf16")])
+@pytest.mark.parametrize("extra", [0, 1])
+def test_activations_types_and_entries(act, B, N, y, p, extra):
+    """extra = 1: a padded batch, whose entries do not follow each other evenly."""
+    t = make(B, N, 200, 264, y, p, seed=N, extra=extra)
+    out, z = forward(t, act, extra=extra)
+    check_forward(t, act, out, z)
+    g = backward(t, z, act, extra=extra)
+    check_backward(t, z, act, g)
+
+
+@pytest.mark.parametrize("bias,gate,residual", [(False, False, False), (True, False, False), (False, True, False), (False, False, True)])
+@pytest.mark.parametrize("N", [3, 200])
+def test_parts_that_are_left_out(bias, gate, residual, N):
+    t = make(2, N, 130, 96, bias=bias, gate=gate, residual=residual)
+    for act in (cn.ACT_NONE, cn.ACT_SILU):
+        y, _ = forward(t, act, keep=False)
+        check_forward(t, act, y)
+
+
+GRAD_SIZES = [(1, 1, 1), (1, 300, 200), (2, 37, 19), (17, 1541, 333), (64, 64, 64), (129, 65, 257), (300, 96, 4099), (333, 1000, 1541), (700, 513, 129),
+              (2500, 200, 264), (9001, 64, 130), (6000, 1500, 2100)]
+
+
+@pytest.mark.parametrize("N,K,M", GRAD_SIZES)
+@pytest.mark.parametrize("act,gate,dy", [(cn.ACT_GELU, True, "f32"), (cn.ACT_NONE, False, "bf16"), (cn.ACT_GELU_TANH, False, "bf16")])
+def test_gradients_of_every_size(N, K, M, act, gate, dy):
+    t = make(1, N, K, M, dy, gate=gate, seed=N)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    z = padded((1, N, M), torch.bfloat16, gen, 1.5, extra=1)
+    g = backward(t, z, act)
+    check_backward(t, z, act, g)
+
+
+def test_only_what_is_wanted():
+    t = make(2, 150, 96, 200)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    z = padded((2, 150, 200), torch.bfloat16, gen, extra=1)
+    full = backward(t, z, cn.ACT_SILU)
+    for need, want in ((("x",), ()), (("w",), ("bias",)), ((), ("gate",)), ((), ("bias", "gate")), (("x", "w"), ())):
+        g = backward(t, z, cn.ACT_SILU, need, want)
+        for name, on in (("dX", "x" in need), ("dW", "w" in need), ("dbias", "bias" in want), ("dgate", "gate" in want)):
+            got = getattr(g, name)
+            assert (got is not None) == on and (not on or torch.equal(got, getattr(full, name)))
+    plain = {**t, "gate": None}
+    g = backward(plain, None, cn.ACT_NONE)        # no pre-activation is needed
+    check_backward(plain, None, cn.ACT_NONE, g)
+
+
+@pytest.mark.parametrize("N", [5, 300])
+@pytest.mark.parametrize("y", ["bf16", "f32"])
+def test_residual_stream_in_place(N, y):
+    t = make(1, N, 256, 384, y)
+    ref, _ = forward(t, cn.ACT_NONE)
+    stream = t["residual"]
+    s = cn.make_linear_shape(t["x"], t["w"], stream, residual=stream, bias=t["bias"], gate=t["gate"])
+    cn.linear(t["x"], t["w"], s, bias=t["bias"], gate=t["gate"], residual=stream, Y=stream)
+    assert torch.equal(stream, ref)
+
+
+@pytest.mark.parametrize("N", [4, 200])
+def test_far_arguments_and_values_that_are_not_finite(N):
+    """The activations at +-1e4 (their limits), and rows that are not finite keep to themselves."""
+    t = make(1, N, 64, 128, "f32", bias=False, gate=False, residual=False)
+    t["x"] *= 1e4
+    for act in ACTS:
+        y, z = forward(t, act)
+        check_forward(t, act, y, z)
+        z = z.clone()
+        g = backward(t, z, act)
+        check_backward(t, z, act, g)
+    clean = forward(t, cn.ACT_NONE)[0].clone()
+    t["x"][0, 1, 5] = float("nan")
+    y = forward(t, cn.ACT_NONE)[0]
+    keep = [i for i in range(N) if i != 1]
+    assert torch.equal(y[:, keep], clean[:, keep]) and torch.isnan(y[0, 1]).all()
+
+
+def test_activation_over_its_range():
+    """z = bias exactly (x = 0): the epilogue's activation alone, fp32 out, against 64 bits."""
+    M = 4096
+    x, w = torch.zeros((1, 40, 64), dtype=torch.bfloat16, device="cuda"), torch.zeros((M, 64), dtype=torch.bfloat16, device="cuda")
+    bias = torch.linspace(-30, 30, M, device="cuda")
+    y = torch.empty((1, 40, M), device="cuda")
+    for act in ACTS:
+        s = cn.make_linear_shape(x, w, y, bias=bias, activation=act)
+        cn.linear(x, w, s, bias=bias, Y=y)
+        ref = act64(bias.double(), act).expand(1, 40, M)
+        check(y, ref, (ACT_ERR * (bias.double().abs() + 1) if act else 0) + U32 * ref.abs(), f"activation {act}")
+
+
+def test_gradients_against_differences():
+    """<dy, y> against <gradient, direction>, central differences of the forward call with fp32 output.  x and w lie on a grid of 2^-6 and
+    move by one step of it, which bf16 holds exactly below 4."""
+    B, N, K, M, act, h = 2, 40, 72, 88, cn.ACT_GELU_TANH, 2.0 ** -6
+    t = make(B, N, K, M, "f32", "f32", residual=False, seed=4, extra=0)
+    for k in ("x", "w"):
+        t[k].copy_((t[k].float() / h).round().clamp(-64, 64) * h)
+    _, z = forward(t, act, extra=0)
+    g = backward(t, z, act, extra=0)
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    for name, grad in (("x", g.dX), ("w", g.dW), ("bias", g.dbias), ("gate", g.dgate)):
+        v = torch.randint(0, 2, t[name].shape, device="cuda", generator=gen) * 2.0 - 1
+        loss = []
+        for sign in (1, -1):
+            u = dict(t)
+            u[name] = (t[name].float() + sign * h * v).to(t[name].dtype)
+            loss.append((forward(u, act, extra=0)[0].double() * t["dy"].double()).sum())
+        slope, ref = (loss[0] - loss[1]) / (2 * h), (grad.double() * v.double()).sum()
+        # The backward call sees z rounded to bf16 (independent errors of at most U16 |z|) and rounds dz and the bf16 gradients: sums of independent
+        # terms, taken as six times their 2-norm.  `along` is how z moves along the direction; for the gate it is act(z) that is read.
+        dy, zz, gate, vd = t["dy"].double(), z.double(), t["gate"].double()[:, None], v.double()
+        along = {"x": lambda: vd @ t["w"].double().T, "w": lambda: t["x"].double() @ vd.T, "bias": lambda: vd.expand_as(zz), "gate": lambda: vd[:, None].expand_as(zz)}[name]()
+        if name == "gate":               # the loss is linear in the gate: no higher terms; the first slope is at most 1.13
+            noise, third = 6 * U16 * SLOPE_MOST * (dy * zz * along).norm(), 0
+        else:                            # second derivative at most 1.2, third at most 2
+            noise = 6 * U16 * (1.2 * (dy * gate * zz * along).norm() + SLOPE_MOST * (dy * gate * along).norm() + (grad.double().norm() if grad.dtype == torch.bfloat16 else 0))
+            third = h * h / 6 * 2 * ((dy * gate).abs() * along.abs() ** 3).sum()
+        _, _, _, ey = linear_ref(t["x"], t["w"], t["bias"], t["gate"], None, act)      # errors of the two forward calls
+        noise = noise + 6 * (dy * ey).norm() / h
+        assert abs(slope - ref) <= noise + third + 1e-5 * abs(ref), (name, float(slope), float(ref))
+
+
+@pytest.mark.parametrize("N,K,M", [(2, 1536, 1536), (300, 4099, 96), (3000, 256, 1300)])
+def test_same_bits_again_streams_graphs_and_two_calls_at_once(N, K, M):
+    t = make(1, N, K, M, "f32")
+    act = cn.ACT_GELU
+    y0, z0 = forward(t, act)
+    g0 = backward(t, z0, act)
+    y1, z1 = forward(t, act)
+    g1 = backward(t, z1, act)
+    assert torch.equal(y0, y1) and torch.equal(z0, z1) and all(torch.equal(a, b) for a, b in zip(g0, g1))
+
+    def plan():
+        y, z, dx, dw = (canvas(a.shape, a.dtype)[1] for a in (t["dy"], z0, t["x"], t["w"]))
+        fs = cn.make_linear_shape(t["x"], t["w"], y, residual=t["residual"], Z=z, bias=t["bias"], gate=t["gate"], activation=act)
+        bs = cn.make_linear_shape(t["x"], t["w"], t["dy"], Z=z, gate=t["gate"], dX=dx, dW=dw, activation=act)
+        ws = torch.empty(max(cn.linear_workspace_bytes(fs), cn.linear_backward_workspace_bytes(bs)), dtype=torch.uint8, device="cuda")
+
+        def run():
+            cn.linear(t["x"], t["w"], fs, bias=t["bias"], gate=t["gate"], residual=t["residual"], Y=y, Z=z, ws=ws)
+            return (y, z, *cn.linear_backward(t["dy"], t["x"], t["w"], bs, Z=z, gate=t["gate"], dX=dx, dW=dw, ws=ws))
+        return run
+
+    want = (y0, z0, *g0)
+    streams, plans = [torch.cuda.Stream() for _ in range(2)], [plan(), plan()]
+    got = []
+    for st, run in zip(streams, plans):
+        st.wait_stream(torch.cuda.current_stream())
+    for st, run in zip(streams, plans):
+        with torch.cuda.stream(st):
+            got.append(run())
+    torch.cuda.synchronize()
+    for out in got:
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
+    run = plan()
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = run()
+    for _ in range(2):
+        for o in out:
+            o.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
