@@ -1005,6 +1005,9 @@ bool axes_ok(const int64_t* stride, const int64_t* size, int n, int64_t row, int
     }
     return true;
 }
+bool rows32(const void* p, const int64_t st[2], int32_t dtype) {      // whether every row starts on a 32-byte boundary
+    return !p || (aligned(p, 32) && st[0] % (2 * dtype_unit(dtype)) == 0 && st[1] % (2 * dtype_unit(dtype)) == 0);
+}
 bool vec16(const void* p, int64_t stride, int32_t dtype) { return !p || (aligned(p, 16) && stride % dtype_unit(dtype) == 0); }
 
 carnator_status check_norm_shape(const carnator_norm_shape* s) {
@@ -1146,6 +1149,7 @@ GradWs grad_ws_layout(void* base, const carnator_linear_shape* s) {
 void plain_epilogue(lin::Epilogue& e, void* y, int64_t batch_stride, int64_t row_stride) {
     e = {};
     e.y = y; e.ys[0] = batch_stride; e.ys[1] = row_stride; e.rows_per_gate = 1;
+    e.wide_ok = rows32(y, e.ys, CARNATOR_DTYPE_BF16);
 }
 }  // namespace
 
@@ -1174,6 +1178,8 @@ extern "C" carnator_status carnator_linear(const void* X, const void* W, const v
     e.act = s->activation; e.y_f32 = s->y_dtype == CARNATOR_DTYPE_F32;
     e.bias_f32 = s->bias_dtype == CARNATOR_DTYPE_F32; e.gate_f32 = s->gate_dtype == CARNATOR_DTYPE_F32;
     e.vec_ok = vec16(bias, 0, s->bias_dtype) && vec16(gate, s->gate_stride, s->gate_dtype);
+    e.wide_ok = e.vec_ok && rows32(Y, s->y_stride, s->y_dtype) && rows32(Z_opt, s->z_stride, CARNATOR_DTYPE_BF16) &&
+                rows32(residual, s->residual_stride, s->y_dtype);
     e.rows_per_gate = s->N;
     const int64_t rows = int64_t(s->B) * s->N;
     if (rows <= lin::kRowsMost) {

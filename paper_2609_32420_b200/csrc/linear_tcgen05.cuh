@@ -10,8 +10,10 @@
 //
 // Warp roles (384 threads, one CTA per SM): warp 0 TMA producer; warp 1 (of the pair's first CTA) MMA issue; warp 2 tensor-memory
 // allocation; warps 4-11 epilogue.
-// The epilogue turns 32 x 32 pieces through shared memory, so that bias, gate and residual are read and y and z written as
-// whole 64- or 128-byte runs of a row.
+// The epilogue stays in registers: a lane holds a row's 32 columns and reads the residual and writes y and z in whole 32-byte sectors of its row.
+// (Turned through shared memory, so that a warp's access covers runs of a row, the same bytes cost the product its operands: the ring's writes
+// and the reads of the products take nearly all of the 128 bytes a clock that shared memory has.  32760 x 1536 x 8960 with z and
+// GELU 754 us that way.)
 // Few tiles: 2 or 4 pairs of one cluster take a share of k each and add their partial tiles through distributed shared memory, in
 // the order of k: no workspace, no atomics, the same bits every time.
 // Every wait on an mbarrier is bounded, as in the attention kernel.
@@ -31,10 +33,8 @@ constexpr int kTileM = 256;              // rows of a pair's tile
 constexpr int kTileK = 64;               // one 128-byte swizzle row of bf16
 constexpr int kMaxStages = 8;
 constexpr uint32_t kABytes = 128 * kTileK * 2;       // a CTA's share of A per stage
-constexpr int kPieceStride = 36;         // floats per row of a 32 x 32 piece: rows start 4 banks apart
-constexpr uint32_t kPieceBytes = 32 * kPieceStride * 4;
-constexpr uint32_t kStageBudget = 232448 - 256 - 1024 - 512 - kEpiWarps * kPieceBytes;     // of the 227 KB, less the static shared memory: ring of stages
-constexpr uint32_t kSmemTc = kStageBudget + 1024 + 512 + kEpiWarps * kPieceBytes;
+constexpr uint32_t kStageBudget = 232448 - 256 - 1024 - 512;     // of the 227 KB, less the static shared memory: ring of stages
+constexpr uint32_t kSmemTc = kStageBudget + 1024 + 512;
 
 enum { kActNone = 0, kActGeluTanh = 1, kActGelu = 2, kActSilu = 3 };
 
@@ -44,6 +44,7 @@ struct Epilogue {
     const void* bias; const void* gate; const void* residual;
     int64_t ys[2], zs[2], rs[2], gate_stride;      // (batch, row)
     int act, y_f32, bias_f32, gate_f32, vec_ok;
+    int wide_ok;                         // y, z and residual: rows start on 32-byte boundaries; bias and gate on 16
     int rows_per_gate;                   // rows that share a gate row (batch entries that follow each other evenly are one)
 };
 
@@ -55,6 +56,7 @@ struct TcArgs {
     int group_m;                         // row tiles that are worked through together, column by column
     int bn;                              // columns of a tile, a multiple of 32 (of 128 where B is MN-major)
     int k_batches, k_tiles;              // k: batch entries (dW) x tiles of 64
+    int a_slabs, b_slabs;                // MN-major operand fetched as 64-column slabs by one copy (0: a copy per slab)
     int stages, splits;
 };
 
@@ -67,14 +69,21 @@ __device__ __forceinline__ uint32_t map_cta(uint32_t addr, uint32_t rank) {
 __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+// What it orders are reads of tensor memory that have completed: CTA scope.  (Releasing at cluster scope waits for the thread's earlier
+// stores to global memory.)
 __device__ __forceinline__ void arrive_remote(uint32_t cluster_bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+    asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
 // the copy lands in this CTA and counts on the barrier of the pair's first CTA
 __device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap* map, uint32_t cluster_bar, int c0, int c1, int c2) {
     asm volatile(
         "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
         ::"r"(dst), "l"(map), "r"(cluster_bar), "r"(c0), "r"(c1), "r"(c2) : "memory");
+}
+__device__ __forceinline__ void tma_load_pair_slabs(uint32_t dst, const CUtensorMap* map, uint32_t cluster_bar, int row, int slab, int batch) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+        ::"r"(dst), "l"(map), "r"(cluster_bar), "r"(0), "r"(row), "r"(slab), "r"(batch) : "memory");
 }
 __device__ __forceinline__ void mma_pair_el(uint32_t d_tmem, uint64_t da, uint64_t db, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
@@ -154,6 +163,86 @@ __device__ __forceinline__ void finish(const Epilogue& e, Columns& c, int b, int
     else norm::store8<false>(e.y, off, v, n);
 }
 
+// 32 bytes: a whole sector per lane.  No clobber of memory: a residual is read by the lane that writes y over it, before.
+struct Sector { uint32_t q[8]; };
+__device__ __forceinline__ Sector load_sector(const void* p) {
+    Sector s;
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];" : "=r"(s.q[0]), "=r"(s.q[1]), "=r"(s.q[2]), "=r"(s.q[3]),
+                 "=r"(s.q[4]), "=r"(s.q[5]), "=r"(s.q[6]), "=r"(s.q[7]) : "l"(p));
+    return s;
+}
+__device__ __forceinline__ void store_sector(void* p, const Sector& s) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(s.q[0]), "r"(s.q[1]), "r"(s.q[2]), "r"(s.q[3]),
+                 "r"(s.q[4]), "r"(s.q[5]), "r"(s.q[6]), "r"(s.q[7]));
+}
+__device__ __forceinline__ Sector pack16(const float (&v)[16]) {
+    Sector s;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s.q[i] = norm::pack_bf16(v[2 * i], v[2 * i + 1]);
+    return s;
+}
+// 16 values of a parameter vector that starts on a 16-byte boundary
+__device__ __forceinline__ void load_param16(const void* base, int64_t off, int f32, float (&v)[16]) {
+    float a[8], b[8];
+    norm::load_param8(base, off, f32, 1, 8, a);
+    norm::load_param8(base, off + 8, f32, 1, 8, b);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { v[i] = a[i]; v[8 + i] = b[i]; }
+}
+// Epilogue of 16 columns of one row, all of them there and everything aligned (wide_ok).  `gate`: the entry's gate row or NULL;
+// `res`: the residual's sectors (one of bf16, two of fp32), loaded before.
+template <bool YF>
+__device__ __forceinline__ void finish16(const Epilogue& e, const void* gate, int64_t gate_off, int64_t y_off, int64_t z_off, int col, float (&v)[16],
+                                         const Sector& r0, const Sector& r1) {
+    if (e.bias) {
+        float t[16];
+        load_param16(e.bias, col, e.bias_f32, t);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] += t[i];
+    }
+    if (e.z) store_sector(static_cast<__nv_bfloat16*>(e.z) + z_off + col, pack16(v));
+    switch (e.act) {
+        case kActGeluTanh:
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i] = activation<kActGeluTanh>(v[i]);
+            break;
+        case kActGelu:
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i] = activation<kActGelu>(v[i]);
+            break;
+        case kActSilu:
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i] = activation<kActSilu>(v[i]);
+            break;
+        default: break;
+    }
+    if (gate) {
+        float t[16];
+        load_param16(gate, gate_off + col, e.gate_f32, t);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] *= t[i];
+    }
+    if (e.residual) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (YF) { v[i] += __uint_as_float(r0.q[i]); v[8 + i] += __uint_as_float(r1.q[i]); }
+            else { float lo, hi; norm::bf16x2_to_float(r0.q[i], lo, hi); v[2 * i] += lo; v[2 * i + 1] += hi; }
+        }
+    }
+    if (YF) {
+        float* p = static_cast<float*>(e.y) + y_off + col;
+        Sector s;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s.q[i] = __float_as_uint(v[8 * h + i]);
+            store_sector(p + 8 * h, s);
+        }
+    } else {
+        store_sector(static_cast<__nv_bfloat16*>(e.y) + y_off + col, pack16(v));
+    }
+}
+
 // Tile t of the launch: group_m row tiles are worked through column by column, so that what runs at one time shares rows of A
 // and of B in L2.
 __device__ __forceinline__ void tile_at(const TcArgs& a, int t, int& b, int& m, int& n) {
@@ -173,7 +262,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
     __shared__ int abort_flag;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t base = (smem_u32(lin_smem) + 1023u) & ~1023u;
-    const uint32_t pieces = base + kStageBudget, bars = pieces + kEpiWarps * kPieceBytes;
+    const uint32_t bars = base + kStageBudget;
     const uint32_t rank = cluster_ctarank(), half = rank & 1u, leader = rank & ~1u, split = rank >> 1;
     const uint32_t b_bytes = uint32_t(a.bn / 2) * kTileK * 2, stage_bytes = kABytes + b_bytes;
     auto bar_full = [&](int s) { return bars + 8 * s; };                       // used in the pair's first CTA: both CTAs' copies have landed
@@ -226,13 +315,17 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
                     }
                     if (half == 0) mbar_expect_tx(bar_full(s), 2 * stage_bytes);
                     const uint32_t sa = base + uint32_t(s) * stage_bytes, sb = sa + kABytes, bar = full0 + 8 * s;
-                    if (AMN) {           // 64 columns of m x 64 rows of k, twice
+                    if (AMN && a.a_slabs) {
+                        tma_load_pair_slabs(sa, &mapA, bar, kt * kTileK, m0 / 64, kb);
+                    } else if (AMN) {    // 64 columns of m x 64 rows of k, twice
                         tma_load_pair(sa, &mapA, bar, m0, kt * kTileK, kb);
                         tma_load_pair(sa + kABytes / 2, &mapA, bar, m0 + 64, kt * kTileK, kb);
                     } else {
                         tma_load_pair(sa, &mapA, bar, kt * kTileK, m0, b);
                     }
-                    if (BMN) {
+                    if (BMN && a.b_slabs) {
+                        tma_load_pair_slabs(sb, &mapB, bar, kt * kTileK, n0 / 64, kb);
+                    } else if (BMN) {
                         for (int c = 0; c < a.bn / 2; c += 64)
                             tma_load_pair(sb + uint32_t(c) * 128, &mapB, bar, n0 + c, kt * kTileK, kb);
                     } else {
@@ -291,11 +384,9 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
         }
     } else if (warp >= 4) {
         // ================= epilogue =================
-        const int w = warp - 4, quarter = warp & 3, side = w >> 2;         // rows 32 quarter .. of this CTA's 128; every other piece of 32 columns
+        const int quarter = warp & 3, side = (warp - 4) >> 2;               // rows 32 quarter .. of this CTA's 128; every other 32 columns
         const uint32_t lane_base = uint32_t(quarter * 32) << 16;
-        const uint32_t piece = pieces + uint32_t(w) * kPieceBytes;
         const uint32_t read0 = map_cta(bar_read(0), leader);
-        const int sub_row = lane >> 2, sub_col = (lane & 3) * 8;
         bool ok = true;
         int i = 0;
         if (a.splits == 1) {
@@ -303,44 +394,63 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
                 const int u = i & 1;
                 int b, m, n;
                 tile_at(a, t, b, m, n);
-                const int row0 = m * kTileM + int(half) * 128 + quarter * 32, left = min(a.cols - n * a.bn, a.bn);
+                const int row = m * kTileM + int(half) * 128 + quarter * 32 + lane, left = min(a.cols - n * a.bn, a.bn);
+                const bool on = row < a.rows;
+                const int64_t y_off = b * a.e.ys[0] + row * a.e.ys[1], z_off = b * a.e.zs[0] + row * a.e.zs[1], r_off = b * a.e.rs[0] + row * a.e.rs[1];
+                const int64_t gate_off = a.e.gate ? (b + row / a.e.rows_per_gate) * a.e.gate_stride : 0;
+                const char* res = static_cast<const char*>(a.e.residual) + (r_off + n * a.bn) * (a.e.y_f32 ? 4 : 2);
                 ok = mbar_wait_warp(bar_done(u), uint32_t(i >> 1) & 1u, abortp, 20, limit);
                 if (!ok) { if (lane == 0) set_status(a.hdr, CARNATOR_ERR_DEVICE_TIMEOUT, 74, i, blockIdx.x); break; }
                 tc_fence_after();
                 for (int c = side * 32; c < left; c += 64) {               // warp-uniform
-                    const int col = n * a.bn + c + sub_col, cn = min(max(a.cols - col, 0), 8);
-                    norm::Raw8<true> res[4];
-                    if (a.e.residual)
-#pragma unroll
-                        for (int p = 0; p < 4; ++p) {
-                            const int row = row0 + p * 8 + sub_row;
-                            load_residual(a.e, b, row, col, row < a.rows ? cn : 0, res[p]);
-                        }
-                    Columns cols;
-                    columns_begin(a.e, cols, col, cn);
+                    const int col = n * a.bn + c;
+                    const bool wide = a.e.wide_ok && c + 32 <= left;
+                    Sector r0, r1, r2, r3;
+                    if (a.e.residual && wide && on) {
+                        const char* p = res + c * (a.e.y_f32 ? 4 : 2);
+                        r0 = load_sector(p); r1 = load_sector(p + 32);
+                        if (a.e.y_f32) { r2 = load_sector(p + 64); r3 = load_sector(p + 96); }
+                    }
                     float v[32];
                     tmem_ld32(tmem + lane_base + uint32_t(u * 256 + c), v);
                     tmem_wait_ld(v);
-                    __syncwarp();
+                    if (c + 64 >= left) {       // this warp has read its part of the tile
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) arrive_remote(read0 + 8 * u);
+                    }
+                    if (wide) {
+                        float lo[16], hi[16];
 #pragma unroll
-                    for (int q = 0; q < 8; ++q)
-                        asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(piece + uint32_t(lane * kPieceStride + 4 * q) * 4u),
-                                     "f"(v[4 * q]), "f"(v[4 * q + 1]), "f"(v[4 * q + 2]), "f"(v[4 * q + 3]) : "memory");
-                    __syncwarp();
+                        for (int q = 0; q < 16; ++q) { lo[q] = v[q]; hi[q] = v[16 + q]; }
+                        if (on && a.e.y_f32) {
+                            finish16<true>(a.e, a.e.gate, gate_off, y_off, z_off, col, lo, r0, r1);
+                            finish16<true>(a.e, a.e.gate, gate_off, y_off, z_off, col + 16, hi, r2, r3);
+                        } else if (on) {
+                            finish16<false>(a.e, a.e.gate, gate_off, y_off, z_off, col, lo, r0, r0);
+                            finish16<false>(a.e, a.e.gate, gate_off, y_off, z_off, col + 16, hi, r1, r1);
+                        }
+                    } else if (on) {
 #pragma unroll
-                    for (int p = 0; p < 4; ++p) {
-                        const int r = p * 8 + sub_row, row = row0 + r;
-                        float f[8];
+                        for (int h = 0; h < 4; ++h) {
+                            const int cn = min(max(left - c - 8 * h, 0), 8);
+                            if (cn > 0) {
+                                norm::Raw8<true> r8;
+                                Columns cols;
+                                columns_begin(a.e, cols, col + 8 * h, cn);
+                                if (a.e.residual) load_residual(a.e, b, row, col + 8 * h, cn, r8);
+                                float f[8];
 #pragma unroll
-                        for (int q = 0; q < 2; ++q)
-                            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(f[4 * q]), "=f"(f[4 * q + 1]), "=f"(f[4 * q + 2]), "=f"(f[4 * q + 3])
-                                         : "r"(piece + uint32_t(r * kPieceStride + sub_col + 4 * q) * 4u) : "memory");
-                        if (row < a.rows && cn > 0) finish(a.e, cols, b, row, col, cn, f, res[p]);
+                                for (int q = 0; q < 8; ++q) f[q] = v[8 * h + q];
+                                finish(a.e, cols, b, row, col + 8 * h, cn, f, r8);
+                            }
+                        }
                     }
                 }
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) arrive_remote(read0 + 8 * u);
+                if (side * 32 >= left) {
+                    __syncwarp();
+                    if (lane == 0) arrive_remote(read0 + 8 * u);
+                }
             }
         } else {
             // partial tile to shared memory (every stage has been read by now: bar_done follows the last product)
@@ -420,11 +530,26 @@ inline bool make_map_3d(CUtensorMap* map, const void* base, int64_t batches, int
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The same for an MN-major operand of whole 64-column slabs: the columns as two dimensions, a box = 64 x 64 rows x `slabs` slabs, each
+// slab landing as make_map_3d's box would.  One copy of 16 KB instead of two of 8: with two, dX and dW of 32760 x 1536 x 8960 took 637 and 650 us
+// instead of 597 and 583.
+inline bool make_map_slabs(CUtensorMap* map, const void* base, int64_t batches, int64_t rows, int64_t cols, int64_t batch_stride, int64_t row_stride, int slabs) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    cuuint64_t dims[4] = {64, cuuint64_t(rows), cuuint64_t(cols / 64), cuuint64_t(batches)};
+    const cuuint64_t row = rows > 1 ? cuuint64_t(row_stride) * 2 : cuuint64_t(cols) * 2;
+    cuuint64_t strides[3] = {row, 128, batches > 1 ? cuuint64_t(batch_stride) * 2 : row};
+    cuuint32_t box[4] = {64, kTileK, cuuint32_t(slabs), 1};
+    cuuint32_t estr[4] = {1, 1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // A bf16 operand as [batches, rows, cols].
 struct Operand { const void* base; int64_t batches, rows, cols, batch_stride, row_stride; };
 
-// Columns of a tile and pairs that share one.  Time of a launch in units of one column of 256 rows: the turns that the pairs of 148 SMs take, times a tile's columns (a tile
-// narrower than 128 columns waits for shared memory instead: its A operand costs as much to read) times its share of k.
+// Columns of a tile and pairs that share one: the least time of a launch in units of one column of 256 rows and 64 of k, which is the turns that the
+// pairs of 148 SMs take, times a tile's share of k, times what 64 of k cost.
 struct Plan { int bn, splits; };
 inline Plan plan_of(int64_t m_tiles, int64_t cols, int64_t k_all, bool b_mn) {
     Plan best = {256, 1};
@@ -435,8 +560,8 @@ inline Plan plan_of(int64_t m_tiles, int64_t cols, int64_t k_all, bool b_mn) {
             if (splits > 1 && (tiles * splits > 72 || k_all < 4 * splits || bn % (8 * splits))) break;
             const int64_t pairs = std::min<int64_t>(74, tiles * splits);
             const double turns = double((tiles * splits + pairs - 1) / pairs);
-            // per tile of k: the product, and what an SM takes to fetch its operands from L2; per tile: filling and draining
-            const double cost = turns * ((double(k_all) / splits) * std::max(bn, 112) + (splits > 1 ? 500 + 2 * bn : 400 + bn));
+            // per tile of k: the product, or what an SM takes to fetch its operands from L2 (68 bytes a clock); per tile: filling and draining
+            const double cost = turns * ((double(k_all) / splits) * std::max(double(bn), 0.47 * (256 + bn)) + (splits > 1 ? 500 + 2 * bn : 400 + bn));
             if (cost < best_cost * 0.995) { best_cost = cost; best = {bn, splits}; }
         }
     }
@@ -455,8 +580,12 @@ inline carnator_status launch_tc_product(const Operand& A, const Operand& B, TcA
     const uint32_t stage = kABytes + uint32_t(a.bn / 2) * kTileK * 2;
     a.stages = int(std::min<uint32_t>(kMaxStages, kStageBudget / stage));
     CUtensorMap ma, mb;
-    if (!make_map_3d(&ma, A.base, A.batches, A.rows, A.cols, A.batch_stride, A.row_stride, AMN ? kTileK : 128) ||
-        !make_map_3d(&mb, B.base, B.batches, B.rows, B.cols, B.batch_stride, B.row_stride, BMN ? kTileK : a.bn / 2)) {
+    a.a_slabs = AMN && A.cols % 64 == 0;          // the last slab of another width would be read past the row
+    a.b_slabs = BMN && B.cols % 64 == 0;
+    if (!(a.a_slabs ? make_map_slabs(&ma, A.base, A.batches, A.rows, A.cols, A.batch_stride, A.row_stride, 2)
+                    : make_map_3d(&ma, A.base, A.batches, A.rows, A.cols, A.batch_stride, A.row_stride, AMN ? kTileK : 128)) ||
+        !(a.b_slabs ? make_map_slabs(&mb, B.base, B.batches, B.rows, B.cols, B.batch_stride, B.row_stride, a.bn / 128)
+                    : make_map_3d(&mb, B.base, B.batches, B.rows, B.cols, B.batch_stride, B.row_stride, BMN ? kTileK : a.bn / 2))) {
         snprintf(err, errlen, "cuTensorMapEncodeTiled failed or is unavailable");
         return CARNATOR_ERR_CUDA;
     }
