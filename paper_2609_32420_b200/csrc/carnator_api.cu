@@ -1206,7 +1206,7 @@ extern "C" carnator_status carnator_linear(const void* X, const void* W, const v
     const lin::Operand Bo = {W, 1, s->out_features, s->in_features, 0, s->w_stride};
     a.cols = s->out_features;
     a.tiles_m = ceil_div(a.rows, lin::kTileM);
-    a.k_batches = 1; a.k_tiles = ceil_div(s->in_features, lin::kTileK);
+    a.k_batches = 1; a.k_len = s->in_features;
     st = lin::launch_tc_product<0, 0>(A, Bo, a, stream, g_cuda_error, sizeof(g_cuda_error));
     if (st == CARNATOR_OK) g_launches.fetch_add(1, std::memory_order_relaxed);
     return st;
@@ -1282,7 +1282,7 @@ extern "C" carnator_status carnator_linear_backward(const void* dY, const void* 
             const lin::Operand Bo = {W, 1, s->out_features, s->in_features, 0, s->w_stride};
             plain_epilogue(a.e, dX_opt, s->dx_stride[0], one_run ? run_stride(s, s->dx_stride) : s->dx_stride[1]);
             a.batches = int(A.batches); a.rows = int(A.rows);
-            a.k_batches = 1; a.k_tiles = ceil_div(s->out_features, lin::kTileK);
+            a.k_batches = 1; a.k_len = s->out_features;
             a.tiles_m = ceil_div(a.rows, lin::kTileM);
             st = lin::launch_tc_product<0, 1>(A, Bo, a, stream, g_cuda_error, sizeof(g_cuda_error));
         } else {
@@ -1290,7 +1290,7 @@ extern "C" carnator_status carnator_linear_backward(const void* dY, const void* 
             if (one_run) { Bo.batches = 1; Bo.rows = rows; Bo.row_stride = run_stride(s, s->x_stride); }
             plain_epilogue(a.e, dW_opt, 0, s->dw_stride);
             a.batches = 1; a.rows = s->out_features;
-            a.k_batches = int(A.batches); a.k_tiles = ceil_div(int(A.rows), lin::kTileK);
+            a.k_batches = int(A.batches); a.k_len = int(A.rows);
             a.tiles_m = ceil_div(a.rows, lin::kTileM);
             st = lin::launch_tc_product<1, 1>(A, Bo, a, stream, g_cuda_error, sizeof(g_cuda_error));
         }

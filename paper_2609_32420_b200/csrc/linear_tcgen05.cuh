@@ -30,11 +30,11 @@ using namespace tc;
 constexpr int kThreadsTc = 384;
 constexpr int kEpiWarps = 8;
 constexpr int kTileM = 256;              // rows of a pair's tile
-constexpr int kTileK = 64;               // one 128-byte swizzle row of bf16
+constexpr int kSlab = 64;                // columns of a slab: one 128-byte swizzle row of bf16
 constexpr int kMaxStages = 8;
-constexpr uint32_t kABytes = 128 * kTileK * 2;       // a CTA's share of A per stage
-constexpr uint32_t kStageBudget = 232448 - 256 - 1024 - 512;     // of the 227 KB, less the static shared memory: ring of stages
-constexpr uint32_t kSmemTc = kStageBudget + 1024 + 512;
+constexpr uint32_t kRingBytes = 225 * 1024;          // stages
+constexpr uint32_t kSmemTc = kRingBytes + 512 + 1024;      // barriers, slack to align the base to 1 KB
+static_assert(kSmemTc + 256 <= 232448, "shared memory of a CTA");
 
 enum { kActNone = 0, kActGeluTanh = 1, kActGelu = 2, kActSilu = 3 };
 
@@ -56,7 +56,8 @@ struct TcArgs {
     int group_m;                         // row tiles that are worked through together, column by column
     int bn;                              // columns of a tile, a multiple of 32 (of 128 where B is MN-major)
     int k_batches, k_tiles;              // k: batch entries (dW) x tiles of 64
-    int a_slabs, b_slabs;                // MN-major operand fetched as 64-column slabs by one copy (0: a copy per slab)
+    int k_len;                           // k of a batch entry
+    int a_slabs, b_slabs;                // MN-major: the slabs of a stage in one copy (0: a copy per slab)
     int stages, splits;
 };
 
@@ -85,12 +86,13 @@ __device__ __forceinline__ void tma_load_pair_slabs(uint32_t dst, const CUtensor
         "cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
         ::"r"(dst), "l"(map), "r"(cluster_bar), "r"(0), "r"(row), "r"(slab), "r"(batch) : "memory");
 }
-__device__ __forceinline__ void mma_pair_el(uint32_t d_tmem, uint64_t da, uint64_t db, uint32_t idesc, uint32_t accumulate) {
+__device__ __forceinline__ void mma_pair_el(uint32_t d_tmem, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
-        "{\n\t.reg .pred p, e;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "{\n\t.reg .pred p, e;\n\t.reg .b64 da, db;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+        "mov.b64 da, {%1, %2};\n\tmov.b64 db, {%3, %4};\n\t"
         "elect.sync _|e, 0xffffffff;\n\t"
-        "@e tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-        ::"r"(d_tmem), "l"(da), "l"(db), "r"(idesc), "r"(accumulate) : "memory");
+        "@e tcgen05.mma.cta_group::2.kind::f16 [%0], da, db, %5, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate) : "memory");
 }
 // arrives on the barrier at this offset in both CTAs of the pair once every product issued so far has completed
 __device__ __forceinline__ void commit_pair_el(uint32_t bar, uint16_t mask) {
@@ -254,15 +256,18 @@ __device__ __forceinline__ void tile_at(const TcArgs& a, int t, int& b, int& m, 
     m = mt - b * a.tiles_m;
 }
 
-template <int AMN, int BMN>
+// kSub: slabs of 64 columns of k per stage
+template <int AMN, int BMN, int kSub>
 __global__ void __launch_bounds__(kThreadsTc, 1)
 linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB, const TcArgs a) {
+    constexpr int kTileK = kSub * kSlab;                 // k of a stage
+    constexpr uint32_t kABytes = 128 * kTileK * 2;       // a CTA's share of A per stage
     extern __shared__ unsigned char lin_smem[];
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t base = (smem_u32(lin_smem) + 1023u) & ~1023u;
-    const uint32_t bars = base + kStageBudget;
+    const uint32_t bars = base + kRingBytes;
     const uint32_t rank = cluster_ctarank(), half = rank & 1u, leader = rank & ~1u, split = rank >> 1;
     const uint32_t b_bytes = uint32_t(a.bn / 2) * kTileK * 2, stage_bytes = kABytes + b_bytes;
     auto bar_full = [&](int s) { return bars + 8 * s; };                       // used in the pair's first CTA: both CTAs' copies have landed
@@ -278,19 +283,21 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
         for (int s = 0; s < kMaxStages; ++s) { mbar_init(bar_full(s), 1); mbar_init(bar_empty(s), 1); }
         for (int u = 0; u < 2; ++u) { mbar_init(bar_done(u), 1); mbar_init(bar_read(u), 2 * kEpiWarps); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        // the status word of the call: nothing sets it before its wait limit has passed, which is after this
-        if (blockIdx.x == 0) a.hdr->status = 0;
     }
     if (warp == 2) {
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }
     if (warp == 0 && lane == 0) { prefetch_tmap(&mapA); prefetch_tmap(&mapB); }
+    grid_launch_dependents();
     tc_fence_before();
     __syncwarp();
     cluster_sync();
     tc_fence_after();
     const uint32_t tmem = tmem_slot;
+    grid_wait();                         // launched while the kernel ahead drains: nothing of global memory is touched before this
+    // the status word of the call: nothing sets it before its wait limit has passed, which is after this
+    if (tid == 0 && blockIdx.x == 0) a.hdr->status = 0;
 
     // the clusters take the tiles in turn; with splits > 1 there is one cluster per tile and a pair has its share of k
     const int first = int(blockIdx.x / (2 * a.splits)), step = int(gridDim.x / (2 * a.splits));
@@ -309,27 +316,28 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
                 tile_at(a, t, b, m, n);
                 const int m0 = m * kTileM + int(half) * 128, n0 = n * a.bn + int(half) * (a.bn / 2);
                 int kb = k0 / a.k_tiles, kt = k0 - kb * a.k_tiles;
-                for (int k = k0; k < k1; ++k) {
+                for (int i = k0; i < k1; ++i) {
                     if (issued >= a.stages && !mbar_wait(bar_empty(s), phase ^ 1u, abortp, 0, limit)) {
-                        set_status(a.hdr, CARNATOR_ERR_DEVICE_TIMEOUT, 70, k, blockIdx.x); ok = false; break;
+                        set_status(a.hdr, CARNATOR_ERR_DEVICE_TIMEOUT, 70, i, blockIdx.x); ok = false; break;
                     }
                     if (half == 0) mbar_expect_tx(bar_full(s), 2 * stage_bytes);
                     const uint32_t sa = base + uint32_t(s) * stage_bytes, sb = sa + kABytes, bar = full0 + 8 * s;
-                    if (AMN && a.a_slabs) {
-                        tma_load_pair_slabs(sa, &mapA, bar, kt * kTileK, m0 / 64, kb);
-                    } else if (AMN) {    // 64 columns of m x 64 rows of k, twice
-                        tma_load_pair(sa, &mapA, bar, m0, kt * kTileK, kb);
-                        tma_load_pair(sa + kABytes / 2, &mapA, bar, m0 + 64, kt * kTileK, kb);
-                    } else {
-                        tma_load_pair(sa, &mapA, bar, kt * kTileK, m0, b);
+                    const int k = kt * kTileK;
+                    if (AMN) {           // two slabs of 64 columns of m, the stage's rows of k
+                        if (a.a_slabs) tma_load_pair_slabs(sa, &mapA, bar, k, m0 / kSlab, kb);
+                        else {
+                            tma_load_pair(sa, &mapA, bar, m0, k, kb);
+                            tma_load_pair(sa + kABytes / 2, &mapA, bar, m0 + kSlab, k, kb);
+                        }
+                    } else {             // slabs of 64 columns of k, 128 rows of m
+                        for (int c = 0; c < kSub; ++c) tma_load_pair(sa + c * (kABytes / kSub), &mapA, bar, k + c * kSlab, m0, b);
                     }
-                    if (BMN && a.b_slabs) {
-                        tma_load_pair_slabs(sb, &mapB, bar, kt * kTileK, n0 / 64, kb);
-                    } else if (BMN) {
-                        for (int c = 0; c < a.bn / 2; c += 64)
-                            tma_load_pair(sb + uint32_t(c) * 128, &mapB, bar, n0 + c, kt * kTileK, kb);
+                    if (BMN) {
+                        if (a.b_slabs) tma_load_pair_slabs(sb, &mapB, bar, k, n0 / kSlab, kb);
+                        else
+                            for (int c = 0; c < a.bn / 2; c += kSlab) tma_load_pair(sb + uint32_t(c) * kTileK * 2, &mapB, bar, n0 + c, k, kb);
                     } else {
-                        tma_load_pair(sb, &mapB, bar, kt * kTileK, n0, 0);
+                        for (int c = 0; c < kSub; ++c) tma_load_pair(sb + uint32_t(c) * (b_bytes / kSub), &mapB, bar, k + c * kSlab, n0, 0);
                     }
                     ++issued;
                     if (++s == a.stages) { s = 0; phase ^= 1u; }
@@ -353,10 +361,13 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
         // ================= MMA issuer (converged warp, one elected lane issues) =================
         if (half == 0) {
             const uint32_t idesc = instr_desc(kTileM, 0, BMN) | (uint32_t(a.bn >> 3) << 17) | (uint32_t(AMN) << 15);
-            // K-major: 8-row groups 1024 B apart, 16 columns of k = 32 B.  MN-major: 64-column slabs of 8 KB, 16 rows of k = 2 KB.
+            // K-major: 8-row groups 1024 B apart, 16 columns of k = 32 B, the next 64 in the next slab.  MN-major: 64-column slabs one behind the
+            // other, 16 rows of k = 2 KB.
             const uint64_t da0 = AMN ? smem_desc(base, kABytes / 2, 1024) : smem_desc(base, 16, 1024);
-            const uint64_t db0 = BMN ? smem_desc(base + kABytes, 8192, 1024) : smem_desc(base + kABytes, 16, 1024);
-            constexpr uint32_t step_a = (AMN ? 2048 : 32) >> 4, step_b = (BMN ? 2048 : 32) >> 4;
+            const uint64_t db0 = BMN ? smem_desc(base + kABytes, kTileK * 128, 1024) : smem_desc(base + kABytes, 16, 1024);
+            const uint32_t a_lo = uint32_t(da0), a_hi = uint32_t(da0 >> 32), b_lo = uint32_t(db0), b_hi = uint32_t(db0 >> 32);
+            const uint32_t slab_b = (b_bytes / kSub) >> 4;
+            const int last = (a.k_len - (a.k_tiles - 1) * kTileK + 15) / 16;
             int s = 0, i = 0;
             uint32_t phase = 0;
             bool ok = true;
@@ -368,14 +379,24 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
                     tc_fence_after();
                 }
                 const uint32_t d = tmem + uint32_t(u) * 256u;
+                int to_end = a.k_tiles - k0 % a.k_tiles;
                 for (int k = k0; k < k1; ++k) {
                     ok = mbar_wait_warp(bar_full(s), phase, abortp, 0, limit);
                     if (!ok) { if (lane == 0) set_status(a.hdr, CARNATOR_ERR_DEVICE_TIMEOUT, 73, k, blockIdx.x); break; }
                     tc_fence_after();
                     const uint32_t off = (uint32_t(s) * stage_bytes) >> 4;
+                    auto product = [&](int kk) {
+                        const uint32_t off_a = AMN ? kk * (2048 >> 4) : (kk / 4) * (kABytes / kSub >> 4) + (kk % 4) * 2;
+                        const uint32_t off_b = BMN ? kk * (2048 >> 4) : (kk / 4) * slab_b + (kk % 4) * 2;
+                        mma_pair_el(d, a_lo + off + off_a, a_hi, b_lo + off + off_b, b_hi, idesc, (k > k0 || kk > 0) ? 1u : 0u);
+                    };
+                    if (--to_end > 0) {
 #pragma unroll
-                    for (int kk = 0; kk < kTileK / 16; ++kk)
-                        mma_pair_el(d, da0 + off + kk * step_a, db0 + off + kk * step_b, idesc, (k > k0 || kk > 0) ? 1u : 0u);
+                        for (int kk = 0; kk < kTileK / 16; ++kk) product(kk);
+                    } else {             // the end of a batch entry's k: what is all zero is left out
+                        for (int kk = 0; kk < last; ++kk) product(kk);
+                        to_end = a.k_tiles;
+                    }
                     commit_pair_el(bar_empty(s), pair_mask);
                     if (++s == a.stages) { s = 0; phase ^= 1u; }
                 }
@@ -530,16 +551,17 @@ inline bool make_map_3d(CUtensorMap* map, const void* base, int64_t batches, int
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// The same for an MN-major operand of whole 64-column slabs: the columns as two dimensions, a box = 64 x 64 rows x `slabs` slabs, each
+// The same for an MN-major operand whose columns are whole slabs of 64: the columns as two dimensions, a box = 64 x box_rows x `slabs`, each
 // slab landing as make_map_3d's box would.  One copy of 16 KB instead of two of 8: with two, dX and dW of 32760 x 1536 x 8960 took 637 and 650 us
 // instead of 597 and 583.
-inline bool make_map_slabs(CUtensorMap* map, const void* base, int64_t batches, int64_t rows, int64_t cols, int64_t batch_stride, int64_t row_stride, int slabs) {
+inline bool make_map_slabs(CUtensorMap* map, const void* base, int64_t batches, int64_t rows, int64_t cols, int64_t batch_stride, int64_t row_stride, int box_rows,
+                           int slabs) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
     cuuint64_t dims[4] = {64, cuuint64_t(rows), cuuint64_t(cols / 64), cuuint64_t(batches)};
     const cuuint64_t row = rows > 1 ? cuuint64_t(row_stride) * 2 : cuuint64_t(cols) * 2;
     cuuint64_t strides[3] = {row, 128, batches > 1 ? cuuint64_t(batch_stride) * 2 : row};
-    cuuint32_t box[4] = {64, kTileK, cuuint32_t(slabs), 1};
+    cuuint32_t box[4] = {64, cuuint32_t(box_rows), cuuint32_t(slabs), 1};
     cuuint32_t estr[4] = {1, 1, 1, 1};
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
@@ -557,7 +579,7 @@ inline Plan plan_of(int64_t m_tiles, int64_t cols, int64_t k_all, bool b_mn) {
     for (int bn = 256; bn >= (b_mn ? 128 : 64); bn -= b_mn ? 128 : 32) {
         const int64_t tiles = m_tiles * ((cols + bn - 1) / bn);
         for (int splits = 1; splits <= 4; splits *= 2) {
-            if (splits > 1 && (tiles * splits > 72 || k_all < 4 * splits || bn % (8 * splits))) break;
+            if (splits > 1 && (tiles * splits > 72 || k_all < 8 * splits || bn % (8 * splits))) break;
             const int64_t pairs = std::min<int64_t>(74, tiles * splits);
             const double turns = double((tiles * splits + pairs - 1) / pairs);
             // per tile of k: the product, or what an SM takes to fetch its operands from L2 (68 bytes a clock); per tile: filling and draining
@@ -568,28 +590,24 @@ inline Plan plan_of(int64_t m_tiles, int64_t cols, int64_t k_all, bool b_mn) {
     return best;
 }
 
-template <int AMN, int BMN>
-inline carnator_status launch_tc_product(const Operand& A, const Operand& B, TcArgs a, cudaStream_t stream, char* err, size_t errlen) {
-    const Plan p = plan_of(int64_t(a.batches) * a.tiles_m, a.cols, int64_t(a.k_batches) * a.k_tiles, BMN);
-    a.bn = p.bn; a.splits = p.splits;
-    a.tiles_n = ceil_div(a.cols, a.bn);
-    const int64_t tiles = int64_t(a.batches) * a.tiles_m * a.tiles_n;
-    if (tiles > (int64_t(1) << 30)) return CARNATOR_ERR_UNSUPPORTED;
-    a.tiles = int(tiles);
-    a.group_m = 8;
-    const uint32_t stage = kABytes + uint32_t(a.bn / 2) * kTileK * 2;
-    a.stages = int(std::min<uint32_t>(kMaxStages, kStageBudget / stage));
+template <int AMN, int BMN, int kSub>
+inline carnator_status launch_tc_stages(const Operand& A, const Operand& B, TcArgs a, cudaStream_t stream, char* err, size_t errlen) {
+    constexpr int kTileK = kSub * kSlab;
+    const uint32_t stage = 128 * kTileK * 2 + uint32_t(a.bn / 2) * kTileK * 2;
+    a.k_tiles = ceil_div(a.k_len, kTileK);
+    a.stages = int(std::min<uint32_t>(kMaxStages, kRingBytes / stage));
+    a.a_slabs = AMN && A.cols % kSlab == 0;       // the last slab of another width would be read past the row
+    a.b_slabs = BMN && B.cols % kSlab == 0;
     CUtensorMap ma, mb;
-    a.a_slabs = AMN && A.cols % 64 == 0;          // the last slab of another width would be read past the row
-    a.b_slabs = BMN && B.cols % 64 == 0;
-    if (!(a.a_slabs ? make_map_slabs(&ma, A.base, A.batches, A.rows, A.cols, A.batch_stride, A.row_stride, 2)
-                    : make_map_3d(&ma, A.base, A.batches, A.rows, A.cols, A.batch_stride, A.row_stride, AMN ? kTileK : 128)) ||
-        !(a.b_slabs ? make_map_slabs(&mb, B.base, B.batches, B.rows, B.cols, B.batch_stride, B.row_stride, a.bn / 128)
-                    : make_map_3d(&mb, B.base, B.batches, B.rows, B.cols, B.batch_stride, B.row_stride, BMN ? kTileK : a.bn / 2))) {
+    auto map = [](CUtensorMap* m, const Operand& o, bool slabs, int rows, int n) {
+        return slabs ? make_map_slabs(m, o.base, o.batches, o.rows, o.cols, o.batch_stride, o.row_stride, rows, n)
+                     : make_map_3d(m, o.base, o.batches, o.rows, o.cols, o.batch_stride, o.row_stride, rows);
+    };
+    if (!map(&ma, A, a.a_slabs, AMN ? kTileK : 128, 2) || !map(&mb, B, a.b_slabs, BMN ? kTileK : a.bn / 2, a.bn / 128)) {
         snprintf(err, errlen, "cuTensorMapEncodeTiled failed or is unavailable");
         return CARNATOR_ERR_CUDA;
     }
-    auto kern = linear_tc_kernel<AMN, BMN>;
+    auto kern = linear_tc_kernel<AMN, BMN, kSub>;
     static SmemAllowed allowed;
     const unsigned long long ctx = context_id();
     if (!allowed.has(ctx)) {
@@ -597,16 +615,35 @@ inline carnator_status launch_tc_product(const Operand& A, const Operand& B, TcA
         if (e != cudaSuccess) return cuda_error(e, "cudaFuncSetAttribute(linear_tc_kernel)", err, errlen);
         allowed.add(ctx);
     }
-    cudaLaunchAttribute at[1];
+    cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = unsigned(2 * a.splits); at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg = {};
     const int clusters = a.splits > 1 ? a.tiles : std::min(a.tiles, 74);
     cfg.gridDim = dim3(unsigned(clusters * 2 * a.splits)); cfg.blockDim = dim3(kThreadsTc); cfg.dynamicSmemBytes = kSmemTc; cfg.stream = stream;
-    cfg.attrs = at; cfg.numAttrs = 1;
+    cfg.attrs = at; cfg.numAttrs = 2;
     const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, ma, mb, a);
     if (e != cudaSuccess) return cuda_error(e, "linear_tc_kernel", err, errlen);
     return CARNATOR_OK;
+}
+
+// The issuing warp spends about 200 clocks on a stage besides its products, which take it some 55 each, and a product of bn columns takes bn / 2: stages of 64 k
+// keep up with 256 columns and leave the ring finer (32760 x 1536 x 8960 613 us, with 128 k 627 us), narrower tiles want stages of 128 k (512 x 4096
+// x 5120 with 160 columns 23.5 and 19.5 us), as do MN-major operands, whose copies then are 32 KB each (dW of the former 627 and 615 us).
+template <int AMN, int BMN>
+inline carnator_status launch_tc_product(const Operand& A, const Operand& B, TcArgs a, cudaStream_t stream, char* err, size_t errlen) {
+    const Plan p = plan_of(int64_t(a.batches) * a.tiles_m, a.cols, int64_t(a.k_batches) * ceil_div(a.k_len, kSlab), BMN);
+    a.bn = p.bn; a.splits = p.splits;
+    a.tiles_n = ceil_div(a.cols, a.bn);
+    const int64_t tiles = int64_t(a.batches) * a.tiles_m * a.tiles_n;
+    if (tiles > (int64_t(1) << 30)) return CARNATOR_ERR_UNSUPPORTED;
+    a.tiles = int(tiles);
+    a.group_m = 8;
+    if constexpr (!AMN && !BMN)
+        if (a.bn == 256) return launch_tc_stages<AMN, BMN, 1>(A, B, a, stream, err, errlen);
+    return launch_tc_stages<AMN, BMN, 2>(A, B, a, stream, err, errlen);
 }
 
 }  // namespace lin
