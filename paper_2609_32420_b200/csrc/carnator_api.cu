@@ -1022,6 +1022,10 @@ bool norm_axes_ok(const carnator_norm_shape* s, const int64_t st[3], int32_t dty
     const int64_t size[3] = {s->B, s->H, s->N};
     return axes_ok(st, size, 3, s->C, dtype, written, false);
 }
+bool norm_rows32(const void* p, const int64_t st[3], int32_t dtype) {      // whether every row starts on a 32-byte boundary
+    const int64_t unit = 2 * dtype_unit(dtype);
+    return aligned(p, 32) && st[0] % unit == 0 && st[1] % unit == 0 && st[2] % unit == 0;
+}
 // The rows of an entry in the order of x's memory: the axis with the smaller stride inside.
 void norm_order(const carnator_norm_shape* s, norm::Args& a, const int64_t xs[3], const int64_t ys[3], const int64_t ds[3]) {
     const bool heads_inside = s->H > 1 && (s->N == 1 || xs[1] < xs[2]);
@@ -1057,8 +1061,9 @@ extern "C" carnator_status carnator_layer_norm(const void* X, const void* weight
     a.mean = mean_opt; a.rstd = rstd_opt;
     norm_order(s, a, s->x_stride, s->y_stride, s->y_stride);
     a.vec_ok = vec16(weight, 0, s->weight_dtype) && vec16(bias, 0, s->weight_dtype) && vec16(shift, s->shift_stride, s->mod_dtype) && vec16(scale, s->scale_stride, s->mod_dtype);
-    const norm::Form f = norm::form_of(s->C);
-    a.chunks = norm::chunks_of(f, s->B, a.rows, false);
+    a.wide = norm_rows32(Y, s->y_stride, s->y_dtype);
+    const norm::Form f = norm::form_of(s->C, false);
+    a.chunks = norm::chunks_of(f, s->B, s->C, a.rows, false);
     const cudaError_t e = norm::launch<false>(a, s->B, f, s->x_dtype == CARNATOR_DTYPE_F32, s->y_dtype == CARNATOR_DTYPE_F32, static_cast<cudaStream_t>(stream_));
     if (e != cudaSuccess) return cuda_fail(e, "norm_forward_kernel");
     g_launches.fetch_add(1, std::memory_order_relaxed);
@@ -1067,7 +1072,7 @@ extern "C" carnator_status carnator_layer_norm(const void* X, const void* weight
 
 extern "C" size_t carnator_layer_norm_backward_workspace_bytes(const carnator_norm_shape* s) {
     if (check_norm_shape(s) != CARNATOR_OK) return 0;
-    const int chunks = norm::chunks_of(norm::form_of(s->C), s->B, int64_t(s->H) * s->N, true);
+    const int chunks = norm::chunks_of(norm::form_of(s->C, true), s->B, s->C, int64_t(s->H) * s->N, true);
     return align256(size_t(s->B) * chunks * 2 * s->C * 4);
 }
 
@@ -1094,8 +1099,9 @@ extern "C" carnator_status carnator_layer_norm_backward(const void* dY, const vo
     a.part = sums ? static_cast<float*>(ws) : nullptr;
     norm_order(s, a, s->x_stride, s->dx_stride, s->dy_stride);
     a.vec_ok = vec16(weight, 0, s->weight_dtype) && vec16(scale, s->scale_stride, s->mod_dtype);
-    const norm::Form f = norm::form_of(s->C);
-    a.chunks = norm::chunks_of(f, s->B, a.rows, true);
+    a.wide = norm_rows32(dX, s->dx_stride, s->x_dtype);
+    const norm::Form f = norm::form_of(s->C, true);
+    a.chunks = norm::chunks_of(f, s->B, s->C, a.rows, true);
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     cudaError_t e = norm::launch<true>(a, s->B, f, s->x_dtype == CARNATOR_DTYPE_F32, s->y_dtype == CARNATOR_DTYPE_F32, stream);
     if (e != cudaSuccess) return cuda_fail(e, "norm_backward_kernel");

@@ -19,30 +19,10 @@ struct GradArgs {
 };
 
 constexpr int kGradCols = 256, kGradLanes = 8;       // columns and row lanes of a CTA
-
-// value and slope of the activation
-template <int ACT>
-__device__ __forceinline__ void act_and_slope(float z, float& f, float& s) {
-    if (ACT == kActSilu) {
-        const float g = __fdividef(1.f, 1.f + ex2_approx(-kLog2e * z));
-        f = z * g;
-        s = fmaf(f, 1.f - g, g);
-    } else if (ACT == kActGelu) {
-        const float c = 0.5f * (1.f + erff(z * 0.7071067811865476f));
-        f = z * c;
-        s = fmaf(z * 0.3989422804014327f, ex2_approx(-0.5f * kLog2e * z * z), c);
-    } else if (ACT == kActGeluTanh) {    // (1 + tanh u) / 2 = g, (1 - tanh^2 u) / 2 = 2 g (1 - g)
-        const float zz = z * z, e = ex2_approx((-2.f * kLog2e * kGeluA) * fmaf(kGeluB * zz, z, z));
-        const float g = __fdividef(1.f, 1.f + e);
-        f = z * g;
-        s = fmaf(2.f * f * (1.f - g), kGeluA * fmaf(3.f * kGeluB, zz, 1.f), g);
-    } else {
-        f = z; s = 1.f;
-    }
-}
+constexpr int kGradPerSm = 2;                        // CTAs that share an SM
 
 template <int ACT, bool DYF>
-__global__ void __launch_bounds__(32 * kGradLanes) linear_grad_kernel(const GradArgs a) {
+__global__ void __launch_bounds__(32 * kGradLanes, kGradPerSm) linear_grad_kernel(const GradArgs a) {
     __shared__ float sums[2][kGradLanes][kGradCols + 8];
     grid_launch_dependents();
     const int cv = threadIdx.x & 31, rl = threadIdx.x >> 5, b = blockIdx.z;
@@ -75,8 +55,9 @@ __global__ void __launch_bounds__(32 * kGradLanes) linear_grad_kernel(const Grad
                 for (int i = 0; i < 8; ++i) {
                     float f = 0.f, s = 1.f;
                     if (a.z) act_and_slope<ACT>(z[i], f, s);
-                    sg[i] = fmaf(d[i], f, sg[i]);
-                    d[i] *= gate[i] * s;
+                    if (a.part_gate) sg[i] = fmaf(d[i], f, sg[i]);
+                    if (a.gate) d[i] *= gate[i];
+                    if (ACT != kActNone) d[i] *= s;
                     sb[i] += d[i];
                 }
                 if (a.dz) norm::store8<false>(a.dz, b * a.dzs[0] + row * a.dzs[1] + col, d, n);
@@ -128,9 +109,9 @@ __global__ void __launch_bounds__(32 * kGradReduceWarps) linear_grad_reduce_kern
     if (warp == 0 && c < a.cols && a.dbias) a.dbias[c] = total;
 }
 
-// Chunks of rows per batch entry: about four CTAs an SM over the columns, none with fewer than 32 rows.
+// Chunks of rows per batch entry: one wave of CTAs over the columns, none with fewer than 32 rows.
 inline int grad_chunks(int64_t batches, int64_t rows, int64_t cols) {
-    const int64_t strips = (cols + kGradCols - 1) / kGradCols, want = (148 * 4 + strips * batches - 1) / (strips * batches);
+    const int64_t strips = (cols + kGradCols - 1) / kGradCols, want = 148 * kGradPerSm / (strips * batches);
     return int(std::max<int64_t>(1, std::min(want, rows / 32)));
 }
 

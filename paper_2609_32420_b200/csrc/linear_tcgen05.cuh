@@ -103,14 +103,48 @@ __device__ __forceinline__ void commit_pair_el(uint32_t bar, uint16_t mask) {
 }
 
 // ---- activations ----------------------------------------------------------------------------------
-// gelu_tanh(z) = z (1 + tanh u) / 2 = z / (1 + exp(-2u)), u = sqrt(2/pi) (z + 0.044715 z^3): no cancellation where tanh is near -1
+// Value and slope, each from one exponential and one reciprocal (the pipe for these takes 8 clocks for a warp's 32, which bounds the pass that
+// computes both for the gradients as soon as it is not memory).
+//   silu       z g, g = 1 / (1 + exp(-z));  slope g + z g (1 - g)
+//   gelu_tanh  z (1 + tanh u) / 2 = z g, g = 1 / (1 + exp(-2u)), u = A (z + B z^3): no cancellation where tanh is near -1;
+//              slope g + 2 z g (1 - g) u', u' = A (1 + 3 B z^2)
+//   gelu       z Phi(z); Phi by the approximation 7.1.26 of Abramowitz and Stegun, Handbook of Mathematical Functions:
+//              erfc(x) = (a1 t + .. + a5 t^5) exp(-x^2), t = 1 / (1 + 0.3275911 x), x >= 0, off by at most 1.5e-7; its exponential is the density's.
+//              slope Phi + z exp(-z^2 / 2) / sqrt(2 pi)
 constexpr float kGeluA = 0.7978845608028654f, kGeluB = 0.044715f;
+__device__ __forceinline__ float rcp_approx(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+template <int ACT>
+__device__ __forceinline__ void act_and_slope(float z, float& f, float& s) {
+    if (ACT == kActSilu) {
+        const float g = rcp_approx(1.f + ex2_approx(-kLog2e * z));
+        f = z * g;
+        s = fmaf(f, 1.f - g, g);
+    } else if (ACT == kActGelu) {
+        const float t = rcp_approx(fmaf(0.3275911f * 0.7071067811865476f, fabsf(z), 1.f)), e = ex2_approx((-0.5f * kLog2e * z) * z);
+        float p = fmaf(0.5f * 1.061405429f, t, 0.5f * -1.453152027f);
+        p = fmaf(p, t, 0.5f * 1.421413741f);
+        p = fmaf(p, t, 0.5f * -0.284496736f);
+        p = fmaf(p, t, 0.5f * 0.254829592f);
+        const float q = p * t * e, c = z >= 0.f ? 1.f - q : q;
+        f = z * c;
+        s = fmaf(z * 0.3989422804014327f, e, c);
+    } else if (ACT == kActGeluTanh) {
+        const float zz = z * z, g = rcp_approx(1.f + ex2_approx(z * fmaf(-2.f * kLog2e * kGeluA * kGeluB, zz, -2.f * kLog2e * kGeluA)));
+        f = z * g;
+        s = fmaf(fmaf(-f, g, f), fmaf(6.f * kGeluA * kGeluB, zz, 2.f * kGeluA), g);
+    } else {
+        f = z; s = 1.f;
+    }
+}
 template <int ACT>
 __device__ __forceinline__ float activation(float z) {
-    if (ACT == kActSilu) return __fdividef(z, 1.f + ex2_approx(-kLog2e * z));
-    if (ACT == kActGelu) return 0.5f * z * (1.f + erff(z * 0.7071067811865476f));
-    if (ACT == kActGeluTanh) return __fdividef(z, 1.f + ex2_approx((-2.f * kLog2e * kGeluA) * fmaf(kGeluB * z * z, z, z)));
-    return z;
+    float f, s;
+    act_and_slope<ACT>(z, f, s);
+    return f;
 }
 template <int ACT>
 __device__ __forceinline__ void activate8(float (&v)[8]) {
