@@ -511,16 +511,24 @@ def _dtype_code(t, what: str) -> int:
     raise ValueError(f"{what} must be float32 or bfloat16, not {t.dtype}")
 
 
-def _want(t, what: str, code: int, size, device) -> None:
-    """What the record says of a tensor, and what the call is about to do with it, have to agree."""
-    if t is None:
+def _dtype_of(code: int):
+    import torch
+    return torch.float32 if code == DTYPE_F32 else torch.bfloat16
+
+
+def _fit(t, what: str, dtype, size, stride, device) -> None:
+    """A tensor has to be what the shape record says: type, shape, device, and strides (that of an axis of one entry does not matter)."""
+    if t.dtype is dtype and t.shape == size and t.stride() == stride and t.device == device:
         return
-    if _dtype_code(t, what) != code:
-        raise ValueError(f"{what} has another type than the shape record says")
+    if t.dtype is not dtype:
+        raise ValueError(f"{what} is {t.dtype}, the shape record says {dtype}")
     if t.device != device:
         raise ValueError(f"{what} is on {t.device}, not on {device}")
-    if tuple(t.shape) != size:
+    if t.shape != size:
         raise ValueError(f"{what} has shape {tuple(t.shape)}, not {size}")
+    for n, a, b in zip(size, t.stride(), stride):
+        if n > 1 and a != b:
+            raise ValueError(f"{what} has strides {t.stride()}, the shape record says {stride}")
 
 
 def _on_current_device(device) -> None:
@@ -530,25 +538,41 @@ def _on_current_device(device) -> None:
         raise ValueError(f"the tensors are on {device}, the current device is cuda:{torch.cuda.current_device()}")
 
 
-def _want_strides(t, what: str, recorded) -> None:
-    """The record was made for tensors laid out like this one (the stride of an axis of one entry does not matter)."""
-    if t is not None:
-        for i, (n, a, b) in enumerate(zip(t.shape, t.stride(), recorded)):
-            if n > 1 and a != b:
-                raise ValueError(f"{what} has stride {a} on axis {i}, the shape record says {b}")
-        if t.stride(-1) != 1 and t.shape[-1] > 1:
-            raise ValueError(f"{what}: the last axis must be contiguous")
+class _Said:
+    """What a record says of the tensors of its call, (type, shape, strides) each, worked out again whenever the record has changed."""
+    __slots__ = ("of", "x", "y", "dy", "dx", "residual", "z", "w", "dw", "vec", "shift", "scale", "gate", "bias", "stat", "ref")
 
 
-def _want_vector(t, what: str, code: int, size, device, stride: int = 0) -> None:
-    """A parameter vector [C], or one row per batch entry [B,C] with the record's batch stride."""
-    if t is None:
-        return
-    _want(t, what, code, size, device)
-    if size[-1] > 1 and t.stride(-1) != 1:
-        raise ValueError(f"{what}: the last axis must be contiguous")
-    if len(size) == 2 and size[0] > 1 and t.stride(0) != stride:
-        raise ValueError(f"{what} has batch stride {t.stride(0)}, the shape record says {stride}")
+def _norm_said(s: NormShape) -> _Said:
+    said = getattr(s, "_said", None)
+    of = bytes(s)
+    if said is None or said.of != of:
+        said = s._said = _Said()
+        size, x, y, w, m = (s.B, s.H, s.N, s.C), _dtype_of(s.x_dtype), _dtype_of(s.y_dtype), _dtype_of(s.weight_dtype), _dtype_of(s.mod_dtype)
+        said.of, said.ref = of, ctypes.byref(s)
+        said.x, said.y = (x, size, (*s.x_stride, 1)), (y, size, (*s.y_stride, 1))
+        said.dy, said.dx = (y, size, (*s.dy_stride, 1)), (x, size, (*s.dx_stride, 1))
+        said.vec = (w, (s.C,), (1,))
+        said.shift, said.scale = (m, (s.B, s.C), (s.shift_stride, 1)), (m, (s.B, s.C), (s.scale_stride, 1))
+        said.stat = (_dtype_of(DTYPE_F32), size[:3], (s.H * s.N, s.N, 1))
+    return said
+
+
+def _linear_said(s: LinearShape) -> _Said:
+    said = getattr(s, "_said", None)
+    of = bytes(s)
+    if said is None or said.of != of:
+        said = s._said = _Said()
+        y, bf16 = _dtype_of(s.y_dtype), _dtype_of(DTYPE_BF16)
+        rows = lambda n, dtype, st: (dtype, (s.B, s.N, n), (*st, 1))  # noqa: E731
+        said.of, said.ref = of, ctypes.byref(s)
+        said.x, said.dx = rows(s.in_features, bf16, s.x_stride), rows(s.in_features, bf16, s.dx_stride)
+        said.y, said.z = rows(s.out_features, y, s.y_stride), rows(s.out_features, bf16, s.z_stride)
+        said.residual = rows(s.out_features, y, s.residual_stride)
+        said.w, said.dw = (bf16, (s.out_features, s.in_features), (s.w_stride, 1)), (bf16, (s.out_features, s.in_features), (s.dw_stride, 1))
+        said.bias = (_dtype_of(s.bias_dtype), (s.out_features,), (1,))
+        said.gate = (_dtype_of(s.gate_dtype), (s.B, s.out_features), (s.gate_stride, 1))
+    return said
 
 
 def _rows_of(stride, *tensors):
@@ -585,34 +609,32 @@ def make_norm_shape(X, Y, weight=None, scale=None, shift=None, dX=None, eps: flo
     return s
 
 
-def _dtype_of(code: int):
-    import torch
-    return torch.float32 if code == DTYPE_F32 else torch.bfloat16
-
-
 def layer_norm(X, shape: NormShape, weight=None, bias=None, shift=None, scale=None, Y=None, mean=None, rstd=None, stream=None):
     """carnator_layer_norm.  Returns Y [B,H,N,C]; mean and rstd fp32 [B,H,N] (contiguous) are written if given."""
-    import torch
-    dev, size = X.device, (shape.B, shape.H, shape.N, shape.C)
+    dev = X.device
     if Y is None:
-        Y = torch.empty(size, dtype=_dtype_of(shape.y_dtype), device=dev)
+        import torch
+        Y = torch.empty((shape.B, shape.H, shape.N, -(-shape.C // 8) * 8), dtype=_dtype_of(shape.y_dtype), device=dev)[..., :shape.C]
         shape.y_stride = _rows_of(shape.y_stride, Y)
+    said = _norm_said(shape)
     _on_current_device(dev)
-    _want(X, "X", shape.x_dtype, size, dev)
-    _want(Y, "Y", shape.y_dtype, size, dev)
-    _want_strides(X, "X", shape.x_stride)
-    _want_strides(Y, "Y", shape.y_stride)
-    for t, what in ((weight, "weight"), (bias, "bias")):
-        _want_vector(t, what, shape.weight_dtype, size[3:], dev)
-    _want_vector(shift, "shift", shape.mod_dtype, (shape.B, shape.C), dev, shape.shift_stride)
-    _want_vector(scale, "scale", shape.mod_dtype, (shape.B, shape.C), dev, shape.scale_stride)
-    for t, what in ((mean, "mean"), (rstd, "rstd")):
-        _want(t, what, DTYPE_F32, size[:3], dev)
-        if t is not None and not t.is_contiguous():
-            raise ValueError(f"{what} must be contiguous")
-    st = lib().carnator_layer_norm(_ptr(X), _ptr(weight), _ptr(bias), _ptr(shift), _ptr(scale), ctypes.byref(shape), _ptr(Y),
-                                   _ptr(mean), _ptr(rstd), _stream(stream))
-    _check(st, "carnator_layer_norm")
+    _fit(X, "X", *said.x, dev)
+    _fit(Y, "Y", *said.y, dev)
+    if weight is not None:
+        _fit(weight, "weight", *said.vec, dev)
+    if bias is not None:
+        _fit(bias, "bias", *said.vec, dev)
+    if shift is not None:
+        _fit(shift, "shift", *said.shift, dev)
+    if scale is not None:
+        _fit(scale, "scale", *said.scale, dev)
+    if mean is not None:
+        _fit(mean, "mean", *said.stat, dev)
+    if rstd is not None:
+        _fit(rstd, "rstd", *said.stat, dev)
+    st = lib().carnator_layer_norm(_ptr(X), _ptr(weight), _ptr(bias), _ptr(shift), _ptr(scale), said.ref, _ptr(Y), _ptr(mean), _ptr(rstd), _stream(stream))
+    if st != OK:
+        _check(st, "carnator_layer_norm")
     return Y
 
 
@@ -634,36 +656,42 @@ def layer_norm_backward(dY, X, mean, rstd, shape: NormShape, weight=None, bias=N
     """carnator_layer_norm_backward.  ``want`` names the vector gradients to compute: weight and bias (if the norm has a
     weight), shift and scale (if it has a scale, or ``modulated`` says that it has a shift only)."""
     import torch
-    dev, size = X.device, (shape.B, shape.H, shape.N, shape.C)
+    dev = X.device
     if dX is None:
-        dX = torch.empty(size, dtype=_dtype_of(shape.x_dtype), device=dev)
+        dX = torch.empty((shape.B, shape.H, shape.N, -(-shape.C // 8) * 8), dtype=_dtype_of(shape.x_dtype), device=dev)[..., :shape.C]
         shape.dx_stride = _rows_of(shape.dx_stride, dX)
+    said = _norm_said(shape)
     _on_current_device(dev)
-    _want(dY, "dY", shape.y_dtype, size, dev)
-    _want(X, "X", shape.x_dtype, size, dev)
-    _want(dX, "dX", shape.x_dtype, size, dev)
-    _want_strides(dY, "dY", shape.dy_stride)
-    _want_strides(X, "X", shape.x_stride)
-    _want_strides(dX, "dX", shape.dx_stride)
-    for t, what in ((weight, "weight"), (bias, "bias")):
-        _want_vector(t, what, shape.weight_dtype, size[3:], dev)
-    _want_vector(scale, "scale", shape.mod_dtype, (shape.B, shape.C), dev, shape.scale_stride)
-    for t, what in ((mean, "mean"), (rstd, "rstd")):
-        _want(t, what, DTYPE_F32, size[:3], dev)
-        if not t.is_contiguous():
-            raise ValueError(f"{what} must be contiguous")
-    if modulated is None:
-        modulated = scale is not None
-    new = lambda has, name, n: torch.empty(n, dtype=torch.float32, device=dev) if has and name in want else None  # noqa: E731
-    g = NormGrads(dX, new(weight is not None, "weight", size[3:]), new(weight is not None, "bias", size[3:]),
-                  new(modulated, "shift", (shape.B, shape.C)), new(modulated, "scale", (shape.B, shape.C)))
+    _fit(dY, "dY", *said.dy, dev)
+    _fit(X, "X", *said.x, dev)
+    _fit(dX, "dX", *said.dx, dev)
+    _fit(mean, "mean", *said.stat, dev)
+    _fit(rstd, "rstd", *said.stat, dev)
+    if weight is not None:
+        _fit(weight, "weight", *said.vec, dev)
+    if bias is not None:
+        _fit(bias, "bias", *said.vec, dev)
+    if scale is not None:
+        _fit(scale, "scale", *said.scale, dev)
+    B, C = shape.B, shape.C
+    dweight = dbias = dshift = dscale = None
+    if weight is not None:
+        if "weight" in want:
+            dweight = torch.empty(C, dtype=torch.float32, device=dev)
+        if "bias" in want:
+            dbias = torch.empty(C, dtype=torch.float32, device=dev)
+    if scale is not None if modulated is None else modulated:
+        if "shift" in want:
+            dshift = torch.empty((B, C), dtype=torch.float32, device=dev)
+        if "scale" in want:
+            dscale = torch.empty((B, C), dtype=torch.float32, device=dev)
     if ws is None:
         ws = _new_ws(layer_norm_backward_workspace_bytes(shape), dev)
-    st = lib().carnator_layer_norm_backward(_ptr(dY), _ptr(X), _ptr(mean), _ptr(rstd), _ptr(weight), _ptr(bias), _ptr(scale),
-                                            ctypes.byref(shape), _ptr(dX), _ptr(g.dweight), _ptr(g.dbias), _ptr(g.dshift), _ptr(g.dscale),
-                                            _ptr(ws), ws.numel(), _stream(stream))
-    _check(st, "carnator_layer_norm_backward")
-    return g
+    st = lib().carnator_layer_norm_backward(_ptr(dY), _ptr(X), _ptr(mean), _ptr(rstd), _ptr(weight), _ptr(bias), _ptr(scale), said.ref, _ptr(dX),
+                                            _ptr(dweight), _ptr(dbias), _ptr(dshift), _ptr(dscale), _ptr(ws), ws.numel(), _stream(stream))
+    if st != OK:
+        _check(st, "carnator_layer_norm_backward")
+    return NormGrads(dX, dweight, dbias, dshift, dscale)
 
 
 def make_linear_shape(X, W, Y, residual=None, Z=None, bias=None, gate=None, dX=None, dW=None, activation: int = ACT_NONE) -> LinearShape:
@@ -697,30 +725,30 @@ def linear_workspace_bytes(shape: LinearShape) -> int:
 
 def linear(X, W, shape: LinearShape, bias=None, gate=None, residual=None, Y=None, Z=None, ws=None, stream=None):
     """carnator_linear.  Returns (Y [B,N,out_features], ws); Z (bf16, the pre-activation) is written if given."""
-    import torch
-    dev, B, N, K, M = X.device, shape.B, shape.N, shape.in_features, shape.out_features
+    dev = X.device
     if Y is None:
-        wide = -(-M // 8) * 8                      # rows on 16-byte boundaries
-        Y = torch.empty((B, N, wide), dtype=_dtype_of(shape.y_dtype), device=dev)[..., :M]
+        import torch
+        M = shape.out_features                     # rows on 16-byte boundaries
+        Y = torch.empty((shape.B, shape.N, -(-M // 8) * 8), dtype=_dtype_of(shape.y_dtype), device=dev)[..., :M]
         shape.y_stride = _rows_of(shape.y_stride, Y)
+    said = _linear_said(shape)
     _on_current_device(dev)
-    _want(X, "X", DTYPE_BF16, (B, N, K), dev)
-    _want(W, "W", DTYPE_BF16, (M, K), dev)
-    _want(Y, "Y", shape.y_dtype, (B, N, M), dev)
-    _want(Z, "Z", DTYPE_BF16, (B, N, M), dev)
-    _want(residual, "residual", shape.y_dtype, (B, N, M), dev)
-    _want_strides(X, "X", shape.x_stride)
-    _want_strides(W, "W", (shape.w_stride,))
-    _want_strides(Y, "Y", shape.y_stride)
-    _want_strides(Z, "Z", shape.z_stride)
-    _want_strides(residual, "residual", shape.residual_stride)
-    _want_vector(bias, "bias", shape.bias_dtype, (M,), dev)
-    _want_vector(gate, "gate", shape.gate_dtype, (B, M), dev, shape.gate_stride)
+    _fit(X, "X", *said.x, dev)
+    _fit(W, "W", *said.w, dev)
+    _fit(Y, "Y", *said.y, dev)
+    if Z is not None:
+        _fit(Z, "Z", *said.z, dev)
+    if residual is not None:
+        _fit(residual, "residual", *said.residual, dev)
+    if bias is not None:
+        _fit(bias, "bias", *said.bias, dev)
+    if gate is not None:
+        _fit(gate, "gate", *said.gate, dev)
     if ws is None:
         ws = _new_ws(linear_workspace_bytes(shape), dev)
-    st = lib().carnator_linear(_ptr(X), _ptr(W), _ptr(bias), _ptr(gate), _ptr(residual), ctypes.byref(shape), _ptr(Y), _ptr(Z),
-                               _ptr(ws), ws.numel(), _stream(stream))
-    _check(st, "carnator_linear")
+    st = lib().carnator_linear(_ptr(X), _ptr(W), _ptr(bias), _ptr(gate), _ptr(residual), said.ref, _ptr(Y), _ptr(Z), _ptr(ws), ws.numel(), _stream(stream))
+    if st != OK:
+        _check(st, "carnator_linear")
     return Y, ws
 
 
@@ -741,29 +769,29 @@ def linear_backward(dY, X, W, shape: LinearShape, Z=None, gate=None, dX=None, dW
     """carnator_linear_backward.  dX and dW are computed where given (bf16); ``want`` names the fp32 vector gradients: bias, gate
     (if there is one).  Z is the pre-activation that the forward call wrote."""
     import torch
-    dev, B, N, K, M = dY.device, shape.B, shape.N, shape.in_features, shape.out_features
+    dev = dY.device
+    said = _linear_said(shape)
     _on_current_device(dev)
-    _want(dY, "dY", shape.y_dtype, (B, N, M), dev)
-    _want(X, "X", DTYPE_BF16, (B, N, K), dev)
-    _want(W, "W", DTYPE_BF16, (M, K), dev)
-    _want(Z, "Z", DTYPE_BF16, (B, N, M), dev)
-    _want(dX, "dX", DTYPE_BF16, (B, N, K), dev)
-    _want(dW, "dW", DTYPE_BF16, (M, K), dev)
-    _want_strides(dY, "dY", shape.y_stride)
-    _want_strides(X, "X", shape.x_stride)
-    _want_strides(W, "W", (shape.w_stride,))
-    _want_strides(Z, "Z", shape.z_stride)
-    _want_strides(dX, "dX", shape.dx_stride)
-    _want_strides(dW, "dW", (shape.dw_stride,))
-    _want_vector(gate, "gate", shape.gate_dtype, (B, M), dev, shape.gate_stride)
-    g = LinearGrads(dX, dW, torch.empty(M, dtype=torch.float32, device=dev) if "bias" in want else None,
-                    torch.empty((B, M), dtype=torch.float32, device=dev) if "gate" in want and gate is not None else None)
+    _fit(dY, "dY", *said.y, dev)
+    _fit(X, "X", *said.x, dev)
+    _fit(W, "W", *said.w, dev)
+    if Z is not None:
+        _fit(Z, "Z", *said.z, dev)
+    if gate is not None:
+        _fit(gate, "gate", *said.gate, dev)
+    if dX is not None:
+        _fit(dX, "dX", *said.dx, dev)
+    if dW is not None:
+        _fit(dW, "dW", *said.dw, dev)
+    dbias = torch.empty(shape.out_features, dtype=torch.float32, device=dev) if "bias" in want else None
+    dgate = torch.empty((shape.B, shape.out_features), dtype=torch.float32, device=dev) if gate is not None and "gate" in want else None
     if ws is None:
         ws = _new_ws(linear_backward_workspace_bytes(shape), dev)
-    st = lib().carnator_linear_backward(_ptr(dY), _ptr(X), _ptr(W), _ptr(Z), _ptr(gate), ctypes.byref(shape), _ptr(dX), _ptr(dW),
-                                        _ptr(g.dbias), _ptr(g.dgate), _ptr(ws), ws.numel(), _stream(stream))
-    _check(st, "carnator_linear_backward")
-    return g
+    st = lib().carnator_linear_backward(_ptr(dY), _ptr(X), _ptr(W), _ptr(Z), _ptr(gate), said.ref, _ptr(dX), _ptr(dW), _ptr(dbias), _ptr(dgate),
+                                        _ptr(ws), ws.numel(), _stream(stream))
+    if st != OK:
+        _check(st, "carnator_linear_backward")
+    return LinearGrads(dX, dW, dbias, dgate)
 
 
 # ---- host-side scalars (no GPU) ---------------------------------------------------------------------

@@ -25,6 +25,7 @@ template <int ACT, bool DYF>
 __global__ void __launch_bounds__(32 * kGradLanes, kGradPerSm) linear_grad_kernel(const GradArgs a) {
     __shared__ float sums[2][kGradLanes][kGradCols + 8];
     grid_launch_dependents();
+    grid_wait();
     const int cv = threadIdx.x & 31, rl = threadIdx.x >> 5, b = blockIdx.z;
     const int col = blockIdx.x * kGradCols + cv * 8, n = min(max(a.cols - col, 0), 8);
     const int r0 = int(int64_t(blockIdx.y) * a.rows / a.chunks), r1 = int(int64_t(blockIdx.y + 1) * a.rows / a.chunks);
@@ -82,6 +83,7 @@ struct GradReduceArgs { const float* part_bias; const float* part_gate; float* d
 constexpr int kGradReduceWarps = 16;
 __global__ void __launch_bounds__(32 * kGradReduceWarps) linear_grad_reduce_kernel(const GradReduceArgs a) {
     __shared__ float sums[2][kGradReduceWarps][32];
+    grid_launch_dependents();
     grid_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
     float total = 0.f;
@@ -116,19 +118,17 @@ inline int grad_chunks(int64_t batches, int64_t rows, int64_t cols) {
 }
 
 template <int ACT>
-inline void launch_grad_act(const GradArgs& a, dim3 grid, cudaStream_t stream) {
-    if (a.dy_f32) linear_grad_kernel<ACT, true><<<grid, 32 * kGradLanes, 0, stream>>>(a);
-    else linear_grad_kernel<ACT, false><<<grid, 32 * kGradLanes, 0, stream>>>(a);
+inline cudaError_t launch_grad_act(const GradArgs& a, dim3 grid, cudaStream_t stream) {
+    return launch_dependent(a.dy_f32 ? linear_grad_kernel<ACT, true> : linear_grad_kernel<ACT, false>, grid, dim3(32 * kGradLanes), 0, stream, a);
 }
 inline cudaError_t launch_grad(const GradArgs& a, int batches, cudaStream_t stream) {
     const dim3 grid(ceil_div(a.cols, kGradCols), a.chunks, batches);
     switch (a.act) {
-        case kActGeluTanh: launch_grad_act<kActGeluTanh>(a, grid, stream); break;
-        case kActGelu: launch_grad_act<kActGelu>(a, grid, stream); break;
-        case kActSilu: launch_grad_act<kActSilu>(a, grid, stream); break;
-        default: launch_grad_act<kActNone>(a, grid, stream); break;
+        case kActGeluTanh: return launch_grad_act<kActGeluTanh>(a, grid, stream);
+        case kActGelu: return launch_grad_act<kActGelu>(a, grid, stream);
+        case kActSilu: return launch_grad_act<kActSilu>(a, grid, stream);
+        default: return launch_grad_act<kActNone>(a, grid, stream);
     }
-    return cudaGetLastError();
 }
 
 }  // namespace lin

@@ -38,6 +38,8 @@ template <int NT>                        // column tiles of 8 rows of x
 __global__ void __launch_bounds__(32 * kRowsWarps) linear_rows_kernel(const RowsArgs a) {
     __shared__ float sums[kRowsWarps][16][8 * NT + 1];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+    grid_launch_dependents();
+    grid_wait();                         // launched while the kernel ahead drains
     if (blockIdx.x == 0 && tid == 0) a.hdr->status = 0;
     const int f0 = blockIdx.x * 16;
     const bool on0 = f0 + g < a.cols, on1 = f0 + g + 8 < a.cols;
@@ -107,9 +109,7 @@ __global__ void __launch_bounds__(32 * kRowsWarps) linear_rows_kernel(const Rows
 
 inline cudaError_t launch_rows(const RowsArgs& a, cudaStream_t stream) {
     const int grid = ceil_div(a.cols, 16);
-    if (a.rows <= 8) linear_rows_kernel<1><<<grid, 32 * kRowsWarps, 0, stream>>>(a);
-    else linear_rows_kernel<2><<<grid, 32 * kRowsWarps, 0, stream>>>(a);
-    return cudaGetLastError();
+    return launch_dependent(a.rows <= 8 ? linear_rows_kernel<1> : linear_rows_kernel<2>, dim3(grid), dim3(32 * kRowsWarps), 0, stream, a);
 }
 
 }  // namespace lin

@@ -544,19 +544,23 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
                 if (a.e.residual) load_residual(a.e, b, row, col, cn, res);
                 Columns cols;
                 columns_begin(a.e, cols, col, cn);
+                // all of the cluster's shares on their way before the first is added
+                float g[4][8];
+#pragma unroll
+                for (int sp = 0; sp < 4; ++sp)
+                    if (sp < a.splits) {
+                        const uint32_t src = map_cta(base + uint32_t(r) * pitch + uint32_t(c) * 4u, uint32_t(2 * sp) + half);
+#pragma unroll
+                        for (int q = 0; q < 2; ++q)
+                            asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(g[sp][4 * q]), "=f"(g[sp][4 * q + 1]), "=f"(g[sp][4 * q + 2]),
+                                         "=f"(g[sp][4 * q + 3]) : "r"(src + 16u * q) : "memory");
+                    } else {
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) g[sp][q] = 0.f;
+                    }
                 float f[8];
 #pragma unroll
-                for (int q = 0; q < 8; ++q) f[q] = 0.f;
-                for (int sp = 0; sp < a.splits; ++sp) {
-                    const uint32_t src = map_cta(base + uint32_t(r) * pitch + uint32_t(c) * 4u, uint32_t(2 * sp) + half);
-                    float g[8];
-#pragma unroll
-                    for (int q = 0; q < 2; ++q)
-                        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(g[4 * q]), "=f"(g[4 * q + 1]), "=f"(g[4 * q + 2]), "=f"(g[4 * q + 3])
-                                     : "r"(src + 16u * q) : "memory");
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) f[q] += g[q];
-                }
+                for (int q = 0; q < 8; ++q) f[q] = ((g[0][q] + g[1][q]) + g[2][q]) + g[3][q];
                 finish(a.e, cols, b, row, col, cn, f, res);
             }
     }
@@ -604,8 +608,11 @@ inline bool make_map_slabs(CUtensorMap* map, const void* base, int64_t batches, 
 // A bf16 operand as [batches, rows, cols].
 struct Operand { const void* base; int64_t batches, rows, cols, batch_stride, row_stride; };
 
-// Columns of a tile and pairs that share one: the least time of a launch in units of one column of 256 rows and 64 of k, which is the turns that the
-// pairs of 148 SMs take, times a tile's share of k, times what 64 of k cost.
+// Columns of a tile and pairs that share one: the least time by a model in nanoseconds that was fitted to launches of 20 to 1000 rows.  A pair takes
+// 75 + 0.85 columns per 64 of k (bounded by its products at 256 columns, by fetching its operands, 64 bytes a clock and SM, below), and an epilogue that is
+// hidden except under very short k.  Joining two pairs costs 1.5 us, four 4.5 us (226 x 4096 x 1536: one pair per tile of 64 23.0 us, two per tile of 96
+// 12.2, four per tile of 128 13.3; 64 x 9216 x 1536 20.3 with two, 15.4 with four).  33 clusters of 4 CTAs or 15 of 8 find room at a time; near
+// that they start late.
 struct Plan { int bn, splits; };
 inline Plan plan_of(int64_t m_tiles, int64_t cols, int64_t k_all, bool b_mn) {
     Plan best = {256, 1};
@@ -613,11 +620,10 @@ inline Plan plan_of(int64_t m_tiles, int64_t cols, int64_t k_all, bool b_mn) {
     for (int bn = 256; bn >= (b_mn ? 128 : 64); bn -= b_mn ? 128 : 32) {
         const int64_t tiles = m_tiles * ((cols + bn - 1) / bn);
         for (int splits = 1; splits <= 4; splits *= 2) {
-            if (splits > 1 && (tiles * splits > 72 || k_all < 8 * splits || bn % (8 * splits))) break;
-            const int64_t pairs = std::min<int64_t>(74, tiles * splits);
-            const double turns = double((tiles * splits + pairs - 1) / pairs);
-            // per tile of k: the product, or what an SM takes to fetch its operands from L2 (68 bytes a clock); per tile: filling and draining
-            const double cost = turns * ((double(k_all) / splits) * std::max(double(bn), 0.47 * (256 + bn)) + (splits > 1 ? 500 + 2 * bn : 400 + bn));
+            if ((splits == 2 && tiles > 32) || (splits == 4 && tiles > 14) || k_all < 4 * splits * (splits > 1) || bn % (8 * splits)) break;
+            const int64_t turns = splits > 1 ? 1 : (tiles + 73) / 74;
+            const double k_ns = double((k_all + splits - 1) / splits) * (75 + 0.85 * bn), join = splits == 1 ? 0 : splits == 4 ? 4500 : tiles > 24 ? 4000 : 1500;
+            const double cost = double(turns) * std::max(k_ns, 500.0 + 4 * bn) + join;
             if (cost < best_cost * 0.995) { best_cost = cost; best = {bn, splits}; }
         }
     }

@@ -312,6 +312,8 @@ __global__ void __launch_bounds__(most_threads(LANES, V)) __maxnreg__(regs_of(V,
     char* y = static_cast<char*>(a.y) + (b * a.ys[0] + col0) * (YF ? 4 : 2);
 
     Row ahead(a, r0 + pl.slot), now(ahead);
+    grid_launch_dependents();
+    grid_wait();                         // launched while the kernel ahead drains: nothing of global memory is touched before this
     auto fetch = [&](int s) {
         in.copy(ring + uint32_t(s) * stage, ahead.row < r1 ? x + ahead.off(a.xs) * (XF ? 4 : 2) : x, a.C, col_step, ahead.row < r1);
         copies_commit();
@@ -424,6 +426,7 @@ __global__ void __launch_bounds__(most_threads(LANES, V)) __maxnreg__(regs_of(V,
     const int b = blockIdx.y, groups = (a.C + kGroup - 1) / kGroup;
     const int r0 = int(int64_t(blockIdx.x) * a.rows / a.chunks), r1 = int(int64_t(blockIdx.x + 1) * a.rows / a.chunks);
     grid_launch_dependents();
+    grid_wait();
     const int col0 = kGroup * pl.at, col_step = kGroup * pl.stride, by_o = pl.slots / a.inner, by_i = pl.slots - by_o * a.inner;
     int n[V];
     Eight P[V], S[V];
@@ -590,6 +593,7 @@ struct ReduceArgs {
 constexpr int kReduceWarps = 16;
 __global__ void __launch_bounds__(32 * kReduceWarps) norm_reduce_kernel(const ReduceArgs a) {
     __shared__ float sums[2][kReduceWarps][32];
+    grid_launch_dependents();
     grid_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
     const bool on = c < a.C;
@@ -676,7 +680,7 @@ inline cudaError_t launch_types(Args a, dim3 grid, const Form& f, bool xf, bool 
                 at.add(ctx);
             }
         }
-        kernel<<<grid, f.threads, smem, stream>>>(a);
+        e = launch_dependent(kernel, grid, dim3(f.threads), smem, stream, a);
     };
 #define CARNATOR_NORM(XF, YF)                                                                        \
     if (xf == XF && yf == YF) {                                                                      \
@@ -688,7 +692,7 @@ inline cudaError_t launch_types(Args a, dim3 grid, const Form& f, bool xf, bool 
     CARNATOR_NORM(true, false)
     CARNATOR_NORM(true, true)
 #undef CARNATOR_NORM
-    return e != cudaSuccess ? e : cudaGetLastError();
+    return e;
 }
 template <bool BWD>
 inline cudaError_t launch(const Args& a, int B, const Form& f, bool xf, bool yf, cudaStream_t stream) {
