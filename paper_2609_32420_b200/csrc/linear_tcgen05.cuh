@@ -117,39 +117,57 @@ __device__ __forceinline__ float rcp_approx(float x) {
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+using norm::f2; using norm::two; using norm::one_each; using norm::add2; using norm::mul2; using norm::fma2;
+__device__ __forceinline__ f2 ex2_each(f2 v) { float a, b; one_each(v, a, b); return two(ex2_approx(a), ex2_approx(b)); }
+__device__ __forceinline__ f2 rcp_each(f2 v) { float a, b; one_each(v, a, b); return two(rcp_approx(a), rcp_approx(b)); }
+__device__ __forceinline__ f2 less_from(f2 v, float from) { return fma2(v, two(-1.f), two(from)); }
+// of two arguments, two fp32 values per instruction
 template <int ACT>
-__device__ __forceinline__ void act_and_slope(float z, float& f, float& s) {
+__device__ __forceinline__ void act_and_slope(f2 z, f2& f, f2& s) {
     if (ACT == kActSilu) {
-        const float g = rcp_approx(1.f + ex2_approx(-kLog2e * z));
-        f = z * g;
-        s = fmaf(f, 1.f - g, g);
+        const f2 g = rcp_each(add2(ex2_each(mul2(z, two(-kLog2e))), two(1.f)));
+        f = mul2(z, g);
+        s = fma2(f, less_from(g, 1.f), g);
     } else if (ACT == kActGelu) {
-        const float t = rcp_approx(fmaf(0.3275911f * 0.7071067811865476f, fabsf(z), 1.f)), e = ex2_approx((-0.5f * kLog2e * z) * z);
-        float p = fmaf(0.5f * 1.061405429f, t, 0.5f * -1.453152027f);
-        p = fmaf(p, t, 0.5f * 1.421413741f);
-        p = fmaf(p, t, 0.5f * -0.284496736f);
-        p = fmaf(p, t, 0.5f * 0.254829592f);
-        const float q = p * t * e, c = z >= 0.f ? 1.f - q : q;
-        f = z * c;
-        s = fmaf(z * 0.3989422804014327f, e, c);
+        float lo, hi;
+        one_each(z, lo, hi);
+        const f2 t = rcp_each(fma2(two(fabsf(lo), fabsf(hi)), two(0.3275911f * 0.7071067811865476f), two(1.f)));
+        const f2 e = ex2_each(mul2(mul2(z, two(-0.5f * kLog2e)), z));
+        f2 p = fma2(t, two(0.5f * 1.061405429f), two(0.5f * -1.453152027f));
+        p = fma2(p, t, two(0.5f * 1.421413741f));
+        p = fma2(p, t, two(0.5f * -0.284496736f));
+        p = fma2(p, t, two(0.5f * 0.254829592f));
+        float a, b;                      // 1/2 - erfc / 2 = |Phi - 1/2|
+        one_each(less_from(mul2(mul2(p, t), e), 0.5f), a, b);
+        const f2 c = add2(two(copysignf(a, lo), copysignf(b, hi)), two(0.5f));
+        f = mul2(z, c);
+        s = fma2(mul2(z, two(0.3989422804014327f)), e, c);
     } else if (ACT == kActGeluTanh) {
-        const float zz = z * z, g = rcp_approx(1.f + ex2_approx(z * fmaf(-2.f * kLog2e * kGeluA * kGeluB, zz, -2.f * kLog2e * kGeluA)));
-        f = z * g;
-        s = fmaf(fmaf(-f, g, f), fmaf(6.f * kGeluA * kGeluB, zz, 2.f * kGeluA), g);
+        const f2 zz = mul2(z, z);
+        const f2 u = mul2(z, fma2(zz, two(-2.f * kLog2e * kGeluA * kGeluB), two(-2.f * kLog2e * kGeluA)));
+        const f2 g = rcp_each(add2(ex2_each(u), two(1.f)));
+        f = mul2(z, g);
+        s = fma2(mul2(f, less_from(g, 1.f)), fma2(zz, two(6.f * kGeluA * kGeluB), two(2.f * kGeluA)), g);
     } else {
-        f = z; s = 1.f;
+        f = z; s = two(1.f);
     }
 }
 template <int ACT>
+__device__ __forceinline__ void activation2(float& a, float& b) {
+    f2 f, s;
+    act_and_slope<ACT>(two(a, b), f, s);
+    one_each(f, a, b);
+}
+template <int ACT>
 __device__ __forceinline__ float activation(float z) {
-    float f, s;
-    act_and_slope<ACT>(z, f, s);
-    return f;
+    float a = z, b = z;
+    activation2<ACT>(a, b);
+    return a;
 }
 template <int ACT>
 __device__ __forceinline__ void activate8(float (&v)[8]) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = activation<ACT>(v[i]);
+    for (int i = 0; i < 8; i += 2) activation2<ACT>(v[i], v[i + 1]);
 }
 __device__ __forceinline__ void activate8(float (&v)[8], int act) {
     switch (act) {
@@ -240,15 +258,15 @@ __device__ __forceinline__ void finish16(const Epilogue& e, const void* gate, in
     switch (e.act) {
         case kActGeluTanh:
 #pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] = activation<kActGeluTanh>(v[i]);
+            for (int i = 0; i < 16; i += 2) activation2<kActGeluTanh>(v[i], v[i + 1]);
             break;
         case kActGelu:
 #pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] = activation<kActGelu>(v[i]);
+            for (int i = 0; i < 16; i += 2) activation2<kActGelu>(v[i], v[i + 1]);
             break;
         case kActSilu:
 #pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] = activation<kActSilu>(v[i]);
+            for (int i = 0; i < 16; i += 2) activation2<kActSilu>(v[i], v[i + 1]);
             break;
         default: break;
     }
