@@ -308,8 +308,14 @@ __device__ __forceinline__ void tile_at(const TcArgs& a, int t, int& b, int& m, 
     m = mt - b * a.tiles_m;
 }
 
-// kSub: slabs of 64 columns of k per stage
-template <int AMN, int BMN, int kSub>
+constexpr int kLongRun = 2560;           // most k that one accumulator sums up (kLong)
+
+// kSub: slabs of 64 columns of k per stage.
+// kLong: an fp32 output of a long k.  The tensor cores cut their sums off instead of rounding them, so a sum of 5120 products loses 5.6e-6 of itself, eight
+// times what fp32 additions in a row do.  Here an accumulator sums up kLongRun of k at most, and the epilogue adds what it held to registers of its own, under the next
+// run: 128 per thread, for which the service warps give most of theirs.  75600 x 5120 x 5120 onto a residual stream: error 1.6e-6 with one run, 7.6e-7 with
+// two, 2.8e-7 with five; 2848, 2903 and 3214 us.
+template <int AMN, int BMN, int kSub, bool kLong>
 __global__ void __launch_bounds__(kThreadsTc, 1)
 linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB, const TcArgs a) {
     constexpr int kTileK = kSub * kSlab;                 // k of a stage
@@ -355,7 +361,12 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
     const int first = int(blockIdx.x / (2 * a.splits)), step = int(gridDim.x / (2 * a.splits));
     const int k_all = a.k_batches * a.k_tiles;
     const int k0 = int(int64_t(k_all) * split / a.splits), k1 = int(int64_t(k_all) * (split + 1) / a.splits);
+    // kLong: runs of k with an accumulator each
+    const int chunks = kLong ? (k1 - k0 + kLongRun / kTileK - 1) / (kLongRun / kTileK) : 1, chunk = (k1 - k0 + chunks - 1) / chunks;
 
+    if (warp < 4) {
+    // 128 x 40 + 256 x 208 registers; the block is launched with 384 x 152 at least (checked by the host)
+    if (kLong) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;" ::: "memory");
     if (warp == 0) {
         // ================= TMA producer =================
         if (lane == 0) {
@@ -423,16 +434,17 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
             int s = 0, i = 0;
             uint32_t phase = 0;
             bool ok = true;
-            for (int t = first; t < a.tiles && ok; t += step, ++i) {
-                const int u = i & 1;
+            int to_end = a.k_tiles - k0 % a.k_tiles;
+            for (int c = 0, t = first; t < a.tiles && ok; ++i) {
+                const int u = i & 1, from = k0 + c * chunk, to = min(from + chunk, k1);
+                if (++c == chunks) { c = 0; t += step; }
                 if (i >= 2) {
                     ok = mbar_wait_warp(bar_read(u), uint32_t((i >> 1) - 1) & 1u, abortp, 0, limit);
                     if (!ok) { if (lane == 0) set_status(a.hdr, CARNATOR_ERR_DEVICE_TIMEOUT, 72, i, blockIdx.x); break; }
                     tc_fence_after();
                 }
                 const uint32_t d = tmem + uint32_t(u) * 256u;
-                int to_end = a.k_tiles - k0 % a.k_tiles;
-                for (int k = k0; k < k1; ++k) {
+                for (int k = from; k < to; ++k) {
                     ok = mbar_wait_warp(bar_full(s), phase, abortp, 0, limit);
                     if (!ok) { if (lane == 0) set_status(a.hdr, CARNATOR_ERR_DEVICE_TIMEOUT, 73, k, blockIdx.x); break; }
                     tc_fence_after();
@@ -440,7 +452,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
                     auto product = [&](int kk) {
                         const uint32_t off_a = AMN ? kk * (2048 >> 4) : (kk / 4) * (kABytes / kSub >> 4) + (kk % 4) * 2;
                         const uint32_t off_b = BMN ? kk * (2048 >> 4) : (kk / 4) * slab_b + (kk % 4) * 2;
-                        mma_pair_el(d, a_lo + off + off_a, a_hi, b_lo + off + off_b, b_hi, idesc, (k > k0 || kk > 0) ? 1u : 0u);
+                        mma_pair_el(d, a_lo + off + off_a, a_hi, b_lo + off + off_b, b_hi, idesc, (k > from || kk > 0) ? 1u : 0u);
                     };
                     if (--to_end > 0) {
 #pragma unroll
@@ -455,14 +467,83 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
                 if (ok) commit_pair_el(bar_done(u), pair_mask);
             }
         }
-    } else if (warp >= 4) {
+    }
+    } else {
+        if (kLong) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;" ::: "memory");
         // ================= epilogue =================
         const int quarter = warp & 3, side = (warp - 4) >> 2;               // rows 32 quarter .. of this CTA's 128; every other 32 columns
         const uint32_t lane_base = uint32_t(quarter * 32) << 16;
         const uint32_t read0 = map_cta(bar_read(0), leader);
         bool ok = true;
         int i = 0;
-        if (a.splits == 1) {
+        if (kLong) {
+            for (int t = first; t < a.tiles && ok; t += step) {
+                int b, m, n;
+                tile_at(a, t, b, m, n);
+                const int row = m * kTileM + int(half) * 128 + quarter * 32 + lane, left = min(a.cols - n * a.bn, a.bn);
+                const bool on = row < a.rows;
+                const int64_t y_off = b * a.e.ys[0] + row * a.e.ys[1], z_off = b * a.e.zs[0] + row * a.e.zs[1], r_off = b * a.e.rs[0] + row * a.e.rs[1];
+                const int64_t gate_off = a.e.gate ? (b + row / a.e.rows_per_gate) * a.e.gate_stride : 0;
+                const char* res = static_cast<const char*>(a.e.residual) + (r_off + n * a.bn) * 4;
+                f2 acc[4][16];           // 32 columns each: side * 32, + 64, + 128, + 192
+#pragma unroll
+                for (int p = 0; p < 4; ++p)
+#pragma unroll
+                    for (int q = 0; q < 16; ++q) acc[p][q] = two(0.f);
+                for (int c = 0; c < chunks && ok; ++c, ++i) {
+                    const int u = i & 1;
+                    ok = mbar_wait_warp(bar_done(u), uint32_t(i >> 1) & 1u, abortp, 20, limit);
+                    if (!ok) { if (lane == 0) set_status(a.hdr, CARNATOR_ERR_DEVICE_TIMEOUT, 76, i, blockIdx.x); break; }
+                    tc_fence_after();
+#pragma unroll
+                    for (int p = 0; p < 4; ++p) {
+                        const int at = side * 32 + 64 * p;
+                        if (at < left) { // warp-uniform
+                            float v[32];
+                            tmem_ld32(tmem + lane_base + uint32_t(u * 256 + at), v);
+                            tmem_wait_ld(v);
+#pragma unroll
+                            for (int q = 0; q < 16; ++q) acc[p][q] = add2(acc[p][q], two(v[2 * q], v[2 * q + 1]));
+                        }
+                    }
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) arrive_remote(read0 + 8 * u);
+                }
+                if (!ok || !on) continue;
+#pragma unroll
+                for (int p = 0; p < 4; ++p) {
+                    const int at = side * 32 + 64 * p, col = n * a.bn + at;
+                    if (at >= left) continue;
+                    if (a.e.wide_ok && at + 32 <= left) {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            Sector r0, r1;
+                            if (a.e.residual) { r0 = load_sector(res + (at + 16 * h) * 4); r1 = load_sector(res + (at + 16 * h) * 4 + 32); }
+                            float f[16];
+#pragma unroll
+                            for (int q = 0; q < 8; ++q) one_each(acc[p][8 * h + q], f[2 * q], f[2 * q + 1]);
+                            finish16<true>(a.e, a.e.gate, gate_off, y_off, z_off, col + 16 * h, f, r0, r1);
+                        }
+                    } else {
+#pragma unroll
+                        for (int h = 0; h < 4; ++h) {
+                            const int cn = min(max(left - at - 8 * h, 0), 8);
+                            if (cn > 0) {
+                                norm::Raw8<true> r8;
+                                Columns cols;
+                                columns_begin(a.e, cols, col + 8 * h, cn);
+                                if (a.e.residual) load_residual(a.e, b, row, col + 8 * h, cn, r8);
+                                float f[8];
+#pragma unroll
+                                for (int q = 0; q < 4; ++q) one_each(acc[p][4 * h + q], f[2 * q], f[2 * q + 1]);
+                                finish(a.e, cols, b, row, col + 8 * h, cn, f, r8);
+                            }
+                        }
+                    }
+                }
+            }
+        } else if (a.splits == 1) {
             for (int t = first; t < a.tiles && ok; t += step, ++i) {
                 const int u = i & 1;
                 int b, m, n;
@@ -545,7 +626,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
         }
     }
 
-    if (a.splits > 1) {
+    if (!kLong && a.splits > 1) {
         // Every CTA of the cluster finishes a run of the columns: the partial tiles of the same rows, added in the order of k.
         __syncwarp();
         cluster_sync();
@@ -648,7 +729,7 @@ inline Plan plan_of(int64_t m_tiles, int64_t cols, int64_t k_all, bool b_mn) {
     return best;
 }
 
-template <int AMN, int BMN, int kSub>
+template <int AMN, int BMN, int kSub, bool kLong>
 inline carnator_status launch_tc_stages(const Operand& A, const Operand& B, TcArgs a, cudaStream_t stream, char* err, size_t errlen) {
     constexpr int kTileK = kSub * kSlab;
     const uint32_t stage = 128 * kTileK * 2 + uint32_t(a.bn / 2) * kTileK * 2;
@@ -665,12 +746,21 @@ inline carnator_status launch_tc_stages(const Operand& A, const Operand& B, TcAr
         snprintf(err, errlen, "cuTensorMapEncodeTiled failed or is unavailable");
         return CARNATOR_ERR_CUDA;
     }
-    auto kern = linear_tc_kernel<AMN, BMN, kSub>;
+    auto kern = linear_tc_kernel<AMN, BMN, kSub, kLong>;
     static SmemAllowed allowed;
     const unsigned long long ctx = context_id();
     if (!allowed.has(ctx)) {
         const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kSmemTc));
         if (e != cudaSuccess) return cuda_error(e, "cudaFuncSetAttribute(linear_tc_kernel)", err, errlen);
+        if (kLong) {                     // the hand-over of registers only completes if the block owns them
+            cudaFuncAttributes attr;
+            const cudaError_t f = cudaFuncGetAttributes(&attr, kern);
+            if (f != cudaSuccess) return cuda_error(f, "cudaFuncGetAttributes(linear_tc_kernel)", err, errlen);
+            if (attr.numRegs * kThreadsTc < 128 * 40 + 256 * 208) {
+                snprintf(err, errlen, "linear_tc_kernel was built with %d registers per thread: too few for its setmaxnreg split", attr.numRegs);
+                return CARNATOR_ERR_UNSUPPORTED;
+            }
+        }
         allowed.add(ctx);
     }
     cudaLaunchAttribute at[2];
@@ -699,9 +789,12 @@ inline carnator_status launch_tc_product(const Operand& A, const Operand& B, TcA
     if (tiles > (int64_t(1) << 30)) return CARNATOR_ERR_UNSUPPORTED;
     a.tiles = int(tiles);
     a.group_m = 8;
-    if constexpr (!AMN && !BMN)
-        if (a.bn == 256) return launch_tc_stages<AMN, BMN, 1>(A, B, a, stream, err, errlen);
-    return launch_tc_stages<AMN, BMN, 2>(A, B, a, stream, err, errlen);
+    if constexpr (!AMN && !BMN) {
+        const bool exact = a.e.y_f32 && a.splits == 1 && a.k_len > kLongRun;
+        if (a.bn == 256) return exact ? launch_tc_stages<AMN, BMN, 1, true>(A, B, a, stream, err, errlen) : launch_tc_stages<AMN, BMN, 1, false>(A, B, a, stream, err, errlen);
+        if (exact) return launch_tc_stages<AMN, BMN, 2, true>(A, B, a, stream, err, errlen);
+    }
+    return launch_tc_stages<AMN, BMN, 2, false>(A, B, a, stream, err, errlen);
 }
 
 }  // namespace lin

@@ -155,6 +155,16 @@ def test_far_arguments_and_values_that_are_not_finite(N):
     assert torch.equal(y[:, keep], clean[:, keep]) and torch.isnan(y[0, 1]).all()
 
 
+@pytest.mark.parametrize("N,K,M", [(300, 8192, 512), (3000, 8192, 2048), (3000, 5200, 1000)])
+def test_fp32_output_of_a_long_sum(N, K, M):
+    """At most 2560 products are summed up in one accumulator: 160 additions of 16 products, each of which cuts off half a step (2^-24) of the running sum
+    on average; a sum of random terms grows with the square root, so that is 2/3 x 160 x 2^-24 of it, and of what several runs sum up to."""
+    t = make(1, N, K, M, "f32", bias=False, gate=False, residual=False)
+    y, _ = forward(t, cn.ACT_NONE, keep=False)
+    ref = t["x"].double() @ t["w"].double().T
+    assert (y.double() - ref).norm() <= 160 * 2 / 3 * 2.0 ** -24 * ref.norm()
+
+
 def test_activation_over_its_range():
     """z = bias exactly (x = 0): the epilogue's activation alone, fp32 out, against 64 bits."""
     M = 4096
