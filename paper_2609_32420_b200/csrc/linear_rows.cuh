@@ -11,7 +11,6 @@ namespace carnator {
 namespace lin {
 
 constexpr int kRowsMost = 16;            // rows of x per call that this kernel takes: two column tiles of the instruction
-constexpr int kRowsWarps = 8;
 
 struct RowsArgs {
     Epilogue e;
@@ -34,7 +33,7 @@ __device__ __forceinline__ void mma_16x8x16(float (&d)[4], uint32_t a0, uint32_t
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-template <int NT>                        // column tiles of 8 rows of x
+template <int NT, int kRowsWarps>        // column tiles of 8 rows of x; warps that share k
 __global__ void __launch_bounds__(32 * kRowsWarps) linear_rows_kernel(const RowsArgs a) {
     __shared__ float sums[kRowsWarps][16][8 * NT + 1];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
@@ -88,13 +87,13 @@ __global__ void __launch_bounds__(32 * kRowsWarps) linear_rows_kernel(const Rows
         sums[warp][g + 8][j * 8 + 2 * t + 1] = d[j][3];
     }
     __syncthreads();
-    const int f = tid & 15, col = f0 + f, row = tid >> 4;
-    if (row < 8 * NT && row < a.rows && col < a.cols) {
+    auto param = [&](const void* p, int64_t i, int f32) { return f32 ? static_cast<const float*>(p)[i] : __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]); };
+    const int f = tid & 15, col = f0 + f;
+    for (int row = tid >> 4; row < a.rows && col < a.cols; row += 2 * kRowsWarps) {
         float z = 0.f;
 #pragma unroll
         for (int k = 0; k < kRowsWarps; ++k) z += sums[k][f][row];
         const int b = row / a.per_batch, r = row - b * a.per_batch;
-        auto param = [&](const void* p, int64_t i, int f32) { return f32 ? static_cast<const float*>(p)[i] : __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]); };
         if (a.e.bias) z += param(a.e.bias, col, a.e.bias_f32);
         if (a.e.z) static_cast<__nv_bfloat16*>(a.e.z)[b * a.e.zs[0] + r * a.e.zs[1] + col] = __float2bfloat16_rn(z);
         float y = a.e.act == kActGeluTanh ? activation<kActGeluTanh>(z) : a.e.act == kActGelu ? activation<kActGelu>(z)
@@ -107,9 +106,18 @@ __global__ void __launch_bounds__(32 * kRowsWarps) linear_rows_kernel(const Rows
     }
 }
 
-inline cudaError_t launch_rows(const RowsArgs& a, cudaStream_t stream) {
+// Warps that share k: many where there are few CTAs, so that all of W is on its way at once (1536 x 1536, 96 CTAs: 16 warps 3.0 us, 8 4.5), few where
+// CTAs fill the SMs several times over (30720 x 5120, 1920 CTAs: 4 warps 49.0 us, 8 53.5, 16 82; 5120 x 5120, 320 CTAs: 8 warps 8.7 us, 4 14, 16 15).
+template <int NT>
+inline cudaError_t launch_rows_tiles(const RowsArgs& a, cudaStream_t stream) {
     const int grid = ceil_div(a.cols, 16);
-    return launch_dependent(a.rows <= 8 ? linear_rows_kernel<1> : linear_rows_kernel<2>, dim3(grid), dim3(32 * kRowsWarps), 0, stream, a);
+    const int warps = grid <= 148 ? 16 : grid <= 3 * 148 ? 8 : 4;
+    auto kern = warps == 16 ? linear_rows_kernel<NT, 16> : warps == 8 ? linear_rows_kernel<NT, 8> : linear_rows_kernel<NT, 4>;
+    return launch_dependent(kern, dim3(grid), dim3(32 * warps), 0, stream, a);
+}
+
+inline cudaError_t launch_rows(const RowsArgs& a, cudaStream_t stream) {
+    return a.rows <= 8 ? launch_rows_tiles<1>(a, stream) : launch_rows_tiles<2>(a, stream);
 }
 
 }  // namespace lin
