@@ -1143,7 +1143,7 @@ GradWs grad_ws_layout(void* base, const carnator_linear_shape* s) {
     GradWs w;
     char* p = static_cast<char*>(base);
     size_t off = align256(sizeof(WsHeader));
-    w.dz_stride = (int64_t(s->out_features) + 7) / 8 * 8;
+    w.dz_stride = (int64_t(s->out_features) + 63) / 64 * 64;        // rows on whole lines, as the products fetch them
     w.dz = reinterpret_cast<__nv_bfloat16*>(p + off);    off += align256(size_t(s->B) * s->N * w.dz_stride * 2);
     w.chunks = lin::grad_chunks(s->B, s->N, s->out_features);
     const size_t part = align256(size_t(std::max(s->B * w.chunks, lin::grad_chunks(1, int64_t(s->B) * s->N, s->out_features))) * s->out_features * 4);
@@ -1184,7 +1184,7 @@ extern "C" carnator_status carnator_linear(const void* X, const void* W, const v
     e.act = s->activation; e.y_f32 = s->y_dtype == CARNATOR_DTYPE_F32;
     e.bias_f32 = s->bias_dtype == CARNATOR_DTYPE_F32; e.gate_f32 = s->gate_dtype == CARNATOR_DTYPE_F32;
     e.vec_ok = vec16(bias, 0, s->bias_dtype) && vec16(gate, s->gate_stride, s->gate_dtype);
-    e.wide_ok = e.vec_ok && rows32(Y, s->y_stride, s->y_dtype) && rows32(Z_opt, s->z_stride, CARNATOR_DTYPE_BF16) &&
+    e.wide_ok = rows32(Y, s->y_stride, s->y_dtype) && rows32(Z_opt, s->z_stride, CARNATOR_DTYPE_BF16) &&
                 rows32(residual, s->residual_stride, s->y_dtype);
     e.rows_per_gate = s->N;
     const int64_t rows = int64_t(s->B) * s->N;

@@ -44,7 +44,7 @@ struct Epilogue {
     const void* bias; const void* gate; const void* residual;
     int64_t ys[2], zs[2], rs[2], gate_stride;      // (batch, row)
     int act, y_f32, bias_f32, gate_f32, vec_ok;
-    int wide_ok;                         // y, z and residual: rows start on 32-byte boundaries; bias and gate on 16
+    int wide_ok;                         // rows of y, z and residual start on 32-byte boundaries
     int rows_per_gate;                   // rows that share a gate row (batch entries that follow each other evenly are one)
 };
 
@@ -57,7 +57,7 @@ struct TcArgs {
     int bn;                              // columns of a tile, a multiple of 32 (of 128 where B is MN-major)
     int k_batches, k_tiles;              // k: batch entries (dW) x tiles of 64
     int k_len;                           // k of a batch entry
-    int a_slabs, b_slabs;                // MN-major: the slabs of a stage in one copy (0: a copy per slab)
+    int a_slabs, b_slabs;                // MN-major: whole 64-column slabs of the operand, which a tile fetches in one copy where all of its slabs are whole
     int stages, splits;
 };
 
@@ -219,15 +219,26 @@ __device__ __forceinline__ void finish(const Epilogue& e, Columns& c, int b, int
 
 // 32 bytes: a whole sector per lane.  No clobber of memory: a residual is read by the lane that writes y over it, before.
 struct Sector { uint32_t q[8]; };
-__device__ __forceinline__ Sector load_sector(const void* p) {
+// `wide`: it starts on a 32-byte boundary; else on a 16-byte one.
+__device__ __forceinline__ Sector load_sector(const void* p, int wide) {
     Sector s;
-    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];" : "=r"(s.q[0]), "=r"(s.q[1]), "=r"(s.q[2]), "=r"(s.q[3]),
-                 "=r"(s.q[4]), "=r"(s.q[5]), "=r"(s.q[6]), "=r"(s.q[7]) : "l"(p));
+    if (wide) {
+        asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];" : "=r"(s.q[0]), "=r"(s.q[1]), "=r"(s.q[2]), "=r"(s.q[3]),
+                     "=r"(s.q[4]), "=r"(s.q[5]), "=r"(s.q[6]), "=r"(s.q[7]) : "l"(p));
+    } else {
+        asm volatile("ld.global.v4.b32 {%0, %1, %2, %3}, [%8];\n\tld.global.v4.b32 {%4, %5, %6, %7}, [%8+16];" : "=&r"(s.q[0]), "=&r"(s.q[1]), "=&r"(s.q[2]), "=&r"(s.q[3]),
+                     "=&r"(s.q[4]), "=&r"(s.q[5]), "=&r"(s.q[6]), "=&r"(s.q[7]) : "l"(p));
+    }
     return s;
 }
-__device__ __forceinline__ void store_sector(void* p, const Sector& s) {
-    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(s.q[0]), "r"(s.q[1]), "r"(s.q[2]), "r"(s.q[3]),
-                 "r"(s.q[4]), "r"(s.q[5]), "r"(s.q[6]), "r"(s.q[7]));
+__device__ __forceinline__ void store_sector(void* p, const Sector& s, int wide) {
+    if (wide) {
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(s.q[0]), "r"(s.q[1]), "r"(s.q[2]), "r"(s.q[3]),
+                     "r"(s.q[4]), "r"(s.q[5]), "r"(s.q[6]), "r"(s.q[7]));
+    } else {
+        asm volatile("st.global.v4.b32 [%0], {%1, %2, %3, %4};\n\tst.global.v4.b32 [%0+16], {%5, %6, %7, %8};" ::"l"(p), "r"(s.q[0]), "r"(s.q[1]), "r"(s.q[2]), "r"(s.q[3]),
+                     "r"(s.q[4]), "r"(s.q[5]), "r"(s.q[6]), "r"(s.q[7]));
+    }
 }
 __device__ __forceinline__ Sector pack16(const float (&v)[16]) {
     Sector s;
@@ -235,26 +246,26 @@ __device__ __forceinline__ Sector pack16(const float (&v)[16]) {
     for (int i = 0; i < 8; ++i) s.q[i] = norm::pack_bf16(v[2 * i], v[2 * i + 1]);
     return s;
 }
-// 16 values of a parameter vector that starts on a 16-byte boundary
-__device__ __forceinline__ void load_param16(const void* base, int64_t off, int f32, float (&v)[16]) {
+// 16 values of a parameter vector
+__device__ __forceinline__ void load_param16(const void* base, int64_t off, int f32, int vec_ok, float (&v)[16]) {
     float a[8], b[8];
-    norm::load_param8(base, off, f32, 1, 8, a);
-    norm::load_param8(base, off + 8, f32, 1, 8, b);
+    norm::load_param8(base, off, f32, vec_ok, 8, a);
+    norm::load_param8(base, off + 8, f32, vec_ok, 8, b);
 #pragma unroll
     for (int i = 0; i < 8; ++i) { v[i] = a[i]; v[8 + i] = b[i]; }
 }
-// Epilogue of 16 columns of one row, all of them there and everything aligned (wide_ok).  `gate`: the entry's gate row or NULL;
+// Epilogue of 16 columns of one row, all of them there.  `gate`: the entry's gate row or NULL;
 // `res`: the residual's sectors (one of bf16, two of fp32), loaded before.
 template <bool YF>
 __device__ __forceinline__ void finish16(const Epilogue& e, const void* gate, int64_t gate_off, int64_t y_off, int64_t z_off, int col, float (&v)[16],
                                          const Sector& r0, const Sector& r1) {
     if (e.bias) {
         float t[16];
-        load_param16(e.bias, col, e.bias_f32, t);
+        load_param16(e.bias, col, e.bias_f32, e.vec_ok, t);
 #pragma unroll
         for (int i = 0; i < 16; ++i) v[i] += t[i];
     }
-    if (e.z) store_sector(static_cast<__nv_bfloat16*>(e.z) + z_off + col, pack16(v));
+    if (e.z) store_sector(static_cast<__nv_bfloat16*>(e.z) + z_off + col, pack16(v), e.wide_ok);
     switch (e.act) {
         case kActGeluTanh:
 #pragma unroll
@@ -272,7 +283,7 @@ __device__ __forceinline__ void finish16(const Epilogue& e, const void* gate, in
     }
     if (gate) {
         float t[16];
-        load_param16(gate, gate_off + col, e.gate_f32, t);
+        load_param16(gate, gate_off + col, e.gate_f32, e.vec_ok, t);
 #pragma unroll
         for (int i = 0; i < 16; ++i) v[i] *= t[i];
     }
@@ -290,10 +301,10 @@ __device__ __forceinline__ void finish16(const Epilogue& e, const void* gate, in
         for (int h = 0; h < 2; ++h) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) s.q[i] = __float_as_uint(v[8 * h + i]);
-            store_sector(p + 8 * h, s);
+            store_sector(p + 8 * h, s, e.wide_ok);
         }
     } else {
-        store_sector(static_cast<__nv_bfloat16*>(e.y) + y_off + col, pack16(v));
+        store_sector(static_cast<__nv_bfloat16*>(e.y) + y_off + col, pack16(v), e.wide_ok);
     }
 }
 
@@ -317,7 +328,8 @@ constexpr int kLongRun = 2560;           // most k that one accumulator sums up 
 // two, 2.8e-7 with five; 2848, 2903 and 3214 us.
 template <int AMN, int BMN, int kSub, bool kLong>
 __global__ void __launch_bounds__(kThreadsTc, 1)
-linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB, const TcArgs a) {
+linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB, const __grid_constant__ CUtensorMap mapAs,
+                 const __grid_constant__ CUtensorMap mapBs, const TcArgs a) {
     constexpr int kTileK = kSub * kSlab;                 // k of a stage
     constexpr uint32_t kABytes = 128 * kTileK * 2;       // a CTA's share of A per stage
     extern __shared__ unsigned char lin_smem[];
@@ -346,7 +358,11 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }
-    if (warp == 0 && lane == 0) { prefetch_tmap(&mapA); prefetch_tmap(&mapB); }
+    if (warp == 0 && lane == 0) {
+        prefetch_tmap(&mapA); prefetch_tmap(&mapB);
+        if (AMN) prefetch_tmap(&mapAs);
+        if (BMN) prefetch_tmap(&mapBs);
+    }
     grid_launch_dependents();
     tc_fence_before();
     __syncwarp();
@@ -387,7 +403,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
                     const uint32_t sa = base + uint32_t(s) * stage_bytes, sb = sa + kABytes, bar = full0 + 8 * s;
                     const int k = kt * kTileK;
                     if (AMN) {           // two slabs of 64 columns of m, the stage's rows of k
-                        if (a.a_slabs) tma_load_pair_slabs(sa, &mapA, bar, k, m0 / kSlab, kb);
+                        if (m0 / kSlab + 2 <= a.a_slabs) tma_load_pair_slabs(sa, &mapAs, bar, k, m0 / kSlab, kb);
                         else {
                             tma_load_pair(sa, &mapA, bar, m0, k, kb);
                             tma_load_pair(sa + kABytes / 2, &mapA, bar, m0 + kSlab, k, kb);
@@ -396,7 +412,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
                         for (int c = 0; c < kSub; ++c) tma_load_pair(sa + c * (kABytes / kSub), &mapA, bar, k + c * kSlab, m0, b);
                     }
                     if (BMN) {
-                        if (a.b_slabs) tma_load_pair_slabs(sb, &mapB, bar, k, n0 / kSlab, kb);
+                        if (n0 / kSlab + a.bn / 128 <= a.b_slabs) tma_load_pair_slabs(sb, &mapBs, bar, k, n0 / kSlab, kb);
                         else
                             for (int c = 0; c < a.bn / 2; c += kSlab) tma_load_pair(sb + uint32_t(c) * kTileK * 2, &mapB, bar, n0 + c, k, kb);
                     } else {
@@ -515,11 +531,11 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
                 for (int p = 0; p < 4; ++p) {
                     const int at = side * 32 + 64 * p, col = n * a.bn + at;
                     if (at >= left) continue;
-                    if (a.e.wide_ok && at + 32 <= left) {
+                    if (at + 32 <= left) {
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
                             Sector r0, r1;
-                            if (a.e.residual) { r0 = load_sector(res + (at + 16 * h) * 4); r1 = load_sector(res + (at + 16 * h) * 4 + 32); }
+                            if (a.e.residual) { r0 = load_sector(res + (at + 16 * h) * 4, a.e.wide_ok); r1 = load_sector(res + (at + 16 * h) * 4 + 32, a.e.wide_ok); }
                             float f[16];
 #pragma unroll
                             for (int q = 0; q < 8; ++q) one_each(acc[p][8 * h + q], f[2 * q], f[2 * q + 1]);
@@ -558,12 +574,12 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
                 tc_fence_after();
                 for (int c = side * 32; c < left; c += 64) {               // warp-uniform
                     const int col = n * a.bn + c;
-                    const bool wide = a.e.wide_ok && c + 32 <= left;
+                    const bool whole = c + 32 <= left;
                     Sector r0, r1, r2, r3;
-                    if (a.e.residual && wide && on) {
+                    if (a.e.residual && whole && on) {
                         const char* p = res + c * (a.e.y_f32 ? 4 : 2);
-                        r0 = load_sector(p); r1 = load_sector(p + 32);
-                        if (a.e.y_f32) { r2 = load_sector(p + 64); r3 = load_sector(p + 96); }
+                        r0 = load_sector(p, a.e.wide_ok); r1 = load_sector(p + 32, a.e.wide_ok);
+                        if (a.e.y_f32) { r2 = load_sector(p + 64, a.e.wide_ok); r3 = load_sector(p + 96, a.e.wide_ok); }
                     }
                     float v[32];
                     tmem_ld32(tmem + lane_base + uint32_t(u * 256 + c), v);
@@ -573,7 +589,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
                         __syncwarp();
                         if (lane == 0) arrive_remote(read0 + 8 * u);
                     }
-                    if (wide) {
+                    if (whole) {
                         float lo[16], hi[16];
 #pragma unroll
                         for (int q = 0; q < 16; ++q) { lo[q] = v[q]; hi[q] = v[16 + q]; }
@@ -688,7 +704,7 @@ inline bool make_map_3d(CUtensorMap* map, const void* base, int64_t batches, int
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// The same for an MN-major operand whose columns are whole slabs of 64: the columns as two dimensions, a box = 64 x box_rows x `slabs`, each
+// The same for the whole slabs of 64 columns of an MN-major operand (the last one of another width would be read past the row): the columns as two dimensions, a box = 64 x box_rows x `slabs`, each
 // slab landing as make_map_3d's box would.  One copy of 16 KB instead of two of 8: with two, dX and dW of 32760 x 1536 x 8960 took 637 and 650 us
 // instead of 597 and 583.
 inline bool make_map_slabs(CUtensorMap* map, const void* base, int64_t batches, int64_t rows, int64_t cols, int64_t batch_stride, int64_t row_stride, int box_rows,
@@ -696,7 +712,7 @@ inline bool make_map_slabs(CUtensorMap* map, const void* base, int64_t batches, 
     EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
     cuuint64_t dims[4] = {64, cuuint64_t(rows), cuuint64_t(cols / 64), cuuint64_t(batches)};
-    const cuuint64_t row = rows > 1 ? cuuint64_t(row_stride) * 2 : cuuint64_t(cols) * 2;
+    const cuuint64_t row = rows > 1 ? cuuint64_t(row_stride) * 2 : cuuint64_t((cols + 7) / 8 * 16);
     cuuint64_t strides[3] = {row, 128, batches > 1 ? cuuint64_t(batch_stride) * 2 : row};
     cuuint32_t box[4] = {64, cuuint32_t(box_rows), cuuint32_t(slabs), 1};
     cuuint32_t estr[4] = {1, 1, 1, 1};
@@ -709,11 +725,11 @@ struct Operand { const void* base; int64_t batches, rows, cols, batch_stride, ro
 
 // Columns of a tile and pairs that share one: the least time by a model in nanoseconds that was fitted to launches of 20 to 1000 rows.  A pair takes
 // 75 + 0.85 columns per 64 of k (bounded by its products at 256 columns, by fetching its operands, 64 bytes a clock and SM, below), and an epilogue that is
-// hidden except under very short k.  Joining two pairs costs 1.5 us, four 4.5 us (226 x 4096 x 1536: one pair per tile of 64 23.0 us, two per tile of 96
+// hidden except under very short k.  Joining two pairs costs 2.5 us, four 4.5 us (226 x 4096 x 1536: one pair per tile of 64 23.0 us, two per tile of 96
 // 12.2, four per tile of 128 13.3; 64 x 9216 x 1536 20.3 with two, 15.4 with four).  33 clusters of 4 CTAs or 15 of 8 find room at a time; near
-// that they start late.
+// that they start late.  Rows that start within a 64-byte piece (crooked) are fetched as more sectors: 1.6 times the time.
 struct Plan { int bn, splits; };
-inline Plan plan_of(int64_t m_tiles, int64_t cols, int64_t k_all, bool b_mn) {
+inline Plan plan_of(int64_t m_tiles, int64_t cols, int64_t k_all, bool b_mn, bool crooked) {
     Plan best = {256, 1};
     double best_cost = 1e30;
     for (int bn = 256; bn >= (b_mn ? 128 : 64); bn -= b_mn ? 128 : 32) {
@@ -721,7 +737,7 @@ inline Plan plan_of(int64_t m_tiles, int64_t cols, int64_t k_all, bool b_mn) {
         for (int splits = 1; splits <= 4; splits *= 2) {
             if ((splits == 2 && tiles > 32) || (splits == 4 && tiles > 14) || k_all < 4 * splits * (splits > 1) || bn % (8 * splits)) break;
             const int64_t turns = splits > 1 ? 1 : (tiles + 73) / 74;
-            const double k_ns = double((k_all + splits - 1) / splits) * (75 + 0.85 * bn), join = splits == 1 ? 0 : splits == 4 ? 4500 : tiles > 24 ? 4000 : 1500;
+            const double k_ns = double((k_all + splits - 1) / splits) * (75 + 0.85 * bn) * (crooked ? 1.6 : 1.0), join = splits == 1 ? 0 : splits == 4 ? 4500 : tiles > 24 ? 4000 : 2500;
             const double cost = double(turns) * std::max(k_ns, 500.0 + 4 * bn) + join;
             if (cost < best_cost * 0.995) { best_cost = cost; best = {bn, splits}; }
         }
@@ -735,14 +751,16 @@ inline carnator_status launch_tc_stages(const Operand& A, const Operand& B, TcAr
     const uint32_t stage = 128 * kTileK * 2 + uint32_t(a.bn / 2) * kTileK * 2;
     a.k_tiles = ceil_div(a.k_len, kTileK);
     a.stages = int(std::min<uint32_t>(kMaxStages, kRingBytes / stage));
-    a.a_slabs = AMN && A.cols % kSlab == 0;       // the last slab of another width would be read past the row
-    a.b_slabs = BMN && B.cols % kSlab == 0;
-    CUtensorMap ma, mb;
-    auto map = [](CUtensorMap* m, const Operand& o, bool slabs, int rows, int n) {
-        return slabs ? make_map_slabs(m, o.base, o.batches, o.rows, o.cols, o.batch_stride, o.row_stride, rows, n)
-                     : make_map_3d(m, o.base, o.batches, o.rows, o.cols, o.batch_stride, o.row_stride, rows);
+    a.a_slabs = AMN ? int(A.cols / kSlab) : 0;
+    a.b_slabs = BMN ? int(B.cols / kSlab) : 0;
+    auto map = [](CUtensorMap* m, const Operand& o, int rows) { return make_map_3d(m, o.base, o.batches, o.rows, o.cols, o.batch_stride, o.row_stride, rows); };
+    auto slabs = [](CUtensorMap* m, const CUtensorMap& plain, const Operand& o, int whole, int n) {
+        if (whole > 0 && whole >= n) return make_map_slabs(m, o.base, o.batches, o.rows, o.cols, o.batch_stride, o.row_stride, kTileK, n);
+        *m = plain;                      // not used
+        return true;
     };
-    if (!map(&ma, A, a.a_slabs, AMN ? kTileK : 128, 2) || !map(&mb, B, a.b_slabs, BMN ? kTileK : a.bn / 2, a.bn / 128)) {
+    CUtensorMap ma, mb, mas, mbs;
+    if (!map(&ma, A, AMN ? kTileK : 128) || !map(&mb, B, BMN ? kTileK : a.bn / 2) || !slabs(&mas, ma, A, a.a_slabs, 2) || !slabs(&mbs, mb, B, a.b_slabs, a.bn / 128)) {
         snprintf(err, errlen, "cuTensorMapEncodeTiled failed or is unavailable");
         return CARNATOR_ERR_CUDA;
     }
@@ -772,7 +790,7 @@ inline carnator_status launch_tc_stages(const Operand& A, const Operand& B, TcAr
     const int clusters = a.splits > 1 ? a.tiles : std::min(a.tiles, 74);
     cfg.gridDim = dim3(unsigned(clusters * 2 * a.splits)); cfg.blockDim = dim3(kThreadsTc); cfg.dynamicSmemBytes = kSmemTc; cfg.stream = stream;
     cfg.attrs = at; cfg.numAttrs = 2;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, ma, mb, a);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, ma, mb, mas, mbs, a);
     if (e != cudaSuccess) return cuda_error(e, "linear_tc_kernel", err, errlen);
     return CARNATOR_OK;
 }
@@ -782,7 +800,8 @@ inline carnator_status launch_tc_stages(const Operand& A, const Operand& B, TcAr
 // x 5120 with 160 columns 23.5 and 19.5 us), as do MN-major operands, whose copies then are 32 KB each (dW of the former 627 and 615 us).
 template <int AMN, int BMN>
 inline carnator_status launch_tc_product(const Operand& A, const Operand& B, TcArgs a, cudaStream_t stream, char* err, size_t errlen) {
-    const Plan p = plan_of(int64_t(a.batches) * a.tiles_m, a.cols, int64_t(a.k_batches) * ceil_div(a.k_len, kSlab), BMN);
+    const bool crooked = (A.rows > 1 && A.row_stride % 32) || (B.rows > 1 && B.row_stride % 32);
+    const Plan p = plan_of(int64_t(a.batches) * a.tiles_m, a.cols, int64_t(a.k_batches) * ceil_div(a.k_len, kSlab), BMN, crooked);
     a.bn = p.bn; a.splits = p.splits;
     a.tiles_n = ceil_div(a.cols, a.bn);
     const int64_t tiles = int64_t(a.batches) * a.tiles_m * a.tiles_n;
