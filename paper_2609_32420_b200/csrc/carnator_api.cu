@@ -1062,8 +1062,8 @@ extern "C" carnator_status carnator_layer_norm(const void* X, const void* weight
     norm_order(s, a, s->x_stride, s->y_stride, s->y_stride);
     a.vec_ok = vec16(weight, 0, s->weight_dtype) && vec16(bias, 0, s->weight_dtype) && vec16(shift, s->shift_stride, s->mod_dtype) && vec16(scale, s->scale_stride, s->mod_dtype);
     a.wide = norm_rows32(Y, s->y_stride, s->y_dtype);
-    const norm::Form f = norm::form_of(s->C, false);
-    a.chunks = norm::chunks_of(f, s->B, s->C, a.rows, false);
+    const norm::Form f = norm::form_of(s->C, false, s->x_dtype == CARNATOR_DTYPE_F32);
+    a.chunks = norm::chunks_of(f, s->B, s->C, a.rows, false, s->x_dtype == CARNATOR_DTYPE_F32);
     const cudaError_t e = norm::launch<false>(a, s->B, f, s->x_dtype == CARNATOR_DTYPE_F32, s->y_dtype == CARNATOR_DTYPE_F32, static_cast<cudaStream_t>(stream_));
     if (e != cudaSuccess) return cuda_fail(e, "norm_forward_kernel");
     g_launches.fetch_add(1, std::memory_order_relaxed);
@@ -1072,7 +1072,7 @@ extern "C" carnator_status carnator_layer_norm(const void* X, const void* weight
 
 extern "C" size_t carnator_layer_norm_backward_workspace_bytes(const carnator_norm_shape* s) {
     if (check_norm_shape(s) != CARNATOR_OK) return 0;
-    const int chunks = norm::chunks_of(norm::form_of(s->C, true), s->B, s->C, int64_t(s->H) * s->N, true);
+    const int chunks = norm::chunks_of(norm::form_of(s->C, true, s->x_dtype == CARNATOR_DTYPE_F32), s->B, s->C, int64_t(s->H) * s->N, true, s->x_dtype == CARNATOR_DTYPE_F32);
     return align256(size_t(s->B) * chunks * 2 * s->C * 4);
 }
 
@@ -1100,8 +1100,8 @@ extern "C" carnator_status carnator_layer_norm_backward(const void* dY, const vo
     norm_order(s, a, s->x_stride, s->dx_stride, s->dy_stride);
     a.vec_ok = vec16(weight, 0, s->weight_dtype) && vec16(scale, s->scale_stride, s->mod_dtype);
     a.wide = norm_rows32(dX, s->dx_stride, s->x_dtype);
-    const norm::Form f = norm::form_of(s->C, true);
-    a.chunks = norm::chunks_of(f, s->B, s->C, a.rows, true);
+    const norm::Form f = norm::form_of(s->C, true, s->x_dtype == CARNATOR_DTYPE_F32);
+    a.chunks = norm::chunks_of(f, s->B, s->C, a.rows, true, s->x_dtype == CARNATOR_DTYPE_F32);
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     cudaError_t e = norm::launch<true>(a, s->B, f, s->x_dtype == CARNATOR_DTYPE_F32, s->y_dtype == CARNATOR_DTYPE_F32, stream);
     if (e != cudaSuccess) return cuda_fail(e, "norm_backward_kernel");

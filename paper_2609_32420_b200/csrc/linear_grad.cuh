@@ -46,13 +46,13 @@ __global__ void __launch_bounds__(32 * kGradLanes, kGradPerSm) linear_grad_kerne
     const uint32_t ring = uint32_t(__cvta_generic_to_shared(grad_smem)), z_at = kDyBytes, stage = kDyBytes + kZBytes;
     const norm::Stage<DYF, 1, 32> in(blockIdx.x * 32 + cv);
     const norm::Stage<false, 1, 32> in_z(blockIdx.x * 32 + cv);
-    const char* dy = static_cast<const char*>(a.dy) + b * a.ds[0] * (DYF ? 4 : 2);
-    const char* zp = reinterpret_cast<const char*>(a.z) + b * a.zs[0] * 2;
+    const char* dy = static_cast<const char*>(a.dy) + (b * a.ds[0] + in.col) * (DYF ? 4 : 2);
+    const char* zp = reinterpret_cast<const char*>(a.z) + (b * a.zs[0] + in_z.col) * 2;
     int ahead = r0 + rl;
     auto fetch = [&](int s) {
         const bool on = ahead < r1;
-        in.copy(ring + uint32_t(s) * stage, on ? dy + ahead * a.ds[1] * (DYF ? 4 : 2) : dy, a.cols, 0, on);
-        if (a.z) in_z.copy(ring + uint32_t(s) * stage + z_at, on ? zp + ahead * a.zs[1] * 2 : zp, a.cols, 0, on);
+        in.copy(ring + uint32_t(s) * stage, dy + ahead * a.ds[1] * (DYF ? 4 : 2), (a.cols - in.col) * (DYF ? 4 : 2), 0, on);
+        if (a.z) in_z.copy(ring + uint32_t(s) * stage + z_at, zp + ahead * a.zs[1] * 2, (a.cols - in_z.col) * 2, 0, on);
         norm::copies_commit();
         ahead += kGradLanes;
     };

@@ -215,15 +215,16 @@ struct Stage {
         }
     }
     static constexpr uint32_t kPieces = F32 ? 2 : 1;
-    __device__ __forceinline__ void copy(uint32_t dst, const char* row, int C, int col_step, bool on) const {
+    // `row`: where the lane's first channel lies in this row; `left`: bytes from there to the end of the row.  A copy of no bytes names an address, but reads
+    // nothing there.
+    __device__ __forceinline__ void copy(uint32_t dst, const char* row, int left, int col_step, bool on) const {
 #pragma unroll
         for (int v = 0; v < V; ++v)
 #pragma unroll
             for (uint32_t h = 0; h < kPieces; ++h) {
-                const int c = col + v * col_step + int(h) * 4 * LANES;
-                const int bytes = on ? min(max((C - c) * (F32 ? 4 : 2), 0), 16) : 0;
+                const int off = (v * col_step + int(h) * 4 * LANES) * (F32 ? 4 : 2), bytes = on ? min(max(left - off, 0), 16) : 0;
                 asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + put[F32 ? h : 0] + v * kPieces * blockDim.x * 16u),
-                             "l"(row + (bytes ? int64_t(c) * (F32 ? 4 : 2) : 0)), "r"(bytes) : "memory");
+                             "l"(row + off), "r"(bytes) : "memory");
             }
     }
     __device__ __forceinline__ Eight read(uint32_t src, int v) const {
@@ -287,16 +288,20 @@ __device__ __forceinline__ void factors(const Args& a, int b, int col, int n, fl
     }
 }
 
-// Largest CTA of a form (form_of), registers per thread
-constexpr int most_threads(int lanes, int v) { return v < 3 || lanes < 32 ? 256 : 512; }
-constexpr int regs_of(int v, bool backward) { return backward ? (v == 1 ? 96 : 128) : v == 1 ? 64 : v == 2 ? 96 : 112; }
+// Largest CTA of a form (form_of) and registers per thread.  A bf16 row takes half the registers of an fp32 one, so more threads share an SM.
+constexpr int row_warps(bool backward, bool xf) { return backward || xf ? 16 : 20; }
+constexpr int most_threads(int lanes, int v, bool backward, bool xf) { return v < 3 || lanes < 32 ? 256 : 32 * row_warps(backward, xf); }
+// (A register too few is dear where the rows ahead leave the L1 cache little room: 75600 x 5120 in bf16 322 us with 112, 448 with 80 and 12 bytes spilled.)
+constexpr int regs_of(int lanes, int v, bool backward, bool xf) {
+    return backward ? (v == 1 ? 96 : 128) : xf ? (v == 1 ? 64 : v == 2 ? 96 : 112) : lanes == 32 ? 96 : v == 1 ? 56 : 80;
+}
 
 // One CTA takes a run of the rows of one batch entry, a slot one row at a time.
 template <int LANES, int V, bool XF, bool YF>
-__global__ void __launch_bounds__(most_threads(LANES, V)) __maxnreg__(regs_of(V, false)) norm_forward_kernel(const Args a) {
+__global__ void __launch_bounds__(most_threads(LANES, V, false, XF)) __maxnreg__(regs_of(LANES, V, false, XF)) norm_forward_kernel(const Args a) {
     constexpr bool kKeep = V < 3;                                 // few factors per lane: in registers, else in the table
     extern __shared__ float4 smem[];                              // tables (V > 2), then the stages
-    __shared__ float4 part[2][16];                                // each warp's mean, squared deviations and channels
+    __shared__ float4 part[2][24];                                // each warp's mean, squared deviations and channels
     const Place<LANES> pl(a.warps);
     const int b = blockIdx.y, groups = (a.C + kGroup - 1) / kGroup;
     const int r0 = int(int64_t(blockIdx.x) * a.rows / a.chunks), r1 = int(int64_t(blockIdx.x + 1) * a.rows / a.chunks);
@@ -308,14 +313,15 @@ __global__ void __launch_bounds__(most_threads(LANES, V)) __maxnreg__(regs_of(V,
     const uint32_t ring = uint32_t(__cvta_generic_to_shared(smem)) + (kKeep ? 0u : uint32_t(groups) * 64u);
     const uint32_t stage = uint32_t(V * (XF ? 2 : 1)) * blockDim.x * 16u;
     const Stage<XF, V, LANES> in(pl.at);
-    const char* x = static_cast<const char*>(a.x) + b * a.xs[0] * (XF ? 4 : 2);
+    const char* x = static_cast<const char*>(a.x) + (b * a.xs[0] + in.col) * (XF ? 4 : 2);
+    const int left_x = (a.C - in.col) * (XF ? 4 : 2);
     char* y = static_cast<char*>(a.y) + (b * a.ys[0] + col0) * (YF ? 4 : 2);
 
     Row ahead(a, r0 + pl.slot), now(ahead);
     grid_launch_dependents();
     grid_wait();                         // launched while the kernel ahead drains: nothing of global memory is touched before this
     auto fetch = [&](int s) {
-        in.copy(ring + uint32_t(s) * stage, ahead.row < r1 ? x + ahead.off(a.xs) * (XF ? 4 : 2) : x, a.C, col_step, ahead.row < r1);
+        in.copy(ring + uint32_t(s) * stage, x + ahead.off(a.xs) * (XF ? 4 : 2), left_x, col_step, ahead.row < r1);
         copies_commit();
         ahead.step(a, pl.slots, by_o, by_i);
     };
@@ -418,7 +424,7 @@ __global__ void __launch_bounds__(most_threads(LANES, V)) __maxnreg__(regs_of(V,
 
 // dX, and the CTA's partial rows of P and S.
 template <int LANES, int V, bool XF, bool YF>
-__global__ void __launch_bounds__(most_threads(LANES, V)) __maxnreg__(regs_of(V, true)) norm_backward_kernel(const Args a) {
+__global__ void __launch_bounds__(most_threads(LANES, V, true, XF)) __maxnreg__(regs_of(LANES, V, true, XF)) norm_backward_kernel(const Args a) {
     constexpr bool kKeep = V < 3;
     extern __shared__ float4 smem[];                              // table (V > 2), then the stages, which the slots' sums use afterwards
     __shared__ float2 part[2][16];
@@ -442,15 +448,16 @@ __global__ void __launch_bounds__(most_threads(LANES, V)) __maxnreg__(regs_of(V,
     const uint32_t x_bytes = uint32_t(V * (XF ? 2 : 1)) * blockDim.x * 16u, stage = x_bytes + uint32_t(V * (YF ? 2 : 1)) * blockDim.x * 16u;
     const Stage<XF, V, LANES> in(pl.at);
     const Stage<YF, V, LANES> in_dy(pl.at);
-    const char* x = static_cast<const char*>(a.x) + b * a.xs[0] * (XF ? 4 : 2);
-    const char* dy = static_cast<const char*>(a.dy) + b * a.ds[0] * (YF ? 4 : 2);
+    const char* x = static_cast<const char*>(a.x) + (b * a.xs[0] + in.col) * (XF ? 4 : 2);
+    const char* dy = static_cast<const char*>(a.dy) + (b * a.ds[0] + in_dy.col) * (YF ? 4 : 2);
+    const int left_x = (a.C - in.col) * (XF ? 4 : 2), left_dy = (a.C - in_dy.col) * (YF ? 4 : 2);
     char* dx = static_cast<char*>(a.y) + (b * a.ys[0] + col0) * (XF ? 4 : 2);
 
     Row ahead(a, r0 + pl.slot), now(ahead), after(ahead);
     auto fetch = [&](int s) {
         const bool on = ahead.row < r1;
-        in.copy(ring + uint32_t(s) * stage, on ? x + ahead.off(a.xs) * (XF ? 4 : 2) : x, a.C, col_step, on);
-        in_dy.copy(ring + uint32_t(s) * stage + x_bytes, on ? dy + ahead.off(a.ds) * (YF ? 4 : 2) : dy, a.C, col_step, on);
+        in.copy(ring + uint32_t(s) * stage, x + ahead.off(a.xs) * (XF ? 4 : 2), left_x, col_step, on);
+        in_dy.copy(ring + uint32_t(s) * stage + x_bytes, dy + ahead.off(a.ds) * (YF ? 4 : 2), left_dy, col_step, on);
         copies_commit();
         ahead.step(a, pl.slots, by_o, by_i);
     };
@@ -634,29 +641,29 @@ __global__ void __launch_bounds__(32 * kReduceWarps) norm_reduce_kernel(const Re
 // Lanes (of a warp) and warps per row, groups of 8 channels per lane, threads of a CTA.
 // The backward kernel keeps two sums per channel in registers, so where rows share a warp it has fewer channels per lane.
 struct Form { int lanes, warps, v, threads; };
-inline Form form_of(int C, bool backward) {
+inline Form form_of(int C, bool backward, bool xf) {
     const int groups = ceil_div(C, kGroup);
     if (groups <= 8) return {8, 1, 1, 256};
     if (groups <= 16) return {8, 1, 2, 256};
     if (groups <= 32) return backward ? Form{16, 1, 2, 256} : Form{8, 1, 4, 256};
     if (groups <= 64) return backward ? Form{32, 1, 2, 256} : Form{16, 1, 4, 256};
-    // as many slots as 16 warps give, which share the table of factors
+    // as many slots as a CTA's warps give, which share the table of factors
     const int warps = ceil_div(groups, 128), v = ceil_div(groups, 32 * warps);
-    return {32, warps, v < 3 ? 3 : v, 32 * warps * (16 / warps)};
+    return {32, warps, v < 3 ? 3 : v, 32 * warps * (row_warps(backward, xf) / warps)};
 }
 constexpr int kSmemPerSm = 220 * 1024;
 // bytes of shared memory of a CTA: tables, one stage of rows (fp32, the wider type, unless the types are known)
 inline int table_bytes(const Form& f, int C, bool backward) { return f.v < 3 ? 0 : ceil_div(C, kGroup) * (backward ? 32 : 64); }
 inline int stage_bytes(const Form& f, bool backward, bool xf, bool yf) { return f.v * f.threads * 16 * ((xf ? 2 : 1) + (backward ? (yf ? 2 : 1) : 0)); }
 // CTAs that share an SM: as many as its registers hold and its shared memory does with one stage each.
-inline int ctas_per_sm(const Form& f, int C, bool backward) {
-    const int regs = 65536 / (regs_of(f.v, backward) * f.threads), smem = kSmemPerSm / (table_bytes(f, C, backward) + stage_bytes(f, backward, true, true) + 2048);
+inline int ctas_per_sm(const Form& f, int C, bool backward, bool xf) {
+    const int regs = 65536 / (regs_of(f.lanes, f.v, backward, xf) * f.threads), smem = kSmemPerSm / (table_bytes(f, C, backward) + stage_bytes(f, backward, xf, true) + 2048);
     return std::max(1, std::min({2048 / f.threads, regs, smem}));
 }
 // CTAs per batch entry: one wave, and not more than there are rows for.
-inline int chunks_of(const Form& f, int B, int C, int64_t rows, bool backward) {
+inline int chunks_of(const Form& f, int B, int C, int64_t rows, bool backward, bool xf) {
     const int64_t slots = f.threads / (f.lanes * f.warps);
-    const int64_t want = std::max<int64_t>(1, int64_t(148) * ctas_per_sm(f, C, backward) / B);
+    const int64_t want = std::max<int64_t>(1, int64_t(148) * ctas_per_sm(f, C, backward, xf) / B);
     return int(std::min<int64_t>(want, (rows + slots - 1) / slots));
 }
 
@@ -666,7 +673,7 @@ inline cudaError_t launch_types(Args a, dim3 grid, const Form& f, bool xf, bool 
     const int tables = table_bytes(f, a.C, BWD), stage = stage_bytes(f, BWD, xf, yf);
     const int sums = BWD && slots > 1 ? f.threads * V * kGroup * 4 : 0;      // the slots' sums, in the stages' place
     a.warps = f.warps;
-    a.stages = std::max(1, std::min({kMostStages, (kSmemPerSm / ctas_per_sm(f, a.C, BWD) - 2048 - tables) / stage, turns}));
+    a.stages = std::max(1, std::min({kMostStages, (kSmemPerSm / ctas_per_sm(f, a.C, BWD, xf) - 2048 - tables) / stage, turns}));
     const int smem = tables + std::max(a.stages * stage, sums);
     cudaError_t e = cudaSuccess;
     static SmemAllowed allowed[4];       // of the four kernels below
