@@ -375,9 +375,12 @@ carnator_status carnator_layer_norm_backward(const void* dY, const void* X, cons
  *   dX     [B,N,in_features] with dx_stride, or NULL;  dW  [out_features,in_features] with row stride dw_stride, or NULL
  *   dbias  fp32 [out_features] or NULL;  dgate  fp32 [B,out_features] contiguous or NULL (wants gate)
  *   ws     device workspace, >= carnator_linear_backward_workspace_bytes (header, dz, partial sums)
- * Up to 16 rows in all run on a kernel that streams W once through the registers of mma.sync; more rows on tcgen05 with
- * bounded waits, whose status carnator_query_status(ws) returns.
- * Limits: B N, in_features, out_features <= 2^30, B <= 65535.
+ * Up to 8 rows in all (16 unless W is large) run on a kernel that streams W once through the registers of mma.sync; more rows on tcgen05 with
+ * bounded waits, whose status carnator_query_status(ws) returns.  An fp32 y of more than 2560 input features is summed up in
+ * runs of 2560 at most, as the tensor cores cut their sums off (2^-24 of a running sum per 16 products on average).
+ * Calls that may run at the same time (streams, captured graphs) need a workspace each, as everywhere.  The kernels of these
+ * calls may be launched while the kernel ahead of them on the stream drains; they touch no memory before it has ended.
+ * Limits: B N, in_features, out_features <= 2^27, B <= 65535.
  * ------------------------------------------------------------------------ */
 enum { CARNATOR_ACT_NONE = 0, CARNATOR_ACT_GELU_TANH = 1, CARNATOR_ACT_GELU = 2, CARNATOR_ACT_SILU = 3 };
 

@@ -991,8 +991,9 @@ bool axes_ok(const int64_t* stride, const int64_t* size, int n, int64_t row, int
     int64_t st[3], sz[3];
     int used = 0;
     for (int i = 0; i < n; ++i) {
-        if (stride[i] < 0 || stride[i] % dtype_unit(dtype) || stride[i] > (int64_t(1) << 38)) return false;
-        if (size[i] > 1) { if (positive && stride[i] == 0) return false; st[used] = stride[i]; sz[used] = size[i]; ++used; }
+        if (size[i] == 1) continue;                   // never used
+        if (stride[i] < 0 || stride[i] % dtype_unit(dtype) || stride[i] > (int64_t(1) << 38) || (positive && stride[i] == 0)) return false;
+        st[used] = stride[i]; sz[used] = size[i]; ++used;
     }
     if (!written) return true;
     int64_t extent = row;
@@ -1122,7 +1123,7 @@ carnator_status check_linear_shape(const carnator_linear_shape* s) {
     if (!s || s->B <= 0 || s->N <= 0 || s->in_features <= 0 || s->out_features <= 0) return CARNATOR_ERR_INVALID_ARG;
     if (s->activation < CARNATOR_ACT_NONE || s->activation > CARNATOR_ACT_SILU) return CARNATOR_ERR_INVALID_ARG;
     if (!dtype_ok(s->y_dtype) || !dtype_ok(s->bias_dtype) || !dtype_ok(s->gate_dtype) || s->gate_stride < 0) return CARNATOR_ERR_INVALID_ARG;
-    const int64_t most = int64_t(1) << 30;
+    const int64_t most = int64_t(1) << 27;           // products of a longer sum would outlast the bounded waits for them
     if (int64_t(s->B) * s->N > most || s->in_features > most || s->out_features > most || s->B > 65535) return CARNATOR_ERR_UNSUPPORTED;
     return CARNATOR_OK;
 }
@@ -1131,7 +1132,7 @@ bool linear_axes_ok(const carnator_linear_shape* s, const int64_t st[2], int64_t
     return axes_ok(st, size, 2, row, dtype, written, true) && (s->N == 1 || st[1] >= row);
 }
 bool matrix_ok(int64_t rows, int64_t cols, int64_t stride) {
-    return stride >= 0 && stride % 8 == 0 && stride <= (int64_t(1) << 38) && (rows == 1 || stride >= cols);
+    return rows == 1 || (stride >= cols && stride % 8 == 0 && stride <= (int64_t(1) << 38));
 }
 // Batch entries that follow each other evenly are one run of rows.
 bool runs_on(const carnator_linear_shape* s, const int64_t st[2]) { return s->B == 1 || s->N == 1 || st[0] == int64_t(s->N) * st[1]; }
@@ -1188,7 +1189,7 @@ extern "C" carnator_status carnator_linear(const void* X, const void* W, const v
                 rows32(residual, s->residual_stride, s->y_dtype);
     e.rows_per_gate = s->N;
     const int64_t rows = int64_t(s->B) * s->N;
-    if (rows <= lin::kRowsMost) {
+    if (lin::rows_take(rows, s->in_features, s->out_features)) {
         lin::RowsArgs a;
         a.e = e; a.x = static_cast<const __nv_bfloat16*>(X); a.w = static_cast<const __nv_bfloat16*>(W);
         a.xs[0] = s->x_stride[0]; a.xs[1] = s->x_stride[1]; a.w_stride = s->w_stride;
@@ -1201,7 +1202,7 @@ extern "C" carnator_status carnator_linear(const void* X, const void* W, const v
     }
     lin::TcArgs a = {};
     a.e = e;
-    a.hdr = static_cast<WsHeader*>(ws);
+    a.hdr = static_cast<WsHeader*>(ws); a.clears = 1;
     lin::Operand A = {X, s->B, s->N, s->in_features, s->x_stride[0], s->x_stride[1]};
     a.batches = s->B; a.rows = s->N;
     if (runs_on(s, s->x_stride) && runs_on(s, s->y_stride) && (!residual || runs_on(s, s->residual_stride)) && (!Z_opt || runs_on(s, s->z_stride))) {
@@ -1278,7 +1279,7 @@ extern "C" carnator_status carnator_linear_backward(const void* dY, const void* 
     for (int pass = 0; pass < 2; ++pass) {
         if (pass == 0 ? !dX_opt : !dW_opt) continue;
         lin::TcArgs a = {};
-        a.hdr = static_cast<WsHeader*>(ws);
+        a.hdr = static_cast<WsHeader*>(ws); a.clears = pass == 0 || !dX_opt;
         a.cols = s->in_features;
         lin::Operand A = dz;
         const int64_t* other = pass == 0 ? s->dx_stride : s->x_stride;

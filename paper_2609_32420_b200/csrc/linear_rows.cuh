@@ -10,7 +10,13 @@
 namespace carnator {
 namespace lin {
 
-constexpr int kRowsMost = 16;            // rows of x per call that this kernel takes: two column tiles of the instruction
+// Rows of x per call that this kernel takes: one column tile of the instruction, or two where W is not large (16 rows of 1536 x 1536: 4.0 us, on tcgen05
+// 10.2; of 1536 x 9216 6.9 and 14.2; of 8960 x 1536 12.3 and 13.4; but of 5120 x 30720, whose x every CTA reads again, 78.9 and 63.3).
+constexpr int kRowsMost = 16, kRowsOneTile = 8;
+constexpr int64_t kRowsWeights = int64_t(1) << 26;
+inline bool rows_take(int64_t rows, int64_t in_features, int64_t out_features) {
+    return rows <= kRowsOneTile || (rows <= kRowsMost && in_features * out_features < kRowsWeights);
+}
 
 struct RowsArgs {
     Epilogue e;
@@ -53,11 +59,11 @@ __global__ void __launch_bounds__(32 * kRowsWarps) linear_rows_kernel(const Rows
         const int b = xon[j] ? row / a.per_batch : 0;
         xr[j] = a.x + b * a.xs[0] + (xon[j] ? row - b * a.per_batch : 0) * a.xs[1];
     }
-    float d[NT][4];
+    float d[NT][4], d2[NT][4];           // two sums per warp: the instruction cuts its sums off, and what that loses grows with their length
 #pragma unroll
     for (int j = 0; j < NT; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) d[j][i] = 0.f;
+        for (int i = 0; i < 4; ++i) { d[j][i] = 0.f; d2[j][i] = 0.f; }
     const uint4 zero = make_uint4(0, 0, 0, 0);
     constexpr int U = 4;                 // pieces of 32 k in flight per warp
     const int pieces = (a.K + 31) / 32;
@@ -76,15 +82,15 @@ __global__ void __launch_bounds__(32 * kRowsWarps) linear_rows_kernel(const Rows
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
                 mma_16x8x16(d[j], u0[q].x, u1[q].x, u0[q].y, u1[q].y, xv[q][j].x, xv[q][j].y);
-                mma_16x8x16(d[j], u0[q].z, u1[q].z, u0[q].w, u1[q].w, xv[q][j].z, xv[q][j].w);
+                mma_16x8x16(d2[j], u0[q].z, u1[q].z, u0[q].w, u1[q].w, xv[q][j].z, xv[q][j].w);
             }
     }
 #pragma unroll
     for (int j = 0; j < NT; ++j) {       // d0, d1: feature g, rows 2t and 2t + 1 of x; d2, d3: feature g + 8
-        sums[warp][g][j * 8 + 2 * t] = d[j][0];
-        sums[warp][g][j * 8 + 2 * t + 1] = d[j][1];
-        sums[warp][g + 8][j * 8 + 2 * t] = d[j][2];
-        sums[warp][g + 8][j * 8 + 2 * t + 1] = d[j][3];
+        sums[warp][g][j * 8 + 2 * t] = d[j][0] + d2[j][0];
+        sums[warp][g][j * 8 + 2 * t + 1] = d[j][1] + d2[j][1];
+        sums[warp][g + 8][j * 8 + 2 * t] = d[j][2] + d2[j][2];
+        sums[warp][g + 8][j * 8 + 2 * t + 1] = d[j][3] + d2[j][3];
     }
     __syncthreads();
     auto param = [&](const void* p, int64_t i, int f32) { return f32 ? static_cast<const float*>(p)[i] : __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]); };

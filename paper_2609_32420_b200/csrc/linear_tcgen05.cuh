@@ -59,6 +59,7 @@ struct TcArgs {
     int k_len;                           // k of a batch entry
     int a_slabs, b_slabs;                // MN-major: whole 64-column slabs of the operand, which a tile fetches in one copy where all of its slabs are whole
     int stages, splits;
+    int clears;                          // the first product of a call clears its status word
 };
 
 __device__ __forceinline__ uint32_t cluster_ctarank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
@@ -371,7 +372,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
     const uint32_t tmem = tmem_slot;
     grid_wait();                         // launched while the kernel ahead drains: nothing of global memory is touched before this
     // the status word of the call: nothing sets it before its wait limit has passed, which is after this
-    if (tid == 0 && blockIdx.x == 0) a.hdr->status = 0;
+    if (tid == 0 && blockIdx.x == 0 && a.clears) a.hdr->status = 0;
 
     // the clusters take the tiles in turn; with splits > 1 there is one cluster per tile and a pair has its share of k
     const int first = int(blockIdx.x / (2 * a.splits)), step = int(gridDim.x / (2 * a.splits));
@@ -380,7 +381,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
     // kLong: runs of k with an accumulator each
     const int chunks = kLong ? (k1 - k0 + kLongRun / kTileK - 1) / (kLongRun / kTileK) : 1, chunk = (k1 - k0 + chunks - 1) / chunks;
 
-    if (warp < 4) {
+    if (warp < 4) {                      // ---- service warps
     // 128 x 40 + 256 x 208 registers; the block is launched with 384 x 152 at least (checked by the host)
     if (kLong) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;" ::: "memory");
     if (warp == 0) {
@@ -423,7 +424,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
                     if (++kt == a.k_tiles) { kt = 0; ++kb; }
                 }
             }
-            // The last products' completion on every stage: no copy is in flight and no arrival on its way to this CTA afterwards.
+            // The completion of the last products on every stage: no copy is in flight and no arrival on its way to this CTA afterwards.
             const int used = min(issued, a.stages);
             for (int i = 0; i < used; ++i) {
                 const int q = issued - used + i, sq = q % a.stages;

@@ -647,8 +647,9 @@ inline Form form_of(int C, bool backward, bool xf) {
     if (groups <= 16) return {8, 1, 2, 256};
     if (groups <= 32) return backward ? Form{16, 1, 2, 256} : Form{8, 1, 4, 256};
     if (groups <= 64) return backward ? Form{32, 1, 2, 256} : Form{16, 1, 4, 256};
-    // as many slots as a CTA's warps give, which share the table of factors
-    const int warps = ceil_div(groups, 128), v = ceil_div(groups, 32 * warps);
+    // As many slots as a CTA's warps give, which share the table of factors.  Three groups per lane leave the fp32 backward kernel its registers (75600 x
+    // 5120: 713 us with four and 36 bytes spilled, 651 with three); bf16 wants four (466 us, with three 547).
+    const int warps = ceil_div(groups, backward && xf && groups <= 16 * 96 ? 96 : 128), v = ceil_div(groups, 32 * warps);
     return {32, warps, v < 3 ? 3 : v, 32 * warps * (row_warps(backward, xf) / warps)};
 }
 constexpr int kSmemPerSm = 220 * 1024;

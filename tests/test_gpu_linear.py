@@ -126,6 +126,21 @@ def test_only_what_is_wanted():
     check_backward(plain, None, cn.ACT_NONE, g)
 
 
+@pytest.mark.parametrize("N", [7, 200])
+def test_strides_of_axes_of_one_entry_do_not_matter(N):
+    t = make(1, N, 128, 72)
+    ref, z = forward(t, cn.ACT_SILU)
+    u = {k: torch.as_strided(v, v.shape, (12345, *v.stride()[1:])) if k in ("x", "dy", "residual") else v for k, v in t.items()}
+    y, _ = forward(u, cn.ACT_SILU)
+    assert torch.equal(y, ref)
+    for a, b in zip(backward(t, z, cn.ACT_SILU), backward(u, z, cn.ACT_SILU)):
+        assert torch.equal(a, b)
+    one = make(1, N, 128, 1)                 # a weight of one row
+    one["w"] = torch.as_strided(one["w"], (1, 128), (13, 1))
+    y, z = forward(one, cn.ACT_NONE)
+    check_forward(one, cn.ACT_NONE, y, z)
+
+
 @pytest.mark.parametrize("N", [5, 300])
 @pytest.mark.parametrize("y", ["bf16", "f32"])
 def test_residual_stream_in_place(N, y):

@@ -92,7 +92,8 @@ LINEAR_BAD = [
     (dict(B=0), cn.ERR_INVALID_ARG), (dict(N=-3), cn.ERR_INVALID_ARG), (dict(in_features=0), cn.ERR_INVALID_ARG), (dict(out_features=0), cn.ERR_INVALID_ARG),
     (dict(activation=4), cn.ERR_INVALID_ARG), (dict(activation=-1), cn.ERR_INVALID_ARG), (dict(y_dtype=2), cn.ERR_INVALID_ARG),
     (dict(bias_dtype=3), cn.ERR_INVALID_ARG), (dict(gate_dtype=3), cn.ERR_INVALID_ARG), (dict(gate_stride=-8), cn.ERR_INVALID_ARG),
-    (dict(B=1 << 15, N=1 << 16), cn.ERR_UNSUPPORTED), (dict(B=70000, N=1), cn.ERR_UNSUPPORTED),
+    (dict(B=1 << 15, N=1 << 16), cn.ERR_UNSUPPORTED), (dict(B=70000, N=1), cn.ERR_UNSUPPORTED), (dict(N=1 << 27), cn.ERR_UNSUPPORTED),
+    (dict(in_features=(1 << 27) + 1), cn.ERR_UNSUPPORTED), (dict(out_features=(1 << 27) + 1), cn.ERR_UNSUPPORTED),
 ]
 
 
