@@ -115,3 +115,48 @@ def test_a_layer():
     for name, got, ref in (("mid", d_mid, m.grad), ("down", gd.dW, leaf["down"].grad), ("up", gu.dW, leaf["up"].grad), ("down_b", gd.dbias, leaf["down_b"].grad),
                            ("up_b", gu.dbias, leaf["up_b"].grad), ("gate", gd.dgate, s6.grad[:, 5]), ("shift", gn.dshift, s6.grad[:, 3]), ("scale", gn.dscale, s6.grad[:, 4])):
         assert (got.double() - ref).norm() <= 8 * U16 * ref.norm(), name
+
+
+@pytest.mark.parametrize("rows,width", [(5, 256), (300, 384), (3000, 640)])
+def test_calls_behind_one_another_wait_for_one_another(rows, width):
+    """Kernels may be launched while the one ahead drains.  A long chain in which every call needs the one before it, library calls, torch
+    operations and buffers used again mixed, gives the bits that the same chain gives with a wait after every call."""
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    w = [(torch.randn((width, width), device="cuda", generator=gen) * width ** -0.5).bfloat16() for _ in range(3)]
+    x0 = torch.randn((1, rows, width), device="cuda", generator=gen)
+    mod = torch.randn((1, 2, width), device="cuda", generator=gen) * 0.1
+
+    def run(wait):
+        def after():
+            if wait:
+                torch.cuda.synchronize()
+        stream, h, z, dx, dw = x0.clone(), *(torch.empty((1, rows, width), dtype=torch.bfloat16, device="cuda") for _ in range(3)), torch.empty_like(w[0])
+        up = torch.empty_like(h)
+        mean, rstd = (torch.empty((1, 1, rows), device="cuda") for _ in range(2))
+        ws = torch.empty(1 << 24, dtype=torch.uint8, device="cuda")
+        ns = cn.make_norm_shape(stream[:, None], h[:, None], None, mod[:, 1], shift=mod[:, 0], eps=EPS)
+        us = cn.make_linear_shape(h, w[0], up, Z=z, dX=dx, dW=dw, activation=cn.ACT_GELU_TANH)
+        ds = cn.make_linear_shape(up, w[1], stream, residual=stream)
+        bs = cn.make_norm_shape(stream[:, None], dx[:, None], None, mod[:, 1], shift=mod[:, 0], dX=stream[:, None].clone(), eps=EPS)
+        for i in range(12):
+            cn.layer_norm(stream[:, None], ns, shift=mod[:, 0], scale=mod[:, 1], Y=h[:, None], mean=mean, rstd=rstd)
+            after()
+            cn.linear(h, w[i % 3], us, Y=up, Z=z, ws=ws)
+            after()
+            g = cn.linear_backward(up, h, w[i % 3], us, Z=z, dX=dx, dW=dw, ws=ws)
+            after()
+            n = cn.layer_norm_backward(dx[:, None], stream[:, None], mean, rstd, bs, scale=mod[:, 1], ws=ws[:cn.layer_norm_backward_workspace_bytes(bs)])
+            after()
+            up += g.dbias.bfloat16() * 1e-3
+            after()
+            cn.linear(up, w[1], ds, residual=stream, Y=stream, ws=ws)
+            after()
+            stream *= 0.5
+            stream += 0.01 * n.dX[:, 0]
+            after()
+        torch.cuda.synchronize()
+        return stream, h, z, dx, dw, n.dscale, g.dbias
+    want = run(True)
+    for _ in range(3):
+        assert all(torch.equal(a, b) for a, b in zip(run(False), want))
+    assert torch.isfinite(want[0]).all()

@@ -239,3 +239,16 @@ def test_same_bits_again_streams_and_graphs():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(y, y0) and all(torch.equal(a, b) for a, b in zip(g, g0))
+
+
+def test_gradients_of_a_norm_that_is_shifted_only():
+    t = make(2, 1, 90, 264, "bf16", "f32", "f32", True, True, seed=6)
+    t["scale"] = None
+    out, mean, rstd = forward(t, torch.float32)
+    check_forward(t, out, mean, rstd)
+    s = cn.make_norm_shape(t["x"], t["dy"], t["weight"], shift=t["shift"], dX=t["x"].clone(), eps=EPS)
+    g = cn.layer_norm_backward(t["dy"], t["x"], mean, rstd, s, weight=t["weight"], bias=t["bias"], modulated=True)
+    one = dict(t, scale=torch.zeros((2, 264), device="cuda"))             # a scale of zero is no scale
+    s = cn.make_norm_shape(t["x"], t["dy"], t["weight"], one["scale"], shift=t["shift"], dX=t["x"].clone(), eps=EPS)
+    ref = cn.layer_norm_backward(t["dy"], t["x"], mean, rstd, s, weight=t["weight"], bias=t["bias"], scale=one["scale"])
+    assert all(torch.equal(a, b) for a, b in zip(g, ref))
