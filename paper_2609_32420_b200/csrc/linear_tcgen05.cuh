@@ -502,6 +502,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
                 const int64_t y_off = b * a.e.ys[0] + row * a.e.ys[1], z_off = b * a.e.zs[0] + row * a.e.zs[1], r_off = b * a.e.rs[0] + row * a.e.rs[1];
                 const int64_t gate_off = a.e.gate ? (b + row / a.e.rows_per_gate) * a.e.gate_stride : 0;
                 const char* res = static_cast<const char*>(a.e.residual) + (r_off + n * a.bn) * 4;
+                __syncwarp();            // rows behind the last one have left the tile before early
                 f2 acc[4][16];           // 32 columns each: side * 32, + 64, + 128, + 192
 #pragma unroll
                 for (int p = 0; p < 4; ++p)
@@ -527,11 +528,12 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
                     __syncwarp();
                     if (lane == 0) arrive_remote(read0 + 8 * u);
                 }
-                if (!ok || !on) continue;
+                __syncwarp();
+                if (!ok) break;
 #pragma unroll
                 for (int p = 0; p < 4; ++p) {
                     const int at = side * 32 + 64 * p, col = n * a.bn + at;
-                    if (at >= left) continue;
+                    if (at >= left || !on) continue;
                     if (at + 32 <= left) {
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
