@@ -531,11 +531,16 @@ def _fit(t, what: str, dtype, size, stride, device) -> None:
             raise ValueError(f"{what} has strides {t.stride()}, the shape record says {stride}")
 
 
-def _on_current_device(device) -> None:
-    """The kernels run on the current device, on its current stream; a machine without a GPU only checks arguments."""
+def _stream_on(device, stream):
+    """The stream of a call: the current one unless given.  The kernels run on the current device, so the tensors have to be there; a machine without a
+    GPU only checks arguments."""
+    if device.type != "cuda":
+        return _stream(stream)
     import torch
-    if device.type == "cuda" and device.index != torch.cuda.current_device():
-        raise ValueError(f"the tensors are on {device}, the current device is cuda:{torch.cuda.current_device()}")
+    current = torch.cuda.current_device()
+    if device.index != current:
+        raise ValueError(f"the tensors are on {device}, the current device is cuda:{current}")
+    return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(current) if stream is None else stream.cuda_stream)
 
 
 class _Said:
@@ -617,7 +622,7 @@ def layer_norm(X, shape: NormShape, weight=None, bias=None, shift=None, scale=No
         Y = torch.empty((shape.B, shape.H, shape.N, -(-shape.C // 8) * 8), dtype=_dtype_of(shape.y_dtype), device=dev)[..., :shape.C]
         shape.y_stride = _rows_of(shape.y_stride, Y)
     said = _norm_said(shape)
-    _on_current_device(dev)
+    on = _stream_on(dev, stream)
     _fit(X, "X", *said.x, dev)
     _fit(Y, "Y", *said.y, dev)
     if weight is not None:
@@ -632,7 +637,7 @@ def layer_norm(X, shape: NormShape, weight=None, bias=None, shift=None, scale=No
         _fit(mean, "mean", *said.stat, dev)
     if rstd is not None:
         _fit(rstd, "rstd", *said.stat, dev)
-    st = lib().carnator_layer_norm(_ptr(X), _ptr(weight), _ptr(bias), _ptr(shift), _ptr(scale), said.ref, _ptr(Y), _ptr(mean), _ptr(rstd), _stream(stream))
+    st = lib().carnator_layer_norm(_ptr(X), _ptr(weight), _ptr(bias), _ptr(shift), _ptr(scale), said.ref, _ptr(Y), _ptr(mean), _ptr(rstd), on)
     if st != OK:
         _check(st, "carnator_layer_norm")
     return Y
@@ -661,7 +666,7 @@ def layer_norm_backward(dY, X, mean, rstd, shape: NormShape, weight=None, bias=N
         dX = torch.empty((shape.B, shape.H, shape.N, -(-shape.C // 8) * 8), dtype=_dtype_of(shape.x_dtype), device=dev)[..., :shape.C]
         shape.dx_stride = _rows_of(shape.dx_stride, dX)
     said = _norm_said(shape)
-    _on_current_device(dev)
+    on = _stream_on(dev, stream)
     _fit(dY, "dY", *said.dy, dev)
     _fit(X, "X", *said.x, dev)
     _fit(dX, "dX", *said.dx, dev)
@@ -688,7 +693,7 @@ def layer_norm_backward(dY, X, mean, rstd, shape: NormShape, weight=None, bias=N
     if ws is None:
         ws = _new_ws(layer_norm_backward_workspace_bytes(shape), dev)
     st = lib().carnator_layer_norm_backward(_ptr(dY), _ptr(X), _ptr(mean), _ptr(rstd), _ptr(weight), _ptr(bias), _ptr(scale), said.ref, _ptr(dX),
-                                            _ptr(dweight), _ptr(dbias), _ptr(dshift), _ptr(dscale), _ptr(ws), ws.numel(), _stream(stream))
+                                            _ptr(dweight), _ptr(dbias), _ptr(dshift), _ptr(dscale), _ptr(ws), ws.numel(), on)
     if st != OK:
         _check(st, "carnator_layer_norm_backward")
     return NormGrads(dX, dweight, dbias, dshift, dscale)
@@ -732,7 +737,7 @@ def linear(X, W, shape: LinearShape, bias=None, gate=None, residual=None, Y=None
         Y = torch.empty((shape.B, shape.N, -(-M // 8) * 8), dtype=_dtype_of(shape.y_dtype), device=dev)[..., :M]
         shape.y_stride = _rows_of(shape.y_stride, Y)
     said = _linear_said(shape)
-    _on_current_device(dev)
+    on = _stream_on(dev, stream)
     _fit(X, "X", *said.x, dev)
     _fit(W, "W", *said.w, dev)
     _fit(Y, "Y", *said.y, dev)
@@ -746,7 +751,7 @@ def linear(X, W, shape: LinearShape, bias=None, gate=None, residual=None, Y=None
         _fit(gate, "gate", *said.gate, dev)
     if ws is None:
         ws = _new_ws(linear_workspace_bytes(shape), dev)
-    st = lib().carnator_linear(_ptr(X), _ptr(W), _ptr(bias), _ptr(gate), _ptr(residual), said.ref, _ptr(Y), _ptr(Z), _ptr(ws), ws.numel(), _stream(stream))
+    st = lib().carnator_linear(_ptr(X), _ptr(W), _ptr(bias), _ptr(gate), _ptr(residual), said.ref, _ptr(Y), _ptr(Z), _ptr(ws), ws.numel(), on)
     if st != OK:
         _check(st, "carnator_linear")
     return Y, ws
@@ -771,7 +776,7 @@ def linear_backward(dY, X, W, shape: LinearShape, Z=None, gate=None, dX=None, dW
     import torch
     dev = dY.device
     said = _linear_said(shape)
-    _on_current_device(dev)
+    on = _stream_on(dev, stream)
     _fit(dY, "dY", *said.y, dev)
     _fit(X, "X", *said.x, dev)
     _fit(W, "W", *said.w, dev)
@@ -788,7 +793,7 @@ def linear_backward(dY, X, W, shape: LinearShape, Z=None, gate=None, dX=None, dW
     if ws is None:
         ws = _new_ws(linear_backward_workspace_bytes(shape), dev)
     st = lib().carnator_linear_backward(_ptr(dY), _ptr(X), _ptr(W), _ptr(Z), _ptr(gate), said.ref, _ptr(dX), _ptr(dW), _ptr(dbias), _ptr(dgate),
-                                        _ptr(ws), ws.numel(), _stream(stream))
+                                        _ptr(ws), ws.numel(), on)
     if st != OK:
         _check(st, "carnator_linear_backward")
     return LinearGrads(dX, dW, dbias, dgate)
