@@ -160,3 +160,35 @@ def test_calls_behind_one_another_wait_for_one_another(rows, width):
     for _ in range(3):
         assert all(torch.equal(a, b) for a, b in zip(run(False), want))
     assert torch.isfinite(want[0]).all()
+
+
+def test_offsets_that_pass_32_bits():
+    """600000 rows of 4096 channels, 2.4e9 elements: the last rows, whose offsets do not fit 32 bits, against the same rows on their own."""
+    rows, wide, tail = 600_000, 4096, 300
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.zeros((1, 1, rows, wide), dtype=torch.bfloat16, device="cuda")
+    x[:, :, -tail:] = torch.randn((tail, wide), device="cuda", generator=gen)
+    last = x[:, :, -tail:].clone()
+    y = torch.empty_like(x)
+    cn.layer_norm(x, cn.make_norm_shape(x, y), Y=y)
+    assert torch.equal(y[:, :, -tail:], cn.layer_norm(last, cn.make_norm_shape(last, last)))
+    assert not y[:, :, :-tail].any()
+    # into and out of that width
+    w = (torch.randn((wide, 64), device="cuda", generator=gen) / 8).bfloat16()
+    small = torch.zeros((1, rows, 64), dtype=torch.bfloat16, device="cuda")
+    small[:, -tail:] = torch.randn((tail, 64), device="cuda", generator=gen)
+    z, out = x[:, 0], y[:, 0]                                     # rows of zeros but for the last
+    s = cn.make_linear_shape(small, w, out, activation=cn.ACT_GELU)
+    _, ws = cn.linear(small, w, s, Y=out)
+    assert cn.query_status(ws) == cn.OK
+    ry, _, _, ey = linear_ref(small[:, -tail:], w, None, None, None, cn.ACT_GELU)
+    check(out[:, -tail:], ry, ey + U16 * (ry.abs() + ey), "y")
+    assert not out[:, :-tail].any()
+    dx, dw = torch.empty_like(small), torch.empty_like(w)
+    s = cn.make_linear_shape(small, w, out, Z=z, dX=dx, dW=dw, activation=cn.ACT_GELU)
+    g = cn.linear_backward(out, small, w, s, Z=z, dX=dx, dW=dw)
+    ref = linear_grad_ref(out[:, -tail:], small[:, -tail:], w, z[:, -tail:], None, cn.ACT_GELU)
+    for name, got in (("dX", dx[:, -tail:]), ("dW", dw), ("dbias", g.dbias)):
+        r, e = ref[name]
+        check(got, r, e + half_step(got.dtype) * (r.abs() + e), name)
+    assert not dx[:, :-tail].any()
