@@ -373,6 +373,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
     grid_wait();                         // launched while the kernel ahead drains: nothing of global memory is touched before this
     // the status word of the call: nothing sets it before its wait limit has passed, which is after this
     if (tid == 0 && blockIdx.x == 0 && a.clears) a.hdr->status = 0;
+    __syncwarp();                        // whole warps hand over registers (setmaxnreg)
 
     // the clusters take the tiles in turn; with splits > 1 there is one cluster per tile and a pair has its share of k
     const int first = int(blockIdx.x / (2 * a.splits)), step = int(gridDim.x / (2 * a.splits));
@@ -584,6 +585,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
                         r0 = load_sector(p, a.e.wide_ok); r1 = load_sector(p + 32, a.e.wide_ok);
                         if (a.e.y_f32) { r2 = load_sector(p + 64, a.e.wide_ok); r3 = load_sector(p + 96, a.e.wide_ok); }
                     }
+                    __syncwarp();        // lanes of rows behind the last one have neither fetched this residual nor finished the columns before
                     float v[32];
                     tmem_ld32(tmem + lane_base + uint32_t(u * 256 + c), v);
                     tmem_wait_ld(v);

@@ -269,3 +269,15 @@ def test_same_bits_again_streams_graphs_and_two_calls_at_once(N, K, M):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+@pytest.mark.parametrize("N", [257, 5003])
+@pytest.mark.parametrize("y,gate", [("bf16", False), ("bf16", True), ("f32", True)])
+def test_warps_with_rows_behind_the_last(N, y, gate):
+    """The last warp of the rows holds lanes without a row, which skip residual, activation and stores of every piece of a wide tile; the loads from tensor
+    memory between those pieces want the whole warp."""
+    t = make(1, N, 192, 1000, y, gate=gate, seed=N)
+    for act in (cn.ACT_GELU_TANH, cn.ACT_NONE):
+        out, z = forward(t, act)
+        check_forward(t, act, out, z)
+    assert torch.equal(forward(t, cn.ACT_NONE)[0], out)
