@@ -8,6 +8,7 @@ fallback of any kind.
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 import os
 from typing import NamedTuple, Optional
@@ -544,39 +545,39 @@ def _stream_on(device, stream):
 
 
 class _Said:
-    """What a record says of the tensors of its call, (type, shape, strides) each, worked out again whenever the record has changed."""
-    __slots__ = ("of", "x", "y", "dy", "dx", "residual", "z", "w", "dw", "vec", "shift", "scale", "gate", "bias", "stat", "ref")
+    """What a record says of the tensors of its call, (type, shape, strides) each, and a copy of it for the library.  Made for each content of a record
+    and never changed afterwards, so that records may be copied, changed between calls and shared among threads."""
+    __slots__ = ("record", "ref", "x", "y", "dy", "dx", "residual", "z", "w", "dw", "vec", "shift", "scale", "gate", "bias", "stat")
+
+    def __init__(self, record):
+        self.record, self.ref = record, ctypes.byref(record)
 
 
-def _norm_said(s: NormShape) -> _Said:
-    said = getattr(s, "_said", None)
-    of = bytes(s)
-    if said is None or said.of != of:
-        said = s._said = _Said()
-        size, x, y, w, m = (s.B, s.H, s.N, s.C), _dtype_of(s.x_dtype), _dtype_of(s.y_dtype), _dtype_of(s.weight_dtype), _dtype_of(s.mod_dtype)
-        said.of, said.ref = of, ctypes.byref(s)
-        said.x, said.y = (x, size, (*s.x_stride, 1)), (y, size, (*s.y_stride, 1))
-        said.dy, said.dx = (y, size, (*s.dy_stride, 1)), (x, size, (*s.dx_stride, 1))
-        said.vec = (w, (s.C,), (1,))
-        said.shift, said.scale = (m, (s.B, s.C), (s.shift_stride, 1)), (m, (s.B, s.C), (s.scale_stride, 1))
-        said.stat = (_dtype_of(DTYPE_F32), size[:3], (s.H * s.N, s.N, 1))
+@functools.lru_cache(maxsize=1024)
+def _norm_said(of: bytes) -> _Said:
+    s = NormShape.from_buffer_copy(of)
+    said = _Said(s)
+    size, x, y, w, m = (s.B, s.H, s.N, s.C), _dtype_of(s.x_dtype), _dtype_of(s.y_dtype), _dtype_of(s.weight_dtype), _dtype_of(s.mod_dtype)
+    said.x, said.y = (x, size, (*s.x_stride, 1)), (y, size, (*s.y_stride, 1))
+    said.dy, said.dx = (y, size, (*s.dy_stride, 1)), (x, size, (*s.dx_stride, 1))
+    said.vec = (w, (s.C,), (1,))
+    said.shift, said.scale = (m, (s.B, s.C), (s.shift_stride, 1)), (m, (s.B, s.C), (s.scale_stride, 1))
+    said.stat = (_dtype_of(DTYPE_F32), size[:3], (s.H * s.N, s.N, 1))
     return said
 
 
-def _linear_said(s: LinearShape) -> _Said:
-    said = getattr(s, "_said", None)
-    of = bytes(s)
-    if said is None or said.of != of:
-        said = s._said = _Said()
-        y, bf16 = _dtype_of(s.y_dtype), _dtype_of(DTYPE_BF16)
-        rows = lambda n, dtype, st: (dtype, (s.B, s.N, n), (*st, 1))  # noqa: E731
-        said.of, said.ref = of, ctypes.byref(s)
-        said.x, said.dx = rows(s.in_features, bf16, s.x_stride), rows(s.in_features, bf16, s.dx_stride)
-        said.y, said.z = rows(s.out_features, y, s.y_stride), rows(s.out_features, bf16, s.z_stride)
-        said.residual = rows(s.out_features, y, s.residual_stride)
-        said.w, said.dw = (bf16, (s.out_features, s.in_features), (s.w_stride, 1)), (bf16, (s.out_features, s.in_features), (s.dw_stride, 1))
-        said.bias = (_dtype_of(s.bias_dtype), (s.out_features,), (1,))
-        said.gate = (_dtype_of(s.gate_dtype), (s.B, s.out_features), (s.gate_stride, 1))
+@functools.lru_cache(maxsize=1024)
+def _linear_said(of: bytes) -> _Said:
+    s = LinearShape.from_buffer_copy(of)
+    said = _Said(s)
+    y, bf16 = _dtype_of(s.y_dtype), _dtype_of(DTYPE_BF16)
+    rows = lambda n, dtype, st: (dtype, (s.B, s.N, n), (*st, 1))  # noqa: E731
+    said.x, said.dx = rows(s.in_features, bf16, s.x_stride), rows(s.in_features, bf16, s.dx_stride)
+    said.y, said.z = rows(s.out_features, y, s.y_stride), rows(s.out_features, bf16, s.z_stride)
+    said.residual = rows(s.out_features, y, s.residual_stride)
+    said.w, said.dw = (bf16, (s.out_features, s.in_features), (s.w_stride, 1)), (bf16, (s.out_features, s.in_features), (s.dw_stride, 1))
+    said.bias = (_dtype_of(s.bias_dtype), (s.out_features,), (1,))
+    said.gate = (_dtype_of(s.gate_dtype), (s.B, s.out_features), (s.gate_stride, 1))
     return said
 
 
@@ -621,7 +622,7 @@ def layer_norm(X, shape: NormShape, weight=None, bias=None, shift=None, scale=No
         import torch
         Y = torch.empty((shape.B, shape.H, shape.N, -(-shape.C // 8) * 8), dtype=_dtype_of(shape.y_dtype), device=dev)[..., :shape.C]
         shape.y_stride = _rows_of(shape.y_stride, Y)
-    said = _norm_said(shape)
+    said = _norm_said(bytes(shape))
     on = _stream_on(dev, stream)
     _fit(X, "X", *said.x, dev)
     _fit(Y, "Y", *said.y, dev)
@@ -665,7 +666,7 @@ def layer_norm_backward(dY, X, mean, rstd, shape: NormShape, weight=None, bias=N
     if dX is None:
         dX = torch.empty((shape.B, shape.H, shape.N, -(-shape.C // 8) * 8), dtype=_dtype_of(shape.x_dtype), device=dev)[..., :shape.C]
         shape.dx_stride = _rows_of(shape.dx_stride, dX)
-    said = _norm_said(shape)
+    said = _norm_said(bytes(shape))
     on = _stream_on(dev, stream)
     _fit(dY, "dY", *said.dy, dev)
     _fit(X, "X", *said.x, dev)
@@ -678,7 +679,7 @@ def layer_norm_backward(dY, X, mean, rstd, shape: NormShape, weight=None, bias=N
         _fit(bias, "bias", *said.vec, dev)
     if scale is not None:
         _fit(scale, "scale", *said.scale, dev)
-    B, C = shape.B, shape.C
+    B, C = said.record.B, said.record.C
     dweight = dbias = dshift = dscale = None
     if weight is not None:
         if "weight" in want:
@@ -691,7 +692,7 @@ def layer_norm_backward(dY, X, mean, rstd, shape: NormShape, weight=None, bias=N
         if "scale" in want:
             dscale = torch.empty((B, C), dtype=torch.float32, device=dev)
     if ws is None:
-        ws = _new_ws(layer_norm_backward_workspace_bytes(shape), dev)
+        ws = _new_ws(layer_norm_backward_workspace_bytes(said.record), dev)
     st = lib().carnator_layer_norm_backward(_ptr(dY), _ptr(X), _ptr(mean), _ptr(rstd), _ptr(weight), _ptr(bias), _ptr(scale), said.ref, _ptr(dX),
                                             _ptr(dweight), _ptr(dbias), _ptr(dshift), _ptr(dscale), _ptr(ws), ws.numel(), on)
     if st != OK:
@@ -736,7 +737,7 @@ def linear(X, W, shape: LinearShape, bias=None, gate=None, residual=None, Y=None
         M = shape.out_features                     # rows on 16-byte boundaries
         Y = torch.empty((shape.B, shape.N, -(-M // 8) * 8), dtype=_dtype_of(shape.y_dtype), device=dev)[..., :M]
         shape.y_stride = _rows_of(shape.y_stride, Y)
-    said = _linear_said(shape)
+    said = _linear_said(bytes(shape))
     on = _stream_on(dev, stream)
     _fit(X, "X", *said.x, dev)
     _fit(W, "W", *said.w, dev)
@@ -750,7 +751,7 @@ def linear(X, W, shape: LinearShape, bias=None, gate=None, residual=None, Y=None
     if gate is not None:
         _fit(gate, "gate", *said.gate, dev)
     if ws is None:
-        ws = _new_ws(linear_workspace_bytes(shape), dev)
+        ws = _new_ws(linear_workspace_bytes(said.record), dev)
     st = lib().carnator_linear(_ptr(X), _ptr(W), _ptr(bias), _ptr(gate), _ptr(residual), said.ref, _ptr(Y), _ptr(Z), _ptr(ws), ws.numel(), on)
     if st != OK:
         _check(st, "carnator_linear")
@@ -775,7 +776,7 @@ def linear_backward(dY, X, W, shape: LinearShape, Z=None, gate=None, dX=None, dW
     (if there is one).  Z is the pre-activation that the forward call wrote."""
     import torch
     dev = dY.device
-    said = _linear_said(shape)
+    said = _linear_said(bytes(shape))
     on = _stream_on(dev, stream)
     _fit(dY, "dY", *said.y, dev)
     _fit(X, "X", *said.x, dev)
@@ -788,10 +789,11 @@ def linear_backward(dY, X, W, shape: LinearShape, Z=None, gate=None, dX=None, dW
         _fit(dX, "dX", *said.dx, dev)
     if dW is not None:
         _fit(dW, "dW", *said.dw, dev)
-    dbias = torch.empty(shape.out_features, dtype=torch.float32, device=dev) if "bias" in want else None
-    dgate = torch.empty((shape.B, shape.out_features), dtype=torch.float32, device=dev) if gate is not None and "gate" in want else None
+    of = said.record
+    dbias = torch.empty(of.out_features, dtype=torch.float32, device=dev) if "bias" in want else None
+    dgate = torch.empty((of.B, of.out_features), dtype=torch.float32, device=dev) if gate is not None and "gate" in want else None
     if ws is None:
-        ws = _new_ws(linear_backward_workspace_bytes(shape), dev)
+        ws = _new_ws(linear_backward_workspace_bytes(said.record), dev)
     st = lib().carnator_linear_backward(_ptr(dY), _ptr(X), _ptr(W), _ptr(Z), _ptr(gate), said.ref, _ptr(dX), _ptr(dW), _ptr(dbias), _ptr(dgate),
                                         _ptr(ws), ws.numel(), on)
     if st != OK:

@@ -1,5 +1,9 @@
 """Layer norm, matrix product and their gradients: what the calls refuse, before anything is launched (no GPU needed)."""
+import copy
 import ctypes
+import pickle
+import sys
+import threading
 
 import pytest
 import torch
@@ -163,3 +167,105 @@ def test_python_calls_check_tensors_against_the_record():
             cn.linear(x, w, s, Y=y)
         with pytest.raises(cn.CarnatorError):
             cn.layer_norm(t, ns)
+
+
+# ---- records: copied, shared, used again -----------------------------------------------------------------
+DEVICE = "cuda" if torch.cuda.is_available() else "cpu"
+
+
+class Library:
+    """In the place of the library: keeps the record that each call was given and launches nothing."""
+
+    def __init__(self):
+        self.records = []
+
+    def __getattr__(self, name):
+        def call(*args):
+            record = next(a._obj for a in args if hasattr(a, "_obj"))
+            self.records.append(type(record).from_buffer_copy(record))
+            return 256 if name.endswith("_workspace_bytes") else cn.OK
+        return call
+
+
+@pytest.fixture
+def library(monkeypatch):
+    fake = Library()
+    monkeypatch.setattr(cn, "lib", lambda: fake)
+    return fake
+
+
+def norm_call(s=None, packed=False):
+    x, y = (torch.empty((1, 2, 4, 72), dtype=torch.bfloat16, device=DEVICE) for _ in range(2))
+    s = s or cn.make_norm_shape(x, y)
+    return s, lambda r=s: cn.layer_norm(x, r, Y=None if packed else y)
+
+
+def norm_backward_call(packed=False):
+    x, y = (torch.empty((1, 2, 4, 72), dtype=torch.bfloat16, device=DEVICE) for _ in range(2))
+    stat = torch.empty((1, 2, 4), device=DEVICE)
+    s = cn.make_norm_shape(x, y)
+    return s, lambda r=s: cn.layer_norm_backward(y, x, stat, stat, r, dX=None if packed else torch.empty_like(x))
+
+
+def linear_call(packed=False):
+    x, w, y = (torch.empty(n, dtype=torch.bfloat16, device=DEVICE) for n in ((1, 4, 64), (40, 64), (1, 4, 40)))
+    s = cn.make_linear_shape(x, w, y, activation=cn.ACT_GELU)
+    return s, lambda r=s: cn.linear(x, w, r, Y=None if packed else y)
+
+
+def linear_backward_call(packed=False):
+    x, w, y = (torch.empty(n, dtype=torch.bfloat16, device=DEVICE) for n in ((1, 4, 64), (40, 64), (1, 4, 40)))
+    s = cn.make_linear_shape(x, w, y, Z=y, dX=x, dW=w, activation=cn.ACT_GELU)
+    return s, lambda r=s: cn.linear_backward(y, x, w, r, Z=y, dX=torch.empty_like(x), dW=torch.empty_like(w))
+
+
+CALLS = [norm_call, norm_backward_call, linear_call, linear_backward_call]
+
+
+@pytest.mark.parametrize("make", CALLS)
+@pytest.mark.parametrize("how", [copy.copy, copy.deepcopy, lambda s: pickle.loads(pickle.dumps(s))], ids=["copy", "deepcopy", "pickle"])
+def test_a_copied_record_stands_for_itself(library, make, how):
+    """A copy of a record that has been used: its calls pass what it says, whatever becomes of the original."""
+    s, call = make()
+    call()
+    t = how(s)
+    said = bytes(t)
+    s.N = 4000
+    if hasattr(s, "activation"):
+        s.activation = cn.ACT_SILU
+    s.x_stride[1] = 1 << 30
+    call(t)
+    assert bytes(t) == said and bytes(library.records[-1]) == said
+    with pytest.raises(ValueError):
+        call(s)
+
+
+@pytest.mark.parametrize("make", [norm_call, linear_call])
+def test_threads_share_a_record(library, make):
+    """Four threads whose first call with a new record is the same moment."""
+    errors, interval = [], sys.getswitchinterval()
+    sys.setswitchinterval(1e-6)
+
+    def work(call, gate):
+        gate.wait()
+        try:
+            for _ in range(3):
+                call()
+        except Exception as e:  # noqa: BLE001
+            errors.append(e)
+    try:
+        for i in range(200):
+            s, call = make()
+            if make is linear_call:
+                s.gate_stride = 8 * i          # a record that nothing has seen
+            else:
+                s.eps = 1e-6 * (i + 1)
+            gate = threading.Barrier(4)
+            threads = [threading.Thread(target=work, args=(call, gate)) for _ in range(4)]
+            for t in threads:
+                t.start()
+            for t in threads:
+                t.join()
+    finally:
+        sys.setswitchinterval(interval)
+    assert not errors, errors[:3]
