@@ -581,6 +581,16 @@ def _linear_said(of: bytes) -> _Said:
     return said
 
 
+def _with_room(shape, stride: str, rows, row: str, dtype: str, device):
+    """An output with rows on 16-byte boundaries, and a copy of the record that has its strides: the caller's record stays as it is."""
+    import torch
+    of = type(shape).from_buffer_copy(shape)
+    n = getattr(of, row)
+    t = torch.empty((*(getattr(of, r) for r in rows), -(-n // 8) * 8), dtype=_dtype_of(getattr(of, dtype)), device=device)[..., :n]
+    setattr(of, stride, _rows_of(getattr(of, stride), t))
+    return of, t
+
+
 def _rows_of(stride, *tensors):
     for t in tensors:
         if t is not None:
@@ -616,12 +626,10 @@ def make_norm_shape(X, Y, weight=None, scale=None, shift=None, dX=None, eps: flo
 
 
 def layer_norm(X, shape: NormShape, weight=None, bias=None, shift=None, scale=None, Y=None, mean=None, rstd=None, stream=None):
-    """carnator_layer_norm.  Returns Y [B,H,N,C]; mean and rstd fp32 [B,H,N] (contiguous) are written if given."""
+    """carnator_layer_norm.  Returns Y [B,H,N,C] (its own, with rows on 16-byte boundaries, unless given); mean and rstd fp32 [B,H,N] (contiguous) are written if given."""
     dev = X.device
     if Y is None:
-        import torch
-        Y = torch.empty((shape.B, shape.H, shape.N, -(-shape.C // 8) * 8), dtype=_dtype_of(shape.y_dtype), device=dev)[..., :shape.C]
-        shape.y_stride = _rows_of(shape.y_stride, Y)
+        shape, Y = _with_room(shape, "y_stride", ("B", "H", "N"), "C", "y_dtype", dev)
     said = _norm_said(bytes(shape))
     on = _stream_on(dev, stream)
     _fit(X, "X", *said.x, dev)
@@ -664,8 +672,7 @@ def layer_norm_backward(dY, X, mean, rstd, shape: NormShape, weight=None, bias=N
     import torch
     dev = X.device
     if dX is None:
-        dX = torch.empty((shape.B, shape.H, shape.N, -(-shape.C // 8) * 8), dtype=_dtype_of(shape.x_dtype), device=dev)[..., :shape.C]
-        shape.dx_stride = _rows_of(shape.dx_stride, dX)
+        shape, dX = _with_room(shape, "dx_stride", ("B", "H", "N"), "C", "x_dtype", dev)
     said = _norm_said(bytes(shape))
     on = _stream_on(dev, stream)
     _fit(dY, "dY", *said.dy, dev)
@@ -730,13 +737,10 @@ def linear_workspace_bytes(shape: LinearShape) -> int:
 
 
 def linear(X, W, shape: LinearShape, bias=None, gate=None, residual=None, Y=None, Z=None, ws=None, stream=None):
-    """carnator_linear.  Returns (Y [B,N,out_features], ws); Z (bf16, the pre-activation) is written if given."""
+    """carnator_linear.  Returns (Y [B,N,out_features] (as in layer_norm), ws); Z (bf16, the pre-activation) is written if given."""
     dev = X.device
     if Y is None:
-        import torch
-        M = shape.out_features                     # rows on 16-byte boundaries
-        Y = torch.empty((shape.B, shape.N, -(-M // 8) * 8), dtype=_dtype_of(shape.y_dtype), device=dev)[..., :M]
-        shape.y_stride = _rows_of(shape.y_stride, Y)
+        shape, Y = _with_room(shape, "y_stride", ("B", "N"), "out_features", "y_dtype", dev)
     said = _linear_said(bytes(shape))
     on = _stream_on(dev, stream)
     _fit(X, "X", *said.x, dev)

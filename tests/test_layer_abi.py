@@ -240,8 +240,30 @@ def test_a_copied_record_stands_for_itself(library, make, how):
         call(s)
 
 
+@pytest.mark.parametrize("make", CALLS)
+def test_calls_leave_the_record_as_it_is(library, make):
+    s, call = make(packed=True)
+    for name in ("y_stride", "dx_stride"):          # of a tensor that the call does not get: its own output has strides of its own
+        if make in (norm_backward_call, linear_backward_call) and name == "y_stride":
+            continue
+        getattr(s, name)[0], getattr(s, name)[1] = 7777, 88
+    if make is linear_backward_call:                # has no output of its own
+        s.dx_stride[:] = [4 * 64, 64]
+    before = bytes(s)
+    call()
+    assert bytes(s) == before
+    passed = library.records[-1]
+    if make is norm_call:
+        assert list(passed.y_stride) == [2 * 4 * 72, 4 * 72, 72]
+    if make is norm_backward_call:
+        assert list(passed.dx_stride) == [2 * 4 * 72, 4 * 72, 72]
+    if make is linear_call:
+        assert list(passed.y_stride) == [4 * 40, 40]
+
+
 @pytest.mark.parametrize("make", [norm_call, linear_call])
-def test_threads_share_a_record(library, make):
+@pytest.mark.parametrize("packed", [False, True])
+def test_threads_share_a_record(library, make, packed):
     """Four threads whose first call with a new record is the same moment."""
     errors, interval = [], sys.getswitchinterval()
     sys.setswitchinterval(1e-6)
@@ -255,7 +277,7 @@ def test_threads_share_a_record(library, make):
             errors.append(e)
     try:
         for i in range(200):
-            s, call = make()
+            s, call = make(packed=packed)
             if make is linear_call:
                 s.gate_stride = 8 * i          # a record that nothing has seen
             else:
