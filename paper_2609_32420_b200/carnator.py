@@ -535,9 +535,11 @@ def _fit(t, what: str, dtype, size, stride, device) -> None:
 def _stream_on(device, stream):
     """The stream of a call: the current one unless given.  The kernels run on the current device, so the tensors have to be there; a machine without a
     GPU only checks arguments."""
-    if device.type != "cuda":
-        return _stream(stream)
     import torch
+    if device.type != "cuda":
+        if torch.cuda.is_available():
+            raise ValueError(f"the tensors are on {device}: the kernels read memory of the current device only")
+        return _stream(stream)
     current = torch.cuda.current_device()
     if device.index != current:
         raise ValueError(f"the tensors are on {device}, the current device is cuda:{current}")
@@ -700,6 +702,8 @@ def layer_norm_backward(dY, X, mean, rstd, shape: NormShape, weight=None, bias=N
             dscale = torch.empty((B, C), dtype=torch.float32, device=dev)
     if ws is None:
         ws = _new_ws(layer_norm_backward_workspace_bytes(said.record), dev)
+    elif ws.device != dev or not ws.is_contiguous():
+        raise ValueError(f"ws must be contiguous and on {dev}")
     st = lib().carnator_layer_norm_backward(_ptr(dY), _ptr(X), _ptr(mean), _ptr(rstd), _ptr(weight), _ptr(bias), _ptr(scale), said.ref, _ptr(dX),
                                             _ptr(dweight), _ptr(dbias), _ptr(dshift), _ptr(dscale), _ptr(ws), ws.numel(), on)
     if st != OK:
@@ -756,6 +760,8 @@ def linear(X, W, shape: LinearShape, bias=None, gate=None, residual=None, Y=None
         _fit(gate, "gate", *said.gate, dev)
     if ws is None:
         ws = _new_ws(linear_workspace_bytes(said.record), dev)
+    elif ws.device != dev or not ws.is_contiguous():
+        raise ValueError(f"ws must be contiguous and on {dev}")
     st = lib().carnator_linear(_ptr(X), _ptr(W), _ptr(bias), _ptr(gate), _ptr(residual), said.ref, _ptr(Y), _ptr(Z), _ptr(ws), ws.numel(), on)
     if st != OK:
         _check(st, "carnator_linear")
@@ -798,6 +804,8 @@ def linear_backward(dY, X, W, shape: LinearShape, Z=None, gate=None, dX=None, dW
     dgate = torch.empty((of.B, of.out_features), dtype=torch.float32, device=dev) if gate is not None and "gate" in want else None
     if ws is None:
         ws = _new_ws(linear_backward_workspace_bytes(said.record), dev)
+    elif ws.device != dev or not ws.is_contiguous():
+        raise ValueError(f"ws must be contiguous and on {dev}")
     st = lib().carnator_linear_backward(_ptr(dY), _ptr(X), _ptr(W), _ptr(Z), _ptr(gate), said.ref, _ptr(dX), _ptr(dW), _ptr(dbias), _ptr(dgate),
                                         _ptr(ws), ws.numel(), on)
     if st != OK:

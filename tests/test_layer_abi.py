@@ -4,6 +4,7 @@ import ctypes
 import pickle
 import sys
 import threading
+import types
 
 import pytest
 import torch
@@ -291,3 +292,32 @@ def test_threads_share_a_record(library, make, packed):
     finally:
         sys.setswitchinterval(interval)
     assert not errors, errors[:3]
+
+
+# ---- where the tensors are --------------------------------------------------------------------------------
+def test_tensors_in_host_memory_are_refused_where_there_is_a_gpu(library, monkeypatch):
+    """The kernels would be given addresses of the host.  (A machine without a GPU checks arguments and launches nothing.)"""
+    monkeypatch.setattr(torch.cuda, "is_available", lambda: True)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    x, w, y = (torch.empty(n, dtype=torch.bfloat16) for n in ((1, 4, 64), (64, 64), (1, 4, 64)))
+    t, stat = x[:, None], torch.empty((1, 1, 4))
+    ns, ls = cn.make_norm_shape(t, t), cn.make_linear_shape(x, w, y, dX=x, dW=w)
+    for call in (lambda **k: cn.layer_norm(t, ns, Y=t, **k), lambda **k: cn.layer_norm_backward(t, t, stat, stat, ns, dX=t, **k),
+                 lambda **k: cn.linear(x, w, ls, Y=y, **k), lambda **k: cn.linear_backward(y, x, w, ls, dX=x, dW=w, **k)):
+        for stream in (None, types.SimpleNamespace(cuda_stream=0)):
+            with pytest.raises(ValueError, match="cpu"):
+                call(stream=stream)
+    assert not library.records
+
+
+def test_workspaces_are_where_the_tensors_are(library):
+    x, w, y = (torch.empty(n, dtype=torch.bfloat16, device=DEVICE) for n in ((1, 4, 64), (64, 64), (1, 4, 64)))
+    t, stat = x[:, None], torch.empty((1, 1, 4), device=DEVICE)
+    ns, ls = cn.make_norm_shape(t, t), cn.make_linear_shape(x, w, y, dX=x, dW=w)
+    for ws in (torch.empty(1 << 16, dtype=torch.uint8, device="meta"), torch.empty(1, dtype=torch.uint8, device=DEVICE).expand(1 << 16),
+               torch.empty(1 << 16, dtype=torch.uint8, device=DEVICE)[::2]):
+        for call in (lambda: cn.layer_norm_backward(t, t, stat, stat, ns, dX=t, ws=ws), lambda: cn.linear(x, w, ls, Y=y, ws=ws),
+                     lambda: cn.linear_backward(y, x, w, ls, dX=x, dW=w, ws=ws)):
+            with pytest.raises(ValueError, match="ws"):
+                call()
+    assert not library.records
