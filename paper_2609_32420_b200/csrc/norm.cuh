@@ -394,7 +394,12 @@ __global__ void __launch_bounds__(most_threads(LANES, V, false, XF)) __maxnreg__
             }
             t1 *= a.inv_c;
             mean = w0.x + t1;
-            m2 = fmaxf(fmaf(-float(a.C) * t1, t1, t2), 0.f);
+            m2 = fmaf(-float(a.C) * t1, t1, t2);
+            m2 = m2 < 0.f ? 0.f : m2;    // not fmaxf, which takes 0 for the NaN of a row that is not finite
+            if (!isfinite(mean)) {       // infinite or NaN, as the channels' sum is: the differences from an infinite first warp are not
+                mean = 0.f;
+                for (int w = 0; w < a.warps; ++w) mean = fmaf(mine[w].z * a.inv_c, mine[w].x, mean);
+            }
             flip ^= 1;                   // the next row's shares go to the other half: one barrier a row is enough
             minus = two(-mean);
         }

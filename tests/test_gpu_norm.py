@@ -252,3 +252,25 @@ def test_gradients_of_a_norm_that_is_shifted_only():
     s = cn.make_norm_shape(t["x"], t["dy"], t["weight"], one["scale"], shift=t["shift"], dX=t["x"].clone(), eps=EPS)
     ref = cn.layer_norm_backward(t["dy"], t["x"], mean, rstd, s, weight=t["weight"], bias=t["bias"], scale=one["scale"])
     assert all(torch.equal(a, b) for a, b in zip(g, ref))
+
+
+@pytest.mark.parametrize("C", [96, 1000, 1024, 1032, 1536, 5120, 16384])
+@pytest.mark.parametrize("x", ["bf16", "f32"])
+def test_statistics_of_rows_that_are_not_finite(C, x):
+    """By the formula: a NaN or an infinity makes the variance NaN, and so rstd and every channel of y, while the mean is what the channels sum up to.  On both
+    sides of 1024 channels, from which on several warps share a row; in the first warp's channels and in later ones."""
+    t = make(1, 1, 40, C, x, "f32", "f32", True, True)
+    clean = [v.clone() for v in forward(t, torch.float32)]
+    inf, nan = float("inf"), float("nan")
+    bad = {3: (0, nan), 7: (C - 1, nan), 11: (0, inf), 12: (C - 1, inf), 20: (C // 2, -inf), 21: (C * 3 // 4, nan), 30: (0, inf)}
+    for row, (c, v) in bad.items():
+        t["x"][0, 0, row, c] = v
+    t["x"][0, 0, 30, C - 1] = -inf
+    y, mean, rstd = forward(t, torch.float32)
+    keep = [i for i in range(40) if i not in bad]
+    for got, was in zip((y, mean, rstd), clean):
+        assert torch.equal(got[:, :, keep], was[:, :, keep])
+    want = t["x"].double().mean(-1)
+    for row in bad:
+        assert torch.isnan(y[0, 0, row]).all() and torch.isnan(rstd[0, 0, row]), row
+        assert torch.equal(mean[0, 0, row].double().nan_to_num(nan=7.0), want[0, 0, row].nan_to_num(nan=7.0)), row
