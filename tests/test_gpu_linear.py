@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from paper_2609_32420_b200 import carnator as cn
-from tests.layer_util import (ACT_ERR, DTYPES, SLOPE_MOST, U16, U32, act64, canvas, check, half_step, linear_grad_ref, linear_ref, padded, untouched)
+from tests.layer_util import (A, ACT_ERR, Bc, DTYPES, SLOPE_MOST, U16, U32, act64, canvas, check, half_step, linear_grad_ref, linear_ref, padded, untouched)
 
 pytestmark = pytest.mark.gpu
 
@@ -281,3 +281,19 @@ def test_warps_with_rows_behind_the_last(N, y, gate):
         out, z = forward(t, act)
         check_forward(t, act, out, z)
     assert torch.equal(forward(t, cn.ACT_NONE)[0], out)
+
+
+@pytest.mark.parametrize("act", ACTS[1:])
+def test_small_values_keep_their_bits(act):
+    """Relative to the value itself, down to where fp32 ends: an exponential whose argument was rounded four times at most (U32 of it each), and 64 U32 for an
+    approximate exponential and reciprocal (2^-22 each), a polynomial of degree 8 whose terms sum up to twice its value (9 roundings: 18 U32, and 2 U32 of its
+    own), products."""
+    M = 4096
+    x, w = torch.zeros((1, 40, 64), dtype=torch.bfloat16, device="cuda"), torch.zeros((M, 64), dtype=torch.bfloat16, device="cuda")
+    bias = torch.linspace(-12, 12, M, device="cuda")
+    y = torch.empty((1, 40, M), device="cuda")
+    cn.linear(x, w, cn.make_linear_shape(x, w, y, bias=bias, activation=act), bias=bias, Y=y)
+    z = bias.double()
+    ref = {cn.ACT_GELU_TANH: z * torch.sigmoid(2 * A * (z + Bc * z ** 3)), cn.ACT_GELU: act64(z, act), cn.ACT_SILU: z * torch.sigmoid(z)}[act]
+    arg = {cn.ACT_GELU_TANH: 2 * A * (z.abs() + Bc * z.abs() ** 3), cn.ACT_GELU: z * z / 2, cn.ACT_SILU: z.abs()}[act]
+    check(y, ref.expand(1, 40, M), (ref.abs() * (4 * arg + 64) * U32 + 2.0 ** -118).expand(1, 40, M), f"activation {act}")
