@@ -154,7 +154,9 @@ __device__ __forceinline__ void act_and_slope(f2 z, f2& f, f2& s) {
         const f2 u = mul2(z, fma2(zz, two(-2.f * kLog2e * kGeluA * kGeluB), two(-2.f * kLog2e * kGeluA)));
         const f2 g = rcp_each(add2(ex2_each(u), two(1.f)));
         f = mul2(z, g);
-        s = fma2(mul2(f, less_from(g, 1.f)), fma2(zz, two(6.f * kGeluA * kGeluB), two(2.f * kGeluA)), g);
+        float lo, hi;                    // the square of a z beyond 1.8e19 is infinite, and the factor before it 0
+        one_each(zz, lo, hi);
+        s = fma2(mul2(f, less_from(g, 1.f)), fma2(two(fminf(lo, 1e30f), fminf(hi, 1e30f)), two(6.f * kGeluA * kGeluB), two(2.f * kGeluA)), g);
     } else {
         f = z; s = two(1.f);
     }

@@ -297,3 +297,19 @@ def test_small_values_keep_their_bits(act):
     ref = {cn.ACT_GELU_TANH: z * torch.sigmoid(2 * A * (z + Bc * z ** 3)), cn.ACT_GELU: act64(z, act), cn.ACT_SILU: z * torch.sigmoid(z)}[act]
     arg = {cn.ACT_GELU_TANH: 2 * A * (z.abs() + Bc * z.abs() ** 3), cn.ACT_GELU: z * z / 2, cn.ACT_SILU: z.abs()}[act]
     check(y, ref.expand(1, 40, M), (ref.abs() * (4 * arg + 64) * U32 + 2.0 ** -118).expand(1, 40, M), f"activation {act}")
+
+
+@pytest.mark.parametrize("act", ACTS[1:])
+def test_slopes_of_the_largest_values(act):
+    """Up to the largest bf16 of either sign the slopes are 0 and 1 (and 1/2 at 0), as sums of three rows."""
+    big = torch.finfo(torch.bfloat16).max
+    z = torch.tensor([-big, -1e30, -1e20, -1e10, -1e4, 1e4, 1e10, 1e20, 1e30, big, 0.0, -0.0], device="cuda").bfloat16().repeat(4)
+    M = z.numel()
+    x, w = torch.randn((1, 3, 64), device="cuda").bfloat16(), torch.randn((M, 64), device="cuda").bfloat16()
+    zz, dy, gate, dw = z.expand(1, 3, M).contiguous(), torch.ones((1, 3, M), device="cuda"), torch.ones((1, M), device="cuda"), torch.empty_like(w)
+    g = cn.linear_backward(dy, x, w, cn.make_linear_shape(x, w, dy, Z=zz, dW=dw, gate=gate, activation=act), Z=zz, dW=dw, gate=gate)
+    want = (z > 0).double() + 0.5 * (z == 0).double()
+    check(g.dbias, 3 * want, 3 * ACT_ERR * torch.ones_like(want), "dbias")
+    value = 3 * z.double().clamp(min=0)
+    check(g.dgate[0, :9], value[:9], ACT_ERR * (value[:9].abs() + 3), "dgate")          # three times the largest is infinite
+    check(dw, want[:, None] * x.double().sum(1), (ACT_ERR + 2 * U16) * x.double().abs().sum(1).expand(M, 64), "dW")
