@@ -39,7 +39,9 @@ __device__ __forceinline__ void mma_16x8x16(float (&d)[4], uint32_t a0, uint32_t
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-template <int NT, int kRowsWarps>        // column tiles of 8 rows of x; warps that share k
+// NT: column tiles of 8 rows of x; kRowsWarps: warps that share k; kRuns: a warp's sums are longer than kLongRun (a loop around the loop, which takes
+// registers and with them one CTA in seven: 2 x 5120 x 30720 76.7 us with it, 69.6 without, cold caches and launch included).
+template <int NT, int kRowsWarps, bool kRuns>
 __global__ void __launch_bounds__(32 * kRowsWarps) linear_rows_kernel(const RowsArgs a) {
     __shared__ float sums[kRowsWarps][16][8 * NT + 1];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
@@ -59,39 +61,46 @@ __global__ void __launch_bounds__(32 * kRowsWarps) linear_rows_kernel(const Rows
         const int b = xon[j] ? row / a.per_batch : 0;
         xr[j] = a.x + b * a.xs[0] + (xon[j] ? row - b * a.per_batch : 0) * a.xs[1];
     }
-    float d[NT][4], d2[NT][4];           // two sums per warp: the instruction cuts its sums off, and what that loses grows with their length
-#pragma unroll
-    for (int j = 0; j < NT; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { d[j][i] = 0.f; d2[j][i] = 0.f; }
+    // Two sums per warp, emptied into shared memory after every kLongRun of k: the instruction cuts its sums off, and what that loses grows with their length
+    // (1 x 65536 x 7200 onto fp32, four warps: error 9.0e-6 in one run).
+    float d[NT][4], d2[NT][4];
     const uint4 zero = make_uint4(0, 0, 0, 0);
     constexpr int U = 4;                 // pieces of 32 k in flight per warp
     const int pieces = (a.K + 31) / 32;
-    for (int p = warp; p < pieces; p += kRowsWarps * U) {
-        uint4 u0[U], u1[U], xv[U][NT];
+    int p = warp;
+    do {
+        const bool first = !kRuns || p == warp;
+        const int stop = kRuns ? min(pieces, p + kRowsWarps * (kLongRun / 16)) : pieces;        // a piece gives each sum 16 k
 #pragma unroll
-        for (int q = 0; q < U; ++q) {
-            const int k = (p + q * kRowsWarps) * 32 + t * 8;         // past the end: zero
-            u0[q] = on0 ? load_k8(w0, k, a.K) : zero;
-            u1[q] = on1 ? load_k8(w1, k, a.K) : zero;
+        for (int j = 0; j < NT; ++j)
 #pragma unroll
-            for (int j = 0; j < NT; ++j) xv[q][j] = xon[j] ? load_k8(xr[j], k, a.K) : zero;
+            for (int i = 0; i < 4; ++i) { d[j][i] = 0.f; d2[j][i] = 0.f; }
+        for (; p < stop; p += kRowsWarps * U) {
+            uint4 u0[U], u1[U], xv[U][NT];
+#pragma unroll
+            for (int q = 0; q < U; ++q) {
+                const int k = (p + q * kRowsWarps) * 32 + t * 8;         // past the end: zero
+                u0[q] = on0 ? load_k8(w0, k, a.K) : zero;
+                u1[q] = on1 ? load_k8(w1, k, a.K) : zero;
+#pragma unroll
+                for (int j = 0; j < NT; ++j) xv[q][j] = xon[j] ? load_k8(xr[j], k, a.K) : zero;
+            }
+#pragma unroll
+            for (int q = 0; q < U; ++q)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+                    mma_16x8x16(d[j], u0[q].x, u1[q].x, u0[q].y, u1[q].y, xv[q][j].x, xv[q][j].y);
+                    mma_16x8x16(d2[j], u0[q].z, u1[q].z, u0[q].w, u1[q].w, xv[q][j].z, xv[q][j].w);
+                }
         }
 #pragma unroll
-        for (int q = 0; q < U; ++q)
+        for (int j = 0; j < NT; ++j)     // d0, d1: feature g, rows 2t and 2t + 1 of x; d2, d3: feature g + 8
 #pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                mma_16x8x16(d[j], u0[q].x, u1[q].x, u0[q].y, u1[q].y, xv[q][j].x, xv[q][j].y);
-                mma_16x8x16(d2[j], u0[q].z, u1[q].z, u0[q].w, u1[q].w, xv[q][j].z, xv[q][j].w);
+            for (int i = 0; i < 4; ++i) {
+                float& at = sums[warp][g + 8 * (i >> 1)][j * 8 + 2 * t + (i & 1)];
+                at = first ? d[j][i] + d2[j][i] : at + (d[j][i] + d2[j][i]);
             }
-    }
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {       // d0, d1: feature g, rows 2t and 2t + 1 of x; d2, d3: feature g + 8
-        sums[warp][g][j * 8 + 2 * t] = d[j][0] + d2[j][0];
-        sums[warp][g][j * 8 + 2 * t + 1] = d[j][1] + d2[j][1];
-        sums[warp][g + 8][j * 8 + 2 * t] = d[j][2] + d2[j][2];
-        sums[warp][g + 8][j * 8 + 2 * t + 1] = d[j][3] + d2[j][3];
-    }
+    } while (kRuns && p < pieces);
     __syncthreads();
     auto param = [&](const void* p, int64_t i, int f32) { return f32 ? static_cast<const float*>(p)[i] : __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]); };
     const int f = tid & 15, col = f0 + f;
@@ -118,7 +127,10 @@ template <int NT>
 inline cudaError_t launch_rows_tiles(const RowsArgs& a, cudaStream_t stream) {
     const int grid = ceil_div(a.cols, 16);
     const int warps = grid <= 148 ? 16 : grid <= 3 * 148 ? 8 : 4;
-    auto kern = warps == 16 ? linear_rows_kernel<NT, 16> : warps == 8 ? linear_rows_kernel<NT, 8> : linear_rows_kernel<NT, 4>;
+    const bool runs = a.K > 2 * kLongRun * warps;
+    auto kern = warps == 16 ? (runs ? linear_rows_kernel<NT, 16, true> : linear_rows_kernel<NT, 16, false>)
+              : warps == 8  ? (runs ? linear_rows_kernel<NT, 8, true> : linear_rows_kernel<NT, 8, false>)
+                            : (runs ? linear_rows_kernel<NT, 4, true> : linear_rows_kernel<NT, 4, false>);
     return launch_dependent(kern, dim3(grid), dim3(32 * warps), 0, stream, a);
 }
 

@@ -313,3 +313,17 @@ def test_slopes_of_the_largest_values(act):
     value = 3 * z.double().clamp(min=0)
     check(g.dgate[0, :9], value[:9], ACT_ERR * (value[:9].abs() + 3), "dgate")          # three times the largest is infinite
     check(dw, want[:, None] * x.double().sum(1), (ACT_ERR + 2 * U16) * x.double().abs().sum(1).expand(M, 64), "dW")
+
+
+def check_long_sum(N, K, M):
+    """As test_fp32_output_of_a_long_sum: runs of 2560 products at most, whoever shares them out."""
+    t = make(1, N, K, M, "f32", bias=False, gate=False, residual=False)
+    y, _ = forward(t, cn.ACT_NONE, keep=False)
+    ref = t["x"].double() @ t["w"].double().T
+    assert (y.double() - ref).norm() <= 160 * 2 / 3 * 2.0 ** -24 * ref.norm()
+
+
+@pytest.mark.parametrize("N,K,M", [(1, 65536, 7200), (8, 300000, 64), (8, 40961, 7200), (3, 65000, 3000)])
+def test_fp32_output_of_a_long_sum_of_few_rows(N, K, M):
+    """Four, eight and sixteen warps share k, two sums each."""
+    check_long_sum(N, K, M)
