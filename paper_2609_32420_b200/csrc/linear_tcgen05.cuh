@@ -59,6 +59,7 @@ struct TcArgs {
     int k_len;                           // k of a batch entry
     int a_slabs, b_slabs;                // MN-major: whole 64-column slabs of the operand, which a tile fetches in one copy where all of its slabs are whole
     int stages, splits;
+    int run;                             // kLong: most stages of k that one accumulator sums up
     int clears;                          // the first product of a call clears its status word
 };
 
@@ -331,16 +332,19 @@ __device__ __forceinline__ void tile_at(const TcArgs& a, int t, int& b, int& m, 
 constexpr int kLongRun = 2560;           // most k that one accumulator sums up (kLong)
 
 // kSub: slabs of 64 columns of k per stage.
-// kLong: an fp32 output of a long k.  The tensor cores cut their sums off instead of rounding them, so a sum of 5120 products loses 5.6e-6 of itself, eight
-// times what fp32 additions in a row do.  Here an accumulator sums up kLongRun of k at most, and the epilogue adds what it held to registers of its own, under the next
-// run: 128 per thread, for which the service warps give most of theirs.  75600 x 5120 x 5120 onto a residual stream: error 1.6e-6 with one run, 7.6e-7 with
-// two, 2.8e-7 with five; 2848, 2903 and 3214 us.
-template <int AMN, int BMN, int kSub, bool kLong>
+// kLong: an fp32 output of a k that is longer than one accumulator may sum up; 1: a pair has all of it, 3: pairs share it.  The tensor cores cut their sums off
+// instead of rounding them, so a sum of 5120 products loses 5.6e-6 of itself, eight times what fp32 additions in a row do.  Here an accumulator sums up
+// kLongRun of k at most, and the epilogue adds what it held to registers of its own, under the next run: 128 per thread, for which the service
+// warps give most of theirs.  Pairs that share k do the same with their shares before they are joined (512 x 8960 x 2048, shares of 4480: 22.9 us, 21.8 in
+// one run; 64 x 30720 x 1536, shares of 7680: 32.8 both ways, error 8.5e-6 in one run).  75600 x 5120 x 5120 onto a residual stream: error 1.6e-6 with
+// one run, 7.6e-7 with two, 2.8e-7 with five; 2848, 2903 and 3214 us.
+template <int AMN, int BMN, int kSub, int kLong>
 __global__ void __launch_bounds__(kThreadsTc, 1)
 linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB, const __grid_constant__ CUtensorMap mapAs,
                  const __grid_constant__ CUtensorMap mapBs, const TcArgs a) {
     constexpr int kTileK = kSub * kSlab;                 // k of a stage
     constexpr uint32_t kABytes = 128 * kTileK * 2;       // a CTA's share of A per stage
+    constexpr bool kF32 = kLong & 1, kShared = kLong != 1;               // pairs may share k
     extern __shared__ unsigned char lin_smem[];
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
@@ -388,7 +392,42 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
     const int k_all = a.k_batches * a.k_tiles;
     const int k0 = int(int64_t(k_all) * split / a.splits), k1 = int(int64_t(k_all) * (split + 1) / a.splits);
     // kLong: runs of k with an accumulator each
-    const int chunks = kLong ? (k1 - k0 + kLongRun / kTileK - 1) / (kLongRun / kTileK) : 1, chunk = (k1 - k0 + chunks - 1) / chunks;
+    const int chunks = kLong ? (k1 - k0 + a.run - 1) / a.run : 1, chunk = (k1 - k0 + chunks - 1) / chunks;
+
+    // Every CTA of the cluster finishes a run of the columns: the partial tiles of the same rows, added in the order of k.  By `step` threads from `from`.
+    auto join = [&](int from, int step) {
+        int b, m, n;
+        tile_at(a, first, b, m, n);
+        const uint32_t pitch = uint32_t(a.bn + 4) * 4u;
+        const int share = a.bn / a.splits, groups = share / 8, c0 = int(split) * share;
+        for (int i = from; i < 128 * groups; i += step) {
+            const int r = i / groups, c = c0 + (i - r * groups) * 8;
+            const int row = m * kTileM + int(half) * 128 + r, col = n * a.bn + c, cn = min(max(a.cols - col, 0), 8);
+            if (row >= a.rows || cn == 0) continue;
+            norm::Raw8<true> res;
+            if (a.e.residual) load_residual(a.e, b, row, col, cn, res);
+            Columns cols;
+            columns_begin(a.e, cols, col, cn);
+            // all of the cluster's shares on their way before the first is added
+            float g[4][8];
+#pragma unroll
+            for (int sp = 0; sp < 4; ++sp)
+                if (sp < a.splits) {
+                    const uint32_t src = map_cta(base + uint32_t(r) * pitch + uint32_t(c) * 4u, uint32_t(2 * sp) + half);
+#pragma unroll
+                    for (int q = 0; q < 2; ++q)
+                        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(g[sp][4 * q]), "=f"(g[sp][4 * q + 1]), "=f"(g[sp][4 * q + 2]),
+                                     "=f"(g[sp][4 * q + 3]) : "r"(src + 16u * q) : "memory");
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) g[sp][q] = 0.f;
+                }
+            float f[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) f[q] = ((g[0][q] + g[1][q]) + g[2][q]) + g[3][q];
+            finish(a.e, cols, b, row, col, cn, f, res);
+        }
+    };
 
     if (warp < 4) {                      // ---- service warps
     // 128 x 40 + 256 x 208 registers; the block is launched with 384 x 152 at least (checked by the host)
@@ -494,6 +533,10 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
             }
         }
     }
+    if (kLong && kShared && a.splits > 1) {             // the epilogue warps meet the cluster before they join its tiles
+        __syncwarp();
+        cluster_sync();
+    }
     } else {
         if (kLong) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;" ::: "memory");
         // ================= epilogue =================
@@ -510,7 +553,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
                 const bool on = row < a.rows;
                 const int64_t y_off = b * a.e.ys[0] + row * a.e.ys[1], z_off = b * a.e.zs[0] + row * a.e.zs[1], r_off = b * a.e.rs[0] + row * a.e.rs[1];
                 const int64_t gate_off = a.e.gate ? (b + row / a.e.rows_per_gate) * a.e.gate_stride : 0;
-                const char* res = static_cast<const char*>(a.e.residual) + (r_off + n * a.bn) * 4;
+                const char* res = static_cast<const char*>(a.e.residual) + (r_off + n * a.bn) * (kF32 ? 4 : 2);
                 __syncwarp();            // rows behind the last one have left the tile before early
                 f2 acc[4][16];           // 32 columns each: side * 32, + 64, + 128, + 192
 #pragma unroll
@@ -539,6 +582,23 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
                 }
                 __syncwarp();
                 if (!ok) break;
+                if (kShared && a.splits > 1) {         // the one tile of this cluster: this pair's share to shared memory, as below
+                    const uint32_t line = base + uint32_t(quarter * 32 + lane) * (uint32_t(a.bn + 4) * 4u);
+#pragma unroll
+                    for (int p = 0; p < 4; ++p) {
+                        const int at = side * 32 + 64 * p;
+                        if (at < left) {
+#pragma unroll
+                            for (int q = 0; q < 8; ++q) {
+                                float f[4];
+                                one_each(acc[p][2 * q], f[0], f[1]);
+                                one_each(acc[p][2 * q + 1], f[2], f[3]);
+                                asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(line + uint32_t(at + 4 * q) * 4u), "f"(f[0]), "f"(f[1]), "f"(f[2]), "f"(f[3]) : "memory");
+                            }
+                        }
+                    }
+                    break;
+                }
 #pragma unroll
                 for (int p = 0; p < 4; ++p) {
                     const int at = side * 32 + 64 * p, col = n * a.bn + at;
@@ -547,11 +607,14 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
                             Sector r0, r1;
-                            if (a.e.residual) { r0 = load_sector(res + (at + 16 * h) * 4, a.e.wide_ok); r1 = load_sector(res + (at + 16 * h) * 4 + 32, a.e.wide_ok); }
+                            if (a.e.residual) {
+                                r0 = load_sector(res + (at + 16 * h) * (kF32 ? 4 : 2), a.e.wide_ok);
+                                if (kF32) r1 = load_sector(res + (at + 16 * h) * 4 + 32, a.e.wide_ok);
+                            }
                             float f[16];
 #pragma unroll
                             for (int q = 0; q < 8; ++q) one_each(acc[p][8 * h + q], f[2 * q], f[2 * q + 1]);
-                            finish16<true>(a.e, a.e.gate, gate_off, y_off, z_off, col + 16 * h, f, r0, r1);
+                            finish16<kF32>(a.e, a.e.gate, gate_off, y_off, z_off, col + 16 * h, f, r0, kF32 ? r1 : r0);
                         }
                     } else {
 #pragma unroll
@@ -570,6 +633,12 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
                         }
                     }
                 }
+            }
+            if (kShared && a.splits > 1) {
+                tc_fence_before();
+                __syncwarp();
+                cluster_sync();
+                if (!*abortp) join(tid - 128, 32 * kEpiWarps);
             }
         } else if (a.splits == 1) {
             for (int t = first; t < a.tiles && ok; t += step, ++i) {
@@ -656,41 +725,9 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
     }
 
     if (!kLong && a.splits > 1) {
-        // Every CTA of the cluster finishes a run of the columns: the partial tiles of the same rows, added in the order of k.
         __syncwarp();
         cluster_sync();
-        int b, m, n;
-        tile_at(a, first, b, m, n);
-        const uint32_t pitch = uint32_t(a.bn + 4) * 4u;
-        const int share = a.bn / a.splits, groups = share / 8, c0 = int(split) * share;
-        if (!*abortp)
-            for (int i = tid; i < 128 * groups; i += kThreadsTc) {
-                const int r = i / groups, c = c0 + (i - r * groups) * 8;
-                const int row = m * kTileM + int(half) * 128 + r, col = n * a.bn + c, cn = min(max(a.cols - col, 0), 8);
-                if (row >= a.rows || cn == 0) continue;
-                norm::Raw8<true> res;
-                if (a.e.residual) load_residual(a.e, b, row, col, cn, res);
-                Columns cols;
-                columns_begin(a.e, cols, col, cn);
-                // all of the cluster's shares on their way before the first is added
-                float g[4][8];
-#pragma unroll
-                for (int sp = 0; sp < 4; ++sp)
-                    if (sp < a.splits) {
-                        const uint32_t src = map_cta(base + uint32_t(r) * pitch + uint32_t(c) * 4u, uint32_t(2 * sp) + half);
-#pragma unroll
-                        for (int q = 0; q < 2; ++q)
-                            asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(g[sp][4 * q]), "=f"(g[sp][4 * q + 1]), "=f"(g[sp][4 * q + 2]),
-                                         "=f"(g[sp][4 * q + 3]) : "r"(src + 16u * q) : "memory");
-                    } else {
-#pragma unroll
-                        for (int q = 0; q < 8; ++q) g[sp][q] = 0.f;
-                    }
-                float f[8];
-#pragma unroll
-                for (int q = 0; q < 8; ++q) f[q] = ((g[0][q] + g[1][q]) + g[2][q]) + g[3][q];
-                finish(a.e, cols, b, row, col, cn, f, res);
-            }
+        if (!*abortp) join(tid, kThreadsTc);
     }
     tc_fence_before();
     __syncwarp();
@@ -758,12 +795,13 @@ inline Plan plan_of(int64_t m_tiles, int64_t cols, int64_t k_all, bool b_mn, boo
     return best;
 }
 
-template <int AMN, int BMN, int kSub, bool kLong>
+template <int AMN, int BMN, int kSub, int kLong>
 inline carnator_status launch_tc_stages(const Operand& A, const Operand& B, TcArgs a, cudaStream_t stream, char* err, size_t errlen) {
     constexpr int kTileK = kSub * kSlab;
     const uint32_t stage = 128 * kTileK * 2 + uint32_t(a.bn / 2) * kTileK * 2;
     a.k_tiles = ceil_div(a.k_len, kTileK);
     a.stages = int(std::min<uint32_t>(kMaxStages, kRingBytes / stage));
+    a.run = kLongRun / kTileK;
     a.a_slabs = AMN ? int(A.cols / kSlab) : 0;
     a.b_slabs = BMN ? int(B.cols / kSlab) : 0;
     auto map = [](CUtensorMap* m, const Operand& o, int rows) { return make_map_3d(m, o.base, o.batches, o.rows, o.cols, o.batch_stride, o.row_stride, rows); };
@@ -821,12 +859,16 @@ inline carnator_status launch_tc_product(const Operand& A, const Operand& B, TcA
     if (tiles > (int64_t(1) << 30)) return CARNATOR_ERR_UNSUPPORTED;
     a.tiles = int(tiles);
     a.group_m = 8;
+    // whether a pair's share of k is longer than one accumulator may sum up
+    const int64_t share = (int64_t(a.k_batches) * ceil_div(a.k_len, kSlab) + a.splits - 1) / a.splits;
+    const bool longer = a.e.y_f32 && share * kSlab > kLongRun;
     if constexpr (!AMN && !BMN) {
-        const bool exact = a.e.y_f32 && a.splits == 1 && a.k_len > kLongRun;
-        if (a.bn == 256) return exact ? launch_tc_stages<AMN, BMN, 1, true>(A, B, a, stream, err, errlen) : launch_tc_stages<AMN, BMN, 1, false>(A, B, a, stream, err, errlen);
-        if (exact) return launch_tc_stages<AMN, BMN, 2, true>(A, B, a, stream, err, errlen);
+        if (longer && a.splits > 1)
+            return a.bn == 256 ? launch_tc_stages<AMN, BMN, 1, 3>(A, B, a, stream, err, errlen) : launch_tc_stages<AMN, BMN, 2, 3>(A, B, a, stream, err, errlen);
+        if (longer) return a.bn == 256 ? launch_tc_stages<AMN, BMN, 1, 1>(A, B, a, stream, err, errlen) : launch_tc_stages<AMN, BMN, 2, 1>(A, B, a, stream, err, errlen);
+        if (a.bn == 256) return launch_tc_stages<AMN, BMN, 1, 0>(A, B, a, stream, err, errlen);
     }
-    return launch_tc_stages<AMN, BMN, 2, false>(A, B, a, stream, err, errlen);
+    return launch_tc_stages<AMN, BMN, 2, 0>(A, B, a, stream, err, errlen);
 }
 
 }  // namespace lin

@@ -327,3 +327,9 @@ def check_long_sum(N, K, M):
 def test_fp32_output_of_a_long_sum_of_few_rows(N, K, M):
     """Four, eight and sixteen warps share k, two sums each."""
     check_long_sum(N, K, M)
+
+
+@pytest.mark.parametrize("N,K,M", [(64, 30720, 1536), (1000, 13824, 1536), (300, 120000, 600), (512, 8960, 2048), (40, 41000, 5000)])
+def test_fp32_output_of_a_long_sum_whose_k_is_shared(N, K, M):
+    """Two and four pairs share a tile's k, each more than 2560 of it."""
+    check_long_sum(N, K, M)
