@@ -376,8 +376,9 @@ carnator_status carnator_layer_norm_backward(const void* dY, const void* X, cons
  *   dbias  fp32 [out_features] or NULL;  dgate  fp32 [B,out_features] contiguous or NULL (wants gate)
  *   ws     device workspace, >= carnator_linear_backward_workspace_bytes (header, dz, partial sums)
  * Up to 8 rows in all (16 unless W is large) run on a kernel that streams W once through the registers of mma.sync; more rows on tcgen05 with
- * bounded waits, whose status carnator_query_status(ws) returns.  An fp32 y of more than 2560 input features is summed up in
- * runs of 2560 at most, as the tensor cores cut their sums off (2^-24 of a running sum per 16 products on average).
+ * bounded waits, whose status carnator_query_status(ws) returns.  The tensor cores cut their sums off (2^-24 of a running sum per 16 products
+ * on average), so a sum is taken up in runs and the runs are added in fp32: runs of at most 2560 products for an fp32 y, 65536 for bf16 outputs (y, dX, dW), on
+ * the kernel for few rows 2560 for both.
  * Calls that may run at the same time (streams, captured graphs) need a workspace each, as everywhere.  The kernels of these
  * calls may be launched while the kernel ahead of them on the stream drains; they touch no memory before it has ended.
  * Limits: B N, in_features, out_features <= 2^27, B <= 65535.

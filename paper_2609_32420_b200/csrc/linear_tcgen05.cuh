@@ -329,15 +329,17 @@ __device__ __forceinline__ void tile_at(const TcArgs& a, int t, int& b, int& m, 
     m = mt - b * a.tiles_m;
 }
 
-constexpr int kLongRun = 2560;           // most k that one accumulator sums up (kLong)
+constexpr int kLongRun = 2560;           // most k that one accumulator sums up for an fp32 output,
+constexpr int kLongRunBf16 = 65536;      // and for a bf16 one
 
 // kSub: slabs of 64 columns of k per stage.
-// kLong: an fp32 output of a k that is longer than one accumulator may sum up; 1: a pair has all of it, 3: pairs share it.  The tensor cores cut their sums off
-// instead of rounding them, so a sum of 5120 products loses 5.6e-6 of itself, eight times what fp32 additions in a row do.  Here an accumulator sums up
-// kLongRun of k at most, and the epilogue adds what it held to registers of its own, under the next run: 128 per thread, for which the service
-// warps give most of theirs.  Pairs that share k do the same with their shares before they are joined (512 x 8960 x 2048, shares of 4480: 22.9 us, 21.8 in
-// one run; 64 x 30720 x 1536, shares of 7680: 32.8 both ways, error 8.5e-6 in one run).  75600 x 5120 x 5120 onto a residual stream: error 1.6e-6 with
-// one run, 7.6e-7 with two, 2.8e-7 with five; 2848, 2903 and 3214 us.
+// kLong: k is longer than one accumulator may sum up; 1: an fp32 output, a pair has all of k, 3: pairs share it, 2: a bf16 output, either.  The tensor cores cut
+// their sums off instead of rounding them, up to 2^-28 of the sum per product: a sum of 5120 products loses 5.6e-6 of itself, eight times what fp32 additions in a
+// row do, and one of a million of the same sign (the rows of a weight's gradient) 2 to 4e-3, as much as the rounding to bf16.  Here an accumulator sums up a.run
+// stages of k at most, and the epilogue adds what it held to registers of its own, under the next run: 128 per thread, for which the service
+// warps give most of theirs.  Pairs that share k do the same with their shares before they are joined (512 x 8960 x 2048 onto fp32, shares of 4480: 22.9 us,
+// 21.8 in one run; 64 x 30720 x 1536, shares of 7680: 32.8 both ways, error 8.5e-6 in one run).  75600 x 5120 x 5120 onto a residual stream: error 1.6e-6
+// with one run, 7.6e-7 with two, 2.8e-7 with five; 2848, 2903 and 3214 us.
 template <int AMN, int BMN, int kSub, int kLong>
 __global__ void __launch_bounds__(kThreadsTc, 1)
 linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB, const __grid_constant__ CUtensorMap mapAs,
@@ -801,7 +803,7 @@ inline carnator_status launch_tc_stages(const Operand& A, const Operand& B, TcAr
     const uint32_t stage = 128 * kTileK * 2 + uint32_t(a.bn / 2) * kTileK * 2;
     a.k_tiles = ceil_div(a.k_len, kTileK);
     a.stages = int(std::min<uint32_t>(kMaxStages, kRingBytes / stage));
-    a.run = kLongRun / kTileK;
+    a.run = (kLong & 1 ? kLongRun : kLongRunBf16) / kTileK;
     a.a_slabs = AMN ? int(A.cols / kSlab) : 0;
     a.b_slabs = BMN ? int(B.cols / kSlab) : 0;
     auto map = [](CUtensorMap* m, const Operand& o, int rows) { return make_map_3d(m, o.base, o.batches, o.rows, o.cols, o.batch_stride, o.row_stride, rows); };
@@ -861,14 +863,14 @@ inline carnator_status launch_tc_product(const Operand& A, const Operand& B, TcA
     a.group_m = 8;
     // whether a pair's share of k is longer than one accumulator may sum up
     const int64_t share = (int64_t(a.k_batches) * ceil_div(a.k_len, kSlab) + a.splits - 1) / a.splits;
-    const bool longer = a.e.y_f32 && share * kSlab > kLongRun;
+    const bool longer = share * kSlab > (a.e.y_f32 ? kLongRun : kLongRunBf16);
     if constexpr (!AMN && !BMN) {
-        if (longer && a.splits > 1)
+        if (longer && a.e.y_f32 && a.splits > 1)
             return a.bn == 256 ? launch_tc_stages<AMN, BMN, 1, 3>(A, B, a, stream, err, errlen) : launch_tc_stages<AMN, BMN, 2, 3>(A, B, a, stream, err, errlen);
-        if (longer) return a.bn == 256 ? launch_tc_stages<AMN, BMN, 1, 1>(A, B, a, stream, err, errlen) : launch_tc_stages<AMN, BMN, 2, 1>(A, B, a, stream, err, errlen);
-        if (a.bn == 256) return launch_tc_stages<AMN, BMN, 1, 0>(A, B, a, stream, err, errlen);
+        if (longer && a.e.y_f32) return a.bn == 256 ? launch_tc_stages<AMN, BMN, 1, 1>(A, B, a, stream, err, errlen) : launch_tc_stages<AMN, BMN, 2, 1>(A, B, a, stream, err, errlen);
+        if (!longer && a.bn == 256) return launch_tc_stages<AMN, BMN, 1, 0>(A, B, a, stream, err, errlen);
     }
-    return launch_tc_stages<AMN, BMN, 2, 0>(A, B, a, stream, err, errlen);
+    return longer ? launch_tc_stages<AMN, BMN, 2, 2>(A, B, a, stream, err, errlen) : launch_tc_stages<AMN, BMN, 2, 0>(A, B, a, stream, err, errlen);
 }
 
 }  // namespace lin

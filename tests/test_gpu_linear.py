@@ -333,3 +333,41 @@ def test_fp32_output_of_a_long_sum_of_few_rows(N, K, M):
 def test_fp32_output_of_a_long_sum_whose_k_is_shared(N, K, M):
     """Two and four pairs share a tile's k, each more than 2560 of it."""
     check_long_sum(N, K, M)
+
+
+@pytest.mark.parametrize("B,N,K,M", [(1, 1 << 22, 8, 8), (2, 1 << 21, 8, 8), (1, 1 << 20, 64, 200), (3, 100001, 136, 72), (1, 75600, 1536, 1536)])
+def test_weight_gradients_of_very_many_rows(B, N, K, M):
+    """Terms of one sign, where what an accumulator cuts off adds up: at most a step (2^-23 of a running sum that is half the final one on average) per
+    addition, two additions per 16 terms counted, over runs of 65536: 2 x 4096 x 2^-24 = 2^-11 of the sum, the additions of the runs and their shares
+    2^-18 at most, and the rounding to bf16."""
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    x, dy = (torch.rand((B, N, n), device="cuda", generator=gen).add_(0.5).bfloat16() for n in (K, M))
+    w = torch.zeros((M, K), dtype=torch.bfloat16, device="cuda")
+    dw = torch.empty_like(w)
+    s = cn.make_linear_shape(x, w, dy, dW=dw)
+    ws = torch.empty(cn.linear_backward_workspace_bytes(s), dtype=torch.uint8, device="cuda")
+    cn.linear_backward(dy, x, w, s, dW=dw, want=(), ws=ws)
+    assert cn.query_status(ws) == cn.OK
+    ref = sum(d.double().T @ a.double() for d, a in zip(dy.flatten(0, 1).split(1 << 18), x.flatten(0, 1).split(1 << 18)))
+    check(dw, ref, ref * (U16 + 2.0 ** -11 + 2.0 ** -18), "dW")
+
+
+@pytest.mark.parametrize("N,K,M", [(40, 1 << 21, 64), (600, 1 << 18, 256), (2500, 70000, 2000), (3, 1 << 20, 40)])
+def test_bf16_outputs_of_very_long_sums(N, K, M):
+    """y, and dX of the transposed weight: as test_weight_gradients_of_very_many_rows."""
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    x = torch.rand((1, N, K), device="cuda", generator=gen).add_(0.5).bfloat16()
+    w = torch.rand((M, K), device="cuda", generator=gen).add_(0.5).bfloat16()
+    bias, residual = torch.randn(M, device="cuda", generator=gen), torch.randn((1, N, M), device="cuda", generator=gen).bfloat16()
+    y, z, dx = (torch.empty((1, N, M), dtype=torch.bfloat16, device="cuda") for _ in range(3))
+    _, ws = cn.linear(x, w, cn.make_linear_shape(x, w, y, bias=bias, residual=residual, Z=z), bias=bias, residual=residual, Y=y, Z=z)
+    assert cn.query_status(ws) == cn.OK
+    ref = sum(a.double() @ b.double().T for a, b in zip(x[0].split(1 << 17, 1), w.split(1 << 17, 1)))[None]
+    e = ref * (2.0 ** -11 + 2.0 ** -18)
+    zz = ref + bias.double()
+    check(z, zz, e + U16 * (zz.abs() + e), "z")
+    yy = zz + residual.double()
+    check(y, yy, e + U16 * (yy.abs() + e), "y")
+    wt = w.T.contiguous()
+    cn.linear_backward(x, y, wt, cn.make_linear_shape(y, wt, x, dX=dx), dX=dx, want=())
+    check(dx, ref, e + U16 * (ref + e), "dX")
