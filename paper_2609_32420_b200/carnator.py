@@ -605,10 +605,10 @@ def _last_axis(t, what: str):
         raise ValueError(f"{what}: the last axis must be contiguous")
 
 
-def make_norm_shape(X, Y, weight=None, scale=None, shift=None, dX=None, eps: float = 1e-6) -> NormShape:
+def make_norm_shape(X, Y, weight=None, scale=None, shift=None, dX=None, eps: float = 1e-6, bias=None) -> NormShape:
     """Record of a layer norm over the last axis of X [B,H,N,C] (H = 1: whole token rows).  Y is the output of the forward
     call or the gradient dY that the backward call gets; types and strides are taken from the tensors.  shift has the
-    batch stride of scale unless given."""
+    batch stride of scale unless given; bias, which has the type of weight, is looked at only where there is no weight."""
     for t, what in ((X, "X"), (Y, "Y"), (dX, "dX")):
         if t is not None and t.dim() != 4:
             raise ValueError(f"{what} must be [B,H,N,C]")
@@ -618,7 +618,8 @@ def make_norm_shape(X, Y, weight=None, scale=None, shift=None, dX=None, eps: flo
     s.x_stride, s.y_stride = _rows_of(s.x_stride, X), _rows_of(s.y_stride, Y)
     s.dy_stride, s.dx_stride = _rows_of(s.dy_stride, Y), _rows_of(s.dx_stride, dX, X)
     s.x_dtype, s.y_dtype = _dtype_code(X, "X"), _dtype_code(Y, "Y")
-    s.weight_dtype = DTYPE_F32 if weight is None else _dtype_code(weight, "weight")
+    affine = weight if weight is not None else bias
+    s.weight_dtype = DTYPE_F32 if affine is None else _dtype_code(affine, "weight" if weight is not None else "bias")
     mod = scale if scale is not None else shift
     s.mod_dtype = DTYPE_F32 if mod is None else _dtype_code(mod, "scale")
     s.scale_stride = 0 if mod is None else mod.stride(0)
@@ -669,8 +670,8 @@ class NormGrads(NamedTuple):
 
 def layer_norm_backward(dY, X, mean, rstd, shape: NormShape, weight=None, bias=None, scale=None, dX=None,
                         want=("weight", "bias", "shift", "scale"), modulated=None, ws=None, stream=None) -> NormGrads:
-    """carnator_layer_norm_backward.  ``want`` names the vector gradients to compute: weight and bias (if the norm has a
-    weight), shift and scale (if it has a scale, or ``modulated`` says that it has a shift only)."""
+    """carnator_layer_norm_backward.  ``want`` names the vector gradients to compute: weight (if the norm has one), bias (if
+    it has a weight or a bias), shift and scale (if it has a scale, or ``modulated`` says that it has a shift only)."""
     import torch
     dev = X.device
     if dX is None:
@@ -690,11 +691,10 @@ def layer_norm_backward(dY, X, mean, rstd, shape: NormShape, weight=None, bias=N
         _fit(scale, "scale", *said.scale, dev)
     B, C = said.record.B, said.record.C
     dweight = dbias = dshift = dscale = None
-    if weight is not None:
-        if "weight" in want:
-            dweight = torch.empty(C, dtype=torch.float32, device=dev)
-        if "bias" in want:
-            dbias = torch.empty(C, dtype=torch.float32, device=dev)
+    if weight is not None and "weight" in want:
+        dweight = torch.empty(C, dtype=torch.float32, device=dev)
+    if (weight is not None or bias is not None) and "bias" in want:
+        dbias = torch.empty(C, dtype=torch.float32, device=dev)
     if scale is not None if modulated is None else modulated:
         if "shift" in want:
             dshift = torch.empty((B, C), dtype=torch.float32, device=dev)

@@ -274,3 +274,19 @@ def test_statistics_of_rows_that_are_not_finite(C, x):
     for row in bad:
         assert torch.isnan(y[0, 0, row]).all() and torch.isnan(rstd[0, 0, row]), row
         assert torch.equal(mean[0, 0, row].double().nan_to_num(nan=7.0), want[0, 0, row].nan_to_num(nan=7.0)), row
+
+
+@pytest.mark.parametrize("p", ["bf16", "f32"])
+@pytest.mark.parametrize("C", [128, 1541])
+def test_a_norm_with_a_bias_only(p, C):
+    """As with a weight of ones: the same bits, the bias's gradient and the scale's, which reads the bias, among them."""
+    t = make(2, 1, 90, C, "bf16", "bf16", p, True, True)
+    ones = dict(t, weight=torch.ones_like(t["weight"]))
+    y, mean, rstd = forward(ones, torch.bfloat16)
+    ref = backward(ones, mean, rstd)
+    s = cn.make_norm_shape(t["x"], y, None, t["scale"], shift=t["shift"], eps=EPS, bias=t["bias"])
+    out = cn.layer_norm(t["x"], s, bias=t["bias"], shift=t["shift"], scale=t["scale"], Y=torch.empty_strided(y.shape, y.stride(), dtype=y.dtype, device="cuda"))
+    assert torch.equal(out, y)
+    s = cn.make_norm_shape(t["x"], t["dy"], None, t["scale"], shift=t["shift"], eps=EPS, bias=t["bias"])
+    g = cn.layer_norm_backward(t["dy"], t["x"], mean, rstd, s, bias=t["bias"], scale=t["scale"])
+    assert g.dweight is None and all(torch.equal(getattr(g, n), getattr(ref, n)) for n in ("dX", "dbias", "dshift", "dscale"))

@@ -321,3 +321,18 @@ def test_workspaces_are_where_the_tensors_are(library):
             with pytest.raises(ValueError, match="ws"):
                 call()
     assert not library.records
+
+
+# ---- as wide as the C calls ---------------------------------------------------------------------------------
+def test_a_norm_may_have_a_bias_only(library):
+    x = torch.empty((1, 1, 4, 64), dtype=torch.bfloat16, device=DEVICE)
+    stat = torch.empty((1, 1, 4), device=DEVICE)
+    for dtype, code in ((torch.bfloat16, cn.DTYPE_BF16), (torch.float32, cn.DTYPE_F32)):
+        bias = torch.empty(64, dtype=dtype, device=DEVICE)
+        s = cn.make_norm_shape(x, x, bias=bias)
+        assert s.weight_dtype == code
+        cn.layer_norm(x, s, bias=bias, Y=x)
+        g = cn.layer_norm_backward(x, x, stat, stat, s, bias=bias)
+        assert g.dbias.shape == (64,) and g.dweight is None
+        assert cn.layer_norm_backward(x, x, stat, stat, s, bias=bias, want=()).dbias is None
+    assert cn.make_norm_shape(x, x, torch.empty(64, dtype=torch.bfloat16, device=DEVICE)).weight_dtype == cn.DTYPE_BF16
