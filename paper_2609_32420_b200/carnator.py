@@ -782,15 +782,19 @@ class LinearGrads(NamedTuple):
 
 def linear_backward(dY, X, W, shape: LinearShape, Z=None, gate=None, dX=None, dW=None, want=("bias", "gate"), ws=None,
                     stream=None) -> LinearGrads:
-    """carnator_linear_backward.  dX and dW are computed where given (bf16); ``want`` names the fp32 vector gradients: bias, gate
-    (if there is one).  Z is the pre-activation that the forward call wrote."""
+    """carnator_linear_backward.  dX (from W) and dW (from X) are computed where given (bf16); X or W that is not read may be None.
+    ``want`` names the fp32 vector gradients: bias, gate (if there is one).  Z is the pre-activation that the forward call wrote."""
     import torch
     dev = dY.device
     said = _linear_said(bytes(shape))
     on = _stream_on(dev, stream)
     _fit(dY, "dY", *said.y, dev)
-    _fit(X, "X", *said.x, dev)
-    _fit(W, "W", *said.w, dev)
+    if (X is None and dW is not None) or (W is None and dX is not None):
+        raise ValueError("dW is made from X, dX from W")
+    if X is not None:
+        _fit(X, "X", *said.x, dev)
+    if W is not None:
+        _fit(W, "W", *said.w, dev)
     if Z is not None:
         _fit(Z, "Z", *said.z, dev)
     if gate is not None:

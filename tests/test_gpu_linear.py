@@ -371,3 +371,15 @@ def test_bf16_outputs_of_very_long_sums(N, K, M):
     wt = w.T.contiguous()
     cn.linear_backward(x, y, wt, cn.make_linear_shape(y, wt, x, dX=dx), dX=dx, want=())
     check(dx, ref, e + U16 * (ref + e), "dX")
+
+
+def test_gradients_of_one_operand_without_the_other():
+    t = make(2, 150, 96, 200)
+    z = padded((2, 150, 200), torch.bfloat16, torch.Generator(device="cuda").manual_seed(1), extra=1)
+    full = backward(t, z, cn.ACT_SILU)
+    dx, dw = torch.empty_like(t["x"]), torch.empty_like(t["w"])
+    s = cn.make_linear_shape(t["x"], t["w"], t["dy"], Z=z, gate=t["gate"], dX=dx, dW=dw, activation=cn.ACT_SILU)
+    assert torch.equal(cn.linear_backward(t["dy"], None, t["w"], s, Z=z, gate=t["gate"], dX=dx).dX, full.dX)
+    assert torch.equal(cn.linear_backward(t["dy"], t["x"], None, s, Z=z, gate=t["gate"], dW=dw).dW, full.dW)
+    g = cn.linear_backward(t["dy"], None, None, s, Z=z, gate=t["gate"])
+    assert g.dX is None and g.dW is None and torch.equal(g.dbias, full.dbias) and torch.equal(g.dgate, full.dgate)

@@ -336,3 +336,16 @@ def test_a_norm_may_have_a_bias_only(library):
         assert g.dbias.shape == (64,) and g.dweight is None
         assert cn.layer_norm_backward(x, x, stat, stat, s, bias=bias, want=()).dbias is None
     assert cn.make_norm_shape(x, x, torch.empty(64, dtype=torch.bfloat16, device=DEVICE)).weight_dtype == cn.DTYPE_BF16
+
+
+def test_gradients_want_only_what_they_read(library):
+    x, w, y = (torch.empty(n, dtype=torch.bfloat16, device=DEVICE) for n in ((1, 4, 64), (40, 64), (1, 4, 40)))
+    s = cn.make_linear_shape(x, w, y, Z=y, dX=x, dW=w)
+    cn.linear_backward(y, None, w, s, Z=y, dX=x)
+    cn.linear_backward(y, x, None, s, Z=y, dW=w)
+    cn.linear_backward(y, None, None, s, Z=y)
+    calls = len(library.records)
+    for bad in (lambda: cn.linear_backward(y, None, w, s, Z=y, dW=w), lambda: cn.linear_backward(y, x, None, s, Z=y, dX=x)):
+        with pytest.raises(ValueError):
+            bad()
+    assert len(library.records) == calls
