@@ -383,3 +383,43 @@ def test_gradients_of_one_operand_without_the_other():
     assert torch.equal(cn.linear_backward(t["dy"], t["x"], None, s, Z=z, gate=t["gate"], dW=dw).dW, full.dW)
     g = cn.linear_backward(t["dy"], None, None, s, Z=z, gate=t["gate"])
     assert g.dX is None and g.dW is None and torch.equal(g.dbias, full.dbias) and torch.equal(g.dgate, full.dgate)
+
+
+# B, rows, in, out, type of y: sums in runs in tiles of 256 columns and of fewer, of one pair and shared by two and four, for either type; sums that are shared but
+# need no runs.  Odd widths leave columns behind the last whole sector.
+RUNS = [(2, 2000, 2570, 2050, "f32"), (2, 1501, 5200, 1000, "f32"), (2, 1000, 5200, 1000, "f32"), (2, 700, 5200, 517, "f32"), (2, 40, 12000, 1000, "f32"),
+        (2, 900, 70001, 1100, "bf16"), (2, 40, 280001, 72, "bf16"), (2, 300, 2600, 300, "f32"), (2, 300, 2600, 300, "bf16"), (3, 33, 9001, 517, "f32")]
+
+
+@pytest.mark.parametrize("B,N,K,M,y", RUNS)
+@pytest.mark.parametrize("extra", [0, 1])
+@pytest.mark.parametrize("act", [cn.ACT_NONE, cn.ACT_GELU_TANH, cn.ACT_SILU])
+def test_long_sums_with_everything_behind_them(B, N, K, M, y, extra, act):
+    """Bias, pre-activation, activation, the entry's gate and the residual behind sums that are taken up in runs or shared; padded batches and others.  The
+    bounds of linear_ref count a long accumulation, so the 2-norm is compared too: an output in bf16 is off by its rounding, one in fp32 by test_fp32_output_of_a_long_sum's bound."""
+    t = make(B, N, K, M, y, "f32", seed=K, extra=extra)
+    out, z = forward(t, act, extra=extra)
+    check_forward(t, act, out, z)
+    ry, rz, _, _ = linear_ref(t["x"], t["w"], t["bias"], t["gate"], t["residual"], act)
+    assert (z.double() - rz).norm() <= U16 * rz.norm()
+    # gate and slope make no more of the sum's error than themselves; the activation's own errors are ACT_ERR of 1 + |z|
+    g = t["gate"].double()[:, None]
+    bound = U16 * ry.norm() if y == "bf16" else 160 * 2 / 3 * 2.0 ** -24 * SLOPE_MOST * (g * rz).norm() + 2 * U32 * ry.norm() + (ACT_ERR * (g * (1 + rz.abs())).norm() if act else 0)
+    assert (out.double() - ry).norm() <= bound
+    stream = t["residual"]                     # onto the residual itself
+    s = cn.make_linear_shape(t["x"], t["w"], stream, residual=stream, bias=t["bias"], gate=t["gate"], activation=act)
+    cn.linear(t["x"], t["w"], s, bias=t["bias"], gate=t["gate"], residual=stream, Y=stream)
+    assert torch.equal(stream, out)
+
+
+@pytest.mark.parametrize("N,K,M,y", [(2000, 5200, 1000, "f32"), (64, 30720, 1536, "f32"), (40, 280001, 72, "bf16")])
+def test_long_sums_give_the_same_bits_again(N, K, M, y):
+    t = make(1, N, K, M, y, seed=1)
+    out, _ = forward(t, cn.ACT_GELU)
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            again, _ = forward(t, cn.ACT_GELU)
+        torch.cuda.current_stream().wait_stream(side)
+        assert torch.equal(again, out)
