@@ -123,14 +123,15 @@ __global__ void __launch_bounds__(32 * kRowsWarps) linear_rows_kernel(const Rows
 
 // Warps that share k: many where there are few CTAs, so that all of W is on its way at once (1536 x 1536, 96 CTAs: 16 warps 3.0 us, 8 4.5), few where
 // CTAs fill the SMs several times over (30720 x 5120, 1920 CTAs: 4 warps 49.0 us, 8 53.5, 16 82; 5120 x 5120, 320 CTAs: 8 warps 8.7 us, 4 14, 16 15).
+static_assert(kRowsWeights <= int64_t(2 * kLongRun * 8) * 16 * 148, "more than 8 rows: fewer than 16 warps share k only where it needs no runs");
 template <int NT>
 inline cudaError_t launch_rows_tiles(const RowsArgs& a, cudaStream_t stream) {
     const int grid = ceil_div(a.cols, 16);
     const int warps = grid <= 148 ? 16 : grid <= 3 * 148 ? 8 : 4;
-    const bool runs = a.K > 2 * kLongRun * warps;
+    const bool runs = a.K > 2 * kLongRun * warps;        // with two column tiles only where 16 warps share k: W is not large then
     auto kern = warps == 16 ? (runs ? linear_rows_kernel<NT, 16, true> : linear_rows_kernel<NT, 16, false>)
-              : warps == 8  ? (runs ? linear_rows_kernel<NT, 8, true> : linear_rows_kernel<NT, 8, false>)
-                            : (runs ? linear_rows_kernel<NT, 4, true> : linear_rows_kernel<NT, 4, false>);
+              : warps == 8  ? (runs ? linear_rows_kernel<1, 8, true> : linear_rows_kernel<NT, 8, false>)
+                            : (runs ? linear_rows_kernel<1, 4, true> : linear_rows_kernel<NT, 4, false>);
     return launch_dependent(kern, dim3(grid), dim3(32 * warps), 0, stream, a);
 }
 

@@ -423,3 +423,8 @@ def test_long_sums_give_the_same_bits_again(N, K, M, y):
             again, _ = forward(t, cn.ACT_GELU)
         torch.cuda.current_stream().wait_stream(side)
         assert torch.equal(again, out)
+
+
+@pytest.mark.parametrize("N", [8, 9, 16])
+def test_fp32_output_of_a_long_sum_of_two_column_tiles(N):
+    check_long_sum(N, 90001, 72)
