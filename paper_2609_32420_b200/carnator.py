@@ -583,14 +583,33 @@ def _linear_said(of: bytes) -> _Said:
     return said
 
 
-def _with_room(shape, stride: str, rows, row: str, dtype: str, device):
-    """An output with rows on 16-byte boundaries, and a copy of the record that has its strides: the caller's record stays as it is."""
+def _packed(s, stride: str, rows, features: int):
+    """The record with the strides of an output that the call makes (rows on 16-byte boundaries) as ``stride``, and that output's size."""
+    size = (*rows, -(-features // 8) * 8)
+    steps = getattr(s, stride)
+    for i in range(len(steps)):
+        steps[i] = math.prod(size[i + 1:])
+    return bytes(s), size
+
+
+@functools.lru_cache(maxsize=1024)
+def _norm_packed(of: bytes, stride: str):
+    s = NormShape.from_buffer_copy(of)
+    of, size = _packed(s, stride, (s.B, s.H, s.N), s.C)
+    return _norm_said(of), size, s.C
+
+
+@functools.lru_cache(maxsize=1024)
+def _linear_packed(of: bytes):
+    s = LinearShape.from_buffer_copy(of)
+    of, size = _packed(s, "y_stride", (s.B, s.N), s.out_features)
+    return _linear_said(of), size, s.out_features
+
+
+def _room(size, features: int, dtype, device):
     import torch
-    of = type(shape).from_buffer_copy(shape)
-    n = getattr(of, row)
-    t = torch.empty((*(getattr(of, r) for r in rows), -(-n // 8) * 8), dtype=_dtype_of(getattr(of, dtype)), device=device)[..., :n]
-    setattr(of, stride, _rows_of(getattr(of, stride), t))
-    return of, t
+    t = torch.empty(size, dtype=dtype, device=device)
+    return t if size[-1] == features else t[..., :features]
 
 
 def _rows_of(stride, *tensors):
@@ -631,9 +650,11 @@ def make_norm_shape(X, Y, weight=None, scale=None, shift=None, dX=None, eps: flo
 def layer_norm(X, shape: NormShape, weight=None, bias=None, shift=None, scale=None, Y=None, mean=None, rstd=None, stream=None):
     """carnator_layer_norm.  Returns Y [B,H,N,C] (its own, with rows on 16-byte boundaries, unless given); mean and rstd fp32 [B,H,N] (contiguous) are written if given."""
     dev = X.device
-    if Y is None:
-        shape, Y = _with_room(shape, "y_stride", ("B", "H", "N"), "C", "y_dtype", dev)
-    said = _norm_said(bytes(shape))
+    if Y is None:                        # the caller's record stays as it is
+        said, size, n = _norm_packed(bytes(shape), "y_stride")
+        Y = _room(size, n, said.y[0], dev)
+    else:
+        said = _norm_said(bytes(shape))
     on = _stream_on(dev, stream)
     _fit(X, "X", *said.x, dev)
     _fit(Y, "Y", *said.y, dev)
@@ -675,8 +696,10 @@ def layer_norm_backward(dY, X, mean, rstd, shape: NormShape, weight=None, bias=N
     import torch
     dev = X.device
     if dX is None:
-        shape, dX = _with_room(shape, "dx_stride", ("B", "H", "N"), "C", "x_dtype", dev)
-    said = _norm_said(bytes(shape))
+        said, size, n = _norm_packed(bytes(shape), "dx_stride")
+        dX = _room(size, n, said.dx[0], dev)
+    else:
+        said = _norm_said(bytes(shape))
     on = _stream_on(dev, stream)
     _fit(dY, "dY", *said.dy, dev)
     _fit(X, "X", *said.x, dev)
@@ -744,8 +767,10 @@ def linear(X, W, shape: LinearShape, bias=None, gate=None, residual=None, Y=None
     """carnator_linear.  Returns (Y [B,N,out_features] (as in layer_norm), ws); Z (bf16, the pre-activation) is written if given."""
     dev = X.device
     if Y is None:
-        shape, Y = _with_room(shape, "y_stride", ("B", "N"), "out_features", "y_dtype", dev)
-    said = _linear_said(bytes(shape))
+        said, size, n = _linear_packed(bytes(shape))
+        Y = _room(size, n, said.y[0], dev)
+    else:
+        said = _linear_said(bytes(shape))
     on = _stream_on(dev, stream)
     _fit(X, "X", *said.x, dev)
     _fit(W, "W", *said.w, dev)
