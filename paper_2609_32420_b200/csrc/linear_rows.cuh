@@ -27,7 +27,11 @@ struct RowsArgs {
 };
 
 __device__ __forceinline__ uint4 load_k8(const __nv_bfloat16* row, int k, int K) {
-    if (k + 8 <= K) return __ldg(reinterpret_cast<const uint4*>(row + k));
+    if (k + 8 <= K) {                    // not through the read-only path: the kernel ahead may write it while this one is resident
+        uint4 v;
+        asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(row + k));
+        return v;
+    }
     uint32_t t[4] = {0, 0, 0, 0};        // the last k of a row: what lies behind them is not the row's
 #pragma unroll
     for (int i = 0; i < 8; ++i)
