@@ -59,7 +59,6 @@ struct TcArgs {
     int k_len;                           // k of a batch entry
     int a_slabs, b_slabs;                // MN-major: whole 64-column slabs of the operand, which a tile fetches in one copy where all of its slabs are whole
     int stages, splits;
-    int run;                             // kLong: most stages of k that one accumulator sums up
     int clears;                          // the first product of a call clears its status word
 };
 
@@ -329,13 +328,52 @@ __device__ __forceinline__ void tile_at(const TcArgs& a, int t, int& b, int& m, 
     m = mt - b * a.tiles_m;
 }
 
+// Every CTA of the cluster finishes a run of the columns: the partial tiles of the same rows, added in the order of k.  By `step` threads from `from`, whole warps;
+// the other warps of the cluster meet them at its barrier, ahead of which is worked out what does not depend on the shares.
+__device__ __forceinline__ void join_shares(const TcArgs& a, uint32_t base, int first, uint32_t split, uint32_t half, const volatile int* abortp, int from, int step) {
+    int b, m, n;
+    tile_at(a, first, b, m, n);
+    const uint32_t pitch = uint32_t(a.bn + 4) * 4u;
+    const int share = a.bn / a.splits, groups = share / 8, c0 = int(split) * share;
+    __syncwarp();
+    cluster_sync();
+    if (*abortp) return;
+    for (int i = from; i < 128 * groups; i += step) {
+        const int r = i / groups, c = c0 + (i - r * groups) * 8;
+        const int row = m * kTileM + int(half) * 128 + r, col = n * a.bn + c, cn = min(max(a.cols - col, 0), 8);
+        if (row >= a.rows || cn == 0) continue;
+        norm::Raw8<true> res;
+        if (a.e.residual) load_residual(a.e, b, row, col, cn, res);
+        Columns cols;
+        columns_begin(a.e, cols, col, cn);
+        // all of the cluster's shares on their way before the first is added
+        float g[4][8];
+#pragma unroll
+        for (int sp = 0; sp < 4; ++sp)
+            if (sp < a.splits) {
+                const uint32_t src = map_cta(base + uint32_t(r) * pitch + uint32_t(c) * 4u, uint32_t(2 * sp) + half);
+#pragma unroll
+                for (int q = 0; q < 2; ++q)
+                    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(g[sp][4 * q]), "=f"(g[sp][4 * q + 1]), "=f"(g[sp][4 * q + 2]),
+                                 "=f"(g[sp][4 * q + 3]) : "r"(src + 16u * q) : "memory");
+            } else {
+#pragma unroll
+                for (int q = 0; q < 8; ++q) g[sp][q] = 0.f;
+            }
+        float f[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) f[q] = ((g[0][q] + g[1][q]) + g[2][q]) + g[3][q];
+        finish(a.e, cols, b, row, col, cn, f, res);
+    }
+}
+
 constexpr int kLongRun = 2560;           // most k that one accumulator sums up for an fp32 output,
 constexpr int kLongRunBf16 = 65536;      // and for a bf16 one
 
 // kSub: slabs of 64 columns of k per stage.
 // kLong: k is longer than one accumulator may sum up; 1: an fp32 output, a pair has all of k, 3: pairs share it, 2: a bf16 output, either.  The tensor cores cut
 // their sums off instead of rounding them, up to 2^-28 of the sum per product: a sum of 5120 products loses 5.6e-6 of itself, eight times what fp32 additions in a
-// row do, and one of a million of the same sign (the rows of a weight's gradient) 2 to 4e-3, as much as the rounding to bf16.  Here an accumulator sums up a.run
+// row do, and one of a million of the same sign (the rows of a weight's gradient) 2 to 4e-3, as much as the rounding to bf16.  Here an accumulator sums up kRun
 // stages of k at most, and the epilogue adds what it held to registers of its own, under the next run: 128 per thread, for which the service
 // warps give most of theirs.  Pairs that share k do the same with their shares before they are joined (512 x 8960 x 2048 onto fp32, shares of 4480: 22.9 us,
 // 21.8 in one run; 64 x 30720 x 1536, shares of 7680: 32.8 both ways, error 8.5e-6 in one run).  75600 x 5120 x 5120 onto a residual stream: error 1.6e-6
@@ -347,6 +385,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
     constexpr int kTileK = kSub * kSlab;                 // k of a stage
     constexpr uint32_t kABytes = 128 * kTileK * 2;       // a CTA's share of A per stage
     constexpr bool kF32 = kLong & 1, kShared = kLong != 1;               // pairs may share k
+    constexpr int kRun = (kF32 ? kLongRun : kLongRunBf16) / kTileK;      // kLong: most stages of k that one accumulator sums up
     extern __shared__ unsigned char lin_smem[];
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
@@ -394,42 +433,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
     const int k_all = a.k_batches * a.k_tiles;
     const int k0 = int(int64_t(k_all) * split / a.splits), k1 = int(int64_t(k_all) * (split + 1) / a.splits);
     // kLong: runs of k with an accumulator each
-    const int chunks = kLong ? (k1 - k0 + a.run - 1) / a.run : 1, chunk = (k1 - k0 + chunks - 1) / chunks;
-
-    // Every CTA of the cluster finishes a run of the columns: the partial tiles of the same rows, added in the order of k.  By `step` threads from `from`.
-    auto join = [&](int from, int step) {
-        int b, m, n;
-        tile_at(a, first, b, m, n);
-        const uint32_t pitch = uint32_t(a.bn + 4) * 4u;
-        const int share = a.bn / a.splits, groups = share / 8, c0 = int(split) * share;
-        for (int i = from; i < 128 * groups; i += step) {
-            const int r = i / groups, c = c0 + (i - r * groups) * 8;
-            const int row = m * kTileM + int(half) * 128 + r, col = n * a.bn + c, cn = min(max(a.cols - col, 0), 8);
-            if (row >= a.rows || cn == 0) continue;
-            norm::Raw8<true> res;
-            if (a.e.residual) load_residual(a.e, b, row, col, cn, res);
-            Columns cols;
-            columns_begin(a.e, cols, col, cn);
-            // all of the cluster's shares on their way before the first is added
-            float g[4][8];
-#pragma unroll
-            for (int sp = 0; sp < 4; ++sp)
-                if (sp < a.splits) {
-                    const uint32_t src = map_cta(base + uint32_t(r) * pitch + uint32_t(c) * 4u, uint32_t(2 * sp) + half);
-#pragma unroll
-                    for (int q = 0; q < 2; ++q)
-                        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(g[sp][4 * q]), "=f"(g[sp][4 * q + 1]), "=f"(g[sp][4 * q + 2]),
-                                     "=f"(g[sp][4 * q + 3]) : "r"(src + 16u * q) : "memory");
-                } else {
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) g[sp][q] = 0.f;
-                }
-            float f[8];
-#pragma unroll
-            for (int q = 0; q < 8; ++q) f[q] = ((g[0][q] + g[1][q]) + g[2][q]) + g[3][q];
-            finish(a.e, cols, b, row, col, cn, f, res);
-        }
-    };
+    const int chunks = kLong ? (k1 - k0 + kRun - 1) / kRun : 1, chunk = (k1 - k0 + chunks - 1) / chunks;
 
     if (warp < 4) {                      // ---- service warps
     // 128 x 40 + 256 x 208 registers; the block is launched with 384 x 152 at least (checked by the host)
@@ -638,9 +642,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
             }
             if (kShared && a.splits > 1) {
                 tc_fence_before();
-                __syncwarp();
-                cluster_sync();
-                if (!*abortp) join(tid - 128, 32 * kEpiWarps);
+                join_shares(a, base, first, split, half, abortp, tid - 128, 32 * kEpiWarps);
             }
         } else if (a.splits == 1) {
             for (int t = first; t < a.tiles && ok; t += step, ++i) {
@@ -726,11 +728,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
         }
     }
 
-    if (!kLong && a.splits > 1) {
-        __syncwarp();
-        cluster_sync();
-        if (!*abortp) join(tid, kThreadsTc);
-    }
+    if (!kLong && a.splits > 1) join_shares(a, base, first, split, half, abortp, tid, kThreadsTc);
     tc_fence_before();
     __syncwarp();
     cluster_sync();                      // nothing of the cluster reads this CTA's memory or arrives on its barriers any more
@@ -803,7 +801,6 @@ inline carnator_status launch_tc_stages(const Operand& A, const Operand& B, TcAr
     const uint32_t stage = 128 * kTileK * 2 + uint32_t(a.bn / 2) * kTileK * 2;
     a.k_tiles = ceil_div(a.k_len, kTileK);
     a.stages = int(std::min<uint32_t>(kMaxStages, kRingBytes / stage));
-    a.run = (kLong & 1 ? kLongRun : kLongRunBf16) / kTileK;
     a.a_slabs = AMN ? int(A.cols / kSlab) : 0;
     a.b_slabs = BMN ? int(B.cols / kSlab) : 0;
     auto map = [](CUtensorMap* m, const Operand& o, int rows) { return make_map_3d(m, o.base, o.batches, o.rows, o.cols, o.batch_stride, o.row_stride, rows); };
