@@ -327,7 +327,8 @@ carnator_status carnator_seed_expansion(const void* Q, const void* K, const floa
  *          Y may be X and dX may be X or dY (same type and strides).
  *   weight, bias   device, [C] of weight_dtype, or NULL (1, 0);  shift, scale  device, [B,C] of mod_dtype with the batch
  *          strides of `shape`, or NULL (0).  These are aligned to their type only.
- *   mean, rstd     device, fp32 [B,H,N] contiguous; written by the forward call if given, read by the backward call
+ *   mean, rstd     device, fp32 [B,H,N] contiguous; written by the forward call if given, read by the backward call.  A row with a
+ *          NaN or an infinity: rstd and y are NaN, mean is what the channels sum up to
  * carnator_layer_norm_backward: with a = weight (1 + scale_b), g = dy a:
  *   dX = rstd (g - mean(g) - xh mean(g xh));  dweight = sum (1 + scale_b) dy xh,  dbias = sum (1 + scale_b) dy, over all rows;
  *   dscale_b = sum dy (xh weight + bias),  dshift_b = sum dy, over the rows of entry b
@@ -363,10 +364,11 @@ carnator_status carnator_layer_norm_backward(const void* dY, const void* X, cons
  *   residual   device, of y_dtype, [B,N,out_features], or NULL (0); may be Y (same strides)
  *   Y      device, of y_dtype;  Z  device, bf16, or NULL: the pre-activation, which the backward call wants
  *   ws     device workspace, 256-byte aligned, >= carnator_linear_workspace_bytes (the status header)
- * Strides are multiples of 16 bytes, base pointers 16-byte aligned, features contiguous; bias and gate are aligned to
- * their type only.  Any in_features and out_features: a row's features need not fill its stride, and nothing outside
+ * Strides are multiples of 16 bytes (and not 0, but for axes of one entry), base pointers 16-byte aligned, features contiguous; bias
+ * and gate are aligned to their type only; outputs overlap no input but, Y, the residual.  Any in_features and out_features: a row's features need not fill its stride, and nothing outside
  * them is read or written.  The products are bf16 x bf16 with fp32 sums; bias, activation, gate and residual are applied
- * to the unrounded sum and y is rounded once.
+ * to the unrounded sum and y is rounded once.  Exponentials and reciprocals are the approximate instructions: an activation is off by at
+ * most (4 u + 64) 2^-24 of itself, u the exponential's argument (z^2 / 2, |z|, 1.6 |z| (1 + 0.045 z^2)), its slope by 2^-19 (|z| + 1).
  * carnator_linear_backward:  dz = dy gate_b act'(z);
  *   dX = dz W,  dW = dz^T x  (bf16, dz rounded to bf16 as their operand);
  *   dbias = sum of dz over all rows,  dgate_b = sum of dy act(z) over the rows of entry b  (fp32, from unrounded terms).

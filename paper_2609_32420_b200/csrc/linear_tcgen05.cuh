@@ -372,8 +372,8 @@ constexpr int kLongRunBf16 = 65536;      // and for a bf16 one
 
 // kSub: slabs of 64 columns of k per stage.
 // kLong: k is longer than one accumulator may sum up; 1: an fp32 output, a pair has all of k, 3: pairs share it, 2: a bf16 output, either.  The tensor cores cut
-// their sums off instead of rounding them, up to 2^-28 of the sum per product: a sum of 5120 products loses 5.6e-6 of itself, eight times what fp32 additions in a
-// row do, and one of a million of the same sign (the rows of a weight's gradient) 2 to 4e-3, as much as the rounding to bf16.  Here an accumulator sums up kRun
+// their sums off instead of rounding them: a sum of 5120 products loses 5.6e-6 of itself, eight times what fp32 additions in a row do, and one of 524288 of the
+// same sign (the rows of a weight's gradient) 3.8e-3, as much as the rounding to bf16; in runs 2.6e-5.  Here an accumulator sums up kRun
 // stages of k at most, and the epilogue adds what it held to registers of its own, under the next run: 128 per thread, for which the service
 // warps give most of theirs.  Pairs that share k do the same with their shares before they are joined (512 x 8960 x 2048 onto fp32, shares of 4480: 22.9 us,
 // 21.8 in one run; 64 x 30720 x 1536, shares of 7680: 32.8 both ways, error 8.5e-6 in one run).  75600 x 5120 x 5120 onto a residual stream: error 1.6e-6
