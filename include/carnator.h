@@ -259,7 +259,7 @@ carnator_status carnator_build_connectivity_host(const void* Q, const void* K,
  *   active_q uint8 [B,nqb], context_k uint8 [B,nkb], both required.
  * All pointers are device pointers.
  * ------------------------------------------------------------------------ */
-enum { CARNATOR_DTYPE_F32 = 0, CARNATOR_DTYPE_BF16 = 1 };
+enum { CARNATOR_DTYPE_F32 = 0, CARNATOR_DTYPE_BF16 = 1, CARNATOR_DTYPE_E4M3 = 2 /* 8-bit products only */ };
 
 size_t carnator_regions_workspace_bytes(const carnator_shape* shape);
 
@@ -410,6 +410,100 @@ carnator_status carnator_linear_backward(const void* dY, const void* X, const vo
                                          const carnator_linear_shape* shape, void* dX_opt, void* dW_opt,
                                          float* dbias_opt, float* dgate_opt,
                                          void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Rotary positions: what turns Q and K between their norm and the attention.
+ *
+ * The first 2 * (pairs[0] + pairs[1] + pairs[2]) channels of a head are pairs (u, v); pair i turns with the position of its token on axis 0, 1 or 2 (the first
+ * pairs[0] pairs with axis 0, the next pairs[1] with axis 1, ..):  th = position * freq[i],
+ *   (u, v) -> amplitude (u cos th - v sin th, u sin th + v cos th).       The other channels are copied.
+ *   X, Y   device, of x_dtype, [B,H,N,D] with the strides of `shape`; Y may be X (same strides).  Q and K of a fused projection's output are one tensor of 2 H heads
+ *   freq   device, fp64 [pairs]: radians per position; carnator_rope_frequencies computes them
+ *   positions  device, int32 [B,N,axes] with the strides of `shape` and the axes contiguous (axes = 1 .. 3: those that have pairs), or NULL: the token order of the
+ *          other calls, n_text text tokens, which do not turn, then the grid T x Hg x Wg, whose token (t, row, column) has these positions.  A plain sequence is
+ *          T = N, Hg = Wg = 1 with all pairs on axis 0.  offset is added to the position on each axis
+ *   layout CARNATOR_ROPE_INTERLEAVED: pair i is channels 2i and 2i + 1;  CARNATOR_ROPE_HALF: channels i and i + pairs
+ *   inverse  non-zero: th -> -th, which takes the gradient of Y to that of X
+ * Angles are taken in 64 bits at any position; sine and cosine are good to about 2^-22; the turn is computed in fp32 and rounded once.
+ * Strides are multiples of 16 bytes, base pointers 16-byte aligned; inputs may have a stride of 0.  Limits: D <= 256, N <= 2^27, B <= 65535, H <= 65535.
+ *
+ * carnator_rope_frequencies (HOST, no GPU work) fills freq (HOST, room for the pairs) with theta^(-i / pairs[a]) for pair i of axis a, changed for clips or
+ * sequences longer than the model was trained on, by axis (factor >= 1; original: trained length of the axis, RAMP only):
+ *   CARNATOR_ROPE_SCALE_LINEAR  f / factor
+ *   CARNATOR_ROPE_SCALE_BASE    theta taken times factor^(d / (d - 2)), d = 2 pairs[a] (a single pair: as it is)
+ *   CARNATOR_ROPE_SCALE_RAMP    f (g + (1 - g) / factor), g = (original f / 2 pi - low) / (high - low) clamped to [0, 1]: pairs that turn over `high` times in
+ *                               the trained length stay, those under `low` times are slowed down.  amplitude_opt receives 0.1 ln(largest factor) + 1, otherwise 1
+ * ------------------------------------------------------------------------ */
+enum { CARNATOR_ROPE_INTERLEAVED = 0, CARNATOR_ROPE_HALF = 1 };
+enum { CARNATOR_ROPE_SCALE_NONE = 0, CARNATOR_ROPE_SCALE_LINEAR = 1, CARNATOR_ROPE_SCALE_BASE = 2, CARNATOR_ROPE_SCALE_RAMP = 3 };
+
+typedef struct carnator_rope_shape {
+    int32_t B, H, N, D;
+    int32_t n_text, T, Hg, Wg;              /* n_text + T*Hg*Wg == N unless positions are given */
+    int32_t pairs[3];                       /* of channels, per axis */
+    int32_t offset[3];
+    int64_t x_stride[3], y_stride[3];       /* element strides of (batch, head, token) */
+    int64_t pos_stride[2];                  /* of (batch, token); batch 0: the same for all entries */
+    int32_t axes;                           /* of positions */
+    int32_t layout, inverse, x_dtype;       /* x_dtype is also Y's */
+    float   amplitude;
+} carnator_rope_shape;
+
+typedef struct carnator_rope_scaling {
+    int32_t pairs[3];
+    int32_t mode;                           /* CARNATOR_ROPE_SCALE_* */
+    double  theta;                          /* > 1 */
+    double  factor[3], original[3];
+    double  low, high;                      /* RAMP: 0 <= low < high */
+} carnator_rope_scaling;
+
+carnator_status carnator_rope_frequencies(const carnator_rope_scaling* scaling, double* freq, double* amplitude_opt);
+
+carnator_status carnator_rope(const void* X, const double* freq, const int32_t* positions, const carnator_rope_shape* shape, void* Y, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Projections with 8-bit operands (serving): e4m3 values with one fp32 scale per block of 128 in_features.
+ *
+ * carnator_quantize_fp8, for every row of X [B,N,K] (block_rows = 1: activations) or every 128 rows (block_rows = 128: a weight, B = 1) and every 128 of K:
+ *   scale = the smallest power of two with amax <= 448 scale (amax the block's largest magnitude, 2^-100 at least),   q = e4m3(x / scale), to nearest, ties to even
+ *   A block that holds an infinity or a NaN gets the scale NaN and values NaN.
+ *   X      device, of x_dtype (F32, BF16);  Q  device, e4m3 (1 byte), [B,N,K];  scale  device, fp32, [B, N or ceil(N / 128), ceil(K / 128)]
+ *   Strides of X and Q are multiples of 16 bytes, those of scale (batch, row or block of rows, block) are any that keep its values apart.
+ * carnator_linear_fp8, for every row (b, n):
+ *   z = sum_j x_scale[b,n,j] w_scale[m / 128, j] sum_{k in block j} x[b,n,k] W[m,k] + bias,   y = residual + gate_b act(z)
+ *   X      device, [B,N,in_features]: e4m3 with x_scale, or F32 / BF16 and x_scale NULL: the call takes it to 8 bits as carnator_quantize_fp8 does
+ *   W      device, e4m3 [out_features,in_features] with row stride w_stride;  w_scale  device, fp32 [ceil(out_features / 128), ceil(in_features / 128)]
+ *   x_scale, w_scale   any fp32 numbers (powers of two or not), strides of `shape`
+ *   bias, gate, residual, Y, ws   as in carnator_linear (ws >= carnator_linear_fp8_workspace_bytes: the status header and, where the call quantises X, room for it)
+ * The products of a block of 128 are summed up by the tensor cores, whose accumulators lose nothing of them worth naming (measured: none); scales and the sums over the
+ * blocks are fp32; bias, activation, gate and residual are applied to the unrounded sum and y is rounded once.  Up to 16 rows in all run on a kernel that streams W once
+ * through mma.sync; more rows on tcgen05 with bounded waits, whose status carnator_query_status(ws) returns.
+ * Limits: those of carnator_linear.
+ * ------------------------------------------------------------------------ */
+typedef struct carnator_quantize_shape {
+    int32_t B, N, K, block_rows;            /* block_rows: 1 or 128 */
+    int64_t x_stride[2], q_stride[2];       /* element strides of (batch, row) */
+    int64_t scale_stride[3];                /* of (batch, row or block of rows, block of K) */
+    int32_t x_dtype;
+} carnator_quantize_shape;
+
+carnator_status carnator_quantize_fp8(const void* X, const carnator_quantize_shape* shape, void* Q, float* scale, void* stream);
+
+typedef struct carnator_linear_fp8_shape {
+    int32_t B, N, in_features, out_features;
+    int64_t x_stride[2], y_stride[2], residual_stride[2];       /* element strides of (batch, token) */
+    int64_t x_scale_stride[3];              /* of (batch, token, block); e4m3 X only */
+    int64_t w_stride, w_scale_stride[2];    /* row; (block of out_features, block of in_features) */
+    int64_t gate_stride;                    /* batch stride; 0: one row for all entries */
+    int32_t activation;                     /* CARNATOR_ACT_* */
+    int32_t x_dtype;                        /* CARNATOR_DTYPE_F32, _BF16 or _E4M3 */
+    int32_t y_dtype, bias_dtype, gate_dtype;       /* y_dtype is also the residual's */
+} carnator_linear_fp8_shape;
+
+size_t carnator_linear_fp8_workspace_bytes(const carnator_linear_fp8_shape* shape);
+
+carnator_status carnator_linear_fp8(const void* X, const float* x_scale, const void* W, const float* w_scale, const void* bias, const void* gate, const void* residual,
+                                    const carnator_linear_fp8_shape* shape, void* Y, void* ws, size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
  * Host-side scalars of the reuse-validity gate and of its offline risk certificate.  No GPU work; all

@@ -34,6 +34,8 @@ EXPORTS = [
     "carnator_seed_workspace_bytes", "carnator_seed_expansion",
     "carnator_layer_norm", "carnator_layer_norm_backward_workspace_bytes", "carnator_layer_norm_backward",
     "carnator_linear_workspace_bytes", "carnator_linear", "carnator_linear_backward_workspace_bytes", "carnator_linear_backward",
+    "carnator_rope_frequencies", "carnator_rope",
+    "carnator_quantize_fp8", "carnator_linear_fp8_workspace_bytes", "carnator_linear_fp8",
     "carnator_delta_e00", "carnator_context_discrepancy", "carnator_size_discrepancy", "carnator_shape_discrepancy",
     "carnator_compatibility_gate", "carnator_clopper_pearson_upper",
     "carnator_query_status", "carnator_selftest_wait_timeout", "carnator_debug_set_builder_path", "carnator_status_string", "carnator_last_cuda_error",
@@ -90,6 +92,47 @@ class LinearShape(ctypes.Structure):
         ("residual_stride", ctypes.c_int64 * 2), ("z_stride", ctypes.c_int64 * 2), ("dx_stride", ctypes.c_int64 * 2),
         ("w_stride", ctypes.c_int64), ("dw_stride", ctypes.c_int64), ("gate_stride", ctypes.c_int64),
         ("activation", ctypes.c_int32),
+        ("y_dtype", ctypes.c_int32), ("bias_dtype", ctypes.c_int32), ("gate_dtype", ctypes.c_int32),
+    ]
+
+
+class RopeShape(ctypes.Structure):
+    """Mirror of carnator_rope_shape."""
+    _fields_ = [
+        ("B", ctypes.c_int32), ("H", ctypes.c_int32), ("N", ctypes.c_int32), ("D", ctypes.c_int32),
+        ("n_text", ctypes.c_int32), ("T", ctypes.c_int32), ("Hg", ctypes.c_int32), ("Wg", ctypes.c_int32),
+        ("pairs", ctypes.c_int32 * 3), ("offset", ctypes.c_int32 * 3),
+        ("x_stride", ctypes.c_int64 * 3), ("y_stride", ctypes.c_int64 * 3), ("pos_stride", ctypes.c_int64 * 2),
+        ("axes", ctypes.c_int32), ("layout", ctypes.c_int32), ("inverse", ctypes.c_int32), ("x_dtype", ctypes.c_int32),
+        ("amplitude", ctypes.c_float),
+    ]
+
+
+class RopeScaling(ctypes.Structure):
+    """Mirror of carnator_rope_scaling."""
+    _fields_ = [
+        ("pairs", ctypes.c_int32 * 3), ("mode", ctypes.c_int32), ("theta", ctypes.c_double),
+        ("factor", ctypes.c_double * 3), ("original", ctypes.c_double * 3), ("low", ctypes.c_double), ("high", ctypes.c_double),
+    ]
+
+
+class QuantizeShape(ctypes.Structure):
+    """Mirror of carnator_quantize_shape."""
+    _fields_ = [
+        ("B", ctypes.c_int32), ("N", ctypes.c_int32), ("K", ctypes.c_int32), ("block_rows", ctypes.c_int32),
+        ("x_stride", ctypes.c_int64 * 2), ("q_stride", ctypes.c_int64 * 2), ("scale_stride", ctypes.c_int64 * 3),
+        ("x_dtype", ctypes.c_int32),
+    ]
+
+
+class LinearFp8Shape(ctypes.Structure):
+    """Mirror of carnator_linear_fp8_shape."""
+    _fields_ = [
+        ("B", ctypes.c_int32), ("N", ctypes.c_int32), ("in_features", ctypes.c_int32), ("out_features", ctypes.c_int32),
+        ("x_stride", ctypes.c_int64 * 2), ("y_stride", ctypes.c_int64 * 2), ("residual_stride", ctypes.c_int64 * 2),
+        ("x_scale_stride", ctypes.c_int64 * 3), ("w_stride", ctypes.c_int64), ("w_scale_stride", ctypes.c_int64 * 2),
+        ("gate_stride", ctypes.c_int64),
+        ("activation", ctypes.c_int32), ("x_dtype", ctypes.c_int32),
         ("y_dtype", ctypes.c_int32), ("bias_dtype", ctypes.c_int32), ("gate_dtype", ctypes.c_int32),
     ]
 
@@ -179,6 +222,17 @@ def lib() -> ctypes.CDLL:
     L.carnator_linear_backward.restype = ctypes.c_int
     L.carnator_linear_backward.argtypes = [vp, vp, vp, vp, vp, pl, vp, vp, vp, vp, vp, sz, vp]
     dbl, pd = ctypes.c_double, ctypes.POINTER(ctypes.c_double)
+    L.carnator_rope_frequencies.restype = ctypes.c_int
+    L.carnator_rope_frequencies.argtypes = [ctypes.POINTER(RopeScaling), pd, pd]
+    L.carnator_rope.restype = ctypes.c_int
+    L.carnator_rope.argtypes = [vp, vp, vp, ctypes.POINTER(RopeShape), vp, vp]
+    L.carnator_quantize_fp8.restype = ctypes.c_int
+    L.carnator_quantize_fp8.argtypes = [vp, ctypes.POINTER(QuantizeShape), vp, vp, vp]
+    p8 = ctypes.POINTER(LinearFp8Shape)
+    L.carnator_linear_fp8_workspace_bytes.restype = sz
+    L.carnator_linear_fp8_workspace_bytes.argtypes = [p8]
+    L.carnator_linear_fp8.restype = ctypes.c_int
+    L.carnator_linear_fp8.argtypes = [vp, vp, vp, vp, vp, vp, vp, p8, vp, vp, sz, vp]
     L.carnator_delta_e00.restype = dbl
     L.carnator_delta_e00.argtypes = [pd, pd]
     L.carnator_context_discrepancy.restype = dbl
@@ -433,7 +487,7 @@ def static_status(stream=None) -> int:
     return int(lib().carnator_static_status(_stream(stream)))
 
 
-DTYPE_F32, DTYPE_BF16 = 0, 1
+DTYPE_F32, DTYPE_BF16, DTYPE_E4M3 = 0, 1, 2
 
 
 def build_regions(evidence, shape: Shape, r_active: int = 2, r_context: int = 3, stream=None):
@@ -514,7 +568,7 @@ def _dtype_code(t, what: str) -> int:
 
 def _dtype_of(code: int):
     import torch
-    return torch.float32 if code == DTYPE_F32 else torch.bfloat16
+    return torch.float32 if code == DTYPE_F32 else torch.bfloat16 if code == DTYPE_BF16 else torch.float8_e4m3fn
 
 
 def _fit(t, what: str, dtype, size, stride, device) -> None:
@@ -549,7 +603,8 @@ def _stream_on(device, stream):
 class _Said:
     """What a record says of the tensors of its call, (type, shape, strides) each, and a copy of it for the library.  Made for each content of a record
     and never changed afterwards, so that records may be copied, changed between calls and shared among threads."""
-    __slots__ = ("record", "ref", "x", "y", "dy", "dx", "residual", "z", "w", "dw", "vec", "shift", "scale", "gate", "bias", "stat")
+    __slots__ = ("record", "ref", "x", "y", "dy", "dx", "residual", "z", "w", "dw", "vec", "shift", "scale", "gate", "bias", "stat", "freq", "pos", "q",
+                 "x_scale", "w_scale")
 
     def __init__(self, record):
         self.record, self.ref = record, ctypes.byref(record)
@@ -840,6 +895,252 @@ def linear_backward(dY, X, W, shape: LinearShape, Z=None, gate=None, dX=None, dW
     if st != OK:
         _check(st, "carnator_linear_backward")
     return LinearGrads(dX, dW, dbias, dgate)
+
+
+# ---- rotary positions ---------------------------------------------------------------------------------
+ROPE_INTERLEAVED, ROPE_HALF = 0, 1
+ROPE_SCALE_NONE, ROPE_SCALE_LINEAR, ROPE_SCALE_BASE, ROPE_SCALE_RAMP = range(4)
+
+
+def _three(v, fill):
+    v = (v,) if isinstance(v, (int, float)) else tuple(v)
+    if not 1 <= len(v) <= 3:
+        raise ValueError("one to three axes")
+    return v + (fill,) * (3 - len(v))
+
+
+def rope_frequencies(pairs, theta: float = 10000.0, scaling: int = ROPE_SCALE_NONE, factor=1.0, original=0.0, low: float = 1.0, high: float = 32.0, device="cpu"):
+    """carnator_rope_frequencies.  pairs, factor and original: one number, or one per axis (of factor and original, one number stands for every axis).
+    Returns (float64 tensor of radians per position of every pair on ``device``, amplitude)."""
+    import torch
+    s = RopeScaling()
+    s.pairs[:] = _three(pairs, 0)
+    s.mode, s.theta, s.low, s.high = scaling, theta, low, high
+    s.factor[:] = (factor,) * 3 if isinstance(factor, (int, float)) else _three(factor, 1.0)
+    s.original[:] = (original,) * 3 if isinstance(original, (int, float)) else _three(original, 0.0)
+    n = sum(max(p, 0) for p in s.pairs)
+    freq, amplitude = (ctypes.c_double * max(n, 1))(), ctypes.c_double()
+    _check(lib().carnator_rope_frequencies(ctypes.byref(s), freq, ctypes.byref(amplitude)), "carnator_rope_frequencies")
+    return torch.tensor(list(freq)[:n], dtype=torch.float64, device=device), amplitude.value
+
+
+def make_rope_shape(X, Y, pairs, n_text: int = 0, grid=None, positions=None, offset=(0, 0, 0), layout: int = ROPE_INTERLEAVED, amplitude: float = 1.0,
+                    inverse: bool = False) -> RopeShape:
+    """Record of a turn of X [B,H,N,D] into Y (None: strides of X).  pairs: pairs of channels per axis.  grid: (T, Hg, Wg) of the tokens behind n_text text tokens
+    (default: one line); with positions [B or 1, N, axes] the tokens stand where it says instead.  Types and strides are taken from the tensors."""
+    for t, what in ((X, "X"), (Y, "Y")):
+        if t is not None and t.dim() != 4:
+            raise ValueError(f"{what} must be [B,H,N,D]")
+        _last_axis(t, what)
+    s = RopeShape()
+    s.B, s.H, s.N, s.D = X.shape
+    s.x_stride, s.y_stride = _rows_of(s.x_stride, X), _rows_of(s.y_stride, Y, X)
+    s.pairs[:], s.offset[:] = _three(pairs, 0), _three(offset, 0)
+    s.n_text = n_text
+    s.T, s.Hg, s.Wg = grid if grid is not None else (s.N - n_text, 1, 1)
+    if positions is not None:
+        if positions.dim() != 3 or not 1 <= positions.shape[2] <= 3 or (positions.shape[2] > 1 and positions.stride(2) != 1) or positions.shape[0] not in (1, s.B):
+            raise ValueError("positions must be [B or 1, N, 1 to 3] with the last axis contiguous")
+        s.axes = positions.shape[2]
+        s.pos_stride[:] = [0 if positions.shape[0] == 1 else positions.stride(0), positions.stride(1)]
+    s.layout, s.inverse, s.amplitude, s.x_dtype = layout, bool(inverse), amplitude, _dtype_code(X, "X")
+    return s
+
+
+@functools.lru_cache(maxsize=1024)
+def _rope_said(of: bytes) -> _Said:
+    import torch
+    s = RopeShape.from_buffer_copy(of)
+    said = _Said(s)
+    size, x = (s.B, s.H, s.N, s.D), _dtype_of(s.x_dtype)
+    said.x, said.y = (x, size, (*s.x_stride, 1)), (x, size, (*s.y_stride, 1))
+    said.freq = (torch.float64, (sum(s.pairs),), (1,))
+    shared = s.pos_stride[0] == 0
+    said.pos = (torch.int32, (1 if shared else s.B, s.N, s.axes), (*s.pos_stride, 1))
+    return said
+
+
+@functools.lru_cache(maxsize=1024)
+def _rope_packed(of: bytes):
+    s = RopeShape.from_buffer_copy(of)
+    of, size = _packed(s, "y_stride", (s.B, s.H, s.N), s.D)
+    return _rope_said(of), size, s.D
+
+
+def rope(X, freq, shape: RopeShape, positions=None, Y=None, stream=None):
+    """carnator_rope.  freq: float64, from rope_frequencies.  Returns Y [B,H,N,D] (its own, with rows on 16-byte boundaries, unless given; may be X)."""
+    dev = X.device
+    if Y is None:
+        said, size, n = _rope_packed(bytes(shape))
+        Y = _room(size, n, said.y[0], dev)
+    else:
+        said = _rope_said(bytes(shape))
+    on = _stream_on(dev, stream)
+    _fit(X, "X", *said.x, dev)
+    _fit(Y, "Y", *said.y, dev)
+    _fit(freq, "freq", *said.freq, dev)
+    if positions is not None:
+        if said.pos[1][0] == 1 and positions.shape[0] == said.record.B and positions.stride(0) == 0:
+            positions = positions[:1]              # one tensor seen by every entry
+        _fit(positions, "positions", *said.pos, dev)
+    st = lib().carnator_rope(_ptr(X), _ptr(freq), _ptr(positions), said.ref, _ptr(Y), on)
+    if st != OK:
+        _check(st, "carnator_rope")
+    return Y
+
+
+# ---- 8-bit operands and their product ---------------------------------------------------------------------
+FP8_BLOCK = 128                # in_features (and out_features of a weight) that share a scale
+
+
+def _x_code(t, what: str) -> int:
+    import torch
+    return DTYPE_E4M3 if t.dtype == torch.float8_e4m3fn else _dtype_code(t, what)
+
+
+def make_quantize_shape(X, Q, scale, block_rows: int = 1) -> QuantizeShape:
+    """Record of X [B,N,K] taken to e4m3 Q [B,N,K] with scale fp32 [B, N or ceil(N/128), ceil(K/128)]; block_rows 1 (activations) or 128 (a weight).
+    Q and scale may be None: rows on 16-byte boundaries; scales of neighbouring rows (activations) or columns (a weight) beside each other."""
+    for t, what in ((X, "X"), (Q, "Q"), (scale, "scale")):
+        if t is not None and t.dim() != 3:
+            raise ValueError(f"{what} must have 3 axes")
+    _last_axis(X, "X")
+    _last_axis(Q, "Q")
+    s = QuantizeShape()
+    s.B, s.N, s.K = X.shape
+    s.block_rows, s.x_dtype = block_rows, _dtype_code(X, "X")
+    wide, blocks, rows = -(-s.K // 16) * 16, -(-s.K // FP8_BLOCK), -(-s.N // max(block_rows, 1))
+    s.x_stride = _rows_of(s.x_stride, X)
+    s.q_stride[:] = (s.N * wide, wide) if Q is None else Q.stride()[:2]
+    s.scale_stride[:] = scale.stride() if scale is not None else (rows * blocks, 1, rows) if block_rows == 1 else (rows * blocks, blocks, 1)
+    return s
+
+
+@functools.lru_cache(maxsize=1024)
+def _quantize_said(of: bytes) -> _Said:
+    import torch
+    s = QuantizeShape.from_buffer_copy(of)
+    said = _Said(s)
+    size = (s.B, s.N, s.K)
+    said.x, said.q = (_dtype_of(s.x_dtype), size, (*s.x_stride, 1)), (torch.float8_e4m3fn, size, (*s.q_stride, 1))
+    said.scale = (torch.float32, (s.B, -(-s.N // max(s.block_rows, 1)), -(-s.K // FP8_BLOCK)), tuple(s.scale_stride))
+    return said
+
+
+def _room_as(dtype, size, stride, device):
+    import torch
+    return torch.empty_strided(size, stride, dtype=dtype, device=device)
+
+
+def quantize_fp8(X, shape: QuantizeShape, Q=None, scale=None, stream=None):
+    """carnator_quantize_fp8.  Returns (Q float8_e4m3fn [B,N,K], scale fp32); those not given are made with the record's strides."""
+    dev = X.device
+    said = _quantize_said(bytes(shape))
+    on = _stream_on(dev, stream)
+    _fit(X, "X", *said.x, dev)
+    if Q is None:
+        Q = _room_as(*said.q, dev)
+    else:
+        _fit(Q, "Q", *said.q, dev)
+    if scale is None:
+        scale = _room_as(*said.scale, dev)
+    else:
+        _fit(scale, "scale", *said.scale, dev)
+    st = lib().carnator_quantize_fp8(_ptr(X), said.ref, _ptr(Q), _ptr(scale), on)
+    if st != OK:
+        _check(st, "carnator_quantize_fp8")
+    return Q, scale
+
+
+def make_linear_fp8_shape(X, W, w_scale, Y, x_scale=None, residual=None, bias=None, gate=None, activation: int = ACT_NONE) -> LinearFp8Shape:
+    """Record of Y = residual + gate * act(X W^T + bias) with W e4m3 [out_features,in_features] and w_scale fp32 [ceil(out/128), ceil(in/128)]; X [B,N,in_features]
+    is e4m3 with x_scale fp32 [B,N,ceil(in/128)], or float32 / bfloat16 without.  Types and strides are taken from the tensors."""
+    import torch
+    for t, what, dims in ((X, "X", 3), (W, "W", 2), (Y, "Y", 3), (residual, "residual", 3), (x_scale, "x_scale", 3), (w_scale, "w_scale", 2)):
+        if t is not None and t.dim() != dims:
+            raise ValueError(f"{what} must have {dims} axes")
+        if t is not x_scale and t is not w_scale:
+            _last_axis(t, what)
+    s = LinearFp8Shape()
+    s.B, s.N, s.in_features = X.shape
+    s.out_features = W.shape[0]
+    if W.shape[1] != s.in_features or tuple(Y.shape) != (s.B, s.N, s.out_features):
+        raise ValueError(f"X {tuple(X.shape)}, W {tuple(W.shape)} and Y {tuple(Y.shape)} do not belong together")
+    if W.dtype != torch.float8_e4m3fn:
+        raise ValueError(f"W must be float8_e4m3fn, not {W.dtype}")
+    s.x_dtype = _x_code(X, "X")
+    if (x_scale is not None) != (s.x_dtype == DTYPE_E4M3):
+        raise ValueError("an 8-bit X comes with x_scale, any other without")
+    s.x_stride, s.y_stride = _rows_of(s.x_stride, X), _rows_of(s.y_stride, Y)
+    s.residual_stride = _rows_of(s.residual_stride, residual, Y)
+    s.w_stride = W.stride(0)
+    if x_scale is not None:
+        s.x_scale_stride[:] = x_scale.stride()
+    s.w_scale_stride[:] = w_scale.stride()
+    s.gate_stride = 0 if gate is None else gate.stride(0)
+    s.activation = activation
+    s.y_dtype = _dtype_code(Y, "Y")
+    s.bias_dtype = DTYPE_F32 if bias is None else _dtype_code(bias, "bias")
+    s.gate_dtype = DTYPE_F32 if gate is None else _dtype_code(gate, "gate")
+    return s
+
+
+@functools.lru_cache(maxsize=1024)
+def _linear_fp8_said(of: bytes) -> _Said:
+    import torch
+    s = LinearFp8Shape.from_buffer_copy(of)
+    said = _Said(s)
+    y, blocks = _dtype_of(s.y_dtype), -(-s.in_features // FP8_BLOCK)
+    said.x = (_dtype_of(s.x_dtype), (s.B, s.N, s.in_features), (*s.x_stride, 1))
+    said.y, said.residual = ((y, (s.B, s.N, s.out_features), (*st, 1)) for st in (s.y_stride, s.residual_stride))
+    said.w = (torch.float8_e4m3fn, (s.out_features, s.in_features), (s.w_stride, 1))
+    said.x_scale = (torch.float32, (s.B, s.N, blocks), tuple(s.x_scale_stride))
+    said.w_scale = (torch.float32, (-(-s.out_features // FP8_BLOCK), blocks), tuple(s.w_scale_stride))
+    said.bias = (_dtype_of(s.bias_dtype), (s.out_features,), (1,))
+    said.gate = (_dtype_of(s.gate_dtype), (s.B, s.out_features), (s.gate_stride, 1))
+    return said
+
+
+@functools.lru_cache(maxsize=1024)
+def _linear_fp8_packed(of: bytes):
+    s = LinearFp8Shape.from_buffer_copy(of)
+    of, size = _packed(s, "y_stride", (s.B, s.N), s.out_features)
+    return _linear_fp8_said(of), size, s.out_features
+
+
+def linear_fp8_workspace_bytes(shape: LinearFp8Shape) -> int:
+    return int(lib().carnator_linear_fp8_workspace_bytes(ctypes.byref(shape)))
+
+
+def linear_fp8(X, W, w_scale, shape: LinearFp8Shape, x_scale=None, bias=None, gate=None, residual=None, Y=None, ws=None, stream=None):
+    """carnator_linear_fp8.  Returns (Y [B,N,out_features] (as in layer_norm), ws)."""
+    dev = X.device
+    if Y is None:
+        said, size, n = _linear_fp8_packed(bytes(shape))
+        Y = _room(size, n, said.y[0], dev)
+    else:
+        said = _linear_fp8_said(bytes(shape))
+    on = _stream_on(dev, stream)
+    _fit(X, "X", *said.x, dev)
+    _fit(W, "W", *said.w, dev)
+    _fit(w_scale, "w_scale", *said.w_scale, dev)
+    _fit(Y, "Y", *said.y, dev)
+    if x_scale is not None:
+        _fit(x_scale, "x_scale", *said.x_scale, dev)
+    if residual is not None:
+        _fit(residual, "residual", *said.residual, dev)
+    if bias is not None:
+        _fit(bias, "bias", *said.bias, dev)
+    if gate is not None:
+        _fit(gate, "gate", *said.gate, dev)
+    if ws is None:
+        ws = _new_ws(linear_fp8_workspace_bytes(said.record), dev)
+    elif ws.device != dev or not ws.is_contiguous():
+        raise ValueError(f"ws must be contiguous and on {dev}")
+    st = lib().carnator_linear_fp8(_ptr(X), _ptr(x_scale), _ptr(W), _ptr(w_scale), _ptr(bias), _ptr(gate), _ptr(residual), said.ref, _ptr(Y), _ptr(ws), ws.numel(), on)
+    if st != OK:
+        _check(st, "carnator_linear_fp8")
+    return Y, ws
 
 
 # ---- host-side scalars (no GPU) ---------------------------------------------------------------------

@@ -8,6 +8,7 @@
 
 #include "carnator.h"
 #include "common.cuh"
+#include "api.h"
 #include "builder.cuh"
 #include "compact.cuh"
 #include "attn_portable.cuh"
@@ -25,27 +26,27 @@
 
 using namespace carnator;
 
-namespace {
-
+namespace carnator {
 std::atomic<long long> g_launches{0};
 thread_local char g_cuda_error[256] = "";
 
-carnator_status cuda_fail(cudaError_t e, const char* where) { return cuda_error(e, where, g_cuda_error, sizeof(g_cuda_error)); }
+carnator_status check_device() {
+    static thread_local int cached_dev = -1;
+    static thread_local carnator_status cached = CARNATOR_OK;
+    int dev = -1;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) { cudaGetLastError(); snprintf(g_cuda_error, sizeof(g_cuda_error), "cudaGetDevice: %s", cudaGetErrorString(e)); return CARNATOR_ERR_UNSUPPORTED; }
+    if (dev == cached_dev) return cached;
+    int major = 0;
+    e = cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev);
+    if (e != cudaSuccess) { cudaGetLastError(); return CARNATOR_ERR_UNSUPPORTED; }
+    cached_dev = dev;
+    cached = (major == 10) ? CARNATOR_OK : CARNATOR_ERR_UNSUPPORTED;
+    return cached;
+}
+}  // namespace carnator
 
-#define CUDA_TRY(expr)                                              \
-    do {                                                            \
-        cudaError_t e__ = (expr);                                   \
-        if (e__ != cudaSuccess) return cuda_fail(e__, #expr);       \
-    } while (0)
-
-#define LAUNCH_CHECK(name)                                          \
-    do {                                                            \
-        g_launches.fetch_add(1, std::memory_order_relaxed);         \
-        cudaError_t e__ = cudaGetLastError();                       \
-        if (e__ != cudaSuccess) return cuda_fail(e__, name);        \
-    } while (0)
-
-bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+namespace {
 
 bool strides_ok(const int64_t s[3]) {
     return s[0] >= 0 && s[1] >= 0 && s[2] > 0 && s[0] % 8 == 0 && s[1] % 8 == 0 && s[2] % 8 == 0;
@@ -80,21 +81,6 @@ carnator_status check_params(const carnator_build_params* p) {
 }
 
 // The device must be sm_100 (the kernels are built for sm_100a only).
-carnator_status check_device() {
-    static thread_local int cached_dev = -1;
-    static thread_local carnator_status cached = CARNATOR_OK;
-    int dev = -1;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) { cudaGetLastError(); snprintf(g_cuda_error, sizeof(g_cuda_error), "cudaGetDevice: %s", cudaGetErrorString(e)); return CARNATOR_ERR_UNSUPPORTED; }
-    if (dev == cached_dev) return cached;
-    int major = 0;
-    e = cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev);
-    if (e != cudaSuccess) { cudaGetLastError(); return CARNATOR_ERR_UNSUPPORTED; }
-    cached_dev = dev;
-    cached = (major == 10) ? CARNATOR_OK : CARNATOR_ERR_UNSUPPORTED;
-    return cached;
-}
-
 float effective_scale(const carnator_shape* s) {
     return s->softmax_scale > 0.f ? s->softmax_scale : 1.0f / sqrtf(float(s->D));
 }
@@ -981,36 +967,6 @@ extern "C" carnator_status carnator_seed_expansion(const void* Q, const void* K,
 // layer norm, matrix product with its epilogue, and their gradients
 // ------------------------------------------------------------------------------------------------
 namespace {
-bool dtype_ok(int32_t d) { return d == CARNATOR_DTYPE_F32 || d == CARNATOR_DTYPE_BF16; }
-int64_t dtype_bytes(int32_t d) { return d == CARNATOR_DTYPE_F32 ? 4 : 2; }
-int64_t dtype_unit(int32_t d) { return 16 / dtype_bytes(d); }       // elements in 16 bytes
-
-// Element strides of an operand with `n` axes in front of `row` contiguous elements: whole 16-byte steps and at most 2^38, not
-// negative.  For one that is written (or read through TMA, `positive`) no two rows may overlap (be the same).
-bool axes_ok(const int64_t* stride, const int64_t* size, int n, int64_t row, int32_t dtype, bool written, bool positive) {
-    int64_t st[3], sz[3];
-    int used = 0;
-    for (int i = 0; i < n; ++i) {
-        if (size[i] == 1) continue;                   // never used
-        if (stride[i] < 0 || stride[i] % dtype_unit(dtype) || stride[i] > (int64_t(1) << 38) || (positive && stride[i] == 0)) return false;
-        st[used] = stride[i]; sz[used] = size[i]; ++used;
-    }
-    if (!written) return true;
-    int64_t extent = row;
-    for (int k = 0; k < used; ++k) {                  // from the innermost axis out
-        int at = k;
-        for (int i = k + 1; i < used; ++i) if (st[i] < st[at]) at = i;
-        std::swap(st[k], st[at]); std::swap(sz[k], sz[at]);
-        if (st[k] < extent) return false;
-        extent += st[k] * (sz[k] - 1);
-    }
-    return true;
-}
-bool rows32(const void* p, const int64_t st[2], int32_t dtype) {      // whether every row starts on a 32-byte boundary
-    return !p || (aligned(p, 32) && st[0] % (2 * dtype_unit(dtype)) == 0 && st[1] % (2 * dtype_unit(dtype)) == 0);
-}
-bool vec16(const void* p, int64_t stride, int32_t dtype) { return !p || (aligned(p, 16) && stride % dtype_unit(dtype) == 0); }
-
 carnator_status check_norm_shape(const carnator_norm_shape* s) {
     if (!s || s->B <= 0 || s->H <= 0 || s->N <= 0 || s->C <= 0) return CARNATOR_ERR_INVALID_ARG;
     if (!dtype_ok(s->x_dtype) || !dtype_ok(s->y_dtype) || !dtype_ok(s->weight_dtype) || !dtype_ok(s->mod_dtype)) return CARNATOR_ERR_INVALID_ARG;

@@ -1,0 +1,279 @@
+// C-ABI entry points between a layer's attention, its projections and the residual stream: rotary positions, 8-bit operands and their product.
+#include <algorithm>
+#include <cmath>
+#include <cstdio>
+
+#include "carnator.h"
+#include "api.h"
+#include "rope.cuh"
+#include "fp8_quantize.cuh"
+#include "linear_fp8.cuh"
+
+using namespace carnator;
+
+namespace {
+constexpr int64_t kMostStride = int64_t(1) << 38;
+
+void count_launch() { g_launches.fetch_add(1, std::memory_order_relaxed); }
+
+// ------------------------------------------------------------------------------------------------
+// rotary positions
+// ------------------------------------------------------------------------------------------------
+carnator_status check_rope_shape(const carnator_rope_shape* s, bool positions) {
+    if (!s || s->B <= 0 || s->H <= 0 || s->N <= 0 || s->D <= 0) return CARNATOR_ERR_INVALID_ARG;
+    if (!dtype_ok(s->x_dtype) || (s->layout != CARNATOR_ROPE_INTERLEAVED && s->layout != CARNATOR_ROPE_HALF)) return CARNATOR_ERR_INVALID_ARG;
+    if (!std::isfinite(s->amplitude)) return CARNATOR_ERR_INVALID_ARG;
+    int64_t pairs = 0;
+    for (int p : s->pairs) {
+        if (p < 0) return CARNATOR_ERR_INVALID_ARG;
+        pairs += p;
+    }
+    if (pairs == 0 || 2 * pairs > s->D) return CARNATOR_ERR_INVALID_ARG;
+    if (positions) {
+        if (s->axes < 1 || s->axes > 3) return CARNATOR_ERR_INVALID_ARG;
+        for (int i = s->axes; i < 3; ++i) if (s->pairs[i]) return CARNATOR_ERR_INVALID_ARG;
+        if ((s->B > 1 && (s->pos_stride[0] < 0 || s->pos_stride[0] > kMostStride)) || (s->N > 1 && (s->pos_stride[1] < 0 || s->pos_stride[1] > kMostStride))) return CARNATOR_ERR_INVALID_ARG;
+    } else {
+        if (s->n_text < 0 || s->T < 0 || s->Hg < 0 || s->Wg < 0) return CARNATOR_ERR_INVALID_ARG;
+        const int64_t frame = int64_t(s->Hg) * s->Wg;            // below 2^62
+        const int64_t video = int64_t(s->N) - s->n_text;
+        if (s->T == 0 || frame == 0 ? video != 0 : (frame > video || video % frame || video / frame != s->T)) return CARNATOR_ERR_INVALID_ARG;
+    }
+    if (s->D > rope::kMaxHead || s->B > 65535 || s->H > 65535 || s->N > (1 << 27)) return CARNATOR_ERR_UNSUPPORTED;
+    return CARNATOR_OK;
+}
+}  // namespace
+
+extern "C" carnator_status carnator_rope_frequencies(const carnator_rope_scaling* s, double* freq, double* amplitude_opt) {
+    if (!s || !freq || !(s->theta > 1) || !std::isfinite(s->theta) || s->mode < CARNATOR_ROPE_SCALE_NONE || s->mode > CARNATOR_ROPE_SCALE_RAMP) return CARNATOR_ERR_INVALID_ARG;
+    const bool ramp = s->mode == CARNATOR_ROPE_SCALE_RAMP;
+    if (ramp && !(s->low >= 0 && s->high > s->low && std::isfinite(s->high))) return CARNATOR_ERR_INVALID_ARG;
+    double most = 1;
+    for (int a = 0; a < 3; ++a) {
+        if (s->pairs[a] < 0 || s->pairs[a] > (1 << 20)) return CARNATOR_ERR_INVALID_ARG;
+        if (s->pairs[a] == 0 || s->mode == CARNATOR_ROPE_SCALE_NONE) continue;
+        if (!(s->factor[a] >= 1) || !std::isfinite(s->factor[a]) || (ramp && !(s->original[a] > 0 && std::isfinite(s->original[a])))) return CARNATOR_ERR_INVALID_ARG;
+        most = std::max(most, s->factor[a]);
+    }
+    int at = 0;
+    for (int a = 0; a < 3; ++a) {
+        const double n = s->pairs[a];
+        double theta = s->theta;
+        if (s->mode == CARNATOR_ROPE_SCALE_BASE && s->pairs[a] > 1) theta *= std::pow(s->factor[a], n / (n - 1));
+        for (int i = 0; i < s->pairs[a]; ++i) {
+            double f = std::pow(theta, -i / n);
+            if (s->mode == CARNATOR_ROPE_SCALE_LINEAR) f /= s->factor[a];
+            if (ramp) {
+                const double turns = s->original[a] * f / (2 * M_PI), g = std::min(std::max((turns - s->low) / (s->high - s->low), 0.0), 1.0);
+                f *= g + (1 - g) / s->factor[a];
+            }
+            freq[at++] = f;
+        }
+    }
+    if (amplitude_opt) *amplitude_opt = ramp ? 0.1 * std::log(most) + 1 : 1;
+    return CARNATOR_OK;
+}
+
+extern "C" carnator_status carnator_rope(const void* X, const double* freq, const int32_t* positions, const carnator_rope_shape* s, void* Y, void* stream_) {
+    carnator_status st = check_rope_shape(s, positions != nullptr);
+    if (st != CARNATOR_OK) return st;
+    if (!X || !Y || !freq || !aligned(X, 16) || !aligned(Y, 16) || !aligned(freq, 8) || !aligned(positions, 4)) return CARNATOR_ERR_INVALID_ARG;
+    const int64_t size[3] = {s->B, s->H, s->N};
+    if (!axes_ok(s->x_stride, size, 3, s->D, s->x_dtype, false, false) || !axes_ok(s->y_stride, size, 3, s->D, s->x_dtype, true, false)) return CARNATOR_ERR_INVALID_ARG;
+    st = check_device();
+    if (st != CARNATOR_OK) return st;
+    rope::Args a = {};
+    a.x = X; a.y = Y; a.freq = freq; a.pos = positions;
+    a.in_place = X == Y;
+    for (int i = 0; i < 3; ++i) {
+        a.xs[i] = size[i] == 1 ? 0 : s->x_stride[i];
+        a.ys[i] = size[i] == 1 ? 0 : s->y_stride[i];
+        if (a.xs[i] != a.ys[i]) a.in_place = 0;
+        a.offset[i] = s->offset[i];
+    }
+    a.ps[0] = s->B == 1 ? 0 : s->pos_stride[0]; a.ps[1] = s->N == 1 ? 0 : s->pos_stride[1];
+    a.H = s->H; a.N = s->N; a.D = s->D; a.axes = s->axes;
+    a.n_text = s->n_text; a.Hg = std::max(s->Hg, 1); a.Wg = std::max(s->Wg, 1);
+    a.end0 = s->pairs[0]; a.end1 = s->pairs[0] + s->pairs[1]; a.pairs = a.end1 + s->pairs[2];
+    a.amplitude = s->amplitude; a.sign = s->inverse ? -1.f : 1.f;
+    const bool half = s->layout == CARNATOR_ROPE_HALF;
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    const cudaError_t e = s->x_dtype == CARNATOR_DTYPE_F32 ? rope::launch<true>(a, s->B, half, stream) : rope::launch<false>(a, s->B, half, stream);
+    if (e != cudaSuccess) return cuda_fail(e, "rope kernel");
+    count_launch();
+    return CARNATOR_OK;
+}
+
+// ------------------------------------------------------------------------------------------------
+// 8-bit operands
+// ------------------------------------------------------------------------------------------------
+namespace {
+// Element strides of scales: those of axes longer than one are not negative and at most 2^38; `written`: values lie apart.
+bool scales_ok(const int64_t* stride, const int64_t* size, int n, bool written) {
+    int64_t st[3], sz[3], extent = 1;
+    int used = 0;
+    for (int i = 0; i < n; ++i) {
+        if (size[i] == 1) continue;
+        if (stride[i] < 0 || stride[i] > kMostStride) return false;
+        st[used] = stride[i]; sz[used] = size[i]; ++used;
+    }
+    for (int k = 0; written && k < used; ++k) {
+        int at = k;
+        for (int i = k + 1; i < used; ++i) if (st[i] < st[at]) at = i;
+        std::swap(st[k], st[at]); std::swap(sz[k], sz[at]);
+        if (st[k] < extent) return false;
+        extent += st[k] * (sz[k] - 1);
+    }
+    return true;
+}
+constexpr int64_t kMostAxis = int64_t(1) << 27;
+}  // namespace
+
+extern "C" carnator_status carnator_quantize_fp8(const void* X, const carnator_quantize_shape* s, void* Q, float* scale, void* stream_) {
+    if (!s || s->B <= 0 || s->N <= 0 || s->K <= 0 || (s->block_rows != 1 && s->block_rows != fp8::kBlock) || !dtype_ok(s->x_dtype)) return CARNATOR_ERR_INVALID_ARG;
+    const int blocks = ceil_div(s->K, fp8::kBlock), row_blocks = s->block_rows == 1 ? s->N : ceil_div(s->N, fp8::kBlock);
+    if (int64_t(s->B) * s->N > kMostAxis || s->K > kMostAxis || s->B > 65535 || (s->block_rows > 1 && int64_t(row_blocks) * blocks > (int64_t(1) << 30))) return CARNATOR_ERR_UNSUPPORTED;
+    if (!X || !Q || !scale || !aligned(X, 16) || !aligned(Q, 16) || !aligned(scale, 4)) return CARNATOR_ERR_INVALID_ARG;
+    const int64_t size[2] = {s->B, s->N}, sizes[3] = {s->B, row_blocks, blocks};
+    if (!axes_ok(s->x_stride, size, 2, s->K, s->x_dtype, false, false) || !axes_ok(s->q_stride, size, 2, s->K, CARNATOR_DTYPE_E4M3, true, false) ||
+        !scales_ok(s->scale_stride, sizes, 3, true)) return CARNATOR_ERR_INVALID_ARG;
+    const carnator_status st = check_device();
+    if (st != CARNATOR_OK) return st;
+    fp8::QuantArgs a = {};
+    a.x = X; a.q = static_cast<uint8_t*>(Q); a.scale = scale;
+    for (int i = 0; i < 2; ++i) { a.xs[i] = size[i] == 1 ? 0 : s->x_stride[i]; a.qs[i] = size[i] == 1 ? 0 : s->q_stride[i]; }
+    for (int i = 0; i < 3; ++i) a.ss[i] = sizes[i] == 1 ? 0 : s->scale_stride[i];
+    a.batches = s->B; a.rows = s->N; a.cols = s->K; a.blocks = blocks;
+    const cudaError_t e = fp8::launch_quantize(a, s->x_dtype == CARNATOR_DTYPE_F32, s->block_rows, static_cast<cudaStream_t>(stream_));
+    if (e != cudaSuccess) return cuda_fail(e, "quantize kernel");
+    count_launch();
+    return CARNATOR_OK;
+}
+
+namespace {
+carnator_status check_fp8_shape(const carnator_linear_fp8_shape* s) {
+    if (!s || s->B <= 0 || s->N <= 0 || s->in_features <= 0 || s->out_features <= 0) return CARNATOR_ERR_INVALID_ARG;
+    if (s->activation < CARNATOR_ACT_NONE || s->activation > CARNATOR_ACT_SILU) return CARNATOR_ERR_INVALID_ARG;
+    if ((!dtype_ok(s->x_dtype) && s->x_dtype != CARNATOR_DTYPE_E4M3) || !dtype_ok(s->y_dtype) || !dtype_ok(s->bias_dtype) || !dtype_ok(s->gate_dtype) || s->gate_stride < 0)
+        return CARNATOR_ERR_INVALID_ARG;
+    if (int64_t(s->B) * s->N > kMostAxis || s->in_features > kMostAxis || s->out_features > kMostAxis || s->B > 65535) return CARNATOR_ERR_UNSUPPORTED;
+    return CARNATOR_OK;
+}
+bool few_rows(const carnator_linear_fp8_shape* s) { return int64_t(s->B) * s->N <= lin8::kRowsMost8; }
+
+// Status header, then X in 8 bits (rows of whole blocks) and its scales (rows beside each other), where the call makes them.
+struct Fp8Ws { uint8_t* q; float* scale; int64_t q_stride, scale_stride; size_t bytes; };
+Fp8Ws fp8_ws_layout(void* base, const carnator_linear_fp8_shape* s) {
+    Fp8Ws w = {};
+    char* p = static_cast<char*>(base);
+    size_t off = align256(sizeof(WsHeader));
+    if (s->x_dtype != CARNATOR_DTYPE_E4M3 && !few_rows(s)) {
+        const int64_t rows = int64_t(s->B) * s->N, blocks = ceil_div(s->in_features, fp8::kBlock);
+        w.q_stride = blocks * fp8::kBlock;
+        w.scale_stride = (rows + 31) / 32 * 32;
+        w.q = reinterpret_cast<uint8_t*>(p + off);       off += align256(size_t(rows) * w.q_stride);
+        w.scale = reinterpret_cast<float*>(p + off);     off += align256(size_t(w.scale_stride) * blocks * 4);
+    }
+    w.bytes = off;
+    return w;
+}
+}  // namespace
+
+extern "C" size_t carnator_linear_fp8_workspace_bytes(const carnator_linear_fp8_shape* s) {
+    return check_fp8_shape(s) == CARNATOR_OK ? fp8_ws_layout(nullptr, s).bytes : 0;
+}
+
+extern "C" carnator_status carnator_linear_fp8(const void* X, const float* x_scale, const void* W, const float* w_scale, const void* bias, const void* gate, const void* residual,
+                                               const carnator_linear_fp8_shape* s, void* Y, void* ws, size_t ws_bytes, void* stream_) {
+    carnator_status st = check_fp8_shape(s);
+    if (st != CARNATOR_OK) return st;
+    const bool ready = s->x_dtype == CARNATOR_DTYPE_E4M3;
+    if (!X || !W || !w_scale || !Y || ready != (x_scale != nullptr)) return CARNATOR_ERR_INVALID_ARG;
+    if (!aligned(X, 16) || !aligned(W, 16) || !aligned(Y, 16) || !aligned(residual, 16) || !aligned(x_scale, 4) || !aligned(w_scale, 4)) return CARNATOR_ERR_INVALID_ARG;
+    if (!aligned(bias, size_t(dtype_bytes(s->bias_dtype))) || !aligned(gate, size_t(dtype_bytes(s->gate_dtype)))) return CARNATOR_ERR_INVALID_ARG;
+    const int blocks = ceil_div(s->in_features, fp8::kBlock);
+    const int64_t size[2] = {s->B, s->N}, xsize[3] = {s->B, s->N, blocks}, wsize[2] = {ceil_div(s->out_features, fp8::kBlock), blocks};
+    auto rows_ok = [&](const int64_t* stride, int64_t row, int32_t dtype, bool written) { return axes_ok(stride, size, 2, row, dtype, written, true) && (s->N == 1 || stride[1] >= row); };
+    if (!rows_ok(s->x_stride, s->in_features, s->x_dtype, false) || !rows_ok(s->y_stride, s->out_features, s->y_dtype, true) ||
+        (residual && !rows_ok(s->residual_stride, s->out_features, s->y_dtype, false)) || (ready && !scales_ok(s->x_scale_stride, xsize, 3, false)) ||
+        !scales_ok(s->w_scale_stride, wsize, 2, false)) return CARNATOR_ERR_INVALID_ARG;
+    if (s->out_features > 1 && (s->w_stride < s->in_features || s->w_stride % 16 || s->w_stride > kMostStride)) return CARNATOR_ERR_INVALID_ARG;
+    if (!ws || !aligned(ws, 256)) return CARNATOR_ERR_WORKSPACE;
+    const Fp8Ws w = fp8_ws_layout(ws, s);
+    if (ws_bytes < w.bytes) return CARNATOR_ERR_WORKSPACE;
+    st = check_device();
+    if (st != CARNATOR_OK) return st;
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    lin::Epilogue e = {};
+    e.y = Y; e.bias = bias; e.gate = gate; e.residual = residual;
+    // the stride of an axis of one entry may be anything
+    int64_t xs[2], ys[2], rs[2], xss[3], wss[2];
+    for (int i = 0; i < 2; ++i) {
+        const bool one = size[i] == 1;
+        xs[i] = one ? 0 : s->x_stride[i]; ys[i] = one ? 0 : s->y_stride[i]; rs[i] = one || !residual ? 0 : s->residual_stride[i];
+        wss[i] = wsize[i] == 1 ? 0 : s->w_scale_stride[i];
+    }
+    for (int i = 0; i < 3; ++i) xss[i] = xsize[i] == 1 || !ready ? 0 : s->x_scale_stride[i];
+    for (int i = 0; i < 2; ++i) { e.ys[i] = ys[i]; e.rs[i] = rs[i]; }
+    e.gate_stride = s->B == 1 ? 0 : s->gate_stride;
+    e.act = s->activation; e.y_f32 = s->y_dtype == CARNATOR_DTYPE_F32;
+    e.bias_f32 = s->bias_dtype == CARNATOR_DTYPE_F32; e.gate_f32 = s->gate_dtype == CARNATOR_DTYPE_F32;
+    e.vec_ok = vec16(bias, 0, s->bias_dtype) && vec16(gate, e.gate_stride, s->gate_dtype);
+    e.wide_ok = rows32(Y, ys, s->y_dtype) && rows32(residual, rs, s->y_dtype);
+    e.rows_per_gate = s->N;
+    const int64_t rows = int64_t(s->B) * s->N;
+    if (few_rows(s)) {
+        lin8::RowsArgs8 a = {};
+        a.e = e; a.x = X; a.w = static_cast<const uint8_t*>(W); a.xscale = x_scale; a.wscale = w_scale;
+        for (int i = 0; i < 2; ++i) { a.xs[i] = xs[i]; a.wss[i] = wss[i]; }
+        for (int i = 0; i < 3; ++i) a.xss[i] = xss[i];
+        a.w_stride = s->out_features == 1 ? 0 : s->w_stride;
+        a.hdr = static_cast<WsHeader*>(ws);
+        a.rows = int(rows); a.per_batch = s->N; a.K = s->in_features; a.cols = s->out_features;
+        const cudaError_t err = ready ? lin8::launch_rows8<lin8::kXE4m3>(a, stream)
+                              : s->x_dtype == CARNATOR_DTYPE_F32 ? lin8::launch_rows8<lin8::kXF32>(a, stream) : lin8::launch_rows8<lin8::kXBf16>(a, stream);
+        if (err != cudaSuccess) return cuda_fail(err, "linear_fp8_rows_kernel");
+        count_launch();
+        return CARNATOR_OK;
+    }
+    // Batch entries that follow each other evenly are one run of rows.
+    auto runs = [&](const int64_t* st) { return s->B == 1 || s->N == 1 || st[0] == int64_t(s->N) * st[1]; };
+    auto run_stride = [&](const int64_t* st) { return s->N == 1 ? st[0] : st[1]; };
+    lin8::Args8 a = {};
+    a.t.e = e;
+    a.t.hdr = static_cast<WsHeader*>(ws);
+    a.t.clears = ready;
+    a.wscale = w_scale; a.wss[0] = wss[0]; a.wss[1] = wss[1];
+    a.xscale = x_scale;
+    for (int i = 0; i < 3; ++i) a.xss[i] = xss[i];
+    lin::Operand A = {X, s->B, s->N, s->in_features, xs[0], xs[1]};
+    if (!ready) {
+        fp8::QuantArgs q = {};
+        q.x = X; q.q = w.q; q.scale = w.scale;
+        q.xs[0] = xs[0]; q.xs[1] = xs[1];
+        q.qs[0] = w.q_stride * s->N; q.qs[1] = w.q_stride;
+        q.ss[0] = s->N; q.ss[1] = 1; q.ss[2] = w.scale_stride;
+        q.batches = s->B; q.rows = s->N; q.cols = s->in_features; q.blocks = blocks;
+        if (runs(xs)) { q.batches = 1; q.rows = int(rows); q.xs[1] = run_stride(xs); }
+        q.clears = a.t.hdr;
+        const cudaError_t err = fp8::launch_quantize(q, s->x_dtype == CARNATOR_DTYPE_F32, 1, stream);
+        if (err != cudaSuccess) return cuda_fail(err, "quantize_rows_kernel");
+        count_launch();
+        A.base = w.q; A.batch_stride = w.q_stride * s->N; A.row_stride = w.q_stride;
+        a.xscale = w.scale; a.xss[0] = s->N; a.xss[1] = 1; a.xss[2] = w.scale_stride;
+    }
+    a.t.batches = s->B; a.t.rows = s->N;
+    if (runs(ys) && (!residual || runs(rs)) && (!ready || (runs(xs) && runs(xss)))) {
+        a.t.batches = 1; a.t.rows = int(rows);
+        A.batches = 1; A.rows = rows;
+        if (ready) { A.row_stride = run_stride(xs); a.xss[1] = run_stride(xss); }
+        a.t.e.ys[1] = run_stride(ys); a.t.e.rs[1] = run_stride(rs);
+    }
+    const lin::Operand Bo = {W, 1, s->out_features, s->in_features, 0, s->w_stride};
+    a.t.cols = s->out_features;
+    a.t.tiles_m = ceil_div(a.t.rows, lin::kTileM);
+    a.t.k_len = s->in_features;
+    st = lin8::launch_product8(A, Bo, a, stream, g_cuda_error, sizeof(g_cuda_error));
+    if (st == CARNATOR_OK) count_launch();
+    return st;
+}

@@ -1,0 +1,525 @@
+// Matrix product of 8-bit operands with a scale per block of 128 (fp8_quantize.cuh), on the 5th-gen tensor cores, with the epilogue of linear_tcgen05.cuh:
+//   z = sum over blocks j of 128 k of  sx[row, j] sw[col / 128, j] <qx_j, qw_j>  + bias,   y = residual + gate_b act(z).
+//
+// The scales change with every 128 k, so an accumulator of the tensor cores sums up one block only (four products of 32 k, in which nothing is lost: 7
+// significant bits each, 128 terms) and the epilogue warps take it times the block's scale into fp32 sums of their own, 128 per thread, while the next block's
+// products run into another accumulator.  Scales are any fp32 numbers.
+// A pair of CTAs shares a tile of 256 x BN (cta_group::2), as in linear_tcgen05.cuh, whose roles, ring and joining of shared sums these are; what a stage's
+// barrier says, that the products which read it have completed, says too that the accumulator of its block is whole: one commit per block.
+// Per block of a 256 x 256 tile an SM's tensor core works 512 clocks, its epilogue warps read 128 KB of tensor memory and do 128 x 256 multiply-adds.
+#pragma once
+#include "fp8_quantize.cuh"
+#include "linear_tcgen05.cuh"
+
+namespace carnator {
+namespace lin8 {
+using namespace tc;
+using namespace lin;
+using fp8::kBlock;
+
+constexpr uint32_t kABytes8 = 128 * kBlock;          // a CTA's share of A per stage
+
+struct Args8 {
+    TcArgs t;
+    const float* xscale; const float* wscale;
+    int64_t xss[3], wss[2];              // (batch, row, block), (block of columns, block)
+};
+
+__device__ __forceinline__ void mma8_pair_el(uint32_t d_tmem, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p, e;\n\t.reg .b64 da, db;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+        "mov.b64 da, {%1, %2};\n\tmov.b64 db, {%3, %4};\n\t"
+        "elect.sync _|e, 0xffffffff;\n\t"
+        "@e tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], da, db, %5, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ float load_scale(const float* p) {      // not through the read-only path: the kernel ahead may write it while this one is resident
+    float v;
+    asm volatile("ld.global.f32 %0, [%1];" : "=f"(v) : "l"(p));
+    return v;
+}
+
+// kParts: 32-column parts of a thread's columns, of which it has BN / 2 beside each other, within one block of the weight's rows.
+// kAccs: accumulators in tensor memory.
+template <int kParts, bool kF32>
+__global__ void __launch_bounds__(kThreadsTc, 1)
+linear_fp8_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB, const Args8 args) {
+    constexpr int kBn = kParts * 64, kAccs = kParts == 4 ? 2 : 4;
+    constexpr uint32_t kBBytes = kBn / 2 * kBlock, kStage = kABytes8 + kBBytes;
+    const TcArgs& a = args.t;
+    extern __shared__ unsigned char lin_smem[];
+    __shared__ uint32_t tmem_slot;
+    __shared__ int abort_flag;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t base = (smem_u32(lin_smem) + 1023u) & ~1023u;
+    const uint32_t bars = base + kRingBytes;
+    const uint32_t rank = cluster_ctarank(), half = rank & 1u, leader = rank & ~1u, split = rank >> 1;
+    auto bar_full = [&](int s) { return bars + 8 * s; };                       // used in the pair's first CTA: both CTAs' copies have landed
+    auto bar_done = [&](int s) { return bars + 64 + 8 * s; };                  // the products of stage s have completed: it may be filled, its accumulator read
+    auto bar_read = [&](int u) { return bars + 128 + 8 * u; };                 // first CTA: both CTAs have read accumulator u
+    volatile int* abortp = &abort_flag;
+    const unsigned long long limit = kDefaultWaitNs;
+    const uint16_t pair_mask = uint16_t(3u << leader);
+
+    if (tid == 0) {
+        abort_flag = 0;
+        for (int s = 0; s < kMaxStages; ++s) { mbar_init(bar_full(s), 1); mbar_init(bar_done(s), 1); }
+        for (int u = 0; u < kAccs; ++u) mbar_init(bar_read(u), 2 * kEpiWarps);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 2) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    if (warp == 0 && lane == 0) { prefetch_tmap(&mapA); prefetch_tmap(&mapB); }
+    grid_launch_dependents();
+    tc_fence_before();
+    __syncwarp();
+    cluster_sync();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot;
+    grid_wait();                         // launched while the kernel ahead drains: nothing of global memory is touched before this
+    if (tid == 0 && blockIdx.x == 0 && a.clears) a.hdr->status = 0;
+    __syncwarp();                        // whole warps hand over registers (setmaxnreg)
+
+    // the clusters take the tiles in turn; with splits > 1 there is one cluster per tile and a pair has its share of k
+    const int first = int(blockIdx.x / (2 * a.splits)), step = int(gridDim.x / (2 * a.splits));
+    const int k0 = int(int64_t(a.k_tiles) * split / a.splits), k1 = int(int64_t(a.k_tiles) * (split + 1) / a.splits);
+
+    if (warp < 4) {                      // ---- service warps
+    // 128 x 40 + 256 x 208 registers; the block is launched with 384 x 152 at least (checked by the host)
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;" ::: "memory");
+    if (warp == 0) {
+        // ================= TMA producer =================
+        if (lane == 0) {
+            const uint32_t full0 = map_cta(bar_full(0), leader);
+            int s = 0, issued = 0;
+            uint32_t phase = 0;
+            bool ok = true;
+            for (int t = first; t < a.tiles && ok; t += step) {
+                int b, m, n;
+                tile_at(a, t, b, m, n);
+                const int m0 = m * kTileM + int(half) * 128, n0 = n * kBn + int(half) * (kBn / 2);
+                for (int k = k0; k < k1; ++k) {
+                    if (issued >= a.stages && !mbar_wait(bar_done(s), phase ^ 1u, abortp, 0, limit)) {
+                        set_status(a.hdr, CARNATOR_ERR_DEVICE_TIMEOUT, 80, k, blockIdx.x); ok = false; break;
+                    }
+                    if (half == 0) mbar_expect_tx(bar_full(s), 2 * kStage);
+                    const uint32_t sa = base + uint32_t(s) * kStage, bar = full0 + 8 * s;
+                    tma_load_pair(sa, &mapA, bar, k * kBlock, m0, b);
+                    tma_load_pair(sa + kABytes8, &mapB, bar, k * kBlock, n0, 0);
+                    ++issued;
+                    if (++s == a.stages) { s = 0; phase ^= 1u; }
+                }
+            }
+            // The completion of the last products on every stage: no copy is in flight and no arrival on its way to this CTA afterwards.
+            const int used = min(issued, a.stages);
+            for (int i = 0; i < used; ++i) {
+                const int q = issued - used + i, sq = q % a.stages;
+                const uint32_t par = uint32_t(q / a.stages) & 1u;
+                if (*abortp ? !mbar_wait_drain(bar_done(sq), par, 2000000ull) : !mbar_wait(bar_done(sq), par, abortp, 0, limit))
+                    set_status(a.hdr, CARNATOR_ERR_DEVICE_TIMEOUT, 81, i, blockIdx.x);
+            }
+            if (*abortp) {               // given up: copies whose products were never issued land within microseconds
+                const unsigned long long t0 = global_ns();
+                for (int it = 0; it < 20000 && global_ns() - t0 < 1000000ull; ++it) __nanosleep(100);
+            }
+        }
+    } else if (warp == 1) {
+        // ================= MMA issuer (converged warp, one elected lane issues) =================
+        if (half == 0) {
+            // e4m3 x e4m3, fp32 accumulator; K-major operands: 8-row groups 1024 B apart, 32 columns of k = 32 B
+            const uint32_t idesc = (1u << 4) | (uint32_t(kBn >> 3) << 17) | (uint32_t(kTileM >> 4) << 24);
+            const uint64_t da0 = smem_desc(base, 16, 1024), db0 = smem_desc(base + kABytes8, 16, 1024);
+            const uint32_t a_lo = uint32_t(da0), a_hi = uint32_t(da0 >> 32), b_lo = uint32_t(db0), b_hi = uint32_t(db0 >> 32);
+            const int last = (a.k_len - (a.k_tiles - 1) * kBlock + 31) / 32;
+            int s = 0, i = 0;
+            uint32_t phase = 0;
+            bool ok = true;
+            for (int t = first; t < a.tiles && ok; t += step) {
+                for (int k = k0; k < k1; ++k, ++i) {
+                    const int u = i % kAccs;
+                    if (i >= kAccs) {
+                        ok = mbar_wait_warp(bar_read(u), uint32_t(i / kAccs - 1) & 1u, abortp, 0, limit);
+                        if (!ok) { if (lane == 0) set_status(a.hdr, CARNATOR_ERR_DEVICE_TIMEOUT, 82, i, blockIdx.x); break; }
+                    }
+                    ok = mbar_wait_warp(bar_full(s), phase, abortp, 0, limit);
+                    if (!ok) { if (lane == 0) set_status(a.hdr, CARNATOR_ERR_DEVICE_TIMEOUT, 83, k, blockIdx.x); break; }
+                    tc_fence_after();
+                    const uint32_t off = (uint32_t(s) * kStage) >> 4, d = tmem + uint32_t(u * kBn);
+                    if (k + 1 < a.k_tiles) {
+#pragma unroll
+                        for (int kk = 0; kk < 4; ++kk) mma8_pair_el(d, a_lo + off + kk * 2, a_hi, b_lo + off + kk * 2, b_hi, idesc, kk > 0 ? 1u : 0u);
+                    } else {             // the end of k: what is all zero is left out
+                        for (int kk = 0; kk < last; ++kk) mma8_pair_el(d, a_lo + off + kk * 2, a_hi, b_lo + off + kk * 2, b_hi, idesc, kk > 0 ? 1u : 0u);
+                    }
+                    commit_pair_el(bar_done(s), pair_mask);
+                    if (++s == a.stages) { s = 0; phase ^= 1u; }
+                }
+            }
+        }
+    }
+    if (a.splits > 1) {                  // the epilogue warps meet the cluster before they join its tiles
+        __syncwarp();
+        cluster_sync();
+    }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;" ::: "memory");
+        // ================= epilogue =================
+        const int quarter = warp & 3, side = (warp - 4) >> 2;               // rows 32 quarter .. of this CTA's 128; half of the columns
+        const uint32_t lane_base = uint32_t(quarter * 32) << 16;
+        const uint32_t read0 = map_cta(bar_read(0), leader);
+        bool ok = true;
+        int i = 0, s = 0;
+        uint32_t phase = 0;
+        for (int t = first; t < a.tiles && ok; t += step) {
+            int b, m, n;
+            tile_at(a, t, b, m, n);
+            const int row = m * kTileM + int(half) * 128 + quarter * 32 + lane, at0 = side * (kBn / 2), left = min(a.cols - n * kBn, kBn) - at0;
+            const bool on = row < a.rows, some = left > 0;         // `some`: warp-uniform
+            const float* xs = args.xscale + b * args.xss[0] + (on ? row : 0) * args.xss[1];
+            const float* ws = args.wscale + (some ? (n * kBn + at0) / kBlock : 0) * args.wss[0];
+            __syncwarp();                // rows behind the last one have left the tile before early
+            f2 acc[kParts][16];
+#pragma unroll
+            for (int p = 0; p < kParts; ++p)
+#pragma unroll
+                for (int q = 0; q < 16; ++q) acc[p][q] = two(0.f);
+            // scales on their way two blocks ahead
+            float x0 = load_scale(xs + k0 * args.xss[2]), w0 = load_scale(ws + k0 * args.wss[1]), x1 = 0.f, w1 = 0.f;
+            if (k0 + 1 < k1) { x1 = load_scale(xs + (k0 + 1) * args.xss[2]); w1 = load_scale(ws + (k0 + 1) * args.wss[1]); }
+            for (int k = k0; k < k1; ++k, ++i) {
+                const int u = i % kAccs;
+                const f2 by = two(x0 * w0);
+                x0 = x1; w0 = w1;
+                if (k + 2 < k1) { x1 = load_scale(xs + (k + 2) * args.xss[2]); w1 = load_scale(ws + (k + 2) * args.wss[1]); }
+                ok = mbar_wait_warp(bar_done(s), phase, abortp, 0, limit);
+                if (!ok) { if (lane == 0) set_status(a.hdr, CARNATOR_ERR_DEVICE_TIMEOUT, 84, i, blockIdx.x); break; }
+                if (++s == a.stages) { s = 0; phase ^= 1u; }
+                tc_fence_after();
+                const uint32_t from = tmem + lane_base + uint32_t(u * kBn + at0);
+                float v[2][32];
+                tmem_ld32(from, v[0]);
+#pragma unroll
+                for (int p = 0; p < kParts; ++p) {
+                    tmem_wait_ld(v[p & 1]);
+                    if (p + 1 < kParts) tmem_ld32(from + 32 * (p + 1), v[(p + 1) & 1]);
+                    else {               // this warp has read its part of the block
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) arrive_remote(read0 + 8 * u);
+                    }
+#pragma unroll
+                    for (int q = 0; q < 16; ++q) acc[p][q] = norm::fma2(two(v[p & 1][2 * q], v[p & 1][2 * q + 1]), by, acc[p][q]);
+                }
+            }
+            __syncwarp();
+            if (!ok) break;
+            if (a.splits > 1) {          // the one tile of this cluster: this pair's share to shared memory
+                const uint32_t line = base + uint32_t(quarter * 32 + lane) * uint32_t((kBn + 4) * 4);
+#pragma unroll
+                for (int p = 0; p < kParts; ++p)
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) {
+                        float f[4];
+                        one_each(acc[p][2 * q], f[0], f[1]);
+                        one_each(acc[p][2 * q + 1], f[2], f[3]);
+                        asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(line + uint32_t(at0 + 32 * p + 4 * q) * 4u), "f"(f[0]), "f"(f[1]), "f"(f[2]), "f"(f[3]) : "memory");
+                    }
+                break;
+            }
+            const int64_t y_off = b * a.e.ys[0] + row * a.e.ys[1], r_off = b * a.e.rs[0] + row * a.e.rs[1];
+            const int64_t gate_off = a.e.gate ? (b + row / a.e.rows_per_gate) * a.e.gate_stride : 0;
+            const char* res = static_cast<const char*>(a.e.residual) + (r_off + n * kBn + at0) * (kF32 ? 4 : 2);
+#pragma unroll
+            for (int p = 0; p < kParts; ++p) {
+                const int at = 32 * p, col = n * kBn + at0 + at;
+                if (at >= left || !on) continue;
+                if (at + 32 <= left) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        Sector r0, r1;
+                        if (a.e.residual) {
+                            r0 = load_sector(res + (at + 16 * h) * (kF32 ? 4 : 2), a.e.wide_ok);
+                            if (kF32) r1 = load_sector(res + (at + 16 * h) * 4 + 32, a.e.wide_ok);
+                        }
+                        float f[16];
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) one_each(acc[p][8 * h + q], f[2 * q], f[2 * q + 1]);
+                        finish16<kF32>(a.e, a.e.gate, gate_off, y_off, 0, col + 16 * h, f, r0, kF32 ? r1 : r0);
+                    }
+                } else {
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) {
+                        const int cn = min(max(left - at - 8 * h, 0), 8);
+                        if (cn > 0) {
+                            norm::Raw8<true> r8;
+                            Columns cols;
+                            columns_begin(a.e, cols, col + 8 * h, cn);
+                            if (a.e.residual) load_residual(a.e, b, row, col + 8 * h, cn, r8);
+                            float f[8];
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) one_each(acc[p][4 * h + q], f[2 * q], f[2 * q + 1]);
+                            finish(a.e, cols, b, row, col + 8 * h, cn, f, r8);
+                        }
+                    }
+                }
+            }
+        }
+        if (a.splits > 1) {
+            tc_fence_before();
+            join_shares(a, base, first, split, half, abortp, tid - 128, 32 * kEpiWarps);
+        }
+    }
+
+    tc_fence_before();
+    __syncwarp();
+    cluster_sync();                      // nothing of the cluster reads this CTA's memory or arrives on its barriers any more
+    if (warp == 2) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+    }
+}
+
+// ---- a few rows ---------------------------------------------------------------------------------------
+// All that a few rows have to move is W, once: as in linear_rows.cuh a CTA takes 16 rows of W, its warps share k (here in blocks of 128), and lanes fetch W
+// straight into the registers of mma.m16n8k32.  x is taken to 8 bits by every CTA for itself, in the registers of the same instruction: a lane has 2 x 16 channels
+// of a block of one row, four lanes the block.  One launch.
+constexpr int kRowsMost8 = 16;
+struct RowsArgs8 {
+    Epilogue e;
+    const void* x; const uint8_t* w;
+    const float* xscale; const float* wscale;
+    int64_t xs[2], xss[3], w_stride, wss[2];
+    WsHeader* hdr;
+    int rows, per_batch, K, cols;        // rows over all batch entries; rows of an entry
+};
+
+__device__ __forceinline__ uint4 load_q16(const uint8_t* row, int k, int K) {
+    if (k + 16 <= K) {
+        uint4 v;
+        asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(row + k));
+        return v;
+    }
+    uint32_t t[4] = {0, 0, 0, 0};        // the last k of a row: what lies behind them is not the row's
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        if (k + i < K) t[i / 4] |= uint32_t(*reinterpret_cast<const volatile uint8_t*>(row + k + i)) << (8 * (i & 3));
+    return make_uint4(t[0], t[1], t[2], t[3]);
+}
+__device__ __forceinline__ void mma_16x8x32(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+enum { kXBf16 = 0, kXF32 = 1, kXE4m3 = 2 };
+// NT: column tiles of 8 rows of x; kWarps: warps that share k; kType: of x
+template <int NT, int kWarps, int kType>
+__global__ void __launch_bounds__(32 * kWarps) linear_fp8_rows_kernel(const RowsArgs8 a) {
+    __shared__ float sums[kWarps][16][8 * NT + 1];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+    grid_launch_dependents();
+    grid_wait();                         // launched while the kernel ahead drains
+    if (blockIdx.x == 0 && tid == 0) a.hdr->status = 0;
+    const int f0 = blockIdx.x * 16, blocks = (a.K + kBlock - 1) / kBlock;
+    const bool on0 = f0 + g < a.cols, on1 = f0 + g + 8 < a.cols;
+    const uint8_t* w0 = a.w + int64_t(f0 + g) * a.w_stride;
+    const uint8_t* w1 = w0 + 8 * a.w_stride;
+    const float* ws = a.wscale + (f0 / kBlock) * a.wss[0];
+    int64_t xo[NT], so[NT];
+    bool xon[NT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+        const int row = j * 8 + g;
+        xon[j] = row < a.rows;
+        const int b = xon[j] ? row / a.per_batch : 0, r = xon[j] ? row - b * a.per_batch : 0;
+        xo[j] = b * a.xs[0] + r * a.xs[1];
+        so[j] = b * a.xss[0] + r * a.xss[1];
+    }
+    float acc[NT][4];
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[j][i] = 0.f;
+    const uint4 zero = make_uint4(0, 0, 0, 0);
+    constexpr int U = NT == 1 ? 2 : 1;   // blocks in flight per warp
+    for (int blk = warp; blk < blocks; blk += kWarps * U) {
+        uint4 u0[U][2], u1[U][2];
+        float sw[U];
+#pragma unroll
+        for (int q = 0; q < U; ++q) {
+            const int kb = blk + q * kWarps;         // past the end: zeros
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int k = kb * kBlock + h * 64 + t * 16;
+                u0[q][h] = on0 ? load_q16(w0, k, a.K) : zero;
+                u1[q][h] = on1 ? load_q16(w1, k, a.K) : zero;
+            }
+            sw[q] = kb < blocks ? load_scale(ws + kb * a.wss[1]) : 0.f;
+        }
+#pragma unroll
+        for (int q = 0; q < U; ++q) {
+            const int kb = blk + q * kWarps;
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                uint4 xq[2];
+                float sx;
+                if constexpr (kType == kXE4m3) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) xq[h] = xon[j] ? load_q16(static_cast<const uint8_t*>(a.x) + xo[j], kb * kBlock + h * 64 + t * 16, a.K) : zero;
+                    sx = xon[j] && kb < blocks ? load_scale(a.xscale + so[j] + kb * a.xss[2]) : 0.f;
+                } else {
+                    fp8::Lane16<kType == kXF32> v[2];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int k = kb * kBlock + h * 64 + t * 16;
+                        v[h].load(a.x, xo[j] + k, xon[j] ? a.K - k : 0);
+                    }
+                    uint32_t m = max(v[0].most(), v[1].most());
+                    m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+                    m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+                    float inverse;
+                    fp8::scale_of(m, sx, inverse);
+                    xq[0] = v[0].quantized(inverse);
+                    xq[1] = v[1].quantized(inverse);
+                }
+                float d[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    mma_16x8x32(d, u0[q][h].x, u1[q][h].x, u0[q][h].y, u1[q][h].y, xq[h].x, xq[h].y);
+                    mma_16x8x32(d, u0[q][h].z, u1[q][h].z, u0[q][h].w, u1[q][h].w, xq[h].z, xq[h].w);
+                }
+                // d0, d1: feature g, rows 2t and 2t + 1 of x; d2, d3: feature g + 8
+                const float s0 = __shfl_sync(0xffffffffu, sx, 8 * t) * sw[q], s1 = __shfl_sync(0xffffffffu, sx, 8 * t + 4) * sw[q];
+                if (kb < blocks) {       // (0 times an infinite or NaN scale would not be nothing)
+                    acc[j][0] = fmaf(d[0], s0, acc[j][0]); acc[j][1] = fmaf(d[1], s1, acc[j][1]);
+                    acc[j][2] = fmaf(d[2], s0, acc[j][2]); acc[j][3] = fmaf(d[3], s1, acc[j][3]);
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sums[warp][g + 8 * (i >> 1)][j * 8 + 2 * t + (i & 1)] = acc[j][i];
+    __syncthreads();
+    auto param = [&](const void* p, int64_t i, int f32) { return f32 ? static_cast<const float*>(p)[i] : __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]); };
+    const int f = tid & 15, col = f0 + f;
+    for (int row = tid >> 4; row < a.rows && col < a.cols; row += 2 * kWarps) {
+        float z = 0.f;
+#pragma unroll
+        for (int k = 0; k < kWarps; ++k) z += sums[k][f][row];
+        const int b = row / a.per_batch, r = row - b * a.per_batch;
+        if (a.e.bias) z += param(a.e.bias, col, a.e.bias_f32);
+        float y = a.e.act == kActGeluTanh ? activation<kActGeluTanh>(z) : a.e.act == kActGelu ? activation<kActGelu>(z)
+                : a.e.act == kActSilu ? activation<kActSilu>(z) : z;
+        if (a.e.gate) y *= param(a.e.gate, b * a.e.gate_stride + col, a.e.gate_f32);
+        if (a.e.residual) y += param(a.e.residual, b * a.e.rs[0] + r * a.e.rs[1] + col, a.e.y_f32);
+        const int64_t off = b * a.e.ys[0] + r * a.e.ys[1] + col;
+        if (a.e.y_f32) static_cast<float*>(a.e.y)[off] = y;
+        else static_cast<__nv_bfloat16*>(a.e.y)[off] = __float2bfloat16_rn(y);
+    }
+}
+
+// ---- host side ------------------------------------------------------------------------------------
+// 3-D map over [batches, rows, cols] bytes with the columns contiguous: box = 128 columns x box_rows x 1, 128-byte swizzle, what lies outside reads as zero.
+inline bool make_map8(CUtensorMap* map, const Operand& o, int box_rows) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    cuuint64_t dims[3] = {cuuint64_t(o.cols), cuuint64_t(o.rows), cuuint64_t(o.batches)};
+    // the stride of an axis of one entry is never used, but has to be a valid value
+    const cuuint64_t row = o.rows > 1 ? cuuint64_t(o.row_stride) : cuuint64_t((o.cols + 15) / 16 * 16);
+    cuuint64_t strides[2] = {row, o.batches > 1 ? cuuint64_t(o.batch_stride) : row};
+    cuuint32_t box[3] = {kBlock, cuuint32_t(box_rows), 1};
+    cuuint32_t estr[3] = {1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(o.base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int kParts, bool kF32>
+inline carnator_status launch_stages8(const Operand& A, const Operand& B, Args8 a, cudaStream_t stream, char* err, size_t errlen) {
+    constexpr uint32_t kStage = kABytes8 + uint32_t(kParts * 32) * kBlock;
+    a.t.stages = int(std::min<uint32_t>(kMaxStages, kRingBytes / kStage));
+    static_assert(kRingBytes / kStage > 4 && kMaxStages > 4, "more stages than accumulators: a stage's barrier is not a phase ahead of the epilogue");
+    CUtensorMap ma, mb;
+    if (!make_map8(&ma, A, 128) || !make_map8(&mb, B, kParts * 32)) {
+        snprintf(err, errlen, "cuTensorMapEncodeTiled failed or is unavailable");
+        return CARNATOR_ERR_CUDA;
+    }
+    auto kern = linear_fp8_kernel<kParts, kF32>;
+    static SmemAllowed allowed;
+    const unsigned long long ctx = context_id();
+    if (!allowed.has(ctx)) {
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kSmemTc));
+        if (e != cudaSuccess) return cuda_error(e, "cudaFuncSetAttribute(linear_fp8_kernel)", err, errlen);
+        cudaFuncAttributes attr;         // the hand-over of registers only completes if the block owns them
+        const cudaError_t f = cudaFuncGetAttributes(&attr, kern);
+        if (f != cudaSuccess) return cuda_error(f, "cudaFuncGetAttributes(linear_fp8_kernel)", err, errlen);
+        if (attr.numRegs * kThreadsTc < 128 * 40 + 256 * 208) {
+            snprintf(err, errlen, "linear_fp8_kernel was built with %d registers per thread: too few for its setmaxnreg split", attr.numRegs);
+            return CARNATOR_ERR_UNSUPPORTED;
+        }
+        allowed.add(ctx);
+    }
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = unsigned(2 * a.t.splits); at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    const int clusters = a.t.splits > 1 ? a.t.tiles : std::min(a.t.tiles, 74);
+    cfg.gridDim = dim3(unsigned(clusters * 2 * a.t.splits)); cfg.blockDim = dim3(kThreadsTc); cfg.dynamicSmemBytes = kSmemTc; cfg.stream = stream;
+    cfg.attrs = at; cfg.numAttrs = 2;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, ma, mb, a);
+    if (e != cudaSuccess) return cuda_error(e, "linear_fp8_kernel", err, errlen);
+    return CARNATOR_OK;
+}
+
+// Columns of a tile (those of a thread lie within one block of the weight's rows) and pairs that share one: the least time by the model of linear_tcgen05.cuh,
+// for 128 k in the place of 64.
+inline Plan plan_of8(int64_t m_tiles, int64_t cols, int64_t blocks) {
+    Plan best = {256, 1};
+    double best_cost = 1e30;
+    for (int bn = 256; bn >= 64; bn /= 2) {
+        const int64_t tiles = m_tiles * ((cols + bn - 1) / bn);
+        for (int splits = 1; splits <= 4; splits *= 2) {
+            if ((splits == 2 && tiles > 32) || (splits == 4 && tiles > 14) || blocks < 4 * splits * (splits > 1)) break;
+            const int64_t turns = splits > 1 ? 1 : (tiles + 73) / 74;
+            const double k_ns = double((blocks + splits - 1) / splits) * (110 + 0.85 * bn), join = splits == 1 ? 0 : splits == 4 ? 4500 : tiles > 24 ? 4000 : 2500;
+            const double cost = double(turns) * std::max(k_ns, 500.0 + 4 * bn) + join;
+            if (cost < best_cost * 0.995) { best_cost = cost; best = {bn, splits}; }
+        }
+    }
+    return best;
+}
+
+inline carnator_status launch_product8(const Operand& A, const Operand& B, Args8 a, cudaStream_t stream, char* err, size_t errlen) {
+    a.t.k_batches = 1;
+    a.t.k_tiles = ceil_div(a.t.k_len, kBlock);
+    const Plan p = plan_of8(int64_t(a.t.batches) * a.t.tiles_m, a.t.cols, a.t.k_tiles);
+    a.t.bn = p.bn; a.t.splits = p.splits;
+    a.t.tiles_n = ceil_div(a.t.cols, a.t.bn);
+    const int64_t tiles = int64_t(a.t.batches) * a.t.tiles_m * a.t.tiles_n;
+    if (tiles > (int64_t(1) << 30)) return CARNATOR_ERR_UNSUPPORTED;
+    a.t.tiles = int(tiles);
+    a.t.group_m = 8;
+    const bool f = a.t.e.y_f32;
+    if (p.bn == 256) return f ? launch_stages8<4, true>(A, B, a, stream, err, errlen) : launch_stages8<4, false>(A, B, a, stream, err, errlen);
+    if (p.bn == 128) return f ? launch_stages8<2, true>(A, B, a, stream, err, errlen) : launch_stages8<2, false>(A, B, a, stream, err, errlen);
+    return f ? launch_stages8<1, true>(A, B, a, stream, err, errlen) : launch_stages8<1, false>(A, B, a, stream, err, errlen);
+}
+
+template <int NT, int kType>
+inline cudaError_t launch_rows8_warps(const RowsArgs8& a, cudaStream_t stream) {
+    const int grid = ceil_div(a.cols, 16);
+    if (grid <= 148) return launch_dependent(linear_fp8_rows_kernel<NT, 16, kType>, dim3(grid), dim3(512), 0, stream, a);
+    if (grid <= 3 * 148) return launch_dependent(linear_fp8_rows_kernel<NT, 8, kType>, dim3(grid), dim3(256), 0, stream, a);
+    return launch_dependent(linear_fp8_rows_kernel<NT, 4, kType>, dim3(grid), dim3(128), 0, stream, a);
+}
+template <int kType>
+inline cudaError_t launch_rows8(const RowsArgs8& a, cudaStream_t stream) {
+    return a.rows <= 8 ? launch_rows8_warps<1, kType>(a, stream) : launch_rows8_warps<2, kType>(a, stream);
+}
+
+}  // namespace lin8
+}  // namespace carnator

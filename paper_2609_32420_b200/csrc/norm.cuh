@@ -603,7 +603,7 @@ struct ReduceArgs {
 
 // 32 channels per CTA; 16 warps share the partial rows of an entry, and their shares are added in order.
 constexpr int kReduceWarps = 16;
-__global__ void __launch_bounds__(32 * kReduceWarps) norm_reduce_kernel(const ReduceArgs a) {
+static __global__ void __launch_bounds__(32 * kReduceWarps) norm_reduce_kernel(const ReduceArgs a) {
     __shared__ float sums[2][kReduceWarps][32];
     grid_launch_dependents();
     grid_wait();
