@@ -1,4 +1,5 @@
 // C-ABI entry points between a layer's attention, its projections and the residual stream: rotary positions, 8-bit operands and their product.
+#define CARNATOR_NO_ATTENTION_KERNELS
 #include <algorithm>
 #include <cmath>
 #include <cstdio>

@@ -198,19 +198,25 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constan
                 if (++s == a.stages) { s = 0; phase ^= 1u; }
                 tc_fence_after();
                 const uint32_t from = tmem + lane_base + uint32_t(u * kBn + at0);
-                float v[2][32];
-                tmem_ld32(from, v[0]);
+                float v0[32], v1[32];        // parts in turn: one on its way while the other is added
+                tmem_ld32(from, v0);
 #pragma unroll
                 for (int p = 0; p < kParts; ++p) {
-                    tmem_wait_ld(v[p & 1]);
-                    if (p + 1 < kParts) tmem_ld32(from + 32 * (p + 1), v[(p + 1) & 1]);
-                    else {               // this warp has read its part of the block
+                    if (p % 2 == 0) {
+                        tmem_wait_ld(v0);
+                        if (p + 1 < kParts) tmem_ld32(from + 32 * (p + 1), v1);
+                    } else {
+                        tmem_wait_ld(v1);
+                        if (p + 1 < kParts) tmem_ld32(from + 32 * (p + 1), v0);
+                    }
+                    if (p + 1 == kParts) {   // this warp has read its part of the block
                         tc_fence_before();
                         __syncwarp();
                         if (lane == 0) arrive_remote(read0 + 8 * u);
                     }
 #pragma unroll
-                    for (int q = 0; q < 16; ++q) acc[p][q] = norm::fma2(two(v[p & 1][2 * q], v[p & 1][2 * q + 1]), by, acc[p][q]);
+                    for (int q = 0; q < 16; ++q)
+                        acc[p][q] = norm::fma2(p % 2 == 0 ? two(v0[2 * q], v0[2 * q + 1]) : two(v1[2 * q], v1[2 * q + 1]), by, acc[p][q]);
                 }
             }
             __syncwarp();

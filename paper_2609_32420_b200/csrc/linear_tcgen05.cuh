@@ -20,7 +20,7 @@
 #pragma once
 #include <cuda.h>
 
-#include "tcgen05.cuh"
+#include "attn_tcgen05.cuh"
 #include "norm.cuh"
 
 namespace carnator {
