@@ -462,6 +462,51 @@ carnator_status carnator_rope_frequencies(const carnator_rope_scaling* scaling, 
 carnator_status carnator_rope(const void* X, const double* freq, const int32_t* positions, const carnator_rope_shape* shape, void* Y, void* stream);
 
 /* ------------------------------------------------------------------------
+ * The end of a block and the beginning of the next one in one pass: norm of the block's output, gate, residual stream, norm and modulation for what follows; and
+ * the gradients.  For every row (b, n) of C channels:
+ *   p = post(x) post_weight + post_bias,   s = residual_scale r + gate_b p,   y = (pre(s) weight + bias) (1 + scale_b) + shift_b
+ * post is CARNATOR_NORM_NONE (x itself), _LAYER ((x - mean) / sqrt(variance + post_eps)) or _RMS (x / sqrt(mean square + post_eps)); pre, with eps, is one of the latter
+ * two.  pre is taken of the unrounded s.  Statistics and sums in fp32.
+ *   R, S, dS, dR   device, of stream_dtype;  X, dX  of x_dtype;  Y, dY  of y_dtype;  [B,N,C] with the strides of `shape`: multiples of 16 bytes, base pointers 16-byte
+ *          aligned, channels contiguous.  Inputs may have a stride of 0; rows of an output do not overlap.  S may be R, dR may be dS, dX may be X (same strides)
+ *   post_weight, post_bias, weight, bias   device, [C] of weight_dtype, or NULL (1, 0);  gate, shift, scale  device, [B,C] of mod_dtype, or NULL (1, 0, 0).
+ *          These are aligned to their type only
+ *   stats  device, fp32 [4,B,N] contiguous: mean and reciprocal deviation of post, then of pre (an RMS norm's mean is 0, NONE has 0 and 1); written by the forward call if
+ *          given, read by the backward call.  A row with a NaN or an infinity: NaN as in carnator_layer_norm
+ * carnator_block_norm_backward, from dY, dS (the gradient that arrives on the stream, or NULL: none), the saved S and X:
+ *   G = dS + the gradient of y through pre,   dR = residual_scale G,   dX = the gradient of p through post, for gate_b G
+ *   dpost_weight, dpost_bias, dweight, dbias  device, fp32 [C];  dgate, dshift, dscale  device, fp32 [B,C] contiguous; any of them NULL: not wanted
+ *   ws     device workspace, 256-byte aligned, >= carnator_block_norm_backward_workspace_bytes (partial sums)
+ * Limits: C <= 8192, B <= 65535, B N <= 2^30.
+ * ------------------------------------------------------------------------ */
+enum { CARNATOR_NORM_NONE = 0, CARNATOR_NORM_LAYER = 1, CARNATOR_NORM_RMS = 2 };
+
+typedef struct carnator_block_norm_shape {
+    int32_t B, N, C;
+    int32_t post, pre;                      /* CARNATOR_NORM_* */
+    int32_t stream_dtype, x_dtype, y_dtype, weight_dtype, mod_dtype;      /* CARNATOR_DTYPE_F32 or _BF16 */
+    int64_t r_stride[2], x_stride[2], s_stride[2], y_stride[2];           /* element strides of (batch, token); y_stride is also dY's */
+    int64_t ds_stride[2], dr_stride[2], dx_stride[2];                     /* used by the backward call only, which does not use r_stride */
+    int64_t gate_stride, shift_stride, scale_stride;                      /* element strides of the batch axis; 0: one row for all entries */
+    float   post_eps, eps;                  /* >= 0 */
+    float   residual_scale;
+} carnator_block_norm_shape;
+
+carnator_status carnator_block_norm(const void* R, const void* X, const void* post_weight, const void* post_bias, const void* gate,
+                                    const void* weight, const void* bias, const void* shift, const void* scale,
+                                    const carnator_block_norm_shape* shape, void* S, void* Y, float* stats_opt, void* stream);
+
+size_t carnator_block_norm_backward_workspace_bytes(const carnator_block_norm_shape* shape);
+
+carnator_status carnator_block_norm_backward(const void* dY, const void* dS_opt, const void* S, const void* X, const float* stats,
+                                             const void* post_weight, const void* post_bias, const void* gate,
+                                             const void* weight, const void* bias, const void* scale,
+                                             const carnator_block_norm_shape* shape, void* dR, void* dX,
+                                             float* dpost_weight_opt, float* dpost_bias_opt, float* dgate_opt,
+                                             float* dweight_opt, float* dbias_opt, float* dshift_opt, float* dscale_opt,
+                                             void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
  * Projections with 8-bit operands (serving): e4m3 values with one fp32 scale per block of 128 in_features.
  *
  * carnator_quantize_fp8, for every row of X [B,N,K] (block_rows = 1: activations) or every 128 rows (block_rows = 128: a weight, B = 1) and every 128 of K:

@@ -35,6 +35,7 @@ EXPORTS = [
     "carnator_layer_norm", "carnator_layer_norm_backward_workspace_bytes", "carnator_layer_norm_backward",
     "carnator_linear_workspace_bytes", "carnator_linear", "carnator_linear_backward_workspace_bytes", "carnator_linear_backward",
     "carnator_rope_frequencies", "carnator_rope",
+    "carnator_block_norm", "carnator_block_norm_backward_workspace_bytes", "carnator_block_norm_backward",
     "carnator_quantize_fp8", "carnator_linear_fp8_workspace_bytes", "carnator_linear_fp8",
     "carnator_delta_e00", "carnator_context_discrepancy", "carnator_size_discrepancy", "carnator_shape_discrepancy",
     "carnator_compatibility_gate", "carnator_clopper_pearson_upper",
@@ -113,6 +114,18 @@ class RopeScaling(ctypes.Structure):
     _fields_ = [
         ("pairs", ctypes.c_int32 * 3), ("mode", ctypes.c_int32), ("theta", ctypes.c_double),
         ("factor", ctypes.c_double * 3), ("original", ctypes.c_double * 3), ("low", ctypes.c_double), ("high", ctypes.c_double),
+    ]
+
+
+class BlockNormShape(ctypes.Structure):
+    """Mirror of carnator_block_norm_shape."""
+    _fields_ = [
+        ("B", ctypes.c_int32), ("N", ctypes.c_int32), ("C", ctypes.c_int32), ("post", ctypes.c_int32), ("pre", ctypes.c_int32),
+        ("stream_dtype", ctypes.c_int32), ("x_dtype", ctypes.c_int32), ("y_dtype", ctypes.c_int32), ("weight_dtype", ctypes.c_int32), ("mod_dtype", ctypes.c_int32),
+        ("r_stride", ctypes.c_int64 * 2), ("x_stride", ctypes.c_int64 * 2), ("s_stride", ctypes.c_int64 * 2), ("y_stride", ctypes.c_int64 * 2),
+        ("ds_stride", ctypes.c_int64 * 2), ("dr_stride", ctypes.c_int64 * 2), ("dx_stride", ctypes.c_int64 * 2),
+        ("gate_stride", ctypes.c_int64), ("shift_stride", ctypes.c_int64), ("scale_stride", ctypes.c_int64),
+        ("post_eps", ctypes.c_float), ("eps", ctypes.c_float), ("residual_scale", ctypes.c_float),
     ]
 
 
@@ -226,6 +239,13 @@ def lib() -> ctypes.CDLL:
     L.carnator_rope_frequencies.argtypes = [ctypes.POINTER(RopeScaling), pd, pd]
     L.carnator_rope.restype = ctypes.c_int
     L.carnator_rope.argtypes = [vp, vp, vp, ctypes.POINTER(RopeShape), vp, vp]
+    pb = ctypes.POINTER(BlockNormShape)
+    L.carnator_block_norm.restype = ctypes.c_int
+    L.carnator_block_norm.argtypes = [vp] * 9 + [pb, vp, vp, vp, vp]
+    L.carnator_block_norm_backward_workspace_bytes.restype = sz
+    L.carnator_block_norm_backward_workspace_bytes.argtypes = [pb]
+    L.carnator_block_norm_backward.restype = ctypes.c_int
+    L.carnator_block_norm_backward.argtypes = [vp] * 11 + [pb] + [vp] * 10 + [sz, vp]
     L.carnator_quantize_fp8.restype = ctypes.c_int
     L.carnator_quantize_fp8.argtypes = [vp, ctypes.POINTER(QuantizeShape), vp, vp, vp]
     p8 = ctypes.POINTER(LinearFp8Shape)
@@ -604,7 +624,7 @@ class _Said:
     """What a record says of the tensors of its call, (type, shape, strides) each, and a copy of it for the library.  Made for each content of a record
     and never changed afterwards, so that records may be copied, changed between calls and shared among threads."""
     __slots__ = ("record", "ref", "x", "y", "dy", "dx", "residual", "z", "w", "dw", "vec", "shift", "scale", "gate", "bias", "stat", "freq", "pos", "q",
-                 "x_scale", "w_scale")
+                 "x_scale", "w_scale", "r", "s", "ds", "dr")
 
     def __init__(self, record):
         self.record, self.ref = record, ctypes.byref(record)
@@ -987,6 +1007,149 @@ def rope(X, freq, shape: RopeShape, positions=None, Y=None, stream=None):
     if st != OK:
         _check(st, "carnator_rope")
     return Y
+
+
+# ---- the end of a block and the beginning of the next one ----------------------------------------------
+NORM_NONE, NORM_LAYER, NORM_RMS = 0, 1, 2
+
+
+def make_block_norm_shape(R, X, S, Y, post_weight=None, post_bias=None, gate=None, weight=None, bias=None, shift=None, scale=None, dS=None, dR=None, dX=None,
+                          post: int = NORM_NONE, pre: int = NORM_LAYER, post_eps: float = 1e-6, eps: float = 1e-6, residual_scale: float = 1.0) -> BlockNormShape:
+    """Record of S = residual_scale R + gate post(X), Y = pre(S) modulated, all [B,N,C].  Y is the output of the forward call or the gradient dY that the backward call
+    gets; dS, dR, dX are the backward call's (strides of S, S and X unless given).  Types and strides are taken from the tensors; shift has the batch stride of scale
+    unless given, and the four vectors of C channels are of one type."""
+    for t, what in ((R, "R"), (X, "X"), (S, "S"), (Y, "Y"), (dS, "dS"), (dR, "dR"), (dX, "dX")):
+        if t is not None and t.dim() != 3:
+            raise ValueError(f"{what} must be [B,N,C]")
+        _last_axis(t, what)
+    s = BlockNormShape()
+    s.B, s.N, s.C = X.shape
+    s.post, s.pre, s.post_eps, s.eps, s.residual_scale = post, pre, post_eps, eps, residual_scale
+    s.r_stride, s.x_stride, s.s_stride, s.y_stride = (_rows_of(s.r_stride, t) for t in (R, X, S, Y))
+    s.ds_stride, s.dr_stride, s.dx_stride = _rows_of(s.ds_stride, dS, S), _rows_of(s.dr_stride, dR, S), _rows_of(s.dx_stride, dX, X)
+    stream = S if S is not None else R
+    s.stream_dtype, s.x_dtype, s.y_dtype = _dtype_code(stream, "S" if S is not None else "R"), _dtype_code(X, "X"), _dtype_code(Y, "Y")
+    vec = next((v for v in (post_weight, weight, post_bias, bias) if v is not None), None)
+    s.weight_dtype = DTYPE_F32 if vec is None else _dtype_code(vec, "weight")
+    mod = next((v for v in (gate, scale, shift) if v is not None), None)
+    s.mod_dtype = DTYPE_F32 if mod is None else _dtype_code(mod, "gate, shift and scale")
+    s.gate_stride = 0 if gate is None else gate.stride(0)
+    rows = scale if scale is not None else shift
+    s.scale_stride = 0 if rows is None else rows.stride(0)
+    s.shift_stride = s.scale_stride if shift is None else shift.stride(0)
+    return s
+
+
+@functools.lru_cache(maxsize=1024)
+def _block_said(of: bytes) -> _Said:
+    s = BlockNormShape.from_buffer_copy(of)
+    said = _Said(s)
+    size, stream, x, y, m = (s.B, s.N, s.C), _dtype_of(s.stream_dtype), _dtype_of(s.x_dtype), _dtype_of(s.y_dtype), _dtype_of(s.mod_dtype)
+    said.r, said.s, said.ds, said.dr = ((stream, size, (*st, 1)) for st in (s.r_stride, s.s_stride, s.ds_stride, s.dr_stride))
+    said.x, said.dx, said.y = (x, size, (*s.x_stride, 1)), (x, size, (*s.dx_stride, 1)), (y, size, (*s.y_stride, 1))
+    said.vec = (_dtype_of(s.weight_dtype), (s.C,), (1,))
+    said.gate, said.shift, said.scale = ((m, (s.B, s.C), (st, 1)) for st in (s.gate_stride, s.shift_stride, s.scale_stride))
+    said.stat = (_dtype_of(DTYPE_F32), (4, s.B, s.N), (s.B * s.N, s.N, 1))
+    return said
+
+
+@functools.lru_cache(maxsize=1024)
+def _block_packed(of: bytes, strides: tuple):
+    s = BlockNormShape.from_buffer_copy(of)
+    for name in strides:
+        of, size = _packed(s, name, (s.B, s.N), s.C)
+    return _block_said(of), size, s.C
+
+
+def _fit_vectors(said, dev, post_weight, post_bias, gate, weight, bias, shift, scale):
+    for t, what, to in ((post_weight, "post_weight", said.vec), (post_bias, "post_bias", said.vec), (weight, "weight", said.vec), (bias, "bias", said.vec),
+                        (gate, "gate", said.gate), (shift, "shift", said.shift), (scale, "scale", said.scale)):
+        if t is not None:
+            _fit(t, what, *to, dev)
+
+
+def block_norm(R, X, shape: BlockNormShape, post_weight=None, post_bias=None, gate=None, weight=None, bias=None, shift=None, scale=None, S=None, Y=None, stats=None,
+               stream=None):
+    """carnator_block_norm.  Returns (S, Y) [B,N,C] (its own, with rows on 16-byte boundaries, unless given; S may be R); stats fp32 [4,B,N] is written if given."""
+    dev = X.device
+    own = tuple(name for t, name in ((S, "s_stride"), (Y, "y_stride")) if t is None)
+    if own:                              # the caller's record stays as it is
+        said, size, n = _block_packed(bytes(shape), own)
+        S = _room(size, n, said.s[0], dev) if S is None else S
+        Y = _room(size, n, said.y[0], dev) if Y is None else Y
+    else:
+        said = _block_said(bytes(shape))
+    on = _stream_on(dev, stream)
+    _fit(R, "R", *said.r, dev)
+    _fit(X, "X", *said.x, dev)
+    _fit(S, "S", *said.s, dev)
+    _fit(Y, "Y", *said.y, dev)
+    _fit_vectors(said, dev, post_weight, post_bias, gate, weight, bias, shift, scale)
+    if stats is not None:
+        _fit(stats, "stats", *said.stat, dev)
+    st = lib().carnator_block_norm(_ptr(R), _ptr(X), _ptr(post_weight), _ptr(post_bias), _ptr(gate), _ptr(weight), _ptr(bias), _ptr(shift), _ptr(scale), said.ref,
+                                   _ptr(S), _ptr(Y), _ptr(stats), on)
+    if st != OK:
+        _check(st, "carnator_block_norm")
+    return S, Y
+
+
+def block_norm_backward_workspace_bytes(shape: BlockNormShape) -> int:
+    return int(lib().carnator_block_norm_backward_workspace_bytes(ctypes.byref(shape)))
+
+
+class BlockNormGrads(NamedTuple):
+    """Gradients of block_norm; those of vectors that it does not have, or that were not wanted, are None."""
+    dR: object
+    dX: object
+    dpost_weight: object
+    dpost_bias: object
+    dgate: object
+    dweight: object
+    dbias: object
+    dshift: object
+    dscale: object
+
+
+def block_norm_backward(dY, S, X, stats, shape: BlockNormShape, dS=None, post_weight=None, post_bias=None, gate=None, weight=None, bias=None, scale=None, dR=None, dX=None,
+                        want=("post_weight", "post_bias", "gate", "weight", "bias", "shift", "scale"), modulated=None, ws=None, stream=None) -> BlockNormGrads:
+    """carnator_block_norm_backward.  ``want`` names the vector gradients to compute, of those that there are: post_weight, post_bias, gate, weight, bias, and shift and
+    scale (if there is a scale, or ``modulated`` says that there is a shift only)."""
+    import torch
+    dev = X.device
+    own = tuple(name for t, name in ((dR, "dr_stride"), (dX, "dx_stride")) if t is None)
+    if own:
+        said, size, n = _block_packed(bytes(shape), own)
+        dR = _room(size, n, said.dr[0], dev) if dR is None else dR
+        dX = _room(size, n, said.dx[0], dev) if dX is None else dX
+    else:
+        said = _block_said(bytes(shape))
+    on = _stream_on(dev, stream)
+    _fit(dY, "dY", *said.y, dev)
+    _fit(S, "S", *said.s, dev)
+    _fit(X, "X", *said.x, dev)
+    _fit(dR, "dR", *said.dr, dev)
+    _fit(dX, "dX", *said.dx, dev)
+    _fit(stats, "stats", *said.stat, dev)
+    if dS is not None:
+        _fit(dS, "dS", *said.ds, dev)
+    _fit_vectors(said, dev, post_weight, post_bias, gate, weight, bias, None, scale)
+    B, C = said.record.B, said.record.C
+
+    def room(name, there, *size):
+        return torch.empty(size, dtype=torch.float32, device=dev) if there and name in want else None
+    mod = scale is not None if modulated is None else modulated
+    grads = (room("post_weight", post_weight is not None, C), room("post_bias", post_bias is not None, C), room("gate", gate is not None, B, C),
+             room("weight", weight is not None, C), room("bias", bias is not None, C), room("shift", mod, B, C), room("scale", mod, B, C))
+    if ws is None:
+        ws = _new_ws(block_norm_backward_workspace_bytes(said.record), dev)
+    elif ws.device != dev or not ws.is_contiguous():
+        raise ValueError(f"ws must be contiguous and on {dev}")
+    st = lib().carnator_block_norm_backward(_ptr(dY), _ptr(dS), _ptr(S), _ptr(X), _ptr(stats), _ptr(post_weight), _ptr(post_bias), _ptr(gate), _ptr(weight), _ptr(bias),
+                                            _ptr(scale), said.ref, _ptr(dR), _ptr(dX), *(_ptr(g) for g in grads), _ptr(ws), ws.numel(), on)
+    if st != OK:
+        _check(st, "carnator_block_norm_backward")
+    return BlockNormGrads(dR, dX, *grads)
 
 
 # ---- 8-bit operands and their product ---------------------------------------------------------------------

@@ -1,4 +1,4 @@
-// C-ABI entry points between a layer's attention, its projections and the residual stream: rotary positions, 8-bit operands and their product.
+// C-ABI entry points between a layer's attention, its projections and the residual stream: rotary positions, block norms, 8-bit operands and their product.
 #define CARNATOR_NO_ATTENTION_KERNELS
 #include <algorithm>
 #include <cmath>
@@ -7,6 +7,7 @@
 #include "carnator.h"
 #include "api.h"
 #include "rope.cuh"
+#include "block_norm.cuh"
 #include "fp8_quantize.cuh"
 #include "linear_fp8.cuh"
 
@@ -101,6 +102,124 @@ extern "C" carnator_status carnator_rope(const void* X, const double* freq, cons
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     const cudaError_t e = s->x_dtype == CARNATOR_DTYPE_F32 ? rope::launch<true>(a, s->B, half, stream) : rope::launch<false>(a, s->B, half, stream);
     if (e != cudaSuccess) return cuda_fail(e, "rope kernel");
+    count_launch();
+    return CARNATOR_OK;
+}
+
+// ------------------------------------------------------------------------------------------------
+// block norms
+// ------------------------------------------------------------------------------------------------
+namespace {
+carnator_status check_block_shape(const carnator_block_norm_shape* s) {
+    if (!s || s->B <= 0 || s->N <= 0 || s->C <= 0) return CARNATOR_ERR_INVALID_ARG;
+    if (s->post < CARNATOR_NORM_NONE || s->post > CARNATOR_NORM_RMS || s->pre < CARNATOR_NORM_LAYER || s->pre > CARNATOR_NORM_RMS) return CARNATOR_ERR_INVALID_ARG;
+    if (!dtype_ok(s->stream_dtype) || !dtype_ok(s->x_dtype) || !dtype_ok(s->y_dtype) || !dtype_ok(s->weight_dtype) || !dtype_ok(s->mod_dtype)) return CARNATOR_ERR_INVALID_ARG;
+    if (!(s->post_eps >= 0.f) || std::isinf(s->post_eps) || !(s->eps >= 0.f) || std::isinf(s->eps) || !std::isfinite(s->residual_scale)) return CARNATOR_ERR_INVALID_ARG;
+    if (s->gate_stride < 0 || s->shift_stride < 0 || s->scale_stride < 0) return CARNATOR_ERR_INVALID_ARG;
+    if (s->C > blk::kMostChannels || s->B > 65535 || int64_t(s->B) * s->N > (int64_t(1) << 30)) return CARNATOR_ERR_UNSUPPORTED;
+    return CARNATOR_OK;
+}
+bool block_axes_ok(const carnator_block_norm_shape* s, const int64_t st[2], int32_t dtype, bool written) {
+    const int64_t size[2] = {s->B, s->N};
+    return axes_ok(st, size, 2, s->C, dtype, written, false);
+}
+bool block_vectors_ok(const carnator_block_norm_shape* s, const void* w1, const void* b1, const void* w2, const void* b2, const void* gate, const void* shift, const void* scale) {
+    const size_t w = size_t(dtype_bytes(s->weight_dtype)), m = size_t(dtype_bytes(s->mod_dtype));
+    return aligned(w1, w) && aligned(b1, w) && aligned(w2, w) && aligned(b2, w) && aligned(gate, m) && aligned(shift, m) && aligned(scale, m);
+}
+// Strides as the kernels take them (that of an axis of one entry may be anything), parameters, what may be read 16 bytes at a time.
+void block_args(const carnator_block_norm_shape* s, blk::Args2& a, const void* w1, const void* b1, const void* gate, const void* w2, const void* b2, const void* shift, const void* scale) {
+    a.w1 = w1; a.b1 = b1; a.gate = gate; a.w2 = w2; a.b2 = b2; a.shift = shift; a.scale = scale;
+    a.gate_stride = s->B == 1 ? 0 : s->gate_stride; a.shift_stride = s->B == 1 ? 0 : s->shift_stride; a.scale_stride = s->B == 1 ? 0 : s->scale_stride;
+    a.B = s->B; a.N = s->N; a.C = s->C;
+    a.post = s->post; a.pre = s->pre;
+    a.w_f32 = s->weight_dtype == CARNATOR_DTYPE_F32; a.mod_f32 = s->mod_dtype == CARNATOR_DTYPE_F32;
+    a.vec_ok = vec16(w1, 0, s->weight_dtype) && vec16(b1, 0, s->weight_dtype) && vec16(w2, 0, s->weight_dtype) && vec16(b2, 0, s->weight_dtype) &&
+               vec16(gate, a.gate_stride, s->mod_dtype) && vec16(shift, a.shift_stride, s->mod_dtype) && vec16(scale, a.scale_stride, s->mod_dtype);
+    a.alpha = s->residual_scale; a.eps1 = s->post_eps; a.eps2 = s->eps; a.inv_c = 1.0f / float(s->C);
+}
+void block_strides(const carnator_block_norm_shape* s, int64_t (&to)[2], const int64_t (&from)[2]) {
+    to[0] = s->B == 1 ? 0 : from[0];
+    to[1] = s->N == 1 ? 0 : from[1];
+}
+}  // namespace
+
+extern "C" carnator_status carnator_block_norm(const void* R, const void* X, const void* post_weight, const void* post_bias, const void* gate,
+                                               const void* weight, const void* bias, const void* shift, const void* scale,
+                                               const carnator_block_norm_shape* s, void* S, void* Y, float* stats_opt, void* stream_) {
+    carnator_status st = check_block_shape(s);
+    if (st != CARNATOR_OK) return st;
+    if (!R || !X || !S || !Y || !aligned(R, 16) || !aligned(X, 16) || !aligned(S, 16) || !aligned(Y, 16) || !aligned(stats_opt, 4)) return CARNATOR_ERR_INVALID_ARG;
+    if (!block_vectors_ok(s, post_weight, post_bias, weight, bias, gate, shift, scale)) return CARNATOR_ERR_INVALID_ARG;
+    if (!block_axes_ok(s, s->r_stride, s->stream_dtype, false) || !block_axes_ok(s, s->x_stride, s->x_dtype, false) || !block_axes_ok(s, s->s_stride, s->stream_dtype, true) ||
+        !block_axes_ok(s, s->y_stride, s->y_dtype, true)) return CARNATOR_ERR_INVALID_ARG;
+    st = check_device();
+    if (st != CARNATOR_OK) return st;
+    blk::Args2 a = {};
+    block_args(s, a, post_weight, post_bias, gate, weight, bias, shift, scale);
+    a.r = R; a.x = X; a.s = S; a.y = Y; a.stats = stats_opt;
+    block_strides(s, a.rs, s->r_stride); block_strides(s, a.xs, s->x_stride); block_strides(s, a.ss, s->s_stride); block_strides(s, a.ys, s->y_stride);
+    a.wide_s = rows32(S, a.ss, s->stream_dtype); a.wide_y = rows32(Y, a.ys, s->y_dtype);
+    const blk::Form2 f = blk::form2_of(s->C, false);
+    a.chunks = blk::chunks2_of(f, s->B, s->C, s->N, false);
+    const cudaError_t e = blk::launch2<false>(a, f, s->stream_dtype == CARNATOR_DTYPE_F32, s->x_dtype == CARNATOR_DTYPE_F32, s->y_dtype == CARNATOR_DTYPE_F32,
+                                              static_cast<cudaStream_t>(stream_));
+    if (e != cudaSuccess) return cuda_fail(e, "block_forward_kernel");
+    count_launch();
+    return CARNATOR_OK;
+}
+
+extern "C" size_t carnator_block_norm_backward_workspace_bytes(const carnator_block_norm_shape* s) {
+    if (check_block_shape(s) != CARNATOR_OK) return 0;
+    return align256(size_t(s->B) * blk::chunks2_of(blk::form2_of(s->C, true), s->B, s->C, s->N, true) * 4 * s->C * 4);
+}
+
+extern "C" carnator_status carnator_block_norm_backward(const void* dY, const void* dS_opt, const void* S, const void* X, const float* stats,
+                                                        const void* post_weight, const void* post_bias, const void* gate,
+                                                        const void* weight, const void* bias, const void* scale,
+                                                        const carnator_block_norm_shape* s, void* dR, void* dX,
+                                                        float* dpost_weight_opt, float* dpost_bias_opt, float* dgate_opt,
+                                                        float* dweight_opt, float* dbias_opt, float* dshift_opt, float* dscale_opt,
+                                                        void* ws, size_t ws_bytes, void* stream_) {
+    carnator_status st = check_block_shape(s);
+    if (st != CARNATOR_OK) return st;
+    if (!dY || !S || !X || !stats || !dR || !dX) return CARNATOR_ERR_INVALID_ARG;
+    if (!aligned(dY, 16) || !aligned(dS_opt, 16) || !aligned(S, 16) || !aligned(X, 16) || !aligned(dR, 16) || !aligned(dX, 16) || !aligned(stats, 4)) return CARNATOR_ERR_INVALID_ARG;
+    float* const wanted[7] = {dpost_weight_opt, dpost_bias_opt, dgate_opt, dweight_opt, dbias_opt, dshift_opt, dscale_opt};
+    bool sums = false;
+    for (float* p : wanted) {
+        if (!aligned(p, 4)) return CARNATOR_ERR_INVALID_ARG;
+        sums = sums || p;
+    }
+    if (!block_vectors_ok(s, post_weight, post_bias, weight, bias, gate, nullptr, scale)) return CARNATOR_ERR_INVALID_ARG;
+    if (!block_axes_ok(s, s->y_stride, s->y_dtype, false) || (dS_opt && !block_axes_ok(s, s->ds_stride, s->stream_dtype, false)) ||
+        !block_axes_ok(s, s->s_stride, s->stream_dtype, false) || !block_axes_ok(s, s->x_stride, s->x_dtype, false) ||
+        !block_axes_ok(s, s->dr_stride, s->stream_dtype, true) || !block_axes_ok(s, s->dx_stride, s->x_dtype, true)) return CARNATOR_ERR_INVALID_ARG;
+    if (!ws || !aligned(ws, 256) || ws_bytes < carnator_block_norm_backward_workspace_bytes(s)) return CARNATOR_ERR_WORKSPACE;
+    st = check_device();
+    if (st != CARNATOR_OK) return st;
+    blk::Args2 a = {};
+    block_args(s, a, post_weight, nullptr, gate, weight, nullptr, nullptr, scale);
+    a.dy = dY; a.r = dS_opt; a.s = const_cast<void*>(S); a.x = X; a.dr = dR; a.dx = dX;
+    a.stats = const_cast<float*>(stats);
+    a.part = sums ? static_cast<float*>(ws) : nullptr;
+    block_strides(s, a.dys, s->y_stride); block_strides(s, a.rs, s->ds_stride); block_strides(s, a.ss, s->s_stride); block_strides(s, a.xs, s->x_stride);
+    block_strides(s, a.drs, s->dr_stride); block_strides(s, a.dxs, s->dx_stride);
+    a.wide_s = rows32(dR, a.drs, s->stream_dtype); a.wide_dx = rows32(dX, a.dxs, s->x_dtype);
+    const blk::Form2 f = blk::form2_of(s->C, true);
+    a.chunks = blk::chunks2_of(f, s->B, s->C, s->N, true);
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    const cudaError_t e = blk::launch2<true>(a, f, s->stream_dtype == CARNATOR_DTYPE_F32, s->x_dtype == CARNATOR_DTYPE_F32, s->y_dtype == CARNATOR_DTYPE_F32, stream);
+    if (e != cudaSuccess) return cuda_fail(e, "block_backward_kernel");
+    count_launch();
+    if (!sums) return CARNATOR_OK;
+    blk::ReduceArgs2 r = {};
+    r.part = a.part;
+    r.w1 = post_weight; r.b1 = post_bias; r.gate = gate; r.w2 = weight; r.b2 = bias; r.scale = scale;
+    r.dw1 = dpost_weight_opt; r.db1 = dpost_bias_opt; r.dgate = dgate_opt; r.dw2 = dweight_opt; r.db2 = dbias_opt; r.dshift = dshift_opt; r.dscale = dscale_opt;
+    r.gate_stride = a.gate_stride; r.scale_stride = a.scale_stride;
+    r.B = s->B; r.chunks = a.chunks; r.C = s->C; r.w_f32 = a.w_f32; r.mod_f32 = a.mod_f32;
+    CUDA_TRY(launch_dependent(blk::block_reduce_kernel, dim3(unsigned(ceil_div(s->C, 32))), dim3(32 * norm::kReduceWarps), 0, stream, r));
     count_launch();
     return CARNATOR_OK;
 }

@@ -105,6 +105,50 @@ def test_rope_frequencies_refuse():
         cn.rope_frequencies((1, 1, 1, 1))
 
 
+# ---- block norms -------------------------------------------------------------------------------------------
+def block_shape(**kw):
+    x = torch.empty((2, 40, 128), dtype=torch.bfloat16)
+    return changed(cn.make_block_norm_shape(x, x, x, x, post=cn.NORM_RMS), kw)
+
+
+def call_block(s, R=P, X=P, w=P, gate=P, shift=P, S=P, Y=P, stats=P):
+    return cn.lib().carnator_block_norm(R, X, w, P, gate, P, P, shift, P, ctypes.byref(s), S, Y, stats, None)
+
+
+def call_block_backward(s, dY=P, dS=P, S=P, X=P, stats=P, w=P, gate=P, dR=P, dX=P, dw=P, dgate=P, ws=P, ws_bytes=BIG):
+    return cn.lib().carnator_block_norm_backward(dY, dS, S, X, stats, w, P, gate, P, P, P, ctypes.byref(s), dR, dX, dw, P, dgate, P, P, P, P, ws, ws_bytes, None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(B=0), BAD), (dict(N=0), BAD), (dict(C=-8), BAD), (dict(post=3), BAD), (dict(post=-1), BAD), (dict(pre=0), BAD), (dict(pre=3), BAD), (dict(stream_dtype=2), BAD),
+    (dict(x_dtype=2), BAD), (dict(y_dtype=-1), BAD), (dict(weight_dtype=3), BAD), (dict(mod_dtype=2), BAD), (dict(eps=-1e-6), BAD), (dict(post_eps=float("nan")), BAD),
+    (dict(eps=float("inf")), BAD), (dict(residual_scale=float("nan")), BAD), (dict(residual_scale=float("inf")), BAD), (dict(gate_stride=-1), BAD), (dict(shift_stride=-4), BAD),
+    (dict(scale_stride=-4), BAD), (dict(C=8193), NOT), (dict(B=65536), NOT), (dict(B=1 << 15, N=1 << 16), NOT),
+    (dict(x_stride=(1, 132)), BAD), (dict(x_stride=(0, -8)), BAD), (dict(s_stride=(0, 1 << 39)), BAD), (dict(y_stride=(1, 4)), BAD),
+])
+def test_block_norm_refuses_bad_records(kw, status):
+    s = block_shape(**kw)
+    expect(status, lambda: call_block(s))
+    expect(status, lambda: call_block_backward(s))
+    if not any(k.endswith("_stride") and isinstance(v, tuple) for k, v in kw.items()):
+        assert cn.block_norm_backward_workspace_bytes(s) == 0
+
+
+def test_block_norm_refuses_bad_pointers_and_overlapping_outputs():
+    for kw in (dict(R=None), dict(X=None), dict(S=None), dict(Y=None), dict(R=P + 8), dict(X=P + 2), dict(S=P + 4), dict(Y=P + 8), dict(w=P + 1), dict(gate=P + 2), dict(shift=P + 1), dict(stats=P + 2)):
+        expect(BAD, lambda: call_block(block_shape(), **kw))
+    for kw in (dict(s_stride=(1, 0)), dict(s_stride=(0, 0)), dict(y_stride=(1, 64)), dict(r_stride=(1, 60))):
+        expect(BAD, lambda: call_block(block_shape(**kw)))
+    for kw in (dict(dY=None), dict(S=None), dict(X=None), dict(stats=None), dict(dR=None), dict(dX=None), dict(dS=P + 8), dict(dY=P + 2), dict(dR=P + 8), dict(dX=P + 8), dict(dw=P + 2), dict(dgate=P + 1)):
+        expect(BAD, lambda: call_block_backward(block_shape(), **kw))
+    for kw in (dict(dr_stride=(1, 0)), dict(dx_stride=(0, 128)), dict(ds_stride=(1, 4)), dict(s_stride=(1, -8))):
+        expect(BAD, lambda: call_block_backward(block_shape(**kw)))
+    need = cn.block_norm_backward_workspace_bytes(block_shape())
+    assert need >= 4 * 128 * 4
+    for kw in (dict(ws=None), dict(ws=P + 64), dict(ws_bytes=need - 1)):
+        expect(cn.ERR_WORKSPACE, lambda: call_block_backward(block_shape(), **kw))
+
+
 # ---- 8-bit operands ---------------------------------------------------------------------------------------
 def quantize_shape(tile=1, **kw):
     x = torch.empty((2, 300, 200), dtype=torch.bfloat16)
@@ -164,7 +208,7 @@ def test_fp8_product_refuses():
 def test_calls_without_a_gpu_fail_loudly():
     if torch.cuda.is_available():
         pytest.skip("a GPU is present")
-    for st in (call_rope(rope_shape()), call_quantize(quantize_shape()), call_fp8(fp8_shape())):
+    for st in (call_rope(rope_shape()), call_block(block_shape()), call_block_backward(block_shape()), call_quantize(quantize_shape()), call_fp8(fp8_shape())):
         assert st in (cn.ERR_UNSUPPORTED, cn.ERR_CUDA)
 
 
@@ -188,6 +232,12 @@ def test_python_calls_check_tensors_against_the_record():
             lambda: cn.linear_fp8(t, w, sc, ls, Y=y, ws=torch.empty(512, dtype=torch.uint8)[::2]), lambda: cn.make_linear_fp8_shape(t, w.to(bf), sc, y),
             lambda: cn.make_linear_fp8_shape(t.to(e4), w, sc, y), lambda: cn.make_linear_fp8_shape(t, w, sc, y, x_scale=torch.empty((1, 6, 1))), lambda: cn.make_linear_fp8_shape(t, w[:, :32], sc, y),
             lambda: cn.make_linear_fp8_shape(t, w, sc[0], y)]
+    v, st = torch.empty(64), torch.empty((4, 1, 6))
+    bs = cn.make_block_norm_shape(t, t, t, t, weight=v)
+    bad += [lambda: cn.block_norm(t.float(), t, bs), lambda: cn.block_norm(t, t[:, :5], bs), lambda: cn.block_norm(t, t, bs, weight=v[:63]), lambda: cn.block_norm(t, t, bs, bias=v.to(bf)),
+            lambda: cn.block_norm(t, t, bs, gate=torch.empty((2, 64))), lambda: cn.block_norm(t, t, bs, S=torch.empty((1, 6, 128), dtype=bf)[..., :64][:, ::2]),
+            lambda: cn.block_norm(t, t, bs, stats=st[:3]), lambda: cn.block_norm_backward(t, t, t, st.double(), bs), lambda: cn.block_norm_backward(t, t, t, st, bs, dS=t.float()),
+            lambda: cn.block_norm_backward(t, t, t, st, bs, ws=torch.empty(1 << 20, dtype=torch.uint8)[::2]), lambda: cn.make_block_norm_shape(t[0], t, t, t), lambda: cn.make_block_norm_shape(t, t.half(), t, t)]
     for call in bad:
         with pytest.raises(ValueError):
             call()
