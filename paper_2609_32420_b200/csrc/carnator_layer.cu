@@ -281,26 +281,15 @@ carnator_status check_fp8_shape(const carnator_linear_fp8_shape* s) {
 }
 bool few_rows(const carnator_linear_fp8_shape* s) { return int64_t(s->B) * s->N <= lin8::kRowsMost8; }
 
-// Status header, then X in 8 bits (rows of whole blocks) and its scales (rows beside each other), where the call makes them.
-struct Fp8Ws { uint8_t* q; float* scale; int64_t q_stride, scale_stride; size_t bytes; };
-Fp8Ws fp8_ws_layout(void* base, const carnator_linear_fp8_shape* s) {
-    Fp8Ws w = {};
-    char* p = static_cast<char*>(base);
-    size_t off = align256(sizeof(WsHeader));
-    if (s->x_dtype != CARNATOR_DTYPE_E4M3 && !few_rows(s)) {
-        const int64_t rows = int64_t(s->B) * s->N, blocks = ceil_div(s->in_features, fp8::kBlock);
-        w.q_stride = blocks * fp8::kBlock;
-        w.scale_stride = (rows + 31) / 32 * 32;
-        w.q = reinterpret_cast<uint8_t*>(p + off);       off += align256(size_t(rows) * w.q_stride);
-        w.scale = reinterpret_cast<float*>(p + off);     off += align256(size_t(w.scale_stride) * blocks * 4);
-    }
-    w.bytes = off;
-    return w;
+// Status header, then what the two kernels of more than a few rows pass on.
+lin8::Room8 fp8_room(void* ws, const carnator_linear_fp8_shape* s) {
+    return lin8::room8_of(static_cast<char*>(ws) + align256(sizeof(WsHeader)), s->B, s->N, s->out_features, s->in_features, s->x_dtype != CARNATOR_DTYPE_E4M3);
 }
+size_t fp8_ws_bytes(const carnator_linear_fp8_shape* s) { return align256(sizeof(WsHeader)) + (few_rows(s) ? 0 : fp8_room(nullptr, s).bytes); }
 }  // namespace
 
 extern "C" size_t carnator_linear_fp8_workspace_bytes(const carnator_linear_fp8_shape* s) {
-    return check_fp8_shape(s) == CARNATOR_OK ? fp8_ws_layout(nullptr, s).bytes : 0;
+    return check_fp8_shape(s) == CARNATOR_OK ? fp8_ws_bytes(s) : 0;
 }
 
 extern "C" carnator_status carnator_linear_fp8(const void* X, const float* x_scale, const void* W, const float* w_scale, const void* bias, const void* gate, const void* residual,
@@ -318,9 +307,7 @@ extern "C" carnator_status carnator_linear_fp8(const void* X, const float* x_sca
         (residual && !rows_ok(s->residual_stride, s->out_features, s->y_dtype, false)) || (ready && !scales_ok(s->x_scale_stride, xsize, 3, false)) ||
         !scales_ok(s->w_scale_stride, wsize, 2, false)) return CARNATOR_ERR_INVALID_ARG;
     if (s->out_features > 1 && (s->w_stride < s->in_features || s->w_stride % 16 || s->w_stride > kMostStride)) return CARNATOR_ERR_INVALID_ARG;
-    if (!ws || !aligned(ws, 256)) return CARNATOR_ERR_WORKSPACE;
-    const Fp8Ws w = fp8_ws_layout(ws, s);
-    if (ws_bytes < w.bytes) return CARNATOR_ERR_WORKSPACE;
+    if (!ws || !aligned(ws, 256) || ws_bytes < fp8_ws_bytes(s)) return CARNATOR_ERR_WORKSPACE;
     st = check_device();
     if (st != CARNATOR_OK) return st;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
@@ -359,41 +346,35 @@ extern "C" carnator_status carnator_linear_fp8(const void* X, const float* x_sca
     // Batch entries that follow each other evenly are one run of rows.
     auto runs = [&](const int64_t* st) { return s->B == 1 || s->N == 1 || st[0] == int64_t(s->N) * st[1]; };
     auto run_stride = [&](const int64_t* st) { return s->N == 1 ? st[0] : st[1]; };
+    const lin8::Room8 room = fp8_room(ws, s);
     lin8::Args8 a = {};
+    lin8::PrepareArgs p = {};
     a.t.e = e;
     a.t.hdr = static_cast<WsHeader*>(ws);
-    a.t.clears = ready;
-    a.wscale = w_scale; a.wss[0] = wss[0]; a.wss[1] = wss[1];
-    a.xscale = x_scale;
-    for (int i = 0; i < 3; ++i) a.xss[i] = xss[i];
+    a.wscale = p.wscale = w_scale;
+    for (int i = 0; i < 2; ++i) a.wss[i] = p.wss[i] = wss[i];
+    a.t.batches = s->B; a.t.rows = s->N;
     lin::Operand A = {X, s->B, s->N, s->in_features, xs[0], xs[1]};
     if (!ready) {
-        fp8::QuantArgs q = {};
-        q.x = X; q.q = w.q; q.scale = w.scale;
-        q.xs[0] = xs[0]; q.xs[1] = xs[1];
-        q.qs[0] = w.q_stride * s->N; q.qs[1] = w.q_stride;
-        q.ss[0] = s->N; q.ss[1] = 1; q.ss[2] = w.scale_stride;
-        q.batches = s->B; q.rows = s->N; q.cols = s->in_features; q.blocks = blocks;
-        if (runs(xs)) { q.batches = 1; q.rows = int(rows); q.xs[1] = run_stride(xs); }
-        q.clears = a.t.hdr;
-        const cudaError_t err = fp8::launch_quantize(q, s->x_dtype == CARNATOR_DTYPE_F32, 1, stream);
-        if (err != cudaSuccess) return cuda_fail(err, "quantize_rows_kernel");
-        count_launch();
-        A.base = w.q; A.batch_stride = w.q_stride * s->N; A.row_stride = w.q_stride;
-        a.xscale = w.scale; a.xss[0] = s->N; a.xss[1] = 1; a.xss[2] = w.scale_stride;
+        p.q.x = X; p.q.q = room.q;
+        p.q.xs[0] = xs[0]; p.q.xs[1] = xs[1];
+        p.q.qs[0] = room.q_stride * s->N; p.q.qs[1] = room.q_stride;
+        A.base = room.q; A.batch_stride = p.q.qs[0]; A.row_stride = p.q.qs[1];
     }
-    a.t.batches = s->B; a.t.rows = s->N;
-    if (runs(ys) && (!residual || runs(rs)) && (!ready || (runs(xs) && runs(xss)))) {
+    if (runs(xs) && runs(ys) && (!residual || runs(rs)) && (!ready || runs(xss))) {
         a.t.batches = 1; a.t.rows = int(rows);
         A.batches = 1; A.rows = rows;
-        if (ready) { A.row_stride = run_stride(xs); a.xss[1] = run_stride(xss); }
+        if (ready) { A.row_stride = run_stride(xs); xss[1] = run_stride(xss); }
+        else p.q.xs[1] = run_stride(xs);
         a.t.e.ys[1] = run_stride(ys); a.t.e.rs[1] = run_stride(rs);
     }
+    a.xscale = p.xscale = x_scale;
+    for (int i = 0; i < 3; ++i) a.xss[i] = p.xss[i] = xss[i];
     const lin::Operand Bo = {W, 1, s->out_features, s->in_features, 0, s->w_stride};
     a.t.cols = s->out_features;
-    a.t.tiles_m = ceil_div(a.t.rows, lin::kTileM);
     a.t.k_len = s->in_features;
-    st = lin8::launch_product8(A, Bo, a, stream, g_cuda_error, sizeof(g_cuda_error));
-    if (st == CARNATOR_OK) count_launch();
+    const int type = ready ? lin8::kXE4m3 : s->x_dtype == CARNATOR_DTYPE_F32 ? lin8::kXF32 : lin8::kXBf16;
+    st = lin8::launch_product8(A, Bo, room, a, p, type, stream, g_cuda_error, sizeof(g_cuda_error));
+    if (st == CARNATOR_OK) g_launches.fetch_add(2, std::memory_order_relaxed);
     return st;
 }

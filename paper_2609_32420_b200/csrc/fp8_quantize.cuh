@@ -96,20 +96,18 @@ struct QuantArgs {
     int64_t xs[2], qs[2];                // (batch, row)
     int64_t ss[3];                       // (batch, row or block of rows, block)
     int batches, rows, cols, blocks;
-    WsHeader* clears;                    // a call's first kernel clears its status word
 };
 
-// A scale per row: 8 lanes a block, kAhead blocks of a row on their way per lane.  `groups` of 8 lanes in the grid walk over (row, run of kAhead blocks).
+// A scale per row: 8 lanes a block, kAhead blocks of a row on their way per lane.  The groups of 8 lanes of `ctas` CTAs walk over (row, run of kAhead blocks);
+// put(row, block, scale) is called by one lane of each.
 constexpr int kRowThreads = 256;
-template <bool F32, int kAhead>
-__global__ void __launch_bounds__(kRowThreads) quantize_rows_kernel(const QuantArgs a) {
-    const int l = threadIdx.x % kLanes, b = blockIdx.y, runs = (a.blocks + kAhead - 1) / kAhead;
-    grid_launch_dependents();
-    grid_wait();
-    if (a.clears && blockIdx.x == 0 && b == 0 && threadIdx.x == 0) a.clears->status = 0;
-    const int64_t items = int64_t(a.rows) * runs, step = int64_t(gridDim.x) * (kRowThreads / kLanes);
+template <bool F32> constexpr int kAheadOf = F32 ? 2 : 4;
+template <bool F32, int kAhead, typename Put>
+__device__ __forceinline__ void quantize_rows(const QuantArgs& a, int b, int cta, int ctas, Put put) {
+    const int l = threadIdx.x % kLanes, runs = (a.blocks + kAhead - 1) / kAhead;
+    const int64_t items = int64_t(a.rows) * runs, step = int64_t(ctas) * (kRowThreads / kLanes);
     // warp-uniform trips: the lanes of a warp exchange their largest values
-    for (int64_t first = int64_t(blockIdx.x) * (kRowThreads / kLanes) + threadIdx.x / 32 * (32 / kLanes); first < items; first += step) {
+    for (int64_t first = int64_t(cta) * (kRowThreads / kLanes) + threadIdx.x / 32 * (32 / kLanes); first < items; first += step) {
         const int64_t item = first + threadIdx.x % 32 / kLanes;
         const bool on = item < items;
         const int row = on ? int(item / runs) : 0, blk = on ? int(item - int64_t(row) * runs) * kAhead : 0;
@@ -128,10 +126,17 @@ __global__ void __launch_bounds__(kRowThreads) quantize_rows_kernel(const QuantA
             if (n[k] > 0) {
                 const int col = (blk + k) * kBlock + l * kLaneChannels;
                 store_q(a.q + b * a.qs[0] + row * a.qs[1] + col, v[k].quantized(inverse), n[k]);
-                if (l == 0) a.scale[b * a.ss[0] + row * a.ss[1] + (blk + k) * a.ss[2]] = scale;
+                if (l == 0) put(row, blk + k, scale);
             }
         }
     }
+}
+template <bool F32, int kAhead>
+__global__ void __launch_bounds__(kRowThreads) quantize_rows_kernel(const QuantArgs a) {
+    const int b = blockIdx.y;
+    grid_launch_dependents();
+    grid_wait();
+    quantize_rows<F32, kAhead>(a, b, blockIdx.x, gridDim.x, [&](int row, int blk, float scale) { a.scale[b * a.ss[0] + row * a.ss[1] + blk * a.ss[2]] = scale; });
 }
 
 // A scale per 128 x 128: a CTA per block, four rows per lane.
@@ -173,14 +178,16 @@ __global__ void __launch_bounds__(kTileThreads) quantize_tiles_kernel(const Quan
 }
 
 // ---- host side ------------------------------------------------------------------------------------
-template <bool F32, int kAhead>
-inline cudaError_t launch_rows(const QuantArgs& a, cudaStream_t stream) {
-    const int64_t items = int64_t(a.rows) * ceil_div(a.blocks, kAhead), ctas = (items + kRowThreads / kLanes - 1) / (kRowThreads / kLanes);
-    const dim3 grid(unsigned(std::min<int64_t>(ctas, 148 * 8)), unsigned(a.batches));
-    return launch_dependent(quantize_rows_kernel<F32, kAhead>, grid, dim3(kRowThreads), 0, stream, a);
+inline int row_ctas(const QuantArgs& a, bool f32) {      // one wave at most
+    const int64_t items = int64_t(a.rows) * ceil_div(a.blocks, f32 ? kAheadOf<true> : kAheadOf<false>), ctas = (items + kRowThreads / kLanes - 1) / (kRowThreads / kLanes);
+    return int(std::min<int64_t>(ctas, 148 * 8));
 }
 inline cudaError_t launch_quantize(const QuantArgs& a, bool f32, int block_rows, cudaStream_t stream) {
-    if (block_rows == 1) return f32 ? launch_rows<true, 2>(a, stream) : launch_rows<false, 4>(a, stream);
+    if (block_rows == 1) {
+        const dim3 grid(unsigned(row_ctas(a, f32)), unsigned(a.batches));
+        return f32 ? launch_dependent(quantize_rows_kernel<true, kAheadOf<true>>, grid, dim3(kRowThreads), 0, stream, a)
+                   : launch_dependent(quantize_rows_kernel<false, kAheadOf<false>>, grid, dim3(kRowThreads), 0, stream, a);
+    }
     const dim3 grid(unsigned(ceil_div(a.rows, kBlock) * a.blocks), unsigned(a.batches));
     return f32 ? launch_dependent(quantize_tiles_kernel<true>, grid, dim3(kTileThreads), 0, stream, a)
                : launch_dependent(quantize_tiles_kernel<false>, grid, dim3(kTileThreads), 0, stream, a);

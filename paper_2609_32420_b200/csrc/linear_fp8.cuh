@@ -1,12 +1,16 @@
 // Matrix product of 8-bit operands with a scale per block of 128 (fp8_quantize.cuh), on the 5th-gen tensor cores, with the epilogue of linear_tcgen05.cuh:
 //   z = sum over blocks j of 128 k of  sx[row, j] sw[col / 128, j] <qx_j, qw_j>  + bias,   y = residual + gate_b act(z).
 //
-// The scales change with every 128 k, so an accumulator of the tensor cores sums up one block only (four products of 32 k, in which nothing is lost: 7
-// significant bits each, 128 terms) and the epilogue warps take it times the block's scale into fp32 sums of their own, 128 per thread, while the next block's
-// products run into another accumulator.  Scales are any fp32 numbers.
-// A pair of CTAs shares a tile of 256 x BN (cta_group::2), as in linear_tcgen05.cuh, whose roles, ring and joining of shared sums these are; what a stage's
-// barrier says, that the products which read it have completed, says too that the accumulator of its block is whole: one commit per block.
-// Per block of a 256 x 256 tile an SM's tensor core works 512 clocks, its epilogue warps read 128 KB of tensor memory and do 128 x 256 multiply-adds.
+// Scales that are powers of two (fp8_quantize.cuh makes no others) are applied by the tensor cores: kind::mxf8f6f4 takes an exponent per row and 32 k from tensor memory
+// (here the same for the four products of a block), so that an accumulator sums up all of k, or runs of 2560 of it for fp32 outputs, as in linear_tcgen05.cuh.
+// Any other scales: an accumulator sums up one block (kind::f8f6f4, in which nothing is lost: 7 significant bits a product, 128 terms) and the epilogue warps take it
+// times the block's scale into 128 fp32 sums per thread, while the next block's products run into the other accumulator.  That costs the reading of every block's sums
+// from tensor memory, 128 KB per SM and block against 512 clocks of products (75600 x 5120 x 5120: 2068 us, without the epilogue's reads and sums 1584).
+// A first kernel quantises x where the call does, lays the exponents out as the tensor cores read them and notes whether all scales are powers of two; the product
+// goes by its note, so that a caller does not have to say.
+//
+// A pair of CTAs shares a tile of 256 x BN (cta_group::2), as in linear_tcgen05.cuh, whose roles, ring and joining of shared sums these are.  BN <= 224: two accumulators
+// and the exponents of four groups of four blocks fill tensor memory.
 #pragma once
 #include "fp8_quantize.cuh"
 #include "linear_tcgen05.cuh"
@@ -18,13 +22,94 @@ using namespace lin;
 using fp8::kBlock;
 
 constexpr uint32_t kABytes8 = 128 * kBlock;          // a CTA's share of A per stage
+constexpr int kMostColumns = 224;                    // of a tile
+constexpr int kGroupBlocks = 4;                      // blocks whose exponents share 32-bit words
+constexpr uint32_t kSfA = 512, kSfB = 1024;          // bytes of a group's exponents: 128 rows, 256 columns
+constexpr uint32_t kSfSlots = 10, kSfAt = 210 * 1024; // their ring in shared memory, behind the stages
+constexpr uint32_t kSfColumn = 448;                  // first column of the exponents in tensor memory
+static_assert(kSfAt + kSfSlots * (kSfA + kSfB) <= kRingBytes, "shared memory of a CTA");
+enum { kXBf16 = 0, kXF32 = 1, kXE4m3 = 2 };
 
 struct Args8 {
     TcArgs t;
-    const float* xscale; const float* wscale;
+    const float* xscale;                 // of an x that came in 8 bits, else NULL: its exponents are in sfa
+    const float* wscale;
+    const uint8_t* sfa;                  // [row tiles of 128][groups][512]
+    const int* notes; int n_notes;       // not all zero: some scale is no power of two
     int64_t xss[3], wss[2];              // (batch, row, block), (block of columns, block)
+    int groups;
 };
 
+// ---- the first kernel: x in 8 bits, exponents as tensor memory takes them -------------------------------------------------
+// A group's exponents of 128 rows: a 32-bit word per row, byte j of it block 4 g + j; row r at 16 (r mod 32) + 4 (r / 32).
+__device__ __forceinline__ int64_t sf_offset(int64_t tile, int groups, int g, int r) { return (tile * groups + g) * int64_t(kSfA) + (r & 31) * 16 + (r >> 5) * 4; }
+// The exponent byte of a scale; what has none makes a note.  A NaN has one of its own.
+__device__ __forceinline__ uint32_t exponent_of(float scale, int& note) {
+    const uint32_t b = __float_as_uint(scale);
+    if ((b & 0x7FFFFFFFu) > 0x7F800000u) return 255u;
+    const uint32_t e = b >> 23;
+    if ((b & 0x807FFFFFu) != 0u || e == 0u || e == 255u) { note = 1; return 127u; }
+    return e;
+}
+struct PrepareArgs {
+    fp8::QuantArgs q;                    // x (quantised here), or only rows, blocks, batches
+    const float* xscale; const float* wscale;
+    int64_t xss[3], wss[2];
+    uint8_t* sfa; uint8_t* sfb;          // sfb: [column tiles][groups][1024], two times 128 columns
+    int* notes;                          // one per CTA
+    WsHeader* hdr;
+    int groups, row_tiles;               // row tiles of 128 per batch entry
+    int cols, bn, tiles_n;
+    int x_ctas, w_ctas;
+};
+template <int kType>
+__global__ void __launch_bounds__(fp8::kRowThreads) prepare_fp8_kernel(const PrepareArgs a) {
+    const int b = blockIdx.y, cta = blockIdx.x, tid = threadIdx.x;
+    grid_launch_dependents();
+    grid_wait();
+    if (cta == 0 && b == 0 && tid == 0) a.hdr->status = 0;
+    int note = 0;
+    if (cta < a.x_ctas) {
+        if constexpr (kType == kXE4m3) {
+            const int64_t items = int64_t(a.groups) * a.q.rows;
+            for (int64_t i = int64_t(cta) * fp8::kRowThreads + tid; i < items; i += int64_t(a.x_ctas) * fp8::kRowThreads) {
+                const int g = int(i / a.q.rows), row = int(i - int64_t(g) * a.q.rows);
+                const float* p = a.xscale + b * a.xss[0] + row * a.xss[1];
+                uint32_t word = 0;
+#pragma unroll
+                for (int j = 0; j < kGroupBlocks; ++j)
+                    if (g * kGroupBlocks + j < a.q.blocks) word |= exponent_of(p[(g * kGroupBlocks + j) * a.xss[2]], note) << (8 * j);
+                *reinterpret_cast<uint32_t*>(a.sfa + sf_offset(int64_t(b) * a.row_tiles + row / 128, a.groups, g, row % 128)) = word;
+            }
+        } else {
+            constexpr bool kF = kType == kXF32;
+            fp8::quantize_rows<kF, fp8::kAheadOf<kF>>(a.q, b, cta, a.x_ctas, [&](int row, int blk, float scale) {
+                int none = 0;
+                a.sfa[sf_offset(int64_t(b) * a.row_tiles + row / 128, a.groups, blk / kGroupBlocks, row % 128) + blk % kGroupBlocks] = uint8_t(exponent_of(scale, none));
+            });
+        }
+    } else if (b == 0) {
+        const int64_t words = int64_t(a.tiles_n) * a.groups * 256;
+        for (int64_t i = int64_t(cta - a.x_ctas) * fp8::kRowThreads + tid; i < words; i += int64_t(a.w_ctas) * fp8::kRowThreads) {
+            const int c = int(i & 255);
+            const int64_t tg = i >> 8;
+            const int n = int(tg / a.groups), g = int(tg - int64_t(n) * a.groups), col = n * a.bn + c;
+            uint32_t word = 0x7F7F7F7Fu;
+            if (c < a.bn && col < a.cols) {
+                const float* p = a.wscale + (col / kBlock) * a.wss[0];
+                word = 0;
+#pragma unroll
+                for (int j = 0; j < kGroupBlocks; ++j)
+                    if (g * kGroupBlocks + j < a.q.blocks) word |= exponent_of(p[(g * kGroupBlocks + j) * a.wss[1]], note) << (8 * j);
+            }
+            *reinterpret_cast<uint32_t*>(a.sfb + tg * kSfB + (c >> 7) * 512 + (c & 31) * 16 + ((c & 127) >> 5) * 4) = word;
+        }
+    }
+    note = __syncthreads_or(note);
+    if (tid == 0) a.notes[int64_t(b) * gridDim.x + cta] = note;
+}
+
+// ---- the product ------------------------------------------------------------------------------------------
 __device__ __forceinline__ void mma8_pair_el(uint32_t d_tmem, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
         "{\n\t.reg .pred p, e;\n\t.reg .b64 da, db;\n\tsetp.ne.b32 p, %6, 0;\n\t"
@@ -33,19 +118,42 @@ __device__ __forceinline__ void mma8_pair_el(uint32_t d_tmem, uint32_t a_lo, uin
         "@e tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], da, db, %5, p;\n\t}"
         ::"r"(d_tmem), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate) : "memory");
 }
+// the same with an exponent per row of either operand, byte `id` (in the descriptor) of the words at these columns
+__device__ __forceinline__ void mma8_scaled_pair_el(uint32_t d_tmem, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t sa, uint32_t sb,
+                                                    uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p, e;\n\t.reg .b64 da, db;\n\tsetp.ne.b32 p, %8, 0;\n\t"
+        "mov.b64 da, {%1, %2};\n\tmov.b64 db, {%3, %4};\n\t"
+        "elect.sync _|e, 0xffffffff;\n\t"
+        "@e tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], da, db, %5, [%6], [%7], p;\n\t}"
+        ::"r"(d_tmem), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate) : "memory");
+}
+// 512 bytes of shared memory (of both CTAs) into four columns, the same for each of the four quarters of the lanes
+__device__ __forceinline__ void copy_exponents_el(uint32_t tmem, uint32_t smem) {
+    // no swizzle: 8 rows of 16 bytes beside each other, the next 8 rows 128 bytes on
+    const uint64_t desc = uint64_t((smem & 0x3FFFFu) >> 4) | (1ull << 16) | (8ull << 32) | (1ull << 46);
+    asm volatile(
+        "{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
+        "@e tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;\n\t}"
+        ::"r"(tmem), "l"(desc) : "memory");
+}
 __device__ __forceinline__ float load_scale(const float* p) {      // not through the read-only path: the kernel ahead may write it while this one is resident
     float v;
     asm volatile("ld.global.f32 %0, [%1];" : "=f"(v) : "l"(p));
     return v;
 }
+__device__ __forceinline__ float scale_from(uint32_t word, int j) {
+    const uint32_t e = (word >> (8 * j)) & 255u;
+    return __uint_as_float(e == 255u ? 0x7FC00000u : e << 23);
+}
 
-// kParts: 32-column parts of a thread's columns, of which it has BN / 2 beside each other, within one block of the weight's rows.
-// kAccs: accumulators in tensor memory.
-template <int kParts, bool kF32>
+// kRuns: an accumulator sums up runs of k only, which the epilogue adds in registers (fp32 outputs, and bf16 ones of a very long k).
+template <bool kF32, bool kRuns>
 __global__ void __launch_bounds__(kThreadsTc, 1)
-linear_fp8_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB, const Args8 args) {
-    constexpr int kBn = kParts * 64, kAccs = kParts == 4 ? 2 : 4;
-    constexpr uint32_t kBBytes = kBn / 2 * kBlock, kStage = kABytes8 + kBBytes;
+linear_fp8_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB, const __grid_constant__ CUtensorMap mapSa,
+                  const __grid_constant__ CUtensorMap mapSb, const Args8 args) {
+    constexpr int kRun = (kF32 ? kLongRun : kLongRunBf16) / kBlock;
+    static_assert(kRun % kGroupBlocks == 0, "runs are whole groups");
     const TcArgs& a = args.t;
     extern __shared__ unsigned char lin_smem[];
     __shared__ uint32_t tmem_slot;
@@ -54,9 +162,11 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constan
     const uint32_t base = (smem_u32(lin_smem) + 1023u) & ~1023u;
     const uint32_t bars = base + kRingBytes;
     const uint32_t rank = cluster_ctarank(), half = rank & 1u, leader = rank & ~1u, split = rank >> 1;
+    const uint32_t stage_bytes = kABytes8 + uint32_t(a.bn / 2) * kBlock;
     auto bar_full = [&](int s) { return bars + 8 * s; };                       // used in the pair's first CTA: both CTAs' copies have landed
-    auto bar_done = [&](int s) { return bars + 64 + 8 * s; };                  // the products of stage s have completed: it may be filled, its accumulator read
-    auto bar_read = [&](int u) { return bars + 128 + 8 * u; };                 // first CTA: both CTAs have read accumulator u
+    auto bar_done = [&](int s) { return bars + 64 + 8 * s; };                  // the products of stage s have completed
+    auto bar_sum = [&](int u) { return bars + 128 + 8 * u; };                  // accumulator u holds a run
+    auto bar_read = [&](int u) { return bars + 144 + 8 * u; };                 // first CTA: both CTAs have read accumulator u
     volatile int* abortp = &abort_flag;
     const unsigned long long limit = kDefaultWaitNs;
     const uint16_t pair_mask = uint16_t(3u << leader);
@@ -64,14 +174,14 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constan
     if (tid == 0) {
         abort_flag = 0;
         for (int s = 0; s < kMaxStages; ++s) { mbar_init(bar_full(s), 1); mbar_init(bar_done(s), 1); }
-        for (int u = 0; u < kAccs; ++u) mbar_init(bar_read(u), 2 * kEpiWarps);
+        for (int u = 0; u < 2; ++u) { mbar_init(bar_sum(u), 1); mbar_init(bar_read(u), 2 * kEpiWarps); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 2) {
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }
-    if (warp == 0 && lane == 0) { prefetch_tmap(&mapA); prefetch_tmap(&mapB); }
+    if (warp == 0 && lane == 0) { prefetch_tmap(&mapA); prefetch_tmap(&mapB); prefetch_tmap(&mapSa); prefetch_tmap(&mapSb); }
     grid_launch_dependents();
     tc_fence_before();
     __syncwarp();
@@ -79,12 +189,15 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constan
     tc_fence_after();
     const uint32_t tmem = tmem_slot;
     grid_wait();                         // launched while the kernel ahead drains: nothing of global memory is touched before this
-    if (tid == 0 && blockIdx.x == 0 && a.clears) a.hdr->status = 0;
-    __syncwarp();                        // whole warps hand over registers (setmaxnreg)
+    int note = 0;
+    for (int i = tid; i < args.n_notes; i += kThreadsTc) note |= reinterpret_cast<const volatile int*>(args.notes)[i];
+    const bool scaled = __syncthreads_or(note) == 0;       // all of the call's scales are powers of two (the same in every CTA)
 
-    // the clusters take the tiles in turn; with splits > 1 there is one cluster per tile and a pair has its share of k
+    // the clusters take the tiles in turn; with splits > 1 there is one cluster per tile and a pair has its share of k, in whole groups
     const int first = int(blockIdx.x / (2 * a.splits)), step = int(gridDim.x / (2 * a.splits));
-    const int k0 = int(int64_t(a.k_tiles) * split / a.splits), k1 = int(int64_t(a.k_tiles) * (split + 1) / a.splits);
+    const int k0 = int(int64_t(args.groups) * split / a.splits) * kGroupBlocks, k1 = min(int(int64_t(args.groups) * (split + 1) / a.splits) * kGroupBlocks, a.k_tiles);
+    // runs of k with an accumulator each
+    const int chunks = kRuns ? (k1 - k0 + kRun - 1) / kRun : 1, chunk = kRuns ? kRun : k1 - k0;
 
     if (warp < 4) {                      // ---- service warps
     // 128 x 40 + 256 x 208 registers; the block is launched with 384 x 152 at least (checked by the host)
@@ -93,19 +206,27 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constan
         // ================= TMA producer =================
         if (lane == 0) {
             const uint32_t full0 = map_cta(bar_full(0), leader);
-            int s = 0, issued = 0;
+            int s = 0, issued = 0, group = 0;
             uint32_t phase = 0;
             bool ok = true;
             for (int t = first; t < a.tiles && ok; t += step) {
                 int b, m, n;
                 tile_at(a, t, b, m, n);
-                const int m0 = m * kTileM + int(half) * 128, n0 = n * kBn + int(half) * (kBn / 2);
+                const int m0 = m * kTileM + int(half) * 128, n0 = n * a.bn + int(half) * (a.bn / 2);
+                const int sf_row = ((b * a.tiles_m + m) * 2 + int(half)) * args.groups, sf_col = n * args.groups;
                 for (int k = k0; k < k1; ++k) {
                     if (issued >= a.stages && !mbar_wait(bar_done(s), phase ^ 1u, abortp, 0, limit)) {
                         set_status(a.hdr, CARNATOR_ERR_DEVICE_TIMEOUT, 80, k, blockIdx.x); ok = false; break;
                     }
-                    if (half == 0) mbar_expect_tx(bar_full(s), 2 * kStage);
-                    const uint32_t sa = base + uint32_t(s) * kStage, bar = full0 + 8 * s;
+                    const bool sf = scaled && k % kGroupBlocks == 0;
+                    if (half == 0) mbar_expect_tx(bar_full(s), 2 * (stage_bytes + (sf ? kSfA + kSfB : 0u)));
+                    const uint32_t sa = base + uint32_t(s) * stage_bytes, bar = full0 + 8 * s;
+                    if (sf) {            // its slot: of the group kSfSlots back, whose last block lies further back than there are stages
+                        const uint32_t to = base + kSfAt + uint32_t(group % int(kSfSlots)) * (kSfA + kSfB);
+                        tma_load_pair(to, &mapSa, bar, 0, sf_row + k / kGroupBlocks, 0);
+                        tma_load_pair(to + kSfA, &mapSb, bar, 0, sf_col + k / kGroupBlocks, 0);
+                        ++group;
+                    }
                     tma_load_pair(sa, &mapA, bar, k * kBlock, m0, b);
                     tma_load_pair(sa + kABytes8, &mapB, bar, k * kBlock, n0, 0);
                     ++issued;
@@ -129,32 +250,68 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constan
         // ================= MMA issuer (converged warp, one elected lane issues) =================
         if (half == 0) {
             // e4m3 x e4m3, fp32 accumulator; K-major operands: 8-row groups 1024 B apart, 32 columns of k = 32 B
-            const uint32_t idesc = (1u << 4) | (uint32_t(kBn >> 3) << 17) | (uint32_t(kTileM >> 4) << 24);
+            const uint32_t idesc = (1u << 4) | (uint32_t(a.bn >> 3) << 17) | (uint32_t(kTileM >> 4) << 24);
+            const uint32_t idesc_sf = (1u << 23) | (uint32_t(a.bn >> 3) << 17) | (uint32_t(kTileM >> 7) << 27);      // exponents as scales
             const uint64_t da0 = smem_desc(base, 16, 1024), db0 = smem_desc(base + kABytes8, 16, 1024);
             const uint32_t a_lo = uint32_t(da0), a_hi = uint32_t(da0 >> 32), b_lo = uint32_t(db0), b_hi = uint32_t(db0 >> 32);
             const int last = (a.k_len - (a.k_tiles - 1) * kBlock + 31) / 32;
-            int s = 0, i = 0;
+            int s = 0, i = 0, group = 0;
             uint32_t phase = 0;
             bool ok = true;
+            auto free_accumulator = [&](int u) {
+                if (i < 2) return true;
+                if (mbar_wait_warp(bar_read(u), uint32_t((i >> 1) - 1) & 1u, abortp, 0, limit)) return true;
+                if (lane == 0) set_status(a.hdr, CARNATOR_ERR_DEVICE_TIMEOUT, 82, i, blockIdx.x);
+                return false;
+            };
+            auto full_stage = [&](int k) {
+                if (mbar_wait_warp(bar_full(s), phase, abortp, 0, limit)) return true;
+                if (lane == 0) set_status(a.hdr, CARNATOR_ERR_DEVICE_TIMEOUT, 83, k, blockIdx.x);
+                return false;
+            };
             for (int t = first; t < a.tiles && ok; t += step) {
-                for (int k = k0; k < k1; ++k, ++i) {
-                    const int u = i % kAccs;
-                    if (i >= kAccs) {
-                        ok = mbar_wait_warp(bar_read(u), uint32_t(i / kAccs - 1) & 1u, abortp, 0, limit);
-                        if (!ok) { if (lane == 0) set_status(a.hdr, CARNATOR_ERR_DEVICE_TIMEOUT, 82, i, blockIdx.x); break; }
-                    }
-                    ok = mbar_wait_warp(bar_full(s), phase, abortp, 0, limit);
-                    if (!ok) { if (lane == 0) set_status(a.hdr, CARNATOR_ERR_DEVICE_TIMEOUT, 83, k, blockIdx.x); break; }
-                    tc_fence_after();
-                    const uint32_t off = (uint32_t(s) * kStage) >> 4, d = tmem + uint32_t(u * kBn);
-                    if (k + 1 < a.k_tiles) {
+                if (scaled) {
+                    for (int c = 0; c < chunks && ok; ++c, ++i) {
+                        const int u = i & 1, from = k0 + c * chunk, to = min(from + chunk, k1);
+                        if (!(ok = free_accumulator(u))) break;
+                        const uint32_t d = tmem + uint32_t(u * kMostColumns);
+                        uint32_t sf = 0;
+                        for (int k = from; k < to; ++k) {
+                            if (!(ok = full_stage(k))) break;
+                            tc_fence_after();
+                            if (k % kGroupBlocks == 0) {
+                                const uint32_t at = base + kSfAt + uint32_t(group % int(kSfSlots)) * (kSfA + kSfB);
+                                sf = tmem + kSfColumn + uint32_t(group & 3) * 16u;
+                                copy_exponents_el(sf, at);
+                                copy_exponents_el(sf + 4, at + kSfA);
+                                copy_exponents_el(sf + 8, at + kSfA + 512);
+                                ++group;
+                            }
+                            const uint32_t off = (uint32_t(s) * stage_bytes) >> 4, id = uint32_t(k % kGroupBlocks), ids = idesc_sf | id << 4 | id << 29;
+                            if (k + 1 < a.k_tiles) {
 #pragma unroll
-                        for (int kk = 0; kk < 4; ++kk) mma8_pair_el(d, a_lo + off + kk * 2, a_hi, b_lo + off + kk * 2, b_hi, idesc, kk > 0 ? 1u : 0u);
-                    } else {             // the end of k: what is all zero is left out
-                        for (int kk = 0; kk < last; ++kk) mma8_pair_el(d, a_lo + off + kk * 2, a_hi, b_lo + off + kk * 2, b_hi, idesc, kk > 0 ? 1u : 0u);
+                                for (int kk = 0; kk < 4; ++kk)
+                                    mma8_scaled_pair_el(d, a_lo + off + kk * 2, a_hi, b_lo + off + kk * 2, b_hi, ids, sf, sf + 4, k > from || kk > 0 ? 1u : 0u);
+                            } else {     // the end of k: what is all zero is left out
+                                for (int kk = 0; kk < last; ++kk)
+                                    mma8_scaled_pair_el(d, a_lo + off + kk * 2, a_hi, b_lo + off + kk * 2, b_hi, ids, sf, sf + 4, k > from || kk > 0 ? 1u : 0u);
+                            }
+                            commit_pair_el(bar_done(s), pair_mask);
+                            if (++s == a.stages) { s = 0; phase ^= 1u; }
+                        }
+                        if (ok) commit_pair_el(bar_sum(u), pair_mask);
                     }
-                    commit_pair_el(bar_done(s), pair_mask);
-                    if (++s == a.stages) { s = 0; phase ^= 1u; }
+                } else {
+                    for (int k = k0; k < k1 && ok; ++k, ++i) {
+                        const int u = i & 1;
+                        if (!(ok = free_accumulator(u)) || !(ok = full_stage(k))) break;
+                        tc_fence_after();
+                        const uint32_t off = (uint32_t(s) * stage_bytes) >> 4, d = tmem + uint32_t(u * kMostColumns);
+                        const int n = k + 1 < a.k_tiles ? 4 : last;
+                        for (int kk = 0; kk < n; ++kk) mma8_pair_el(d, a_lo + off + kk * 2, a_hi, b_lo + off + kk * 2, b_hi, idesc, kk > 0 ? 1u : 0u);
+                        commit_pair_el(bar_done(s), pair_mask);
+                        if (++s == a.stages) { s = 0; phase ^= 1u; }
+                    }
                 }
             }
         }
@@ -166,93 +323,30 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constan
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 208;" ::: "memory");
         // ================= epilogue =================
-        const int quarter = warp & 3, side = (warp - 4) >> 2;               // rows 32 quarter .. of this CTA's 128; half of the columns
+        const int quarter = warp & 3, side = (warp - 4) >> 2;               // rows 32 quarter .. of this CTA's 128; every other 32 columns
         const uint32_t lane_base = uint32_t(quarter * 32) << 16;
         const uint32_t read0 = map_cta(bar_read(0), leader);
+        const uint32_t line = base + uint32_t(quarter * 32 + lane) * (uint32_t(a.bn + 4) * 4u);        // of a shared tile
         bool ok = true;
         int i = 0, s = 0;
         uint32_t phase = 0;
+        auto release = [&](int u) {      // this warp has read its part of accumulator u
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) arrive_remote(read0 + 8 * u);
+        };
         for (int t = first; t < a.tiles && ok; t += step) {
             int b, m, n;
             tile_at(a, t, b, m, n);
-            const int row = m * kTileM + int(half) * 128 + quarter * 32 + lane, at0 = side * (kBn / 2), left = min(a.cols - n * kBn, kBn) - at0;
-            const bool on = row < a.rows, some = left > 0;         // `some`: warp-uniform
-            const float* xs = args.xscale + b * args.xss[0] + (on ? row : 0) * args.xss[1];
-            const float* ws = args.wscale + (some ? (n * kBn + at0) / kBlock : 0) * args.wss[0];
-            __syncwarp();                // rows behind the last one have left the tile before early
-            f2 acc[kParts][16];
-#pragma unroll
-            for (int p = 0; p < kParts; ++p)
-#pragma unroll
-                for (int q = 0; q < 16; ++q) acc[p][q] = two(0.f);
-            // scales: x's of four blocks on their way while the four before are used (one block ahead, a block had to wait for them: 75600 x 5120 x 5120 2703 us,
-            // four ahead 2068); the weight's of 32 blocks, one per lane
-            float xn[4], wn = load_scale(ws + min(k0 + lane, k1 - 1) * args.wss[1]), wv = 0.f;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) xn[j] = load_scale(xs + min(k0 + j, k1 - 1) * args.xss[2]);
-            for (int g = k0; g < k1 && ok; g += 4) {
-            float xv[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) xv[j] = xn[j];
-            if (((g - k0) & 31) == 0) { wv = wn; wn = load_scale(ws + min(g + 32 + lane, k1 - 1) * args.wss[1]); }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) xn[j] = load_scale(xs + min(g + 4 + j, k1 - 1) * args.xss[2]);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int k = g + j;
-                if (k >= k1) break;
-                const int u = i % kAccs;
-                const f2 by = two(xv[j] * __shfl_sync(0xffffffffu, wv, (k - k0) & 31));
-                ++i;
-                ok = mbar_wait_warp(bar_done(s), phase, abortp, 0, limit);
-                if (!ok) { if (lane == 0) set_status(a.hdr, CARNATOR_ERR_DEVICE_TIMEOUT, 84, i, blockIdx.x); break; }
-                if (++s == a.stages) { s = 0; phase ^= 1u; }
-                tc_fence_after();
-                const uint32_t from = tmem + lane_base + uint32_t(u * kBn + at0);
-                float v0[32], v1[32];        // parts in turn: one on its way while the other is added
-                tmem_ld32(from, v0);
-#pragma unroll
-                for (int p = 0; p < kParts; ++p) {
-                    if (p % 2 == 0) {
-                        tmem_wait_ld(v0);
-                        if (p + 1 < kParts) tmem_ld32(from + 32 * (p + 1), v1);
-                    } else {
-                        tmem_wait_ld(v1);
-                        if (p + 1 < kParts) tmem_ld32(from + 32 * (p + 1), v0);
-                    }
-                    if (p + 1 == kParts) {   // this warp has read its part of the block
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) arrive_remote(read0 + 8 * u);
-                    }
-#pragma unroll
-                    for (int q = 0; q < 16; ++q)
-                        acc[p][q] = norm::fma2(p % 2 == 0 ? two(v0[2 * q], v0[2 * q + 1]) : two(v1[2 * q], v1[2 * q + 1]), by, acc[p][q]);
-                }
-            }
-            }
-            __syncwarp();
-            if (!ok) break;
-            if (a.splits > 1) {          // the one tile of this cluster: this pair's share to shared memory
-                const uint32_t line = base + uint32_t(quarter * 32 + lane) * uint32_t((kBn + 4) * 4);
-#pragma unroll
-                for (int p = 0; p < kParts; ++p)
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) {
-                        float f[4];
-                        one_each(acc[p][2 * q], f[0], f[1]);
-                        one_each(acc[p][2 * q + 1], f[2], f[3]);
-                        asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(line + uint32_t(at0 + 32 * p + 4 * q) * 4u), "f"(f[0]), "f"(f[1]), "f"(f[2]), "f"(f[3]) : "memory");
-                    }
-                break;
-            }
+            const int row = m * kTileM + int(half) * 128 + quarter * 32 + lane, left = min(a.cols - n * a.bn, a.bn);
+            const bool on = row < a.rows;
             const int64_t y_off = b * a.e.ys[0] + row * a.e.ys[1], r_off = b * a.e.rs[0] + row * a.e.rs[1];
             const int64_t gate_off = a.e.gate ? (b + row / a.e.rows_per_gate) * a.e.gate_stride : 0;
-            const char* res = static_cast<const char*>(a.e.residual) + (r_off + n * kBn + at0) * (kF32 ? 4 : 2);
-#pragma unroll
-            for (int p = 0; p < kParts; ++p) {
-                const int at = 32 * p, col = n * kBn + at0 + at;
-                if (at >= left || !on) continue;
+            const char* res = static_cast<const char*>(a.e.residual) + (r_off + n * a.bn) * (kF32 ? 4 : 2);
+            // the end of 32 columns of the tile from `at` on, which a thread holds as 16 pairs
+            auto end_of = [&](int at, const f2 (&v)[16]) {
+                const int col = n * a.bn + at;
+                if (at >= left || !on) return;
                 if (at + 32 <= left) {
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
@@ -263,7 +357,7 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constan
                         }
                         float f[16];
 #pragma unroll
-                        for (int q = 0; q < 8; ++q) one_each(acc[p][8 * h + q], f[2 * q], f[2 * q + 1]);
+                        for (int q = 0; q < 8; ++q) one_each(v[8 * h + q], f[2 * q], f[2 * q + 1]);
                         finish16<kF32>(a.e, a.e.gate, gate_off, y_off, 0, col + 16 * h, f, r0, kF32 ? r1 : r0);
                     }
                 } else {
@@ -277,12 +371,131 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constan
                             if (a.e.residual) load_residual(a.e, b, row, col + 8 * h, cn, r8);
                             float f[8];
 #pragma unroll
-                            for (int q = 0; q < 4; ++q) one_each(acc[p][4 * h + q], f[2 * q], f[2 * q + 1]);
+                            for (int q = 0; q < 4; ++q) one_each(v[4 * h + q], f[2 * q], f[2 * q + 1]);
                             finish(a.e, cols, b, row, col + 8 * h, cn, f, r8);
                         }
                     }
                 }
+            };
+            auto to_shared = [&](int at, const f2 (&v)[16]) {
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    float f[4];
+                    one_each(v[2 * q], f[0], f[1]);
+                    one_each(v[2 * q + 1], f[2], f[3]);
+                    asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(line + uint32_t(at + 4 * q) * 4u), "f"(f[0]), "f"(f[1]), "f"(f[2]), "f"(f[3]) : "memory");
+                }
+            };
+            __syncwarp();                // rows behind the last one have left the tile before early
+            if (scaled && !kRuns) {
+                const int u = i & 1;
+                ok = mbar_wait_warp(bar_sum(u), uint32_t(i >> 1) & 1u, abortp, 20, limit);
+                if (!ok) { if (lane == 0) set_status(a.hdr, CARNATOR_ERR_DEVICE_TIMEOUT, 84, i, blockIdx.x); break; }
+                tc_fence_after();
+                ++i;
+                for (int at = side * 32; at < left; at += 64) {        // warp-uniform
+                    float v[32];
+                    __syncwarp();
+                    tmem_ld32(tmem + lane_base + uint32_t(u * kMostColumns + at), v);
+                    tmem_wait_ld(v);
+                    if (at + 64 >= left) release(u);
+                    f2 w[16];
+#pragma unroll
+                    for (int q = 0; q < 16; ++q) w[q] = two(v[2 * q], v[2 * q + 1]);
+                    if (a.splits > 1) to_shared(at, w);
+                    else end_of(at, w);
+                }
+                if (side * 32 >= left) release(u);
+                if (a.splits > 1) break;
+                continue;
             }
+            f2 acc[4][16];               // 32 columns each: side * 32, + 64, + 128, + 192
+#pragma unroll
+            for (int p = 0; p < 4; ++p)
+#pragma unroll
+                for (int q = 0; q < 16; ++q) acc[p][q] = two(0.f);
+            if (kRuns && scaled) {
+                for (int c = 0; c < chunks && ok; ++c, ++i) {
+                    const int u = i & 1;
+                    ok = mbar_wait_warp(bar_sum(u), uint32_t(i >> 1) & 1u, abortp, 20, limit);
+                    if (!ok) { if (lane == 0) set_status(a.hdr, CARNATOR_ERR_DEVICE_TIMEOUT, 85, i, blockIdx.x); break; }
+                    tc_fence_after();
+#pragma unroll
+                    for (int p = 0; p < 4; ++p) {
+                        const int at = side * 32 + 64 * p;
+                        if (at < left) {
+                            float v[32];
+                            tmem_ld32(tmem + lane_base + uint32_t(u * kMostColumns + at), v);
+                            tmem_wait_ld(v);
+#pragma unroll
+                            for (int q = 0; q < 16; ++q) acc[p][q] = norm::add2(acc[p][q], two(v[2 * q], v[2 * q + 1]));
+                        }
+                    }
+                    release(u);
+                }
+            } else {
+                // x's scales of four blocks on their way while the four before are used (one block ahead, a block had to wait for them: 75600 x 5120 x 5120 2703 us, four
+                // ahead 2068); the weight's of 32 blocks, one per lane, for each 32 columns
+                const float* xs = args.xscale ? args.xscale + b * args.xss[0] + (on ? row : 0) * args.xss[1] : nullptr;
+                const uint8_t* xe = args.sfa + sf_offset((int64_t(b) * a.tiles_m + m) * 2 + half, args.groups, 0, quarter * 32 + lane);
+                const float* ws[4];
+                float wv[4], xn[4];
+#pragma unroll
+                for (int p = 0; p < 4; ++p) ws[p] = args.wscale + (min(n * a.bn + side * 32 + 64 * p, a.cols - 1) / kBlock) * args.wss[0];
+                auto fetch = [&](int g) {
+                    if (xs) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) xn[j] = load_scale(xs + min(g + j, k1 - 1) * args.xss[2]);
+                    } else {
+                        const uint32_t word = __float_as_uint(load_scale(reinterpret_cast<const float*>(xe + int64_t(min(g, k1 - 1) / kGroupBlocks) * kSfA)));
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) xn[j] = scale_from(word, j);
+                    }
+                };
+                fetch(k0);
+                for (int g = k0; g < k1 && ok; g += 4) {
+                    float xv[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) xv[j] = xn[j];
+                    if (((g - k0) & 31) == 0) {
+#pragma unroll
+                        for (int p = 0; p < 4; ++p) wv[p] = load_scale(ws[p] + min(g + lane, k1 - 1) * args.wss[1]);
+                    }
+                    fetch(g + 4);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int k = g + j, u = i & 1;
+                        if (k >= k1) break;
+                        ok = mbar_wait_warp(bar_done(s), phase, abortp, 0, limit);
+                        if (!ok) { if (lane == 0) set_status(a.hdr, CARNATOR_ERR_DEVICE_TIMEOUT, 86, i, blockIdx.x); break; }
+                        ++i;
+                        if (++s == a.stages) { s = 0; phase ^= 1u; }
+                        tc_fence_after();
+#pragma unroll
+                        for (int p = 0; p < 4; ++p) {
+                            const int at = side * 32 + 64 * p;
+                            const f2 by = two(xv[j] * __shfl_sync(0xffffffffu, wv[p], (k - k0) & 31));
+                            if (at < left) {
+                                float v[32];
+                                tmem_ld32(tmem + lane_base + uint32_t(u * kMostColumns + at), v);
+                                tmem_wait_ld(v);
+#pragma unroll
+                                for (int q = 0; q < 16; ++q) acc[p][q] = norm::fma2(two(v[2 * q], v[2 * q + 1]), by, acc[p][q]);
+                            }
+                        }
+                        release(u);
+                    }
+                }
+            }
+            __syncwarp();
+            if (!ok) break;
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+                const int at = side * 32 + 64 * p;
+                if (a.splits == 1) end_of(at, acc[p]);
+                else if (at < left) to_shared(at, acc[p]);
+            }
+            if (a.splits > 1) break;     // the one tile of this cluster
         }
         if (a.splits > 1) {
             tc_fence_before();
@@ -330,7 +543,6 @@ __device__ __forceinline__ void mma_16x8x32(float (&d)[4], uint32_t a0, uint32_t
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-enum { kXBf16 = 0, kXF32 = 1, kXE4m3 = 2 };
 // NT: column tiles of 8 rows of x; kWarps: warps that share k; kType: of x
 template <int NT, int kWarps, int kType>
 __global__ void __launch_bounds__(32 * kWarps) linear_fp8_rows_kernel(const RowsArgs8 a) {
@@ -453,18 +665,69 @@ inline bool make_map8(CUtensorMap* map, const Operand& o, int box_rows) {
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(o.base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+// rows of `words` 32-bit words of exponents, one row a copy
+inline bool make_map_sf(CUtensorMap* map, const void* base, int64_t rows, int words) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    cuuint64_t dims[3] = {cuuint64_t(words), cuuint64_t(rows), 1};
+    cuuint64_t strides[2] = {cuuint64_t(words) * 4, cuuint64_t(words) * 4 * cuuint64_t(rows)};
+    cuuint32_t box[3] = {cuuint32_t(words), 1, 1};
+    cuuint32_t estr[3] = {1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
 
-template <int kParts, bool kF32>
-inline carnator_status launch_stages8(const Operand& A, const Operand& B, Args8 a, cudaStream_t stream, char* err, size_t errlen) {
-    constexpr uint32_t kStage = kABytes8 + uint32_t(kParts * 32) * kBlock;
-    a.t.stages = int(std::min<uint32_t>(kMaxStages, kRingBytes / kStage));
-    static_assert(kRingBytes / kStage > 4 && kMaxStages > 4, "more stages than accumulators: a stage's barrier is not a phase ahead of the epilogue");
-    CUtensorMap ma, mb;
-    if (!make_map8(&ma, A, 128) || !make_map8(&mb, B, kParts * 32)) {
+// Columns of a tile and pairs that share one: the least time by the model of linear_tcgen05.cuh, for 128 k in the place of 64.
+constexpr int kLeastColumns = 64;
+inline Plan plan_of8(int64_t m_tiles, int64_t cols, int64_t groups) {
+    Plan best = {kMostColumns, 1};
+    double best_cost = 1e30;
+    for (int bn = kMostColumns; bn >= kLeastColumns; bn -= 32) {
+        const int64_t tiles = m_tiles * ((cols + bn - 1) / bn);
+        for (int splits = 1; splits <= 4; splits *= 2) {
+            if ((splits == 2 && tiles > 32) || (splits == 4 && tiles > 14) || groups < splits * (splits > 1) || bn % (8 * splits)) break;
+            const int64_t turns = splits > 1 ? 1 : (tiles + 73) / 74;
+            const double k_ns = 4.0 * double((groups + splits - 1) / splits) * (75 + 0.85 * bn), join = splits == 1 ? 0 : splits == 4 ? 4500 : tiles > 24 ? 4000 : 2500;
+            const double cost = double(turns) * std::max(k_ns, 500.0 + 4 * bn) + join;
+            if (cost < best_cost * 0.995) { best_cost = cost; best = {bn, splits}; }
+        }
+    }
+    return best;
+}
+
+// What a call needs besides its arguments: notes, exponents, and x in 8 bits where the call makes it.
+constexpr int kMostWCtas = 64;
+struct Room8 { int* notes; uint8_t* sfa; uint8_t* sfb; uint8_t* q; int64_t q_stride; size_t bytes; };
+inline Room8 room8_of(char* p, int64_t batches, int64_t rows, int64_t cols, int64_t k, bool quantises) {
+    Room8 r = {};
+    size_t off = 0;
+    const int64_t blocks = (k + kBlock - 1) / kBlock, groups = (blocks + kGroupBlocks - 1) / kGroupBlocks;
+    // whichever way the rows are taken, one run or entry by entry, and however wide the tiles are
+    const int64_t tiles = std::max(batches * ((rows + kTileM - 1) / kTileM), (batches * rows + kTileM - 1) / kTileM) * 2;
+    const auto ctas = [&](int64_t n) { return std::min<int64_t>(148 * 8, (n * blocks + 31) / 32) + kMostWCtas; };
+    r.notes = reinterpret_cast<int*>(p + off);       off += align256(size_t(std::max(batches * ctas(rows), ctas(batches * rows))) * 4);
+    r.sfa = reinterpret_cast<uint8_t*>(p + off);     off += align256(size_t(tiles * groups) * kSfA);
+    r.sfb = reinterpret_cast<uint8_t*>(p + off);     off += align256(size_t((cols + kLeastColumns - 1) / kLeastColumns * groups) * kSfB);
+    if (quantises) {
+        r.q_stride = blocks * kBlock;
+        r.q = reinterpret_cast<uint8_t*>(p + off);   off += align256(size_t(batches * rows) * r.q_stride);
+    }
+    r.bytes = off;
+    return r;
+}
+
+template <bool kF32, bool kRuns>
+inline carnator_status launch_stages8(const Operand& A, const Operand& B, const Room8& room, Args8 a, cudaStream_t stream, char* err, size_t errlen) {
+    const uint32_t stage = kABytes8 + uint32_t(a.t.bn / 2) * kBlock;
+    a.t.stages = int(std::min<uint32_t>(kMaxStages, kSfAt / stage));
+    static_assert(kMaxStages <= int(kSfSlots), "groups of one block: a slot of exponents is filled again when the products that read it have completed");
+    CUtensorMap ma, mb, msa, msb;
+    if (!make_map8(&ma, A, 128) || !make_map8(&mb, B, a.t.bn / 2) || !make_map_sf(&msa, room.sfa, int64_t(a.t.batches) * a.t.tiles_m * 2 * a.groups, int(kSfA / 4)) ||
+        !make_map_sf(&msb, room.sfb, int64_t(a.t.tiles_n) * a.groups, int(kSfB / 4))) {
         snprintf(err, errlen, "cuTensorMapEncodeTiled failed or is unavailable");
         return CARNATOR_ERR_CUDA;
     }
-    auto kern = linear_fp8_kernel<kParts, kF32>;
+    auto kern = linear_fp8_kernel<kF32, kRuns>;
     static SmemAllowed allowed;
     const unsigned long long ctx = context_id();
     if (!allowed.has(ctx)) {
@@ -488,43 +751,43 @@ inline carnator_status launch_stages8(const Operand& A, const Operand& B, Args8 
     const int clusters = a.t.splits > 1 ? a.t.tiles : std::min(a.t.tiles, 74);
     cfg.gridDim = dim3(unsigned(clusters * 2 * a.t.splits)); cfg.blockDim = dim3(kThreadsTc); cfg.dynamicSmemBytes = kSmemTc; cfg.stream = stream;
     cfg.attrs = at; cfg.numAttrs = 2;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, ma, mb, a);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, ma, mb, msa, msb, a);
     if (e != cudaSuccess) return cuda_error(e, "linear_fp8_kernel", err, errlen);
     return CARNATOR_OK;
 }
 
-// Columns of a tile (those of a thread lie within one block of the weight's rows) and pairs that share one: the least time by the model of linear_tcgen05.cuh,
-// for 128 k in the place of 64.
-inline Plan plan_of8(int64_t m_tiles, int64_t cols, int64_t blocks) {
-    Plan best = {256, 1};
-    double best_cost = 1e30;
-    for (int bn = 256; bn >= 64; bn /= 2) {
-        const int64_t tiles = m_tiles * ((cols + bn - 1) / bn);
-        for (int splits = 1; splits <= 4; splits *= 2) {
-            if ((splits == 2 && tiles > 32) || (splits == 4 && tiles > 14) || blocks < 4 * splits * (splits > 1)) break;
-            const int64_t turns = splits > 1 ? 1 : (tiles + 73) / 74;
-            const double k_ns = double((blocks + splits - 1) / splits) * (110 + 0.85 * bn), join = splits == 1 ? 0 : splits == 4 ? 4500 : tiles > 24 ? 4000 : 2500;
-            const double cost = double(turns) * std::max(k_ns, 500.0 + 4 * bn) + join;
-            if (cost < best_cost * 0.995) { best_cost = cost; best = {bn, splits}; }
-        }
-    }
-    return best;
-}
-
-inline carnator_status launch_product8(const Operand& A, const Operand& B, Args8 a, cudaStream_t stream, char* err, size_t errlen) {
+// Both kernels of a call.  `a`: everything but the plan; `p`: x, scales and header; A: x in 8 bits.
+inline carnator_status launch_product8(const Operand& A, const Operand& B, const Room8& room, Args8 a, PrepareArgs p, int type, cudaStream_t stream, char* err, size_t errlen) {
     a.t.k_batches = 1;
     a.t.k_tiles = ceil_div(a.t.k_len, kBlock);
-    const Plan p = plan_of8(int64_t(a.t.batches) * a.t.tiles_m, a.t.cols, a.t.k_tiles);
-    a.t.bn = p.bn; a.t.splits = p.splits;
+    a.groups = ceil_div(a.t.k_tiles, kGroupBlocks);
+    a.t.tiles_m = ceil_div(a.t.rows, kTileM);
+    const Plan plan = plan_of8(int64_t(a.t.batches) * a.t.tiles_m, a.t.cols, a.groups);
+    a.t.bn = plan.bn; a.t.splits = plan.splits;
     a.t.tiles_n = ceil_div(a.t.cols, a.t.bn);
     const int64_t tiles = int64_t(a.t.batches) * a.t.tiles_m * a.t.tiles_n;
-    if (tiles > (int64_t(1) << 30)) return CARNATOR_ERR_UNSUPPORTED;
+    if (tiles > (int64_t(1) << 30) || int64_t(a.t.batches) * a.t.tiles_m * 2 * a.groups > (int64_t(1) << 30) || int64_t(a.t.tiles_n) * a.groups > (int64_t(1) << 30))
+        return CARNATOR_ERR_UNSUPPORTED;
     a.t.tiles = int(tiles);
     a.t.group_m = 8;
-    const bool f = a.t.e.y_f32;
-    if (p.bn == 256) return f ? launch_stages8<4, true>(A, B, a, stream, err, errlen) : launch_stages8<4, false>(A, B, a, stream, err, errlen);
-    if (p.bn == 128) return f ? launch_stages8<2, true>(A, B, a, stream, err, errlen) : launch_stages8<2, false>(A, B, a, stream, err, errlen);
-    return f ? launch_stages8<1, true>(A, B, a, stream, err, errlen) : launch_stages8<1, false>(A, B, a, stream, err, errlen);
+
+    p.q.batches = a.t.batches; p.q.rows = a.t.rows; p.q.cols = a.t.k_len; p.q.blocks = a.t.k_tiles;
+    p.sfa = room.sfa; p.sfb = room.sfb; p.notes = room.notes; p.hdr = a.t.hdr;
+    p.groups = a.groups; p.row_tiles = a.t.tiles_m * 2;
+    p.cols = a.t.cols; p.bn = a.t.bn; p.tiles_n = a.t.tiles_n;
+    p.x_ctas = type == kXE4m3 ? int(std::min<int64_t>(148 * 8, (int64_t(a.groups) * a.t.rows + fp8::kRowThreads - 1) / fp8::kRowThreads)) : fp8::row_ctas(p.q, type == kXF32);
+    p.w_ctas = int(std::min<int64_t>(kMostWCtas, (int64_t(a.t.tiles_n) * a.groups + 3) / 4));
+    const dim3 grid(unsigned(p.x_ctas + p.w_ctas), unsigned(a.t.batches));
+    const cudaError_t e = type == kXBf16 ? launch_dependent(prepare_fp8_kernel<kXBf16>, grid, dim3(fp8::kRowThreads), 0, stream, p)
+                        : type == kXF32  ? launch_dependent(prepare_fp8_kernel<kXF32>, grid, dim3(fp8::kRowThreads), 0, stream, p)
+                                         : launch_dependent(prepare_fp8_kernel<kXE4m3>, grid, dim3(fp8::kRowThreads), 0, stream, p);
+    if (e != cudaSuccess) return cuda_error(e, "prepare_fp8_kernel", err, errlen);
+    a.notes = room.notes; a.n_notes = int(grid.x * grid.y);
+    a.sfa = room.sfa;
+    // whether a pair's share of k is longer than one accumulator may sum up
+    const int64_t share = int64_t((a.groups + a.t.splits - 1) / a.t.splits) * kGroupBlocks * kBlock;
+    if (a.t.e.y_f32) return launch_stages8<true, true>(A, B, room, a, stream, err, errlen);
+    return share > kLongRunBf16 ? launch_stages8<false, true>(A, B, room, a, stream, err, errlen) : launch_stages8<false, false>(A, B, room, a, stream, err, errlen);
 }
 
 template <int NT, int kType>
