@@ -2,7 +2,7 @@
 //   z = sum over blocks j of 128 k of  sx[row, j] sw[col / 128, j] <qx_j, qw_j>  + bias,   y = residual + gate_b act(z).
 //
 // Scales that are powers of two (fp8_quantize.cuh makes no others) are applied by the tensor cores: kind::mxf8f6f4 takes an exponent per row and 32 k from tensor memory
-// (here the same for the four products of a block), so that an accumulator sums up all of k, or runs of 2560 of it for fp32 outputs, as in linear_tcgen05.cuh.
+// (here the same for the four products of a block), so that an accumulator sums up all of k, or runs of 5120 of it for fp32 outputs.
 // Any other scales: an accumulator sums up one block (kind::f8f6f4, in which nothing is lost: 7 significant bits a product, 128 terms) and the epilogue warps take it
 // times the block's scale into 128 fp32 sums per thread, while the next block's products run into the other accumulator.  That costs the reading of every block's sums
 // from tensor memory, 128 KB per SM and block against 512 clocks of products (75600 x 5120 x 5120: 2068 us, without the epilogue's reads and sums 1584).
@@ -29,6 +29,9 @@ constexpr uint32_t kSfSlots = 10, kSfAt = 210 * 1024; // their ring in shared me
 constexpr uint32_t kSfColumn = 448;                  // first column of the exponents in tensor memory
 static_assert(kSfAt + kSfSlots * (kSfA + kSfB) <= kRingBytes, "shared memory of a CTA");
 enum { kXBf16 = 0, kXF32 = 1, kXE4m3 = 2 };
+// Most k that one accumulator sums up for an fp32 output: as many products of the tensor cores, which cut their sums off, as kLongRun has (measured, quantised normal
+// values: error of a sum of 2560 1.7e-7, of 5120 3.6e-7, of 10240 8.5e-7; all terms positive 7.0e-7, 2.0e-6, 5.2e-6).
+constexpr int kLongRun8 = 2 * kLongRun;
 
 struct Args8 {
     TcArgs t;
@@ -147,12 +150,218 @@ __device__ __forceinline__ float scale_from(uint32_t word, int j) {
     return __uint_as_float(e == 255u ? 0x7FC00000u : e << 23);
 }
 
-// kRuns: an accumulator sums up runs of k only, which the epilogue adds in registers (fp32 outputs, and bf16 ones of a very long k).
+// What an epilogue warp is told.
+struct Epi {
+    uint32_t tmem, base, bars, read0;    // read0: the first of the barriers on which accumulators are given back, in the pair's first CTA
+    int half, first, step, k0, k1, chunks;
+    volatile int* abortp;
+};
+enum { kAtOnce, kEachRun, kEachBlock };  // an accumulator holds a tile's whole sum, a run of it, or that of one block without its scales
+// Its tiles; a shared one is left in shared memory.  (Three functions, so that what one way holds in registers does not cost another: in one loop, the sums of the
+// third spilled what the first needs: 75600 x 5120 x 5120 onto an fp32 stream 2889 us, now 1830.)
+template <bool kF32, int kMode>
+__device__ __forceinline__ void epilogue_warp(const Args8& args, const Epi& c) {
+    const TcArgs& a = args.t;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int quarter = warp & 3, side = (warp - 4) >> 2;               // rows 32 quarter .. of this CTA's 128; every other 32 columns
+    const uint32_t tmem = c.tmem + (uint32_t(quarter * 32) << 16);
+    const uint32_t line = c.base + uint32_t(quarter * 32 + lane) * (uint32_t(a.bn + 4) * 4u);        // of a shared tile
+    bool ok = true;
+    int i = 0, s = 0;
+    uint32_t phase = 0;
+    auto release = [&](int u) __attribute__((always_inline)) {      // this warp has read its part of accumulator u
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) arrive_remote(c.read0 + 8 * u);
+    };
+    for (int t = c.first; t < a.tiles && ok; t += c.step) {
+        int b, m, n;
+        tile_at(a, t, b, m, n);
+        const int row = m * kTileM + c.half * 128 + quarter * 32 + lane, left = min(a.cols - n * a.bn, a.bn);
+        const bool on = row < a.rows;
+        struct Where { int64_t y, gate; const char* res; };          // of this row, worked out where the tile ends: registers are short before that
+        auto where = [&]() __attribute__((always_inline)) {
+            Where w;
+            w.y = b * a.e.ys[0] + row * a.e.ys[1];
+            w.gate = a.e.gate ? (b + row / a.e.rows_per_gate) * a.e.gate_stride : 0;
+            w.res = static_cast<const char*>(a.e.residual) + (b * a.e.rs[0] + row * a.e.rs[1] + n * a.bn) * (kF32 ? 4 : 2);
+            return w;
+        };
+        // A tile ends in steps of 16 columns.  `r`: their residual, where all of them are there.
+        auto fetch = [&](const Where& w, int at, Sector (&r)[kF32 ? 2 : 1]) __attribute__((always_inline)) {
+            if (a.e.residual && a.splits == 1 && on && at + 16 <= left) {
+#pragma unroll
+                for (int h = 0; h < (kF32 ? 2 : 1); ++h) r[h] = load_sector(w.res + at * (kF32 ? 4 : 2) + 32 * h, a.e.wide_ok);
+            }
+        };
+        auto end_of = [&](const Where& w, int at, float (&f)[16], const Sector (&r)[kF32 ? 2 : 1]) __attribute__((always_inline)) {
+            const int col = n * a.bn + at;
+            if (a.splits > 1) {          // the one tile of this cluster: this pair's share to shared memory
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(line + uint32_t(at + 4 * q) * 4u), "f"(f[4 * q]), "f"(f[4 * q + 1]), "f"(f[4 * q + 2]), "f"(f[4 * q + 3]) : "memory");
+            } else if (at + 16 <= left) {
+                if (on) finish16<kF32>(a.e, a.e.gate, w.gate, w.y, 0, col, f, r[0], r[kF32 ? 1 : 0]);
+            } else if (on) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int cn = min(max(left - at - 8 * h, 0), 8);
+                    if (cn > 0) {
+                        norm::Raw8<true> r8;
+                        Columns cols;
+                        columns_begin(a.e, cols, col + 8 * h, cn);
+                        if (a.e.residual) load_residual(a.e, b, row, col + 8 * h, cn, r8);
+                        float g[8];
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) g[q] = f[8 * h + q];
+                        finish(a.e, cols, b, row, col + 8 * h, cn, g, r8);
+                    }
+                }
+            }
+        };
+        __syncwarp();                // rows behind the last one have left the tile before early
+        if constexpr (kMode == kAtOnce) {
+            const int u = i & 1;
+            // this step's residual, the next one's and the one's behind it, of which the first two are fetched under the products
+            Sector r0[kF32 ? 2 : 1], r1[kF32 ? 2 : 1], r2[kF32 ? 2 : 1];
+            auto column = [&](int st) { return side * 32 + 64 * (st >> 1) + 16 * (st & 1); };
+            const Where w = where();
+            fetch(w, column(0), r0);
+            fetch(w, column(1), r1);
+            ok = mbar_wait_warp(c.bars + 128 + 8 * u, uint32_t(i >> 1) & 1u, c.abortp, 20, kDefaultWaitNs);
+            if (!ok) { if (lane == 0) set_status(a.hdr, CARNATOR_ERR_DEVICE_TIMEOUT, 84, i, blockIdx.x); break; }
+            tc_fence_after();
+            ++i;
+            // `next` is filled for the step after the next: three in turn, so that none is moved while it is on its way
+            auto step_of = [&](int st, const Sector (&mine)[kF32 ? 2 : 1], Sector (&next)[kF32 ? 2 : 1]) __attribute__((always_inline)) {
+                if (column(st) >= left) return;      // warp-uniform
+                float v[16];
+                __syncwarp();            // lanes of rows behind the last one have not finished the columns before
+                tmem_ld16(tmem + uint32_t(u * kMostColumns + column(st)), v);
+                fetch(w, column(st + 2), next);
+                __syncwarp();
+                tmem_wait_ld(v);
+                if (column(st + 1) >= left) release(u);
+                end_of(w, column(st), v, mine);
+            };
+#pragma unroll 1
+            for (int st = 0; column(st) < left; st += 3) {
+                step_of(st, r0, r2);
+                step_of(st + 1, r1, r0);
+                step_of(st + 2, r2, r1);
+            }
+            if (side * 32 >= left) release(u);
+            if (a.splits > 1) break;
+        } else {
+        f2 acc[4][16];               // 32 columns each: side * 32, + 64, + 128, + 192
+#pragma unroll
+        for (int p = 0; p < 4; ++p)
+#pragma unroll
+            for (int q = 0; q < 16; ++q) acc[p][q] = two(0.f);
+        if constexpr (kMode == kEachRun) {
+            for (int r = 0; r < c.chunks && ok; ++r, ++i) {
+                const int u = i & 1;
+                ok = mbar_wait_warp(c.bars + 128 + 8 * u, uint32_t(i >> 1) & 1u, c.abortp, 20, kDefaultWaitNs);
+                if (!ok) { if (lane == 0) set_status(a.hdr, CARNATOR_ERR_DEVICE_TIMEOUT, 85, i, blockIdx.x); break; }
+                tc_fence_after();
+#pragma unroll
+                for (int p = 0; p < 4; ++p) {
+                    const int at = side * 32 + 64 * p;
+                    if (at < left) {
+                        float v[32];
+                        tmem_ld32(tmem + uint32_t(u * kMostColumns + at), v);
+                        tmem_wait_ld(v);
+#pragma unroll
+                        for (int q = 0; q < 16; ++q) acc[p][q] = norm::add2(acc[p][q], two(v[2 * q], v[2 * q + 1]));
+                    }
+                }
+                release(u);
+            }
+        } else {
+            // x's scales of four blocks on their way while the four before are used (one block ahead, a block had to wait for them: 75600 x 5120 x 5120 2703 us, four
+            // ahead 2068); the weight's of 32 blocks, one per lane, for each 32 columns
+            const float* xs = args.xscale ? args.xscale + b * args.xss[0] + (on ? row : 0) * args.xss[1] : nullptr;
+            const uint8_t* xe = args.sfa + sf_offset((int64_t(b) * a.tiles_m + m) * 2 + c.half, args.groups, 0, quarter * 32 + lane);
+            float wv[4], xn[4];
+            auto scales = [&](int g) __attribute__((always_inline)) {
+                if (xs) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) xn[j] = load_scale(xs + min(g + j, c.k1 - 1) * args.xss[2]);
+                } else {
+                    const uint32_t word = __float_as_uint(load_scale(reinterpret_cast<const float*>(xe + int64_t(min(g, c.k1 - 1) / kGroupBlocks) * kSfA)));
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) xn[j] = scale_from(word, j);
+                }
+            };
+            scales(c.k0);
+            for (int g = c.k0; g < c.k1 && ok; g += 4) {
+                float xv[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) xv[j] = xn[j];
+                if (((g - c.k0) & 31) == 0) {
+#pragma unroll
+                    for (int p = 0; p < 4; ++p)
+                        wv[p] = load_scale(args.wscale + (min(n * a.bn + side * 32 + 64 * p, a.cols - 1) / kBlock) * args.wss[0] + min(g + lane, c.k1 - 1) * args.wss[1]);
+                }
+                scales(g + 4);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int k = g + j, u = i & 1;
+                    if (k >= c.k1) break;
+                    ok = mbar_wait_warp(c.bars + 64 + 8 * s, phase, c.abortp, 0, kDefaultWaitNs);
+                    if (!ok) { if (lane == 0) set_status(a.hdr, CARNATOR_ERR_DEVICE_TIMEOUT, 86, i, blockIdx.x); break; }
+                    ++i;
+                    if (++s == a.stages) { s = 0; phase ^= 1u; }
+                    tc_fence_after();
+                    const uint32_t from = tmem + uint32_t(u * kMostColumns + side * 32);
+                    float v0[16], v1[16];        // 16 columns in turn: some on their way while the others are added
+                    if (side * 32 < left) tmem_ld16(from, v0);
+#pragma unroll
+                    for (int p = 0; p < 4; ++p) {
+                        const f2 by = two(xv[j] * __shfl_sync(0xffffffffu, wv[p], (k - c.k0) & 31));
+                        if (side * 32 + 64 * p < left) {       // warp-uniform
+                            tmem_wait_ld(v0);
+                            tmem_ld16(from + 64 * p + 16, v1);
+#pragma unroll
+                            for (int q = 0; q < 8; ++q) acc[p][q] = norm::fma2(two(v0[2 * q], v0[2 * q + 1]), by, acc[p][q]);
+                            tmem_wait_ld(v1);
+                            if (side * 32 + 64 * (p + 1) < left && p < 3) tmem_ld16(from + 64 * (p + 1), v0);
+#pragma unroll
+                            for (int q = 0; q < 8; ++q) acc[p][8 + q] = norm::fma2(two(v1[2 * q], v1[2 * q + 1]), by, acc[p][8 + q]);
+                        }
+                    }
+                    release(u);
+                }
+            }
+        }
+        __syncwarp();
+        if (!ok) break;
+        const Where w = where();
+#pragma unroll
+        for (int p = 0; p < 4; ++p)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int at = side * 32 + 64 * p + 16 * h;
+                if (at < left) {     // warp-uniform
+                    Sector r[kF32 ? 2 : 1];
+                    fetch(w, at, r);
+                    float v[16];
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) one_each(acc[p][8 * h + q], v[2 * q], v[2 * q + 1]);
+                    end_of(w, at, v, r);
+                }
+            }
+        if (a.splits > 1) break;     // the one tile of this cluster
+        }
+    }
+}
+
+// kRuns: an accumulator sums up runs of k only, which the epilogue adds in registers (longer sums than one may take up).
 template <bool kF32, bool kRuns>
 __global__ void __launch_bounds__(kThreadsTc, 1)
 linear_fp8_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB, const __grid_constant__ CUtensorMap mapSa,
                   const __grid_constant__ CUtensorMap mapSb, const Args8 args) {
-    constexpr int kRun = (kF32 ? kLongRun : kLongRunBf16) / kBlock;
+    constexpr int kRun = (kF32 ? kLongRun8 : kLongRunBf16) / kBlock;
     static_assert(kRun % kGroupBlocks == 0, "runs are whole groups");
     const TcArgs& a = args.t;
     extern __shared__ unsigned char lin_smem[];
@@ -323,180 +532,9 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constan
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 208;" ::: "memory");
         // ================= epilogue =================
-        const int quarter = warp & 3, side = (warp - 4) >> 2;               // rows 32 quarter .. of this CTA's 128; every other 32 columns
-        const uint32_t lane_base = uint32_t(quarter * 32) << 16;
-        const uint32_t read0 = map_cta(bar_read(0), leader);
-        const uint32_t line = base + uint32_t(quarter * 32 + lane) * (uint32_t(a.bn + 4) * 4u);        // of a shared tile
-        bool ok = true;
-        int i = 0, s = 0;
-        uint32_t phase = 0;
-        auto release = [&](int u) {      // this warp has read its part of accumulator u
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) arrive_remote(read0 + 8 * u);
-        };
-        for (int t = first; t < a.tiles && ok; t += step) {
-            int b, m, n;
-            tile_at(a, t, b, m, n);
-            const int row = m * kTileM + int(half) * 128 + quarter * 32 + lane, left = min(a.cols - n * a.bn, a.bn);
-            const bool on = row < a.rows;
-            const int64_t y_off = b * a.e.ys[0] + row * a.e.ys[1], r_off = b * a.e.rs[0] + row * a.e.rs[1];
-            const int64_t gate_off = a.e.gate ? (b + row / a.e.rows_per_gate) * a.e.gate_stride : 0;
-            const char* res = static_cast<const char*>(a.e.residual) + (r_off + n * a.bn) * (kF32 ? 4 : 2);
-            // the end of 32 columns of the tile from `at` on, which a thread holds as 16 pairs
-            auto end_of = [&](int at, const f2 (&v)[16]) {
-                const int col = n * a.bn + at;
-                if (at >= left || !on) return;
-                if (at + 32 <= left) {
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        Sector r0, r1;
-                        if (a.e.residual) {
-                            r0 = load_sector(res + (at + 16 * h) * (kF32 ? 4 : 2), a.e.wide_ok);
-                            if (kF32) r1 = load_sector(res + (at + 16 * h) * 4 + 32, a.e.wide_ok);
-                        }
-                        float f[16];
-#pragma unroll
-                        for (int q = 0; q < 8; ++q) one_each(v[8 * h + q], f[2 * q], f[2 * q + 1]);
-                        finish16<kF32>(a.e, a.e.gate, gate_off, y_off, 0, col + 16 * h, f, r0, kF32 ? r1 : r0);
-                    }
-                } else {
-#pragma unroll
-                    for (int h = 0; h < 4; ++h) {
-                        const int cn = min(max(left - at - 8 * h, 0), 8);
-                        if (cn > 0) {
-                            norm::Raw8<true> r8;
-                            Columns cols;
-                            columns_begin(a.e, cols, col + 8 * h, cn);
-                            if (a.e.residual) load_residual(a.e, b, row, col + 8 * h, cn, r8);
-                            float f[8];
-#pragma unroll
-                            for (int q = 0; q < 4; ++q) one_each(v[4 * h + q], f[2 * q], f[2 * q + 1]);
-                            finish(a.e, cols, b, row, col + 8 * h, cn, f, r8);
-                        }
-                    }
-                }
-            };
-            auto to_shared = [&](int at, const f2 (&v)[16]) {
-#pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    float f[4];
-                    one_each(v[2 * q], f[0], f[1]);
-                    one_each(v[2 * q + 1], f[2], f[3]);
-                    asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(line + uint32_t(at + 4 * q) * 4u), "f"(f[0]), "f"(f[1]), "f"(f[2]), "f"(f[3]) : "memory");
-                }
-            };
-            __syncwarp();                // rows behind the last one have left the tile before early
-            if (scaled && !kRuns) {
-                const int u = i & 1;
-                ok = mbar_wait_warp(bar_sum(u), uint32_t(i >> 1) & 1u, abortp, 20, limit);
-                if (!ok) { if (lane == 0) set_status(a.hdr, CARNATOR_ERR_DEVICE_TIMEOUT, 84, i, blockIdx.x); break; }
-                tc_fence_after();
-                ++i;
-                for (int at = side * 32; at < left; at += 64) {        // warp-uniform
-                    float v[32];
-                    __syncwarp();
-                    tmem_ld32(tmem + lane_base + uint32_t(u * kMostColumns + at), v);
-                    tmem_wait_ld(v);
-                    if (at + 64 >= left) release(u);
-                    f2 w[16];
-#pragma unroll
-                    for (int q = 0; q < 16; ++q) w[q] = two(v[2 * q], v[2 * q + 1]);
-                    if (a.splits > 1) to_shared(at, w);
-                    else end_of(at, w);
-                }
-                if (side * 32 >= left) release(u);
-                if (a.splits > 1) break;
-                continue;
-            }
-            f2 acc[4][16];               // 32 columns each: side * 32, + 64, + 128, + 192
-#pragma unroll
-            for (int p = 0; p < 4; ++p)
-#pragma unroll
-                for (int q = 0; q < 16; ++q) acc[p][q] = two(0.f);
-            if (kRuns && scaled) {
-                for (int c = 0; c < chunks && ok; ++c, ++i) {
-                    const int u = i & 1;
-                    ok = mbar_wait_warp(bar_sum(u), uint32_t(i >> 1) & 1u, abortp, 20, limit);
-                    if (!ok) { if (lane == 0) set_status(a.hdr, CARNATOR_ERR_DEVICE_TIMEOUT, 85, i, blockIdx.x); break; }
-                    tc_fence_after();
-#pragma unroll
-                    for (int p = 0; p < 4; ++p) {
-                        const int at = side * 32 + 64 * p;
-                        if (at < left) {
-                            float v[32];
-                            tmem_ld32(tmem + lane_base + uint32_t(u * kMostColumns + at), v);
-                            tmem_wait_ld(v);
-#pragma unroll
-                            for (int q = 0; q < 16; ++q) acc[p][q] = norm::add2(acc[p][q], two(v[2 * q], v[2 * q + 1]));
-                        }
-                    }
-                    release(u);
-                }
-            } else {
-                // x's scales of four blocks on their way while the four before are used (one block ahead, a block had to wait for them: 75600 x 5120 x 5120 2703 us, four
-                // ahead 2068); the weight's of 32 blocks, one per lane, for each 32 columns
-                const float* xs = args.xscale ? args.xscale + b * args.xss[0] + (on ? row : 0) * args.xss[1] : nullptr;
-                const uint8_t* xe = args.sfa + sf_offset((int64_t(b) * a.tiles_m + m) * 2 + half, args.groups, 0, quarter * 32 + lane);
-                const float* ws[4];
-                float wv[4], xn[4];
-#pragma unroll
-                for (int p = 0; p < 4; ++p) ws[p] = args.wscale + (min(n * a.bn + side * 32 + 64 * p, a.cols - 1) / kBlock) * args.wss[0];
-                auto fetch = [&](int g) {
-                    if (xs) {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) xn[j] = load_scale(xs + min(g + j, k1 - 1) * args.xss[2]);
-                    } else {
-                        const uint32_t word = __float_as_uint(load_scale(reinterpret_cast<const float*>(xe + int64_t(min(g, k1 - 1) / kGroupBlocks) * kSfA)));
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) xn[j] = scale_from(word, j);
-                    }
-                };
-                fetch(k0);
-                for (int g = k0; g < k1 && ok; g += 4) {
-                    float xv[4];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) xv[j] = xn[j];
-                    if (((g - k0) & 31) == 0) {
-#pragma unroll
-                        for (int p = 0; p < 4; ++p) wv[p] = load_scale(ws[p] + min(g + lane, k1 - 1) * args.wss[1]);
-                    }
-                    fetch(g + 4);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int k = g + j, u = i & 1;
-                        if (k >= k1) break;
-                        ok = mbar_wait_warp(bar_done(s), phase, abortp, 0, limit);
-                        if (!ok) { if (lane == 0) set_status(a.hdr, CARNATOR_ERR_DEVICE_TIMEOUT, 86, i, blockIdx.x); break; }
-                        ++i;
-                        if (++s == a.stages) { s = 0; phase ^= 1u; }
-                        tc_fence_after();
-#pragma unroll
-                        for (int p = 0; p < 4; ++p) {
-                            const int at = side * 32 + 64 * p;
-                            const f2 by = two(xv[j] * __shfl_sync(0xffffffffu, wv[p], (k - k0) & 31));
-                            if (at < left) {
-                                float v[32];
-                                tmem_ld32(tmem + lane_base + uint32_t(u * kMostColumns + at), v);
-                                tmem_wait_ld(v);
-#pragma unroll
-                                for (int q = 0; q < 16; ++q) acc[p][q] = norm::fma2(two(v[2 * q], v[2 * q + 1]), by, acc[p][q]);
-                            }
-                        }
-                        release(u);
-                    }
-                }
-            }
-            __syncwarp();
-            if (!ok) break;
-#pragma unroll
-            for (int p = 0; p < 4; ++p) {
-                const int at = side * 32 + 64 * p;
-                if (a.splits == 1) end_of(at, acc[p]);
-                else if (at < left) to_shared(at, acc[p]);
-            }
-            if (a.splits > 1) break;     // the one tile of this cluster
-        }
+        const Epi c = {tmem, base, bars, map_cta(bars + 144, leader), int(half), first, step, k0, k1, chunks, abortp};
+        if (!scaled) epilogue_warp<kF32, kEachBlock>(args, c);
+        else epilogue_warp<kF32, kRuns ? kEachRun : kAtOnce>(args, c);
         if (a.splits > 1) {
             tc_fence_before();
             join_shares(a, base, first, split, half, abortp, tid - 128, 32 * kEpiWarps);
@@ -786,7 +824,8 @@ inline carnator_status launch_product8(const Operand& A, const Operand& B, const
     a.sfa = room.sfa;
     // whether a pair's share of k is longer than one accumulator may sum up
     const int64_t share = int64_t((a.groups + a.t.splits - 1) / a.t.splits) * kGroupBlocks * kBlock;
-    if (a.t.e.y_f32) return launch_stages8<true, true>(A, B, room, a, stream, err, errlen);
+    if (a.t.e.y_f32)
+        return share > kLongRun8 ? launch_stages8<true, true>(A, B, room, a, stream, err, errlen) : launch_stages8<true, false>(A, B, room, a, stream, err, errlen);
     return share > kLongRunBf16 ? launch_stages8<false, true>(A, B, room, a, stream, err, errlen) : launch_stages8<false, false>(A, B, room, a, stream, err, errlen);
 }
 

@@ -197,7 +197,7 @@ def test_activations_types_and_entries(act, B, N, x, y, p, extra, powers):
 @pytest.mark.parametrize("y", ["bf16", "f32"])
 @pytest.mark.parametrize("N,K,M", [(40, 30000, 64), (20, 70000, 40), (600, 20000, 700), (300, 5121, 2240), (9000, 3000, 1000)])
 def test_long_sums(N, K, M, y, powers):
-    """Runs of 2560 for fp32 outputs and of 65536 for bf16 ones, in one pair's hands or in several."""
+    """Runs of 5120 for fp32 outputs and of 65536 for bf16 ones, in one pair's hands or in several."""
     check_call(make(1, N, K, M, x="e4m3", y=y, powers=powers), cn.ACT_NONE)
 
 
@@ -236,14 +236,14 @@ def test_parts_that_are_left_out(bias, gate, residual, N):
 @pytest.mark.parametrize("powers", [True, False])
 @pytest.mark.parametrize("N", [4, 40, 500])
 def test_sums_are_taken_in_32_bits(N, powers):
-    """fp32 outputs: blocks of different scale, positive terms only.  A sum in the tensor cores of 2560 terms loses at most a step of 2^-23 for each of its 80 products,
-    on average half of one; sums of blocks in the epilogue less: 40 steps of 2^-24 allowed."""
+    """fp32 outputs: blocks of different scale, positive terms only.  A sum of 5120 terms in the tensor cores is cut off at each of its 160 products, by half a step of 2^-23 of what it
+    has reached on average, which is half of the result on average: 80 times 2^-24; sums of blocks in the epilogue lose less."""
     t = make(1, N, 5120, 300, x="e4m3", y="f32", bias=False, gate=False, residual=False, powers=powers)
     t["x"].copy_(t["x"].float().abs())
     t["w"].copy_(t["w"].float().abs())
     y = check_call(t, cn.ACT_NONE)
     ry, _ = product_ref(t, cn.ACT_NONE)
-    assert (y.double() - ry).norm() <= 40 * U32 * ry.norm()
+    assert (y.double() - ry).norm() <= 80 * U32 * ry.norm()
 
 
 @pytest.mark.parametrize("powers", [True, False])
