@@ -99,7 +99,7 @@ struct QuantArgs {
 };
 
 // A scale per row: 8 lanes a block, kAhead blocks of a row on their way per lane.  The groups of 8 lanes of `ctas` CTAs walk over (row, run of kAhead blocks);
-// put(row, block, scale) is called by one lane of each.
+// put(row, block, scales) is called by one lane of each, with those of kAhead blocks (past the last block: of zeros).
 constexpr int kRowThreads = 256;
 template <bool F32> constexpr int kAheadOf = F32 ? 2 : 4;
 template <bool F32, int kAhead, typename Put>
@@ -119,16 +119,14 @@ __device__ __forceinline__ void quantize_rows(const QuantArgs& a, int b, int cta
             n[k] = on ? min(max(a.cols - col, 0), kLaneChannels) : 0;
             v[k].load(a.x, b * a.xs[0] + row * a.xs[1] + col, n[k]);
         }
+        float scale[kAhead];
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
-            float scale, inverse;
-            scale_of(block_most(v[k].most()), scale, inverse);
-            if (n[k] > 0) {
-                const int col = (blk + k) * kBlock + l * kLaneChannels;
-                store_q(a.q + b * a.qs[0] + row * a.qs[1] + col, v[k].quantized(inverse), n[k]);
-                if (l == 0) put(row, blk + k, scale);
-            }
+            float inverse;
+            scale_of(block_most(v[k].most()), scale[k], inverse);
+            if (n[k] > 0) store_q(a.q + b * a.qs[0] + row * a.qs[1] + (blk + k) * kBlock + l * kLaneChannels, v[k].quantized(inverse), n[k]);
         }
+        if (on && l == 0) put(row, blk, scale);
     }
 }
 template <bool F32, int kAhead>
@@ -136,7 +134,11 @@ __global__ void __launch_bounds__(kRowThreads) quantize_rows_kernel(const QuantA
     const int b = blockIdx.y;
     grid_launch_dependents();
     grid_wait();
-    quantize_rows<F32, kAhead>(a, b, blockIdx.x, gridDim.x, [&](int row, int blk, float scale) { a.scale[b * a.ss[0] + row * a.ss[1] + blk * a.ss[2]] = scale; });
+    quantize_rows<F32, kAhead>(a, b, blockIdx.x, gridDim.x, [&](int row, int blk, const float (&scale)[kAhead]) {
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+            if (blk + k < a.blocks) a.scale[b * a.ss[0] + row * a.ss[1] + (blk + k) * a.ss[2]] = scale[k];
+    });
 }
 
 // A scale per 128 x 128: a CTA per block, four rows per lane.

@@ -59,7 +59,7 @@ struct PrepareArgs {
     const float* xscale; const float* wscale;
     int64_t xss[3], wss[2];
     uint8_t* sfa; uint8_t* sfb;          // sfb: [column tiles][groups][1024], two times 128 columns
-    int* notes;                          // one per CTA
+    int* notes;                          // one per CTA that looks at scales it was given
     WsHeader* hdr;
     int groups, row_tiles;               // row tiles of 128 per batch entry
     int cols, bn, tiles_n;
@@ -86,9 +86,16 @@ __global__ void __launch_bounds__(fp8::kRowThreads) prepare_fp8_kernel(const Pre
             }
         } else {
             constexpr bool kF = kType == kXF32;
-            fp8::quantize_rows<kF, fp8::kAheadOf<kF>>(a.q, b, cta, a.x_ctas, [&](int row, int blk, float scale) {
+            constexpr int kAhead = fp8::kAheadOf<kF>;
+            static_assert(kGroupBlocks % kAhead == 0, "a lane's blocks lie within a word");
+            fp8::quantize_rows<kF, kAhead>(a.q, b, cta, a.x_ctas, [&](int row, int blk, const float (&scale)[kAhead]) {
                 int none = 0;
-                a.sfa[sf_offset(int64_t(b) * a.row_tiles + row / 128, a.groups, blk / kGroupBlocks, row % 128) + blk % kGroupBlocks] = uint8_t(exponent_of(scale, none));
+                uint32_t word = 0;
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k) word |= exponent_of(scale[k], none) << (8 * k);
+                uint8_t* to = a.sfa + sf_offset(int64_t(b) * a.row_tiles + row / 128, a.groups, blk / kGroupBlocks, row % 128) + blk % kGroupBlocks;
+                if (kAhead == 4) *reinterpret_cast<uint32_t*>(to) = word;
+                else *reinterpret_cast<uint16_t*>(to) = uint16_t(word);
             });
         }
     } else if (b == 0) {
@@ -108,8 +115,11 @@ __global__ void __launch_bounds__(fp8::kRowThreads) prepare_fp8_kernel(const Pre
             *reinterpret_cast<uint32_t*>(a.sfb + tg * kSfB + (c >> 7) * 512 + (c & 31) * 16 + ((c & 127) >> 5) * 4) = word;
         }
     }
+    // x that is quantised here has powers of two; a weight's scales are looked at once
+    const int first = kType == kXE4m3 ? 0 : a.x_ctas;
+    if (cta < first || (cta >= a.x_ctas && b > 0)) return;
     note = __syncthreads_or(note);
-    if (tid == 0) a.notes[int64_t(b) * gridDim.x + cta] = note;
+    if (tid == 0) a.notes[cta >= a.x_ctas ? cta - a.x_ctas : a.w_ctas + b * a.x_ctas + cta] = note;
 }
 
 // ---- the product ------------------------------------------------------------------------------------------
@@ -398,9 +408,14 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constan
     tc_fence_after();
     const uint32_t tmem = tmem_slot;
     grid_wait();                         // launched while the kernel ahead drains: nothing of global memory is touched before this
-    int note = 0;
-    for (int i = tid; i < args.n_notes; i += kThreadsTc) note |= reinterpret_cast<const volatile int*>(args.notes)[i];
-    const bool scaled = __syncthreads_or(note) == 0;       // all of the call's scales are powers of two (the same in every CTA)
+    // Whether all of the call's scales are powers of two: the same in every CTA.  Each warp looks for itself, while the first copies are on their way.
+    auto all_powers = [&]() {
+        int note = 0;
+#pragma unroll 4
+        for (int i = lane; i < args.n_notes; i += 32) note |= reinterpret_cast<const volatile int*>(args.notes)[i];
+        return __any_sync(0xffffffffu, note != 0) == 0;
+    };
+    __syncwarp();                        // whole warps hand over registers (setmaxnreg)
 
     // the clusters take the tiles in turn; with splits > 1 there is one cluster per tile and a pair has its share of k, in whole groups
     const int first = int(blockIdx.x / (2 * a.splits)), step = int(gridDim.x / (2 * a.splits));
@@ -427,7 +442,7 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constan
                     if (issued >= a.stages && !mbar_wait(bar_done(s), phase ^ 1u, abortp, 0, limit)) {
                         set_status(a.hdr, CARNATOR_ERR_DEVICE_TIMEOUT, 80, k, blockIdx.x); ok = false; break;
                     }
-                    const bool sf = scaled && k % kGroupBlocks == 0;
+                    const bool sf = k % kGroupBlocks == 0;             // used or not
                     if (half == 0) mbar_expect_tx(bar_full(s), 2 * (stage_bytes + (sf ? kSfA + kSfB : 0u)));
                     const uint32_t sa = base + uint32_t(s) * stage_bytes, bar = full0 + 8 * s;
                     if (sf) {            // its slot: of the group kSfSlots back, whose last block lies further back than there are stages
@@ -464,6 +479,7 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constan
             const uint64_t da0 = smem_desc(base, 16, 1024), db0 = smem_desc(base + kABytes8, 16, 1024);
             const uint32_t a_lo = uint32_t(da0), a_hi = uint32_t(da0 >> 32), b_lo = uint32_t(db0), b_hi = uint32_t(db0 >> 32);
             const int last = (a.k_len - (a.k_tiles - 1) * kBlock + 31) / 32;
+            const bool scaled = all_powers();
             int s = 0, i = 0, group = 0;
             uint32_t phase = 0;
             bool ok = true;
@@ -533,7 +549,7 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constan
         asm volatile("setmaxnreg.inc.sync.aligned.u32 208;" ::: "memory");
         // ================= epilogue =================
         const Epi c = {tmem, base, bars, map_cta(bars + 144, leader), int(half), first, step, k0, k1, chunks, abortp};
-        if (!scaled) epilogue_warp<kF32, kEachBlock>(args, c);
+        if (!all_powers()) epilogue_warp<kF32, kEachBlock>(args, c);
         else epilogue_warp<kF32, kRuns ? kEachRun : kAtOnce>(args, c);
         if (a.splits > 1) {
             tc_fence_before();
@@ -628,6 +644,7 @@ __global__ void __launch_bounds__(32 * kWarps) linear_fp8_rows_kernel(const Rows
 #pragma unroll
         for (int q = 0; q < U; ++q) {
             const int kb = blk + q * kWarps;
+            if (kb >= blocks) break;     // warp-uniform
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
                 uint4 xq[2];
@@ -635,7 +652,7 @@ __global__ void __launch_bounds__(32 * kWarps) linear_fp8_rows_kernel(const Rows
                 if constexpr (kType == kXE4m3) {
 #pragma unroll
                     for (int h = 0; h < 2; ++h) xq[h] = xon[j] ? load_q16(static_cast<const uint8_t*>(a.x) + xo[j], kb * kBlock + h * 64 + t * 16, a.K) : zero;
-                    sx = xon[j] && kb < blocks ? load_scale(a.xscale + so[j] + kb * a.xss[2]) : 0.f;
+                    sx = xon[j] ? load_scale(a.xscale + so[j] + kb * a.xss[2]) : 0.f;
                 } else {
                     fp8::Lane16<kType == kXF32> v[2];
 #pragma unroll
@@ -659,10 +676,8 @@ __global__ void __launch_bounds__(32 * kWarps) linear_fp8_rows_kernel(const Rows
                 }
                 // d0, d1: feature g, rows 2t and 2t + 1 of x; d2, d3: feature g + 8
                 const float s0 = __shfl_sync(0xffffffffu, sx, 8 * t) * sw[q], s1 = __shfl_sync(0xffffffffu, sx, 8 * t + 4) * sw[q];
-                if (kb < blocks) {       // (0 times an infinite or NaN scale would not be nothing)
-                    acc[j][0] = fmaf(d[0], s0, acc[j][0]); acc[j][1] = fmaf(d[1], s1, acc[j][1]);
-                    acc[j][2] = fmaf(d[2], s0, acc[j][2]); acc[j][3] = fmaf(d[3], s1, acc[j][3]);
-                }
+                acc[j][0] = fmaf(d[0], s0, acc[j][0]); acc[j][1] = fmaf(d[1], s1, acc[j][1]);
+                acc[j][2] = fmaf(d[2], s0, acc[j][2]); acc[j][3] = fmaf(d[3], s1, acc[j][3]);
             }
         }
     }
@@ -715,18 +730,22 @@ inline bool make_map_sf(CUtensorMap* map, const void* base, int64_t rows, int wo
               CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Columns of a tile and pairs that share one: the least time by the model of linear_tcgen05.cuh, for 128 k in the place of 64.
+// Columns of a tile and pairs that share one: the least time by a model in nanoseconds that was fitted to launches of 40 to 3000 rows.  A pair takes 260 + 0.55
+// columns per block of 128 k: an SM takes in some 92 bytes a nanosecond (with one product of each block's four left out, 333 instead of 400 ns at 224 columns), and
+// below that its waits take 250 whatever the width.  Joining two pairs costs 1 to 2 us, four 2 to 4 (40 x 4096 x 1536 in 128 columns: one pair 16.9 us, two
+// 13.9, four 12.5; 64 x 9216 x 1536 28.9, 20.5, 17.8).  33 clusters of 4 CTAs or 15 of 8 find room at a time.
 constexpr int kLeastColumns = 64;
-inline Plan plan_of8(int64_t m_tiles, int64_t cols, int64_t groups) {
+inline Plan plan_of8(int64_t m_tiles, int64_t cols, int64_t blocks) {
     Plan best = {kMostColumns, 1};
     double best_cost = 1e30;
+    const int64_t groups = (blocks + kGroupBlocks - 1) / kGroupBlocks;
     for (int bn = kMostColumns; bn >= kLeastColumns; bn -= 32) {
         const int64_t tiles = m_tiles * ((cols + bn - 1) / bn);
         for (int splits = 1; splits <= 4; splits *= 2) {
-            if ((splits == 2 && tiles > 32) || (splits == 4 && tiles > 14) || groups < splits * (splits > 1) || bn % (8 * splits)) break;
+            if ((splits == 2 && tiles > 32) || (splits == 4 && tiles > 14) || groups < splits || bn % (8 * splits)) break;
             const int64_t turns = splits > 1 ? 1 : (tiles + 73) / 74;
-            const double k_ns = 4.0 * double((groups + splits - 1) / splits) * (75 + 0.85 * bn), join = splits == 1 ? 0 : splits == 4 ? 4500 : tiles > 24 ? 4000 : 2500;
-            const double cost = double(turns) * std::max(k_ns, 500.0 + 4 * bn) + join;
+            const double share = splits == 1 ? double(blocks) : double((groups + splits - 1) / splits * kGroupBlocks);
+            const double cost = double(turns) * std::max(share * (260 + 0.55 * bn), 500.0 + 4 * bn) + (splits == 1 ? 0 : splits == 2 ? 1800 : 3600);
             if (cost < best_cost * 0.995) { best_cost = cost; best = {bn, splits}; }
         }
     }
@@ -734,7 +753,7 @@ inline Plan plan_of8(int64_t m_tiles, int64_t cols, int64_t groups) {
 }
 
 // What a call needs besides its arguments: notes, exponents, and x in 8 bits where the call makes it.
-constexpr int kMostWCtas = 64;
+constexpr int kMostWCtas = 512;
 struct Room8 { int* notes; uint8_t* sfa; uint8_t* sfb; uint8_t* q; int64_t q_stride; size_t bytes; };
 inline Room8 room8_of(char* p, int64_t batches, int64_t rows, int64_t cols, int64_t k, bool quantises) {
     Room8 r = {};
@@ -800,7 +819,7 @@ inline carnator_status launch_product8(const Operand& A, const Operand& B, const
     a.t.k_tiles = ceil_div(a.t.k_len, kBlock);
     a.groups = ceil_div(a.t.k_tiles, kGroupBlocks);
     a.t.tiles_m = ceil_div(a.t.rows, kTileM);
-    const Plan plan = plan_of8(int64_t(a.t.batches) * a.t.tiles_m, a.t.cols, a.groups);
+    const Plan plan = plan_of8(int64_t(a.t.batches) * a.t.tiles_m, a.t.cols, a.t.k_tiles);
     a.t.bn = plan.bn; a.t.splits = plan.splits;
     a.t.tiles_n = ceil_div(a.t.cols, a.t.bn);
     const int64_t tiles = int64_t(a.t.batches) * a.t.tiles_m * a.t.tiles_n;
@@ -814,13 +833,13 @@ inline carnator_status launch_product8(const Operand& A, const Operand& B, const
     p.groups = a.groups; p.row_tiles = a.t.tiles_m * 2;
     p.cols = a.t.cols; p.bn = a.t.bn; p.tiles_n = a.t.tiles_n;
     p.x_ctas = type == kXE4m3 ? int(std::min<int64_t>(148 * 8, (int64_t(a.groups) * a.t.rows + fp8::kRowThreads - 1) / fp8::kRowThreads)) : fp8::row_ctas(p.q, type == kXF32);
-    p.w_ctas = int(std::min<int64_t>(kMostWCtas, (int64_t(a.t.tiles_n) * a.groups + 3) / 4));
+    p.w_ctas = int(std::min<int64_t>(kMostWCtas, int64_t(a.t.tiles_n) * a.groups));
     const dim3 grid(unsigned(p.x_ctas + p.w_ctas), unsigned(a.t.batches));
     const cudaError_t e = type == kXBf16 ? launch_dependent(prepare_fp8_kernel<kXBf16>, grid, dim3(fp8::kRowThreads), 0, stream, p)
                         : type == kXF32  ? launch_dependent(prepare_fp8_kernel<kXF32>, grid, dim3(fp8::kRowThreads), 0, stream, p)
                                          : launch_dependent(prepare_fp8_kernel<kXE4m3>, grid, dim3(fp8::kRowThreads), 0, stream, p);
     if (e != cudaSuccess) return cuda_error(e, "prepare_fp8_kernel", err, errlen);
-    a.notes = room.notes; a.n_notes = int(grid.x * grid.y);
+    a.notes = room.notes; a.n_notes = p.w_ctas + (type == kXE4m3 ? p.x_ctas * a.t.batches : 0);
     a.sfa = room.sfa;
     // whether a pair's share of k is longer than one accumulator may sum up
     const int64_t share = int64_t((a.groups + a.t.splits - 1) / a.t.splits) * kGroupBlocks * kBlock;
