@@ -1062,19 +1062,28 @@ def _block_packed(of: bytes, strides: tuple):
 
 
 def _fit_vectors(said, dev, post_weight, post_bias, gate, weight, bias, shift, scale):
-    for t, what, to in ((post_weight, "post_weight", said.vec), (post_bias, "post_bias", said.vec), (weight, "weight", said.vec), (bias, "bias", said.vec),
-                        (gate, "gate", said.gate), (shift, "shift", said.shift), (scale, "scale", said.scale)):
-        if t is not None:
-            _fit(t, what, *to, dev)
+    if post_weight is not None:
+        _fit(post_weight, "post_weight", *said.vec, dev)
+    if post_bias is not None:
+        _fit(post_bias, "post_bias", *said.vec, dev)
+    if weight is not None:
+        _fit(weight, "weight", *said.vec, dev)
+    if bias is not None:
+        _fit(bias, "bias", *said.vec, dev)
+    if gate is not None:
+        _fit(gate, "gate", *said.gate, dev)
+    if shift is not None:
+        _fit(shift, "shift", *said.shift, dev)
+    if scale is not None:
+        _fit(scale, "scale", *said.scale, dev)
 
 
 def block_norm(R, X, shape: BlockNormShape, post_weight=None, post_bias=None, gate=None, weight=None, bias=None, shift=None, scale=None, S=None, Y=None, stats=None,
                stream=None):
     """carnator_block_norm.  Returns (S, Y) [B,N,C] (its own, with rows on 16-byte boundaries, unless given; S may be R); stats fp32 [4,B,N] is written if given."""
     dev = X.device
-    own = tuple(name for t, name in ((S, "s_stride"), (Y, "y_stride")) if t is None)
-    if own:                              # the caller's record stays as it is
-        said, size, n = _block_packed(bytes(shape), own)
+    if S is None or Y is None:           # the caller's record stays as it is
+        said, size, n = _block_packed(bytes(shape), tuple(name for t, name in ((S, "s_stride"), (Y, "y_stride")) if t is None))
         S = _room(size, n, said.s[0], dev) if S is None else S
         Y = _room(size, n, said.y[0], dev) if Y is None else Y
     else:
@@ -1117,9 +1126,8 @@ def block_norm_backward(dY, S, X, stats, shape: BlockNormShape, dS=None, post_we
     scale (if there is a scale, or ``modulated`` says that there is a shift only)."""
     import torch
     dev = X.device
-    own = tuple(name for t, name in ((dR, "dr_stride"), (dX, "dx_stride")) if t is None)
-    if own:
-        said, size, n = _block_packed(bytes(shape), own)
+    if dR is None or dX is None:
+        said, size, n = _block_packed(bytes(shape), tuple(name for t, name in ((dR, "dr_stride"), (dX, "dx_stride")) if t is None))
         dR = _room(size, n, said.dr[0], dev) if dR is None else dR
         dX = _room(size, n, said.dx[0], dev) if dX is None else dX
     else:
@@ -1136,20 +1144,25 @@ def block_norm_backward(dY, S, X, stats, shape: BlockNormShape, dS=None, post_we
     _fit_vectors(said, dev, post_weight, post_bias, gate, weight, bias, None, scale)
     B, C = said.record.B, said.record.C
 
-    def room(name, there, *size):
-        return torch.empty(size, dtype=torch.float32, device=dev) if there and name in want else None
     mod = scale is not None if modulated is None else modulated
-    grads = (room("post_weight", post_weight is not None, C), room("post_bias", post_bias is not None, C), room("gate", gate is not None, B, C),
-             room("weight", weight is not None, C), room("bias", bias is not None, C), room("shift", mod, B, C), room("scale", mod, B, C))
+    new = stats.new_empty                # fp32, where the tensors are: the quickest way to a tensor, and a small call's time is the host's
+    dpw = new(C) if post_weight is not None and "post_weight" in want else None
+    dpb = new(C) if post_bias is not None and "post_bias" in want else None
+    dg = new(B, C) if gate is not None and "gate" in want else None
+    dw = new(C) if weight is not None and "weight" in want else None
+    db = new(C) if bias is not None and "bias" in want else None
+    dsh = new(B, C) if mod and "shift" in want else None
+    dsc = new(B, C) if mod and "scale" in want else None
     if ws is None:
         ws = _new_ws(block_norm_backward_workspace_bytes(said.record), dev)
     elif ws.device != dev or not ws.is_contiguous():
         raise ValueError(f"ws must be contiguous and on {dev}")
     st = lib().carnator_block_norm_backward(_ptr(dY), _ptr(dS), _ptr(S), _ptr(X), _ptr(stats), _ptr(post_weight), _ptr(post_bias), _ptr(gate), _ptr(weight), _ptr(bias),
-                                            _ptr(scale), said.ref, _ptr(dR), _ptr(dX), *(_ptr(g) for g in grads), _ptr(ws), ws.numel(), on)
+                                            _ptr(scale), said.ref, _ptr(dR), _ptr(dX), _ptr(dpw), _ptr(dpb), _ptr(dg), _ptr(dw), _ptr(db), _ptr(dsh), _ptr(dsc),
+                                            _ptr(ws), ws.numel(), on)
     if st != OK:
         _check(st, "carnator_block_norm_backward")
-    return BlockNormGrads(dR, dX, *grads)
+    return BlockNormGrads(dR, dX, dpw, dpb, dg, dw, db, dsh, dsc)
 
 
 # ---- 8-bit operands and their product ---------------------------------------------------------------------

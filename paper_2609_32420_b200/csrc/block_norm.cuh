@@ -258,19 +258,27 @@ __global__ void __launch_bounds__(kThreads, 1) block_forward_kernel(const Args2 
     copies_wait(0);
 }
 
-// Sums of two values over a slot's warps
+// Sums of two values over a slot's warps.  Within a warp the first step hands one value to the lane half across and takes the other from it, so that two sums take five
+// exchanges: the first ends up in the lanes below 16, the second in those above.
 __device__ __forceinline__ void slot_sums(float& s1, float& s2, const Place<32>& pl, int warps, float2* room) {
-    s1 = lanes_sum<32>(s1);
-    s2 = lanes_sum<32>(s2);
-    if (warps > 1) {
-        if ((threadIdx.x & 31) == 0) room[pl.warp] = make_float2(s1, s2);
-        slot_sync(pl.slot, pl.stride);
-        s1 = 0.f; s2 = 0.f;
-        for (int w = 0; w < warps; ++w) { const float2 q = room[w]; s1 += q.x; s2 += q.y; }
+    const int lane = threadIdx.x & 31;
+    float s = (lane & 16 ? s2 : s1) + __shfl_xor_sync(0xffffffffu, lane & 16 ? s1 : s2, 16);
+#pragma unroll
+    for (int m = 8; m > 0; m >>= 1) s += __shfl_xor_sync(0xffffffffu, s, m);
+    if (warps == 1) {
+        s1 = __shfl_sync(0xffffffffu, s, 0);
+        s2 = __shfl_sync(0xffffffffu, s, 16);
+        return;
     }
+    if ((lane & 15) == 0) reinterpret_cast<float*>(room + pl.warp)[lane >> 4] = s;
+    slot_sync(pl.slot, pl.stride);
+    s1 = 0.f; s2 = 0.f;
+    for (int w = 0; w < warps; ++w) { const float2 q = room[w]; s1 += q.x; s2 += q.y; }
 }
 
-// dR, dX, and the CTA's partial rows of the four sums.
+// dR, dX, and the CTA's partial rows of the four sums.  The row lies in shared memory and its values are read there as often as they are needed: registers hold the sums
+// per channel.  Bound by issue slots (51 % busy) and the chains between a row's two means as much as by memory; measured and not kept (32760 x 1536, 198 us as it is): both
+// means from one round of eight sums 243, 8 channels per lane instead of 16 and twice the warps 225 to 230, all of the row in registers 230, pieces of 4 channels 347.
 template <int V, bool RF, bool XF, bool YF>
 __global__ void __launch_bounds__(kThreads, 1) block_backward_kernel(const Args2 a) {
     extern __shared__ float4 smem[];                              // tables, then the stages, which the slots' sums use afterwards
@@ -553,12 +561,15 @@ inline int chunks2_of(const Form2& f, int B, int C, int64_t rows, bool backward)
     return int(std::min<int64_t>(want, (rows + slots - 1) / slots));
 }
 
+// The backward kernel has a few registers more than there are; what shared memory leaves is the L1 cache that holds them (all of it taken for stages: 32760 x 1536 207 us, 198
+// so).
+constexpr int kBwdSmem = 160 * 1024;
 template <int V, bool BWD>
 inline cudaError_t launch2_types(Args2 a, const Form2& f, bool rf, bool xf, bool yf, cudaStream_t stream) {
     const int slots = f.threads / (32 * f.warps), turns = ceil_div(ceil_div(a.N, a.chunks), slots);
     const int tables = table2_bytes(a.C, BWD), stage = stage2_bytes(f, BWD, rf, xf, yf), sums = BWD ? f.threads * V * kGroup * 4 : 0;
     a.warps = f.warps;
-    a.stages = std::max(1, std::min({kMostStages, (kSmemPerSm / ctas2_per_sm(f, a.C, BWD) - 2048 - tables) / stage, turns}));
+    a.stages = std::max(1, std::min({kMostStages, ((BWD ? kBwdSmem : kSmemPerSm) / ctas2_per_sm(f, a.C, BWD) - 2048 - tables) / stage, turns}));
     const int smem = tables + std::max(a.stages * stage, sums);
     cudaError_t e = cudaSuccess;
     static SmemAllowed allowed[8];       // of the eight kernels below

@@ -66,7 +66,7 @@ struct PrepareArgs {
     int x_ctas, w_ctas;
 };
 template <int kType>
-__global__ void __launch_bounds__(fp8::kRowThreads) prepare_fp8_kernel(const PrepareArgs a) {
+__global__ void __launch_bounds__(fp8::kRowThreads, 4) prepare_fp8_kernel(const PrepareArgs a) {
     const int b = blockIdx.y, cta = blockIdx.x, tid = threadIdx.x;
     grid_launch_dependents();
     grid_wait();

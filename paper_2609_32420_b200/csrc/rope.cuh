@@ -230,11 +230,61 @@ __global__ void __launch_bounds__(kThreads) rope_halves_kernel(const Args a) {
     }
 }
 
+// Halves whose channels come in whole pieces of 8, of a head of 8, 16, .. 256 channels: a lane has 8 neighbouring channels, as they lie in memory, and takes the other half of its
+// pairs from the lane that has it.  (Pieces of both halves in one lane touch parts of sectors: 17776 x 24 heads of 64, of which 48 channels turn, 43.7 us.)
+template <bool F32, int HEADS>
+__global__ void __launch_bounds__(kThreads) rope_halves_across_kernel(const Args a) {
+    int unit, n, h0, h1;
+    grid_launch_dependents();
+    grid_wait();
+    const bool there = place(a, unit, n, h0, h1);
+    const int b = blockIdx.y, half = a.pairs / 8;        // units of a half
+    const bool turns = unit < 2 * half, on = there && turns && (a.pos || n >= a.n_text), moves = there && (on || !a.in_place);
+    const int first = turns && unit >= half ? unit - half : unit, other = int(threadIdx.x & 31) + (!turns ? 0 : unit >= half ? -half : half);
+    int64_t xo = b * a.xs[0] + n * a.xs[2] + unit * 8 + h0 * a.xs[1], yo = b * a.ys[0] + n * a.ys[2] + unit * 8 + h0 * a.ys[1];
+    Piece<F32, 8> p[HEADS];
+    int h = h0;
+    auto fetch = [&]() {
+#pragma unroll
+        for (int k = 0; k < HEADS; ++k) if (moves && h + k < h1) p[k].load(a.x, xo + k * a.xs[1], 8);
+    };
+    fetch();
+    float c[8], s[8];
+    if (on) {
+        const Token t(a, b, n);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            t.turn(a, first * 8 + i, c[i], s[i]);
+            if (unit < half) s[i] = -s[i];           // u cos - v sin here, v cos + u sin in the other half
+        }
+    }
+    while (true) {                       // the same trips for every lane
+#pragma unroll
+        for (int k = 0; k < HEADS; ++k)
+            if (h + k < h1) {
+                Piece<F32, 8> q;
+#pragma unroll
+                for (int i = 0; i < Piece<F32, 8>::kWords; ++i) q.w[i] = __shfl_sync(0xffffffffu, p[k].w[i], other);
+                if (on) {
+#pragma unroll
+                    for (int i = 0; i < 8; i += 2) p[k].set2(i, p[k].get(i) * c[i] + q.get(i) * s[i], p[k].get(i + 1) * c[i + 1] + q.get(i + 1) * s[i + 1]);
+                }
+                if (moves) p[k].store(a.y, yo + k * a.ys[1], 8);
+            }
+        h += HEADS;
+        if (h >= h1) break;
+        xo += HEADS * a.xs[1];
+        yo += HEADS * a.ys[1];
+        fetch();
+    }
+}
+
 // ---- host side ------------------------------------------------------------------------------------
 template <bool F32>
 inline cudaError_t launch(Args a, int B, bool half, cudaStream_t stream) {
     const int vec = !half ? 8 : a.pairs % 8 == 0 ? 8 : a.pairs % 4 == 0 ? 4 : a.pairs % 2 == 0 ? 2 : 1;
-    a.units = half ? a.pairs / vec + ceil_div(a.D - 2 * a.pairs, vec) : ceil_div(a.D, 8);
+    const bool across = half && vec == 8 && a.D >= 8 && (a.D & (a.D - 1)) == 0;      // a token's lanes lie within a warp
+    a.units = half && !across ? a.pairs / vec + ceil_div(a.D - 2 * a.pairs, vec) : ceil_div(a.D, 8);
     a.tile = kThreads / a.units;
     if (a.tile > a.N) a.tile = a.N;
     // enough CTAs for every SM; the angles are computed again by each that shares a token
@@ -243,6 +293,7 @@ inline cudaError_t launch(Args a, int B, bool half, cudaStream_t stream) {
     const dim3 grid(unsigned(tiles * a.splits), unsigned(B)), block(unsigned((a.tile * a.units + 31) / 32 * 32));
     auto run = [&](void (*kernel)(Args)) { return launch_dependent(kernel, grid, block, 0, stream, a); };
     if (!half) return run(rope_neighbours_kernel<F32, F32 ? 4 : 8>);
+    if (across) return run(rope_halves_across_kernel<F32, F32 ? 4 : 8>);
     if (vec == 8) return run(rope_halves_kernel<F32, 8, F32 ? 2 : 4>);
     if (vec == 4) return run(rope_halves_kernel<F32, 4, 4>);
     return vec == 2 ? run(rope_halves_kernel<F32, 2, 8>) : run(rope_halves_kernel<F32, 1, 8>);
