@@ -43,6 +43,7 @@ struct Lane16 {
         } else {
 #pragma unroll
             for (int i = 0; i < kWords; ++i) w[i] = 0;
+            if (n <= 0) return;
 #pragma unroll
             for (int i = 0; i < kLaneChannels; ++i)
                 if (i < n) {

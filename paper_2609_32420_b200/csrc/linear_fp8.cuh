@@ -587,6 +587,7 @@ __device__ __forceinline__ uint4 load_q16(const uint8_t* row, int k, int K) {
         return v;
     }
     uint32_t t[4] = {0, 0, 0, 0};        // the last k of a row: what lies behind them is not the row's
+    if (k >= K) return make_uint4(0, 0, 0, 0);
 #pragma unroll
     for (int i = 0; i < 16; ++i)
         if (k + i < K) t[i / 4] |= uint32_t(*reinterpret_cast<const volatile uint8_t*>(row + k + i)) << (8 * (i & 3));
@@ -597,19 +598,17 @@ __device__ __forceinline__ void mma_16x8x32(float (&d)[4], uint32_t a0, uint32_t
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// NT: column tiles of 8 rows of x; kWarps: warps that share k; kType: of x
-template <int NT, int kWarps, int kType>
+// NT: column tiles of 8 rows of x; kWarps: warps that share k; kType: of x; FT: tiles of 16 rows of W, which share x in 8 bits
+template <int NT, int kWarps, int kType, int FT>
 __global__ void __launch_bounds__(32 * kWarps) linear_fp8_rows_kernel(const RowsArgs8 a) {
-    __shared__ float sums[kWarps][16][8 * NT + 1];
+    __shared__ float sums[kWarps][16 * FT][8 * NT + 1];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     grid_launch_dependents();
     grid_wait();                         // launched while the kernel ahead drains
     if (blockIdx.x == 0 && tid == 0) a.hdr->status = 0;
-    const int f0 = blockIdx.x * 16, blocks = (a.K + kBlock - 1) / kBlock;
-    const bool on0 = f0 + g < a.cols, on1 = f0 + g + 8 < a.cols;
+    const int f0 = blockIdx.x * 16 * FT, blocks = (a.K + kBlock - 1) / kBlock;
     const uint8_t* w0 = a.w + int64_t(f0 + g) * a.w_stride;
-    const uint8_t* w1 = w0 + 8 * a.w_stride;
-    const float* ws = a.wscale + (f0 / kBlock) * a.wss[0];
+    const float* ws = a.wscale + (f0 / kBlock) * a.wss[0];       // 16 FT divides a block
     int64_t xo[NT], so[NT];
     bool xon[NT];
 #pragma unroll
@@ -620,25 +619,29 @@ __global__ void __launch_bounds__(32 * kWarps) linear_fp8_rows_kernel(const Rows
         xo[j] = b * a.xs[0] + r * a.xs[1];
         so[j] = b * a.xss[0] + r * a.xss[1];
     }
-    float acc[NT][4];
+    float acc[FT][NT][4];
 #pragma unroll
-    for (int j = 0; j < NT; ++j)
+    for (int f = 0; f < FT; ++f)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[j][i] = 0.f;
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[f][j][i] = 0.f;
     const uint4 zero = make_uint4(0, 0, 0, 0);
-    constexpr int U = NT == 1 ? 2 : 1;   // blocks in flight per warp
+    constexpr int U = NT == 1 && FT <= 2 ? 2 : 1;    // blocks in flight per warp
     for (int blk = warp; blk < blocks; blk += kWarps * U) {
-        uint4 u0[U][2], u1[U][2];
+        uint4 u[U][FT][2][2];            // of rows g and g + 8 of each tile, two pieces of k
         float sw[U];
 #pragma unroll
         for (int q = 0; q < U; ++q) {
             const int kb = blk + q * kWarps;         // past the end: zeros
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int k = kb * kBlock + h * 64 + t * 16;
-                u0[q][h] = on0 ? load_q16(w0, k, a.K) : zero;
-                u1[q][h] = on1 ? load_q16(w1, k, a.K) : zero;
-            }
+            for (int f = 0; f < FT; ++f)
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const bool on = f0 + 16 * f + 8 * r + g < a.cols;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) u[q][f][r][h] = on ? load_q16(w0 + (16 * f + 8 * r) * a.w_stride, kb * kBlock + h * 64 + t * 16, a.K) : zero;
+                }
             sw[q] = kb < blocks ? load_scale(ws + kb * a.wss[1]) : 0.f;
         }
 #pragma unroll
@@ -668,27 +671,34 @@ __global__ void __launch_bounds__(32 * kWarps) linear_fp8_rows_kernel(const Rows
                     xq[0] = v[0].quantized(inverse);
                     xq[1] = v[1].quantized(inverse);
                 }
-                float d[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    mma_16x8x32(d, u0[q][h].x, u1[q][h].x, u0[q][h].y, u1[q][h].y, xq[h].x, xq[h].y);
-                    mma_16x8x32(d, u0[q][h].z, u1[q][h].z, u0[q][h].w, u1[q][h].w, xq[h].z, xq[h].w);
-                }
                 // d0, d1: feature g, rows 2t and 2t + 1 of x; d2, d3: feature g + 8
                 const float s0 = __shfl_sync(0xffffffffu, sx, 8 * t) * sw[q], s1 = __shfl_sync(0xffffffffu, sx, 8 * t + 4) * sw[q];
-                acc[j][0] = fmaf(d[0], s0, acc[j][0]); acc[j][1] = fmaf(d[1], s1, acc[j][1]);
-                acc[j][2] = fmaf(d[2], s0, acc[j][2]); acc[j][3] = fmaf(d[3], s1, acc[j][3]);
+#pragma unroll
+                for (int f = 0; f < FT; ++f) {
+                    float d[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const uint4 lo = u[q][f][0][h], hi = u[q][f][1][h];
+                        mma_16x8x32(d, lo.x, hi.x, lo.y, hi.y, xq[h].x, xq[h].y);
+                        mma_16x8x32(d, lo.z, hi.z, lo.w, hi.w, xq[h].z, xq[h].w);
+                    }
+                    acc[f][j][0] = fmaf(d[0], s0, acc[f][j][0]); acc[f][j][1] = fmaf(d[1], s1, acc[f][j][1]);
+                    acc[f][j][2] = fmaf(d[2], s0, acc[f][j][2]); acc[f][j][3] = fmaf(d[3], s1, acc[f][j][3]);
+                }
             }
         }
     }
 #pragma unroll
-    for (int j = 0; j < NT; ++j)
+    for (int f = 0; f < FT; ++f)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sums[warp][g + 8 * (i >> 1)][j * 8 + 2 * t + (i & 1)] = acc[j][i];
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sums[warp][16 * f + g + 8 * (i >> 1)][j * 8 + 2 * t + (i & 1)] = acc[f][j][i];
     __syncthreads();
     auto param = [&](const void* p, int64_t i, int f32) { return f32 ? static_cast<const float*>(p)[i] : __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]); };
-    const int f = tid & 15, col = f0 + f;
-    for (int row = tid >> 4; row < a.rows && col < a.cols; row += 2 * kWarps) {
+    for (int at = tid; at < 16 * FT * a.rows; at += 32 * kWarps) {
+        const int f = at % (16 * FT), row = at / (16 * FT), col = f0 + f;
+        if (col >= a.cols) continue;
         float z = 0.f;
 #pragma unroll
         for (int k = 0; k < kWarps; ++k) z += sums[k][f][row];
@@ -851,9 +861,14 @@ inline carnator_status launch_product8(const Operand& A, const Operand& B, const
 template <int NT, int kType>
 inline cudaError_t launch_rows8_warps(const RowsArgs8& a, cudaStream_t stream) {
     const int grid = ceil_div(a.cols, 16);
-    if (grid <= 148) return launch_dependent(linear_fp8_rows_kernel<NT, 16, kType>, dim3(grid), dim3(512), 0, stream, a);
-    if (grid <= 3 * 148) return launch_dependent(linear_fp8_rows_kernel<NT, 8, kType>, dim3(grid), dim3(256), 0, stream, a);
-    return launch_dependent(linear_fp8_rows_kernel<NT, 4, kType>, dim3(grid), dim3(128), 0, stream, a);
+    auto run = [&](void (*kernel)(RowsArgs8), int ft, int warps) { return launch_dependent(kernel, dim3(unsigned(ceil_div(a.cols, 16 * ft))), dim3(unsigned(32 * warps)), 0, stream, a); };
+    // Many warps share k where there are few CTAs, so that all of W is on its way at once; where CTAs fill the SMs several times over, tiles share x, which every CTA
+    // takes to 8 bits for itself.  us (1 row, cold W; tiles x warps): 1536 x 1536 1x16 3.0, 2x16 3.8; 1536 x 8960 2x8 5.6, 1x8 7.9; 5120 x 5120 2x8 12.3, 1x8 12.4,
+    // 4x8 17.9; 5120 x 13824 4x8 20.8, 2x8 24.0, 4x4 31.5; 5120 x 30720 4x4 37.9, 4x8 40.7, 1x4 43.9.
+    if (grid <= 148) return run(linear_fp8_rows_kernel<NT, 16, kType, 1>, 1, 16);
+    if (grid <= 4 * 148) return run(linear_fp8_rows_kernel<NT, 8, kType, 2>, 2, 8);
+    if (grid <= 8 * 148) return run(linear_fp8_rows_kernel<NT, 8, kType, 4>, 4, 8);
+    return run(linear_fp8_rows_kernel<NT, 4, kType, 4>, 4, 4);
 }
 template <int kType>
 inline cudaError_t launch_rows8(const RowsArgs8& a, cudaStream_t stream) {
