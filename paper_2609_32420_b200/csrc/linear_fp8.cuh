@@ -4,8 +4,10 @@
 // Scales that are powers of two (fp8_quantize.cuh makes no others) are applied by the tensor cores: kind::mxf8f6f4 takes an exponent per row and 32 k from tensor memory
 // (here the same for the four products of a block), so that an accumulator sums up all of k, or runs of 5120 of it for fp32 outputs.
 // Any other scales: an accumulator sums up one block (kind::f8f6f4, in which nothing is lost: 7 significant bits a product, 128 terms) and the epilogue warps take it
-// times the block's scale into 128 fp32 sums per thread, while the next block's products run into the other accumulator.  That costs the reading of every block's sums
-// from tensor memory, 128 KB per SM and block against 512 clocks of products (75600 x 5120 x 5120: 2068 us, without the epilogue's reads and sums 1584).
+// times the block's scale into 128 fp32 sums per thread, while the next block's products run into the other accumulator.  That costs the reading and scaling of every
+// block's sums, which bounds it: 9472 x 5120 x 5120 358 us against 205.
+// Otherwise bound by what an SM takes in (92 bytes a nanosecond) and, in long loops, by the power limit: 75600 x 5120 x 5120 in 1500 to 1580 us, 2.5 to 2.6 PFLOP/s, onto
+// an fp32 stream with a gate 1820 to 1890.
 // A first kernel quantises x where the call does, lays the exponents out as the tensor cores read them and notes whether all scales are powers of two; the product
 // goes by its note, so that a caller does not have to say.
 //
@@ -288,8 +290,8 @@ __device__ __forceinline__ void epilogue_warp(const Args8& args, const Epi& c) {
                 release(u);
             }
         } else {
-            // x's scales of four blocks on their way while the four before are used (one block ahead, a block had to wait for them: 75600 x 5120 x 5120 2703 us, four
-            // ahead 2068); the weight's of 32 blocks, one per lane, for each 32 columns
+            // x's scales of four blocks are on their way while the four before are used (one block ahead, every block waited for them); the weight's of 32 blocks, one per
+            // lane, for each 32 columns
             const float* xs = args.xscale ? args.xscale + b * args.xss[0] + (on ? row : 0) * args.xss[1] : nullptr;
             const uint8_t* xe = args.sfa + sf_offset((int64_t(b) * a.tiles_m + m) * 2 + c.half, args.groups, 0, quarter * 32 + lane);
             float wv[4], xn[4];
@@ -324,21 +326,16 @@ __device__ __forceinline__ void epilogue_warp(const Args8& args, const Epi& c) {
                     if (++s == a.stages) { s = 0; phase ^= 1u; }
                     tc_fence_after();
                     const uint32_t from = tmem + uint32_t(u * kMostColumns + side * 32);
-                    float v0[16], v1[16];        // 16 columns in turn: some on their way while the others are added
-                    if (side * 32 < left) tmem_ld16(from, v0);
+                    // All four pieces of 32 columns, whether the tile has them or not: what it has not is added to sums that nobody reads.  (9472 x 5120 x 5120, us: as here
+                    // 358, with a branch around each piece 447, pieces of 16 in turn, one on its way while the other is added, 420 and, with branches, 422)
 #pragma unroll
                     for (int p = 0; p < 4; ++p) {
                         const f2 by = two(xv[j] * __shfl_sync(0xffffffffu, wv[p], (k - c.k0) & 31));
-                        if (side * 32 + 64 * p < left) {       // warp-uniform
-                            tmem_wait_ld(v0);
-                            tmem_ld16(from + 64 * p + 16, v1);
+                        float v[32];
+                        tmem_ld32(from + 64 * p, v);
+                        tmem_wait_ld(v);
 #pragma unroll
-                            for (int q = 0; q < 8; ++q) acc[p][q] = norm::fma2(two(v0[2 * q], v0[2 * q + 1]), by, acc[p][q]);
-                            tmem_wait_ld(v1);
-                            if (side * 32 + 64 * (p + 1) < left && p < 3) tmem_ld16(from + 64 * (p + 1), v0);
-#pragma unroll
-                            for (int q = 0; q < 8; ++q) acc[p][8 + q] = norm::fma2(two(v1[2 * q], v1[2 * q + 1]), by, acc[p][8 + q]);
-                        }
+                        for (int q = 0; q < 16; ++q) acc[p][q] = norm::fma2(two(v[2 * q], v[2 * q + 1]), by, acc[p][q]);
                     }
                     release(u);
                 }
@@ -842,7 +839,7 @@ inline carnator_status launch_product8(const Operand& A, const Operand& B, const
     p.sfa = room.sfa; p.sfb = room.sfb; p.notes = room.notes; p.hdr = a.t.hdr;
     p.groups = a.groups; p.row_tiles = a.t.tiles_m * 2;
     p.cols = a.t.cols; p.bn = a.t.bn; p.tiles_n = a.t.tiles_n;
-    p.x_ctas = type == kXE4m3 ? int(std::min<int64_t>(148 * 8, (int64_t(a.groups) * a.t.rows + fp8::kRowThreads - 1) / fp8::kRowThreads)) : fp8::row_ctas(p.q, type == kXF32);
+    p.x_ctas = type == kXE4m3 ? int(std::min<int64_t>(std::max(148 * 8 / a.t.batches, 1), (int64_t(a.groups) * a.t.rows + fp8::kRowThreads - 1) / fp8::kRowThreads)) : fp8::row_ctas(p.q, type == kXF32);
     p.w_ctas = int(std::min<int64_t>(kMostWCtas, int64_t(a.t.tiles_n) * a.groups));
     const dim3 grid(unsigned(p.x_ctas + p.w_ctas), unsigned(a.t.batches));
     const cudaError_t e = type == kXBf16 ? launch_dependent(prepare_fp8_kernel<kXBf16>, grid, dim3(fp8::kRowThreads), 0, stream, p)
