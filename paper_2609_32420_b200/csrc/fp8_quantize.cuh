@@ -5,6 +5,7 @@
 // put x / scale on one.  amax counts as 2^-100 at least.  A block with an infinity or a NaN has the scale NaN and values NaN.
 //
 // Bound by memory: 2 or 4 bytes read and 1 written per value.  A lane has 16 channels (whole sectors), 8 lanes a block of a row.
+// us, bf16: rows of 32760 x 1536 26.0 (0.89 of the copy rate), a weight of 13824 x 5120 33.5 (0.97).
 #pragma once
 #include "norm.cuh"
 

@@ -6,6 +6,7 @@
 // at a time, so that the angles, which all heads share, are computed once per token and stay in registers.  Angles are taken in 64 bits, in turns: the
 // position times f_i / 2 pi, less the nearest whole number, is at most 1/2 and loses nothing to the size of the position before it is rounded to 32 bits
 // (at position 10^6 a 32-bit product is off by up to 0.06 radians); sine and cosine of it are CUDA's.
+// 75600 x 80 heads of 128 in bf16: 476 us, 0.99 of the copy rate.
 #pragma once
 #include "norm.cuh"
 
@@ -231,7 +232,8 @@ __global__ void __launch_bounds__(kThreads) rope_halves_kernel(const Args a) {
 }
 
 // Halves whose channels come in whole pieces of 8, of a head of 8, 16, .. 256 channels: a lane has 8 neighbouring channels, as they lie in memory, and takes the other half of its
-// pairs from the lane that has it.  (Pieces of both halves in one lane touch parts of sectors: 17776 x 24 heads of 64, of which 48 channels turn, 43.7 us.)
+// pairs from the lane that has it.  (2 x 17776 x 24 heads of 64, of which 48 channels turn: 38.6 us; 43.7 with pieces of both halves in one lane, which
+// touch parts of sectors.)
 template <bool F32, int HEADS>
 __global__ void __launch_bounds__(kThreads) rope_halves_across_kernel(const Args a) {
     int unit, n, h0, h1;
