@@ -183,6 +183,13 @@ def test_every_size(N, K, M, x, powers):
     check_call(make(1, N, K, M, x=x, seed=N + K + M, powers=powers), cn.ACT_GELU_TANH)
 
 
+@pytest.mark.parametrize("x", ["bf16", "f32", "e4m3"])
+@pytest.mark.parametrize("B,N,K,M", [(1, 5, 300, 2500), (2, 4, 1541, 9001), (1, 11, 130, 4777), (1, 3, 1541, 10007), (2, 8, 520, 18001), (1, 1, 130, 19009), (1, 13, 700, 30001)])
+def test_few_rows_into_many(B, N, K, M, x):
+    """Tiles of W that share x: 1, 2 and 4 of them, up to 8 and up to 16 rows, the last ones in part."""
+    check_call(make(B, N, K, M, x=x, seed=M), cn.ACT_SILU)
+
+
 @pytest.mark.parametrize("act", ACTS)
 @pytest.mark.parametrize("B,N", [(3, 1), (2, 6), (2, 150), (3, 301)])
 @pytest.mark.parametrize("x,y,p", [("bf16", "bf16", "f32"), ("e4m3", "f32", "bf16"), ("f32", "f32", "f32")])
@@ -306,6 +313,38 @@ def test_captured_and_on_two_streams():
         for t, y, (_, ws) in zip(ts, outs, graphs):
             assert cn.query_status(ws) == cn.OK
             assert torch.equal(y, call(t, cn.ACT_NONE))
+
+
+def test_captured_with_scales_that_change():
+    """A graph whose scales are powers of two in some replays and any numbers in others: each replay looks at its own."""
+    t = make(2, 150, 700, 300, x="e4m3", powers=True)
+    other = make(2, 150, 700, 300, x="e4m3", powers=False, seed=1)
+    _, y = canvas((2, 150, 300), torch.bfloat16)
+    s = cn.make_linear_fp8_shape(t["x"], t["w"], t["w_scale"], y, x_scale=t["x_scale"], residual=t["residual"], bias=t["bias"], gate=t["gate"])
+    ws = torch.empty(cn.linear_fp8_workspace_bytes(s), dtype=torch.uint8, device="cuda")
+    kw = dict(x_scale=t["x_scale"], bias=t["bias"], gate=t["gate"], residual=t["residual"], Y=y, ws=ws)
+    cn.linear_fp8(t["x"], t["w"], t["w_scale"], s, **kw)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        cn.linear_fp8(t["x"], t["w"], t["w_scale"], s, **kw)
+    powers = {k: t[k].clone() for k in ("x_scale", "w_scale")}
+    for xs, wsc in ((powers, powers), (other, powers), (powers, other), (powers, powers), (other, other), (powers, powers)):
+        t["x_scale"].copy_(xs["x_scale"])
+        t["w_scale"].copy_(wsc["w_scale"])
+        g.replay()
+        torch.cuda.synchronize()
+        assert cn.query_status(ws) == cn.OK
+        ry, ey = product_ref(t, cn.ACT_NONE)
+        check(y, ry, ey + half_step(y.dtype) * (ry.abs() + ey), "y")
+
+
+@pytest.mark.parametrize("at", [None, (0, 0, 0), (1299, 16, 1)])
+def test_many_padded_entries(at):
+    """Entries that do not follow each other evenly, more of them than a pass over the scales has CTAs; one scale, the first or the last, that is no power of two."""
+    t = make(1300, 17, 200, 72, x="e4m3", powers=True)
+    if at:
+        t["x_scale"][at] *= 1.5
+    check_call(t, cn.ACT_NONE)
 
 
 def test_offsets_that_pass_32_bits():
