@@ -472,7 +472,8 @@ carnator_status carnator_rope(const void* X, const double* freq, const int32_t* 
  *   post_weight, post_bias, weight, bias   device, [C] of weight_dtype, or NULL (1, 0);  gate, shift, scale  device, [B,C] of mod_dtype, or NULL (1, 0, 0).
  *          These are aligned to their type only
  *   stats  device, fp32 [4,B,N] contiguous: mean and reciprocal deviation of post, then of pre (an RMS norm's mean is 0, NONE has 0 and 1); written by the forward call if
- *          given, read by the backward call.  A row with a NaN or an infinity: NaN as in carnator_layer_norm
+ *          given, read by the backward call.  A norm of a row with a NaN or an infinity, or whose squares (a layer norm's: of deviations) pass fp32's range in their sum:
+ *          reciprocal deviation and all channels NaN, for either kind
  * carnator_block_norm_backward, from dY, dS (the gradient that arrives on the stream, or NULL: none), the saved S and X:
  *   G = dS + the gradient of y through pre,   dR = residual_scale G,   dX = the gradient of p through post, for gate_b G
  *   dpost_weight, dpost_bias, dweight, dbias  device, fp32 [C];  dgate, dshift, dscale  device, fp32 [B,C] contiguous; any of them NULL: not wanted

@@ -133,6 +133,12 @@ __device__ __forceinline__ void moments(const Eight (&f)[V], const int (&n)[V], 
     }
 }
 
+// Squares that fp32 cannot sum up, an infinity's among them, have no deviation: NaN, as a row with a NaN has, and not the 0 that 1 / sqrt(infinity) is, which would leave a row of zeros.
+__device__ __forceinline__ float rstd_of(float m2, float inv_c, float eps) {
+    const float v = fmaf(m2, inv_c, eps);
+    return isfinite(v) ? rsqrtf(v) : __uint_as_float(0x7FC00000u);
+}
+
 __device__ __forceinline__ float warp_channels(int C, int warp, int col_step, int V) {
     float n = 0.f;
     for (int v = 0; v < V; ++v) n += float(min(max(C - v * col_step - warp * 32 * kGroup, 0), 32 * kGroup));
@@ -193,7 +199,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_forward_kernel(const Args2 
         for (int v = 0; v < V; ++v) f[v] = in_x.read(at + r_bytes, v);
         if (a.post != kNone) {
             moments<V>(f, n, a.post, pl, a.warps, n_warp, a.C, a.inv_c, &part[flip][0][pl.slot * a.warps], mean1, m2);
-            rstd1 = rsqrtf(fmaf(m2, a.inv_c, a.eps1));
+            rstd1 = rstd_of(m2, a.inv_c, a.eps1);
         }
         {
             const f2 minus = two(-mean1), rs = two(rstd1), al = two(a.alpha);
@@ -230,7 +236,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_forward_kernel(const Args2 
                 if (n[v] > 0) store_eight<RF>(out_s, so + v * col_step, f[v], n[v], a.wide_s);
         }
         moments<V>(f, n, a.pre, pl, a.warps, n_warp, a.C, a.inv_c, &part[flip][1][pl.slot * a.warps], mean2, m2);
-        rstd2 = rsqrtf(fmaf(m2, a.inv_c, a.eps2));
+        rstd2 = rstd_of(m2, a.inv_c, a.eps2);
         if (on) {
             if (a.stats && pl.at == 0) {
                 const int64_t so = int64_t(b) * a.N + row, all = int64_t(a.B) * a.N;

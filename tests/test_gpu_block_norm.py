@@ -341,3 +341,37 @@ def test_offsets_that_pass_32_bits():
     g = cn.block_norm_backward(y, s, x, stats, cn.make_block_norm_shape(None, x, s, y, **how), dS=s, dX=x, dR=s, want=())
     g1 = cn.block_norm_backward(y1, s1, small[1], st, cn.make_block_norm_shape(None, small[1], s1, y1, **how), dS=s1, want=())
     assert torch.equal(g.dR[:, -tail:], g1.dR) and torch.equal(g.dX[:, -tail:], g1.dX)
+
+
+@pytest.mark.parametrize("C", [5, 100, 1536, 5120])
+@pytest.mark.parametrize("post", [NONE, LAYER, RMS])
+@pytest.mark.parametrize("pre", [LAYER, RMS])
+def test_rows_that_are_not_finite_with_every_norm(C, post, pre):
+    """A NaN or an infinity, or finite values whose squares fp32 cannot sum up: NaN all along what is normed, and as its reciprocal deviation; the gradients likewise."""
+    t = make(1, 30, C, x="f32", y="f32", post=post, pre=pre)
+    clean = forward(t)
+    grads = backward(t, clean[0], clean[2])
+    in_x, in_r = dict(zip((3, 7, 21), ("nan", "inf", "1e25"))), dict(zip((11, 12, 20), ("-inf", "nan", "-1e25")))
+    for row, v in in_x.items():
+        t["x"][0, row, C // 2] = float(v)
+    for row, v in in_r.items():
+        t["r"][0, row, C - 1] = float(v)
+    S, Y, stats = forward(t)
+    bad = torch.zeros(30, dtype=torch.bool, device="cuda")
+    bad[[*in_x, *in_r]] = True
+    bad_x = torch.zeros_like(bad)
+    bad_x[[*in_x]] = True
+    assert torch.equal(S[0, ~bad], clean[0][0, ~bad]) and torch.equal(Y[0, ~bad], clean[1][0, ~bad]) and torch.equal(stats[:, 0, ~bad], clean[2][:, 0, ~bad])
+    assert Y[0, bad].isnan().all() and stats[3, 0, bad].isnan().all()
+    if post == NONE:
+        assert (stats[1] == 1).all()
+        at = S.clone()
+        for rows, c in ((in_x, C // 2), (in_r, C - 1)):
+            for row in rows:
+                at[0, row, c] = 0
+        assert at.isfinite().all()       # an infinity or a NaN reaches the stream in its own channel only
+    else:
+        assert torch.equal(stats[1, 0].isnan(), bad_x) and S[0, bad_x].isnan().all()
+    g = backward(t, S, stats)
+    for got, want in ((g.dR, grads.dR), (g.dX, grads.dX)):
+        assert torch.equal(got[0, ~bad], want[0, ~bad]) and got[0, bad].isnan().all()
