@@ -444,7 +444,7 @@ typedef struct carnator_rope_shape {
     int32_t offset[3];
     int64_t x_stride[3], y_stride[3];       /* element strides of (batch, head, token) */
     int64_t pos_stride[2];                  /* of (batch, token); batch 0: the same for all entries */
-    int32_t axes;                           /* of positions */
+    int32_t axes;                           /* of positions; 0 without (a record of positions is not taken without them) */
     int32_t layout, inverse, x_dtype;       /* x_dtype is also Y's */
     float   amplitude;
 } carnator_rope_shape;

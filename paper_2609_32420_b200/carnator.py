@@ -999,7 +999,10 @@ def rope(X, freq, shape: RopeShape, positions=None, Y=None, stream=None):
     _fit(X, "X", *said.x, dev)
     _fit(Y, "Y", *said.y, dev)
     _fit(freq, "freq", *said.freq, dev)
-    if positions is not None:
+    if positions is None:
+        if said.record.axes:             # without them the tokens would turn as a plain line
+            raise ValueError("the shape record was made with positions, the call has none")
+    else:
         if said.pos[1][0] == 1 and positions.shape[0] == said.record.B and positions.stride(0) == 0:
             positions = positions[:1]              # one tensor seen by every entry
         _fit(positions, "positions", *said.pos, dev)

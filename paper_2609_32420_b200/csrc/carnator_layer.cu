@@ -36,6 +36,7 @@ carnator_status check_rope_shape(const carnator_rope_shape* s, bool positions) {
         for (int i = s->axes; i < 3; ++i) if (s->pairs[i]) return CARNATOR_ERR_INVALID_ARG;
         if ((s->B > 1 && (s->pos_stride[0] < 0 || s->pos_stride[0] > kMostStride)) || (s->N > 1 && (s->pos_stride[1] < 0 || s->pos_stride[1] > kMostStride))) return CARNATOR_ERR_INVALID_ARG;
     } else {
+        if (s->axes != 0) return CARNATOR_ERR_INVALID_ARG;       // a record of positions whose call has forgotten them
         if (s->n_text < 0 || s->T < 0 || s->Hg < 0 || s->Wg < 0) return CARNATOR_ERR_INVALID_ARG;
         const int64_t frame = int64_t(s->Hg) * s->Wg;            // below 2^62
         const int64_t video = int64_t(s->N) - s->n_text;

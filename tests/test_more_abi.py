@@ -245,3 +245,19 @@ def test_python_calls_check_tensors_against_the_record():
         for call in (lambda: cn.rope(x, freq, rs, Y=x), lambda: cn.quantize_fp8(t, qs), lambda: cn.linear_fp8(t, w, sc, ls, Y=y)):
             with pytest.raises(cn.CarnatorError):
                 call()
+
+
+def test_rope_refuses_a_forgotten_positions_argument():
+    """Without them the tokens would turn by their places in a plain line; given to a record that has none, they are refused, too."""
+    for axes in (1, 2, 3, -1):
+        expect(BAD, lambda: call_rope(rope_shape(axes=axes)))
+    expect(BAD, lambda: call_rope(rope_shape(True)))
+    expect(BAD, lambda: call_rope(rope_shape(), pos=P))
+    x, freq = torch.empty((2, 2, 6, 16), dtype=torch.bfloat16), torch.empty(8, dtype=torch.float64)
+    for entries, axes in ((1, 1), (2, 1), (2, 3)):
+        pos = torch.empty((entries, 6, axes), dtype=torch.int32)
+        for Y in (x, None):
+            with pytest.raises(ValueError, match="positions"):
+                cn.rope(x, freq, cn.make_rope_shape(x, x, 8, positions=pos), Y=Y)
+            with pytest.raises(ValueError, match="positions"):
+                cn.rope(x, freq, cn.make_rope_shape(x, x, 8), positions=pos, Y=Y)
