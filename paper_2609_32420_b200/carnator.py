@@ -350,9 +350,22 @@ def params_of(bp) -> BuildParams:
     return p
 
 
-def _new_ws(nbytes: int, device):
+def _made(make, device, stream):
+    """make(), the memory of something that a call makes for itself or hands back.  On a stream of the caller's own the memory is that stream's: what is dropped, by the call or
+    later by its caller, goes to that stream's later work only, behind the kernels that still use it.  Results are read on the current stream, too, as a rule: it is recorded."""
+    if stream is None or device.type != "cuda":
+        return make()
     import torch
-    return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+    reader = torch.cuda.current_stream()
+    with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream.cuda_stream)):
+        t = make()
+    t.record_stream(reader)
+    return t
+
+
+def _new_ws(nbytes: int, device, stream=None):
+    import torch
+    return _made(lambda: torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device), device, stream)
 
 
 # --------------------------------------------------------------------------------------------
@@ -370,9 +383,9 @@ def build_connectivity(Q, K, shape: Shape, params: BuildParams, mask=None, poole
     """carnator_build_connectivity.  Returns (mask uint8 [B,H,nqb,nkb], ws)."""
     import torch
     if mask is None:
-        mask = torch.empty((shape.B, shape.H, shape.nqb, shape.nkb), dtype=torch.uint8, device=Q.device)
+        mask = _made(lambda: torch.empty((shape.B, shape.H, shape.nqb, shape.nkb), dtype=torch.uint8, device=Q.device), Q.device, stream)
     if ws is None:
-        ws = _new_ws(build_workspace_bytes(shape, params), Q.device)
+        ws = _new_ws(build_workspace_bytes(shape, params), Q.device, stream)
     st = lib().carnator_build_connectivity(_ptr(Q), _ptr(K), ctypes.byref(shape), ctypes.byref(params), _ptr(mask),
                                            _ptr(pooled_scores), _ptr(ws), ws.numel(), _stream(stream))
     _check(st, "carnator_build_connectivity")
@@ -388,9 +401,9 @@ def build_connectivity_exact(Q, K, LSE, shape: Shape, params: BuildParams, mask=
     """carnator_build_connectivity_exact.  Returns (mask uint8 [B,H,nqb,nkb], ws)."""
     import torch
     if mask is None:
-        mask = torch.empty((shape.B, shape.H, shape.nqb, shape.nkb), dtype=torch.uint8, device=Q.device)
+        mask = _made(lambda: torch.empty((shape.B, shape.H, shape.nqb, shape.nkb), dtype=torch.uint8, device=Q.device), Q.device, stream)
     if ws is None:
-        ws = _new_ws(exact_workspace_bytes(shape), Q.device)
+        ws = _new_ws(exact_workspace_bytes(shape), Q.device, stream)
     st = lib().carnator_build_connectivity_exact(_ptr(Q), _ptr(K), _ptr(LSE), ctypes.byref(shape), ctypes.byref(params),
                                                  _ptr(mask), _ptr(block_mass), _ptr(ws), ws.numel(), _stream(stream))
     _check(st, "carnator_build_connectivity_exact")
@@ -399,26 +412,26 @@ def build_connectivity_exact(Q, K, LSE, shape: Shape, params: BuildParams, mask=
 
 def compact_mask(mask, recompute_rows, shape: Shape, ws=None, stream=None):
     if ws is None:
-        ws = _new_ws(attn_workspace_bytes(shape), mask.device)
+        ws = _new_ws(attn_workspace_bytes(shape), mask.device, stream)
     st = lib().carnator_compact_mask(_ptr(mask), _ptr(recompute_rows), ctypes.byref(shape), _ptr(ws), ws.numel(),
                                      _stream(stream))
     _check(st, "carnator_compact_mask")
     return ws
 
 
-def _outputs(Q, shape: Shape, O, LSE):
+def _outputs(Q, shape: Shape, O, LSE, stream):
     import torch
     if O is None:
-        O = torch.empty((shape.B, shape.H, shape.N, shape.D), dtype=torch.bfloat16, device=Q.device)
+        O = _made(lambda: torch.empty((shape.B, shape.H, shape.N, shape.D), dtype=torch.bfloat16, device=Q.device), Q.device, stream)
         st, D, nd = shape.o_stride, shape.D, shape.N * shape.D      # contiguous
         st[0], st[1], st[2] = shape.H * nd, nd, D
     if LSE is None:
-        LSE = torch.empty((shape.B, shape.H, shape.N), dtype=torch.float32, device=Q.device)
+        LSE = _made(lambda: torch.empty((shape.B, shape.H, shape.N), dtype=torch.float32, device=Q.device), Q.device, stream)
     return O, LSE
 
 
 def sparse_attn_compacted(Q, K, V, shape: Shape, ws, O=None, LSE=None, stream=None):
-    O, LSE = _outputs(Q, shape, O, LSE)
+    O, LSE = _outputs(Q, shape, O, LSE, stream)
     st = lib().carnator_sparse_attn_compacted(_ptr(Q), _ptr(K), _ptr(V), ctypes.byref(shape), _ptr(O), _ptr(LSE),
                                               _ptr(ws), ws.numel(), _stream(stream))
     _check(st, "carnator_sparse_attn_compacted")
@@ -427,9 +440,9 @@ def sparse_attn_compacted(Q, K, V, shape: Shape, ws, O=None, LSE=None, stream=No
 
 def sparse_attn(Q, K, V, mask, recompute_rows, shape: Shape, O=None, LSE=None, ws=None, stream=None):
     """carnator_sparse_attn.  Returns (O bf16 [B,H,N,D], LSE fp32 [B,H,N], ws)."""
-    O, LSE = _outputs(Q, shape, O, LSE)
+    O, LSE = _outputs(Q, shape, O, LSE, stream)
     if ws is None:
-        ws = _new_ws(attn_workspace_bytes(shape), Q.device)
+        ws = _new_ws(attn_workspace_bytes(shape), Q.device, stream)
     st = lib().carnator_sparse_attn(_ptr(Q), _ptr(K), _ptr(V), _ptr(mask), _ptr(recompute_rows), ctypes.byref(shape),
                                     _ptr(O), _ptr(LSE), _ptr(ws), ws.numel(), _stream(stream))
     _check(st, "carnator_sparse_attn")
@@ -513,10 +526,9 @@ DTYPE_F32, DTYPE_BF16, DTYPE_E4M3 = 0, 1, 2
 def build_regions(evidence, shape: Shape, r_active: int = 2, r_context: int = 3, stream=None):
     """carnator_build_regions.  evidence uint8 [T,Hg,Wg] on the device -> (active, context, W)."""
     import torch
-    active = torch.empty_like(evidence)
-    context = torch.empty_like(evidence)
-    W = torch.empty(evidence.shape, dtype=torch.float32, device=evidence.device)
-    ws = _new_ws(int(lib().carnator_regions_workspace_bytes(ctypes.byref(shape))), evidence.device)
+    active, context = (_made(lambda: torch.empty_like(evidence), evidence.device, stream) for _ in range(2))
+    W = _made(lambda: torch.empty(evidence.shape, dtype=torch.float32, device=evidence.device), evidence.device, stream)
+    ws = _new_ws(int(lib().carnator_regions_workspace_bytes(ctypes.byref(shape))), evidence.device, stream)
     st = lib().carnator_build_regions(_ptr(evidence), ctypes.byref(shape), r_active, r_context, _ptr(active), _ptr(context),
                                       _ptr(W), _ptr(ws), ws.numel(), _stream(stream))
     _check(st, "carnator_build_regions")
@@ -527,7 +539,7 @@ def fuse_latents(z_target, z_hist, W, z_out=None, stream=None):
     """carnator_fuse_latents over [channels, tokens] tensors (fp32 or bf16), W fp32 [tokens]."""
     import torch
     if z_out is None:
-        z_out = torch.empty_like(z_target)
+        z_out = _made(lambda: torch.empty_like(z_target), z_target.device, stream)
     dtype = DTYPE_F32 if z_target.dtype == torch.float32 else DTYPE_BF16
     channels, tokens = z_target.shape[0], z_target[0].numel()
     st = lib().carnator_fuse_latents(_ptr(z_target), _ptr(z_hist), _ptr(W), channels, tokens, dtype, _ptr(z_out), _stream(stream))
@@ -538,7 +550,7 @@ def fuse_latents(z_target, z_hist, W, z_out=None, stream=None):
 def region_block_flags(region, shape: Shape, block: int, text_value: int = 1, stream=None):
     import torch
     n = shape.n_text + shape.T * shape.Hg * shape.Wg
-    flags = torch.empty((-(-n // block),), dtype=torch.uint8, device=region.device)
+    flags = _made(lambda: torch.empty((-(-n // block),), dtype=torch.uint8, device=region.device), region.device, stream)
     st = lib().carnator_region_block_flags(_ptr(region), ctypes.byref(shape), block, text_value, _ptr(flags), _stream(stream))
     _check(st, "carnator_region_block_flags")
     return flags
@@ -547,7 +559,7 @@ def region_block_flags(region, shape: Shape, block: int, text_value: int = 1, st
 def sparse_attn_region(Q, K, V, mask, active_q, context_k, shape: Shape, O, LSE, ws=None, stream=None):
     """carnator_sparse_attn_region: O and LSE are updated in place; rows of inactive query blocks stay as they are."""
     if ws is None:
-        ws = _new_ws(attn_workspace_bytes(shape), Q.device)
+        ws = _new_ws(attn_workspace_bytes(shape), Q.device, stream)
     shape.o_stride = (ctypes.c_int64 * 3)(*O.stride()[:3])
     st = lib().carnator_sparse_attn_region(_ptr(Q), _ptr(K), _ptr(V), _ptr(mask), _ptr(active_q), _ptr(context_k),
                                            ctypes.byref(shape), _ptr(O), _ptr(LSE), _ptr(ws), ws.numel(), _stream(stream))
@@ -564,9 +576,9 @@ def seed_expansion(Q, K, LSE, seeds, n_pos: int, n_neg: int, shape: Shape, per_h
     """carnator_seed_expansion.  seeds: int32 device tensor [n_pos + n_neg].  Returns contrast fp32 [B,N]
     (and the workspace, whose header carries the device status, with ``return_ws``)."""
     import torch
-    out = torch.empty((shape.B, shape.N), dtype=torch.float32, device=Q.device)
+    out = _made(lambda: torch.empty((shape.B, shape.N), dtype=torch.float32, device=Q.device), Q.device, stream)
     if ws is None:
-        ws = _new_ws(int(lib().carnator_seed_workspace_bytes(ctypes.byref(shape))), Q.device)
+        ws = _new_ws(int(lib().carnator_seed_workspace_bytes(ctypes.byref(shape))), Q.device, stream)
     st = lib().carnator_seed_expansion(_ptr(Q), _ptr(K), _ptr(LSE), _ptr(seeds), n_pos, n_neg, ctypes.byref(shape),
                                        _ptr(per_head), _ptr(out), _ptr(ws), ws.numel(), _stream(stream))
     _check(st, "carnator_seed_expansion")
@@ -681,10 +693,15 @@ def _linear_packed(of: bytes):
     return _linear_said(of), size, s.out_features
 
 
-def _room(size, features: int, dtype, device):
+def _room(size, features: int, dtype, device, stream):
     import torch
-    t = torch.empty(size, dtype=dtype, device=device)
+    t = torch.empty(size, dtype=dtype, device=device) if stream is None else _made(lambda: torch.empty(size, dtype=dtype, device=device), device, stream)
     return t if size[-1] == features else t[..., :features]
+
+
+def _vector(size, device, stream):
+    import torch
+    return _made(lambda: torch.empty(size, dtype=torch.float32, device=device), device, stream)
 
 
 def _rows_of(stride, *tensors):
@@ -727,7 +744,7 @@ def layer_norm(X, shape: NormShape, weight=None, bias=None, shift=None, scale=No
     dev = X.device
     if Y is None:                        # the caller's record stays as it is
         said, size, n = _norm_packed(bytes(shape), "y_stride")
-        Y = _room(size, n, said.y[0], dev)
+        Y = _room(size, n, said.y[0], dev, stream)
     else:
         said = _norm_said(bytes(shape))
     on = _stream_on(dev, stream)
@@ -768,11 +785,10 @@ def layer_norm_backward(dY, X, mean, rstd, shape: NormShape, weight=None, bias=N
                         want=("weight", "bias", "shift", "scale"), modulated=None, ws=None, stream=None) -> NormGrads:
     """carnator_layer_norm_backward.  ``want`` names the vector gradients to compute: weight (if the norm has one), bias (if
     it has a weight or a bias), shift and scale (if it has a scale, or ``modulated`` says that it has a shift only)."""
-    import torch
     dev = X.device
     if dX is None:
         said, size, n = _norm_packed(bytes(shape), "dx_stride")
-        dX = _room(size, n, said.dx[0], dev)
+        dX = _room(size, n, said.dx[0], dev, stream)
     else:
         said = _norm_said(bytes(shape))
     on = _stream_on(dev, stream)
@@ -790,16 +806,16 @@ def layer_norm_backward(dY, X, mean, rstd, shape: NormShape, weight=None, bias=N
     B, C = said.record.B, said.record.C
     dweight = dbias = dshift = dscale = None
     if weight is not None and "weight" in want:
-        dweight = torch.empty(C, dtype=torch.float32, device=dev)
+        dweight = _vector(C, dev, stream)
     if (weight is not None or bias is not None) and "bias" in want:
-        dbias = torch.empty(C, dtype=torch.float32, device=dev)
+        dbias = _vector(C, dev, stream)
     if scale is not None if modulated is None else modulated:
         if "shift" in want:
-            dshift = torch.empty((B, C), dtype=torch.float32, device=dev)
+            dshift = _vector((B, C), dev, stream)
         if "scale" in want:
-            dscale = torch.empty((B, C), dtype=torch.float32, device=dev)
+            dscale = _vector((B, C), dev, stream)
     if ws is None:
-        ws = _new_ws(layer_norm_backward_workspace_bytes(said.record), dev)
+        ws = _new_ws(layer_norm_backward_workspace_bytes(said.record), dev, stream)
     elif ws.device != dev or not ws.is_contiguous():
         raise ValueError(f"ws must be contiguous and on {dev}")
     st = lib().carnator_layer_norm_backward(_ptr(dY), _ptr(X), _ptr(mean), _ptr(rstd), _ptr(weight), _ptr(bias), _ptr(scale), said.ref, _ptr(dX),
@@ -843,7 +859,7 @@ def linear(X, W, shape: LinearShape, bias=None, gate=None, residual=None, Y=None
     dev = X.device
     if Y is None:
         said, size, n = _linear_packed(bytes(shape))
-        Y = _room(size, n, said.y[0], dev)
+        Y = _room(size, n, said.y[0], dev, stream)
     else:
         said = _linear_said(bytes(shape))
     on = _stream_on(dev, stream)
@@ -859,7 +875,7 @@ def linear(X, W, shape: LinearShape, bias=None, gate=None, residual=None, Y=None
     if gate is not None:
         _fit(gate, "gate", *said.gate, dev)
     if ws is None:
-        ws = _new_ws(linear_workspace_bytes(said.record), dev)
+        ws = _new_ws(linear_workspace_bytes(said.record), dev, stream)
     elif ws.device != dev or not ws.is_contiguous():
         raise ValueError(f"ws must be contiguous and on {dev}")
     st = lib().carnator_linear(_ptr(X), _ptr(W), _ptr(bias), _ptr(gate), _ptr(residual), said.ref, _ptr(Y), _ptr(Z), _ptr(ws), ws.numel(), on)
@@ -884,7 +900,6 @@ def linear_backward(dY, X, W, shape: LinearShape, Z=None, gate=None, dX=None, dW
                     stream=None) -> LinearGrads:
     """carnator_linear_backward.  dX (from W) and dW (from X) are computed where given (bf16); X or W that is not read may be None.
     ``want`` names the fp32 vector gradients: bias, gate (if there is one).  Z is the pre-activation that the forward call wrote."""
-    import torch
     dev = dY.device
     said = _linear_said(bytes(shape))
     on = _stream_on(dev, stream)
@@ -904,10 +919,10 @@ def linear_backward(dY, X, W, shape: LinearShape, Z=None, gate=None, dX=None, dW
     if dW is not None:
         _fit(dW, "dW", *said.dw, dev)
     of = said.record
-    dbias = torch.empty(of.out_features, dtype=torch.float32, device=dev) if "bias" in want else None
-    dgate = torch.empty((of.B, of.out_features), dtype=torch.float32, device=dev) if gate is not None and "gate" in want else None
+    dbias = _vector(of.out_features, dev, stream) if "bias" in want else None
+    dgate = _vector((of.B, of.out_features), dev, stream) if gate is not None and "gate" in want else None
     if ws is None:
-        ws = _new_ws(linear_backward_workspace_bytes(said.record), dev)
+        ws = _new_ws(linear_backward_workspace_bytes(said.record), dev, stream)
     elif ws.device != dev or not ws.is_contiguous():
         raise ValueError(f"ws must be contiguous and on {dev}")
     st = lib().carnator_linear_backward(_ptr(dY), _ptr(X), _ptr(W), _ptr(Z), _ptr(gate), said.ref, _ptr(dX), _ptr(dW), _ptr(dbias), _ptr(dgate),
@@ -992,7 +1007,7 @@ def rope(X, freq, shape: RopeShape, positions=None, Y=None, stream=None):
     dev = X.device
     if Y is None:
         said, size, n = _rope_packed(bytes(shape))
-        Y = _room(size, n, said.y[0], dev)
+        Y = _room(size, n, said.y[0], dev, stream)
     else:
         said = _rope_said(bytes(shape))
     on = _stream_on(dev, stream)
@@ -1087,8 +1102,8 @@ def block_norm(R, X, shape: BlockNormShape, post_weight=None, post_bias=None, ga
     dev = X.device
     if S is None or Y is None:           # the caller's record stays as it is
         said, size, n = _block_packed(bytes(shape), tuple(name for t, name in ((S, "s_stride"), (Y, "y_stride")) if t is None))
-        S = _room(size, n, said.s[0], dev) if S is None else S
-        Y = _room(size, n, said.y[0], dev) if Y is None else Y
+        S = _room(size, n, said.s[0], dev, stream) if S is None else S
+        Y = _room(size, n, said.y[0], dev, stream) if Y is None else Y
     else:
         said = _block_said(bytes(shape))
     on = _stream_on(dev, stream)
@@ -1127,12 +1142,11 @@ def block_norm_backward(dY, S, X, stats, shape: BlockNormShape, dS=None, post_we
                         want=("post_weight", "post_bias", "gate", "weight", "bias", "shift", "scale"), modulated=None, ws=None, stream=None) -> BlockNormGrads:
     """carnator_block_norm_backward.  ``want`` names the vector gradients to compute, of those that there are: post_weight, post_bias, gate, weight, bias, and shift and
     scale (if there is a scale, or ``modulated`` says that there is a shift only)."""
-    import torch
     dev = X.device
     if dR is None or dX is None:
         said, size, n = _block_packed(bytes(shape), tuple(name for t, name in ((dR, "dr_stride"), (dX, "dx_stride")) if t is None))
-        dR = _room(size, n, said.dr[0], dev) if dR is None else dR
-        dX = _room(size, n, said.dx[0], dev) if dX is None else dX
+        dR = _room(size, n, said.dr[0], dev, stream) if dR is None else dR
+        dX = _room(size, n, said.dx[0], dev, stream) if dX is None else dX
     else:
         said = _block_said(bytes(shape))
     on = _stream_on(dev, stream)
@@ -1148,7 +1162,8 @@ def block_norm_backward(dY, S, X, stats, shape: BlockNormShape, dS=None, post_we
     B, C = said.record.B, said.record.C
 
     mod = scale is not None if modulated is None else modulated
-    new = stats.new_empty                # fp32, where the tensors are: the quickest way to a tensor, and a small call's time is the host's
+    # fp32, where the tensors are: the quickest way to a tensor, and a small call's time is the host's
+    new = stats.new_empty if stream is None else lambda *size: _vector(size, dev, stream)
     dpw = new(C) if post_weight is not None and "post_weight" in want else None
     dpb = new(C) if post_bias is not None and "post_bias" in want else None
     dg = new(B, C) if gate is not None and "gate" in want else None
@@ -1157,7 +1172,7 @@ def block_norm_backward(dY, S, X, stats, shape: BlockNormShape, dS=None, post_we
     dsh = new(B, C) if mod and "shift" in want else None
     dsc = new(B, C) if mod and "scale" in want else None
     if ws is None:
-        ws = _new_ws(block_norm_backward_workspace_bytes(said.record), dev)
+        ws = _new_ws(block_norm_backward_workspace_bytes(said.record), dev, stream)
     elif ws.device != dev or not ws.is_contiguous():
         raise ValueError(f"ws must be contiguous and on {dev}")
     st = lib().carnator_block_norm_backward(_ptr(dY), _ptr(dS), _ptr(S), _ptr(X), _ptr(stats), _ptr(post_weight), _ptr(post_bias), _ptr(gate), _ptr(weight), _ptr(bias),
@@ -1206,9 +1221,9 @@ def _quantize_said(of: bytes) -> _Said:
     return said
 
 
-def _room_as(dtype, size, stride, device):
+def _room_as(dtype, size, stride, device, stream):
     import torch
-    return torch.empty_strided(size, stride, dtype=dtype, device=device)
+    return _made(lambda: torch.empty_strided(size, stride, dtype=dtype, device=device), device, stream)
 
 
 def quantize_fp8(X, shape: QuantizeShape, Q=None, scale=None, stream=None):
@@ -1218,11 +1233,11 @@ def quantize_fp8(X, shape: QuantizeShape, Q=None, scale=None, stream=None):
     on = _stream_on(dev, stream)
     _fit(X, "X", *said.x, dev)
     if Q is None:
-        Q = _room_as(*said.q, dev)
+        Q = _room_as(*said.q, dev, stream)
     else:
         _fit(Q, "Q", *said.q, dev)
     if scale is None:
-        scale = _room_as(*said.scale, dev)
+        scale = _room_as(*said.scale, dev, stream)
     else:
         _fit(scale, "scale", *said.scale, dev)
     st = lib().carnator_quantize_fp8(_ptr(X), said.ref, _ptr(Q), _ptr(scale), on)
@@ -1296,7 +1311,7 @@ def linear_fp8(X, W, w_scale, shape: LinearFp8Shape, x_scale=None, bias=None, ga
     dev = X.device
     if Y is None:
         said, size, n = _linear_fp8_packed(bytes(shape))
-        Y = _room(size, n, said.y[0], dev)
+        Y = _room(size, n, said.y[0], dev, stream)
     else:
         said = _linear_fp8_said(bytes(shape))
     on = _stream_on(dev, stream)
@@ -1313,7 +1328,7 @@ def linear_fp8(X, W, w_scale, shape: LinearFp8Shape, x_scale=None, bias=None, ga
     if gate is not None:
         _fit(gate, "gate", *said.gate, dev)
     if ws is None:
-        ws = _new_ws(linear_fp8_workspace_bytes(said.record), dev)
+        ws = _new_ws(linear_fp8_workspace_bytes(said.record), dev, stream)
     elif ws.device != dev or not ws.is_contiguous():
         raise ValueError(f"ws must be contiguous and on {dev}")
     st = lib().carnator_linear_fp8(_ptr(X), _ptr(x_scale), _ptr(W), _ptr(w_scale), _ptr(bias), _ptr(gate), _ptr(residual), said.ref, _ptr(Y), _ptr(ws), ws.numel(), on)
