@@ -2,7 +2,7 @@
 //   z = sum over blocks j of 128 k of  sx[row, j] sw[col / 128, j] <qx_j, qw_j>  + bias,   y = residual + gate_b act(z).
 //
 // Scales that are powers of two (fp8_quantize.cuh makes no others) are applied by the tensor cores: kind::mxf8f6f4 takes an exponent per row and 32 k from tensor memory
-// (here the same for the four products of a block), so that an accumulator sums up all of k, or runs of 5120 of it for fp32 outputs.
+// (here the same for the four products of a block), so that an accumulator sums up all of k, or runs of 2560 of it for fp32 outputs.
 // Any other scales: an accumulator sums up one block (kind::f8f6f4, in which nothing is lost: 7 significant bits a product, 128 terms) and the epilogue warps take it
 // times the block's scale into 128 fp32 sums per thread, while the next block's products run into the other accumulator.  That costs the reading and scaling of every
 // block's sums, which bounds it: 9472 x 5120 x 5120 358 us against 205.
@@ -31,9 +31,6 @@ constexpr uint32_t kSfSlots = 10, kSfAt = 210 * 1024; // their ring in shared me
 constexpr uint32_t kSfColumn = 448;                  // first column of the exponents in tensor memory
 static_assert(kSfAt + kSfSlots * (kSfA + kSfB) <= kRingBytes, "shared memory of a CTA");
 enum { kXBf16 = 0, kXF32 = 1, kXE4m3 = 2 };
-// Most k that one accumulator sums up for an fp32 output: as many products of the tensor cores, which cut their sums off, as kLongRun has (measured, quantised normal
-// values: error of a sum of 2560 1.7e-7, of 5120 3.6e-7, of 10240 8.5e-7; all terms positive 7.0e-7, 2.0e-6, 5.2e-6).
-constexpr int kLongRun8 = 2 * kLongRun;
 
 struct Args8 {
     TcArgs t;
@@ -368,7 +365,10 @@ template <bool kF32, bool kRuns>
 __global__ void __launch_bounds__(kThreadsTc, 1)
 linear_fp8_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB, const __grid_constant__ CUtensorMap mapSa,
                   const __grid_constant__ CUtensorMap mapSb, const Args8 args) {
-    constexpr int kRun = (kF32 ? kLongRun8 : kLongRunBf16) / kBlock;
+    // Most k that one accumulator sums up, as in linear_tcgen05.cuh: the tensor cores cut their sums off (measured, quantised normal values: error of a sum of 2560 1.7e-7, of
+    // 5120 3.6e-7, of 10240 8.5e-7; all terms positive 7.0e-7, 2.0e-6, 5.2e-6; with scales 16-fold apart, runs of 2560 1.2e-6, of 5120 2.9e-6).  Runs of 5120 for fp32 outputs took 1849 us instead of 1893 at 75600 x 5120 x 5120 with gate and residual,
+    // 24.5 instead of 25.6 at 512 x 4096 x 5120.
+    constexpr int kRun = (kF32 ? kLongRun : kLongRunBf16) / kBlock;
     static_assert(kRun % kGroupBlocks == 0, "runs are whole groups");
     const TcArgs& a = args.t;
     extern __shared__ unsigned char lin_smem[];
@@ -851,7 +851,7 @@ inline carnator_status launch_product8(const Operand& A, const Operand& B, const
     // whether a pair's share of k is longer than one accumulator may sum up
     const int64_t share = int64_t((a.groups + a.t.splits - 1) / a.t.splits) * kGroupBlocks * kBlock;
     if (a.t.e.y_f32)
-        return share > kLongRun8 ? launch_stages8<true, true>(A, B, room, a, stream, err, errlen) : launch_stages8<true, false>(A, B, room, a, stream, err, errlen);
+        return share > kLongRun ? launch_stages8<true, true>(A, B, room, a, stream, err, errlen) : launch_stages8<true, false>(A, B, room, a, stream, err, errlen);
     return share > kLongRunBf16 ? launch_stages8<false, true>(A, B, room, a, stream, err, errlen) : launch_stages8<false, false>(A, B, room, a, stream, err, errlen);
 }
 

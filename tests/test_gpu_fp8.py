@@ -375,3 +375,18 @@ def test_offsets_that_pass_32_bits():
     ry, ey = product_ref({**t, "x": small[:, -tail:]}, cn.ACT_NONE)
     check(x[:, -tail:], ry, ey + half_step(x.dtype) * (ry.abs() + ey), "y")
     assert not x[:, :-tail].any()
+
+
+@pytest.mark.parametrize("powers,most", [(True, 32), (False, 16)])
+@pytest.mark.parametrize("N,K,M", [(4, 5120, 300), (40, 5120, 300), (500, 5120, 300), (300, 10240, 300), (4, 10240, 300), (2000, 5120, 2240), (2000, 10240, 2240)])
+def test_sums_of_blocks_and_of_runs(N, K, M, powers, most):
+    """fp32 outputs, positive terms only.  Any scales: the tensor cores sum up one block, four products of 32 k, each of which cuts off at most 2^-23 of what the block has reached, 5/8 of
+    it on average: 5 times 2^-24; the scales' product is rounded once: 1; K / 128 sums are rounded to nearest, half a step of what each has reached, half of the result on average, up or
+    down: 0.58 sqrt(K / 384) 2^-24, 3 at K = 10240, three times that allowed: 16 in all.  Powers of two: runs of 2560 at most, 80 products, each of which cuts off half a step on average;
+    a step is 2^-24 to 2^-23 of what the run has reached, 1.44 2^-24 on average, and the run has reached half of its sum on average: 80 x 0.72 / 2 = 29, and 3 for joining: 32."""
+    t = make(1, N, K, M, x="e4m3", y="f32", bias=False, gate=False, residual=False, powers=powers)
+    t["x"].copy_(t["x"].float().abs())
+    t["w"].copy_(t["w"].float().abs())
+    y = call(t, cn.ACT_NONE)
+    ry, _ = product_ref(t, cn.ACT_NONE)
+    assert (y.double() - ry).norm() <= most * U32 * ry.norm()
