@@ -282,9 +282,18 @@ carnator_status check_fp8_shape(const carnator_linear_fp8_shape* s) {
 }
 bool few_rows(const carnator_linear_fp8_shape* s) { return int64_t(s->B) * s->N <= lin8::kRowsMost8; }
 
-// Status header, then what the two kernels of more than a few rows pass on.
+// Whether batch entries follow each other evenly, so that they are one run of rows.
+bool entries_run(const carnator_linear_fp8_shape* s, const int64_t* stride) { return s->B == 1 || s->N == 1 || uint64_t(stride[0]) == uint64_t(s->N) * uint64_t(stride[1]); }
+bool one_run(const carnator_linear_fp8_shape* s, bool residual) {
+    return entries_run(s, s->x_stride) && entries_run(s, s->y_stride) && (!residual || entries_run(s, s->residual_stride)) &&
+           (s->x_dtype != CARNATOR_DTYPE_E4M3 || entries_run(s, s->x_scale_stride));
+}
+// Status header, then what the two kernels of more than a few rows pass on; by the record alone: a call without a residual may take entries as one run that are not with it, which
+// needs no more.
 lin8::Room8 fp8_room(void* ws, const carnator_linear_fp8_shape* s) {
-    return lin8::room8_of(static_cast<char*>(ws) + align256(sizeof(WsHeader)), s->B, s->N, s->out_features, s->in_features, s->x_dtype != CARNATOR_DTYPE_E4M3);
+    const bool one = one_run(s, true);
+    return lin8::room8_of(static_cast<char*>(ws) + align256(sizeof(WsHeader)), one ? 1 : s->B, one ? int64_t(s->B) * s->N : s->N, s->out_features, s->in_features,
+                          s->x_dtype != CARNATOR_DTYPE_E4M3);
 }
 size_t fp8_ws_bytes(const carnator_linear_fp8_shape* s) { return align256(sizeof(WsHeader)) + (few_rows(s) ? 0 : fp8_room(nullptr, s).bytes); }
 }  // namespace
@@ -344,8 +353,6 @@ extern "C" carnator_status carnator_linear_fp8(const void* X, const float* x_sca
         count_launch();
         return CARNATOR_OK;
     }
-    // Batch entries that follow each other evenly are one run of rows.
-    auto runs = [&](const int64_t* st) { return s->B == 1 || s->N == 1 || st[0] == int64_t(s->N) * st[1]; };
     auto run_stride = [&](const int64_t* st) { return s->N == 1 ? st[0] : st[1]; };
     const lin8::Room8 room = fp8_room(ws, s);
     lin8::Args8 a = {};
@@ -362,7 +369,7 @@ extern "C" carnator_status carnator_linear_fp8(const void* X, const float* x_sca
         p.q.qs[0] = room.q_stride * s->N; p.q.qs[1] = room.q_stride;
         A.base = room.q; A.batch_stride = p.q.qs[0]; A.row_stride = p.q.qs[1];
     }
-    if (runs(xs) && runs(ys) && (!residual || runs(rs)) && (!ready || runs(xss))) {
+    if (one_run(s, residual != nullptr)) {
         a.t.batches = 1; a.t.rows = int(rows);
         A.batches = 1; A.rows = rows;
         if (ready) { A.row_stride = run_stride(xs); xss[1] = run_stride(xss); }

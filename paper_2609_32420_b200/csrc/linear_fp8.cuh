@@ -62,16 +62,18 @@ struct PrepareArgs {
     WsHeader* hdr;
     int groups, row_tiles;               // row tiles of 128 per batch entry
     int cols, bn, tiles_n;
-    int x_ctas, w_ctas;
+    int x_ctas, w_ctas;                  // CTAs per batch entry of x; behind all of them, those of the weight's scales
 };
 template <int kType>
 __global__ void __launch_bounds__(fp8::kRowThreads, 4) prepare_fp8_kernel(const PrepareArgs a) {
-    const int b = blockIdx.y, cta = blockIdx.x, tid = threadIdx.x;
+    const int x_all = a.x_ctas * a.q.batches, tid = threadIdx.x;
+    const bool of_x = int(blockIdx.x) < x_all;
+    const int b = of_x ? int(blockIdx.x) / a.x_ctas : 0, cta = int(blockIdx.x) - (of_x ? b * a.x_ctas : x_all);
     grid_launch_dependents();
     grid_wait();
-    if (cta == 0 && b == 0 && tid == 0) a.hdr->status = 0;
+    if (blockIdx.x == 0 && tid == 0) a.hdr->status = 0;
     int note = 0;
-    if (cta < a.x_ctas) {
+    if (of_x) {
         if constexpr (kType == kXE4m3) {
             const int64_t items = int64_t(a.groups) * a.q.rows;
             for (int64_t i = int64_t(cta) * fp8::kRowThreads + tid; i < items; i += int64_t(a.x_ctas) * fp8::kRowThreads) {
@@ -97,9 +99,9 @@ __global__ void __launch_bounds__(fp8::kRowThreads, 4) prepare_fp8_kernel(const 
                 else *reinterpret_cast<uint16_t*>(to) = uint16_t(word);
             });
         }
-    } else if (b == 0) {
+    } else {
         const int64_t words = int64_t(a.tiles_n) * a.groups * 256;
-        for (int64_t i = int64_t(cta - a.x_ctas) * fp8::kRowThreads + tid; i < words; i += int64_t(a.w_ctas) * fp8::kRowThreads) {
+        for (int64_t i = int64_t(cta) * fp8::kRowThreads + tid; i < words; i += int64_t(a.w_ctas) * fp8::kRowThreads) {
             const int c = int(i & 255);
             const int64_t tg = i >> 8;
             const int n = int(tg / a.groups), g = int(tg - int64_t(n) * a.groups), col = n * a.bn + c;
@@ -114,11 +116,9 @@ __global__ void __launch_bounds__(fp8::kRowThreads, 4) prepare_fp8_kernel(const 
             *reinterpret_cast<uint32_t*>(a.sfb + tg * kSfB + (c >> 7) * 512 + (c & 31) * 16 + ((c & 127) >> 5) * 4) = word;
         }
     }
-    // x that is quantised here has powers of two; a weight's scales are looked at once
-    const int first = kType == kXE4m3 ? 0 : a.x_ctas;
-    if (cta < first || (cta >= a.x_ctas && b > 0)) return;
+    if (of_x && kType != kXE4m3) return; // x that is quantised here has powers of two
     note = __syncthreads_or(note);
-    if (tid == 0) a.notes[cta >= a.x_ctas ? cta - a.x_ctas : a.w_ctas + b * a.x_ctas + cta] = note;
+    if (tid == 0) a.notes[of_x ? a.w_ctas + int(blockIdx.x) : cta] = note;
 }
 
 // ---- the product ------------------------------------------------------------------------------------------
@@ -759,17 +759,15 @@ inline Plan plan_of8(int64_t m_tiles, int64_t cols, int64_t blocks) {
     return best;
 }
 
-// What a call needs besides its arguments: notes, exponents, and x in 8 bits where the call makes it.
-constexpr int kMostWCtas = 512;
+// What a call needs besides its arguments: notes, exponents, and x in 8 bits where the call makes it.  `batches` entries of `rows`, or one of all rows; however wide the tiles are.
+constexpr int kMostWCtas = 512, kMostXCtas = 148 * 8;      // that look at scales they were given (kMostXCtas, or one for each entry)
 struct Room8 { int* notes; uint8_t* sfa; uint8_t* sfb; uint8_t* q; int64_t q_stride; size_t bytes; };
 inline Room8 room8_of(char* p, int64_t batches, int64_t rows, int64_t cols, int64_t k, bool quantises) {
     Room8 r = {};
     size_t off = 0;
     const int64_t blocks = (k + kBlock - 1) / kBlock, groups = (blocks + kGroupBlocks - 1) / kGroupBlocks;
-    // whichever way the rows are taken, one run or entry by entry, and however wide the tiles are
-    const int64_t tiles = std::max(batches * ((rows + kTileM - 1) / kTileM), (batches * rows + kTileM - 1) / kTileM) * 2;
-    const auto ctas = [&](int64_t n) { return std::min<int64_t>(148 * 8, (n * blocks + 31) / 32) + kMostWCtas; };
-    r.notes = reinterpret_cast<int*>(p + off);       off += align256(size_t(std::max(batches * ctas(rows), ctas(batches * rows))) * 4);
+    const int64_t tiles = batches * ((rows + kTileM - 1) / kTileM) * 2;
+    r.notes = reinterpret_cast<int*>(p + off);       off += align256(size_t(kMostWCtas + std::max<int64_t>(kMostXCtas, batches)) * 4);
     r.sfa = reinterpret_cast<uint8_t*>(p + off);     off += align256(size_t(tiles * groups) * kSfA);
     r.sfb = reinterpret_cast<uint8_t*>(p + off);     off += align256(size_t((cols + kLeastColumns - 1) / kLeastColumns * groups) * kSfB);
     if (quantises) {
@@ -839,9 +837,10 @@ inline carnator_status launch_product8(const Operand& A, const Operand& B, const
     p.sfa = room.sfa; p.sfb = room.sfb; p.notes = room.notes; p.hdr = a.t.hdr;
     p.groups = a.groups; p.row_tiles = a.t.tiles_m * 2;
     p.cols = a.t.cols; p.bn = a.t.bn; p.tiles_n = a.t.tiles_n;
-    p.x_ctas = type == kXE4m3 ? int(std::min<int64_t>(std::max(148 * 8 / a.t.batches, 1), (int64_t(a.groups) * a.t.rows + fp8::kRowThreads - 1) / fp8::kRowThreads)) : fp8::row_ctas(p.q, type == kXF32);
+    p.x_ctas = type == kXE4m3 ? int(std::min<int64_t>(std::max(kMostXCtas / a.t.batches, 1), (int64_t(a.groups) * a.t.rows + fp8::kRowThreads - 1) / fp8::kRowThreads))
+                              : std::min(fp8::row_ctas(p.q, type == kXF32), std::max((1 << 30) / a.t.batches, 1));
     p.w_ctas = int(std::min<int64_t>(kMostWCtas, int64_t(a.t.tiles_n) * a.groups));
-    const dim3 grid(unsigned(p.x_ctas + p.w_ctas), unsigned(a.t.batches));
+    const dim3 grid(unsigned(p.x_ctas * a.t.batches + p.w_ctas));
     const cudaError_t e = type == kXBf16 ? launch_dependent(prepare_fp8_kernel<kXBf16>, grid, dim3(fp8::kRowThreads), 0, stream, p)
                         : type == kXF32  ? launch_dependent(prepare_fp8_kernel<kXF32>, grid, dim3(fp8::kRowThreads), 0, stream, p)
                                          : launch_dependent(prepare_fp8_kernel<kXE4m3>, grid, dim3(fp8::kRowThreads), 0, stream, p);

@@ -390,3 +390,30 @@ def test_sums_of_blocks_and_of_runs(N, K, M, powers, most):
     y = call(t, cn.ACT_NONE)
     ry, _ = product_ref(t, cn.ACT_NONE)
     assert (y.double() - ry).norm() <= most * U32 * ry.norm()
+
+
+@pytest.mark.parametrize("x", ["bf16", "e4m3"])
+def test_a_record_with_a_residual_used_without(x):
+    """A padded residual keeps the record's entries apart; the call without it takes them as one run, in the workspace that the record asks for."""
+    t = make(5, 60, 700, 264, x=x, extra=0, powers=True)
+    if x == "e4m3":
+        t["x_scale"] = t["x_scale"].contiguous()
+    apart = padded((5, 60, 264), torch.bfloat16, torch.Generator(device="cuda").manual_seed(1), extra=3)
+    _, y = canvas((5, 60, 264), torch.bfloat16)
+    s = cn.make_linear_fp8_shape(t["x"], t["w"], t["w_scale"], y, x_scale=t["x_scale"], residual=apart, bias=t["bias"], gate=t["gate"])
+    for residual in (apart, None):
+        need = cn.linear_fp8_workspace_bytes(s)
+        ws = torch.full((need + 256,), 255, dtype=torch.uint8, device="cuda")
+        cn.linear_fp8(t["x"], t["w"], t["w_scale"], s, x_scale=t["x_scale"], bias=t["bias"], gate=t["gate"], residual=residual, Y=y, ws=ws[:need])
+        assert cn.query_status(ws) == cn.OK and (ws[need:] == 255).all()
+        ry, ey = product_ref({**t, "residual": residual}, cn.ACT_NONE)
+        check(y, ry, ey + half_step(y.dtype) * (ry.abs() + ey), "y")
+
+
+@pytest.mark.parametrize("x", ["bf16", "f32"])
+def test_many_padded_entries_quantised_by_the_call(x):
+    """CTAs of every entry's rows, and behind them those of the weight's scales."""
+    for w_scale in (1.0, 1.5):
+        t = make(1300, 17, 200, 72, x=x, powers=True)
+        t["w_scale"] *= w_scale
+        check_call(t, cn.ACT_NONE)

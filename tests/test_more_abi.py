@@ -261,3 +261,18 @@ def test_rope_refuses_a_forgotten_positions_argument():
                 cn.rope(x, freq, cn.make_rope_shape(x, x, 8, positions=pos), Y=Y)
             with pytest.raises(ValueError, match="positions"):
                 cn.rope(x, freq, cn.make_rope_shape(x, x, 8), positions=pos, Y=Y)
+
+
+@pytest.mark.parametrize("x", ["bf16", "e4m3"])
+def test_fp8_workspace_is_no_larger_than_what_a_call_passes_on(x):
+    """A word of exponents per row and 512 k (in tiles of 256 rows), one per column (tiles of 64 in 1 KB), a note per CTA, x in 8 bits where the call makes it; entries that follow each
+    other evenly are one run of rows, padded ones fill tiles of their own."""
+    for B, N, K, M, pad in ((65535, 1, 1536, 64, 0), (4096, 1, 5120, 512, 0), (64, 17, 5120, 5120, 0), (64, 17, 5120, 5120, 1), (3, 77, 4096, 1536, 0), (1, 75600, 5120, 5120, 0)):
+        X = torch.empty((B, N + pad, K), dtype=torch.float8_e4m3fn if x == "e4m3" else torch.bfloat16, device="meta")[:, :N]
+        Y, W = torch.empty((B, N + pad, M), dtype=torch.bfloat16, device="meta")[:, :N], torch.empty((M, K), dtype=torch.float8_e4m3fn, device="meta")
+        ks = -(-K // 128)
+        xs = torch.empty((B, N + pad, ks), device="meta")[:, :N] if x == "e4m3" else None
+        s = cn.make_linear_fp8_shape(X, W, torch.empty((-(-M // 128), ks), device="meta"), Y, x_scale=xs)
+        words, tiles = -(-K // 512), B * -(-N // 256) if pad else -(-B * N // 256)
+        most = tiles * 256 * words * 4 + -(-M // 64) * words * 1024 + (512 + max(1184, B)) * 4 + (B * N * ks * 128 if x == "bf16" else 0) + 5 * 256
+        assert cn.linear_fp8_workspace_bytes(s) <= most, (B, N, K, M, pad)
