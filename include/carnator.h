@@ -424,7 +424,7 @@ carnator_status carnator_linear_backward(const void* dY, const void* X, const vo
  *          T = N, Hg = Wg = 1 with all pairs on axis 0.  offset is added to the position on each axis
  *   layout CARNATOR_ROPE_INTERLEAVED: pair i is channels 2i and 2i + 1;  CARNATOR_ROPE_HALF: channels i and i + pairs
  *   inverse  non-zero: th -> -th, which takes the gradient of Y to that of X
- * Angles are taken in 64 bits at any position; sine and cosine are good to about 2^-22; the turn is computed in fp32 and rounded once.
+ * Angles are taken in 64 bits and more, at any position; sine and cosine are good to 2^-23; the turn is computed in fp32 and rounded once.
  * Strides are multiples of 16 bytes, base pointers 16-byte aligned; inputs may have a stride of 0.  Limits: D <= 256, N <= 2^27, B <= 65535, H <= 65535.
  *
  * carnator_rope_frequencies (HOST, no GPU work) fills freq (HOST, room for the pairs) with theta^(-i / pairs[a]) for pair i of axis a, changed for clips or

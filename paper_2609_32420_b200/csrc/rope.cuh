@@ -4,9 +4,9 @@
 //
 // Bound by memory: every value is read and written once.  A thread has one unit of a token's channels and walks over the heads, several of them on their way
 // at a time, so that the angles, which all heads share, are computed once per token and stay in registers.  Angles are taken in 64 bits, in turns: the
-// position times f_i / 2 pi, less the nearest whole number, is at most 1/2 and loses nothing to the size of the position before it is rounded to 32 bits
-// (at position 10^6 a 32-bit product is off by up to 0.06 radians); sine and cosine of it are CUDA's.
-// 75600 x 80 heads of 128 in bf16: 476 us, 0.99 of the copy rate.
+// position times f_i / 2 pi, less the nearest whole number, is at most 1/2 and loses nothing to the size of the position (at position 10^6 a 32-bit product is off
+// by up to 0.06 radians); sine and cosine of its first 32 bits are CUDA's.
+// 75600 x 80 heads of 128 in bf16: 471 us, the copy rate.
 #pragma once
 #include "norm.cuh"
 
@@ -112,10 +112,17 @@ struct Token {
         }
     }
     __device__ __forceinline__ void turn(const Args& a, int i, float& c, float& s) const {
-        const double turns = (i < a.end0 ? at[0] : i < a.end1 ? at[1] : at[2]) * a.freq[i] * 0.15915494309189533577;
-        sincospif(2.f * float(turns - rint(turns)), &s, &c);
-        c *= a.amplitude;
-        s *= a.amplitude * a.sign;
+        // position x frequency / 2 pi with what either product's rounding leaves (1 / 2 pi in two parts), less the nearest whole number: nothing is lost to the size of the position
+        constexpr double kTurn = 0.15915494309189535, kTurnRest = -9.839338337591243e-18;
+        const double p = i < a.end0 ? at[0] : i < a.end1 ? at[1] : at[2], f = a.freq[i];
+        const double th = __dmul_rn(p, f), turns = __dmul_rn(th, kTurn);
+        const double part = turns - rint(turns) + fma(th, kTurn, -turns) + fma(th, kTurnRest, fma(p, f, -th) * kTurn);
+        // sine and cosine of 32 bits of it, and the rest by their slopes
+        const float hi = float(part), lo = float(part - hi) * 6.2831853f;
+        float sn, cs;
+        sincospif(2.f * hi, &sn, &cs);
+        c = a.amplitude * fmaf(-lo, sn, cs);
+        s = a.amplitude * a.sign * fmaf(lo, cs, sn);
     }
 };
 
@@ -232,7 +239,7 @@ __global__ void __launch_bounds__(kThreads) rope_halves_kernel(const Args a) {
 }
 
 // Halves whose channels come in whole pieces of 8, of a head of 8, 16, .. 256 channels: a lane has 8 neighbouring channels, as they lie in memory, and takes the other half of its
-// pairs from the lane that has it.  (2 x 17776 x 24 heads of 64, of which 48 channels turn: 38.6 us; 43.7 with pieces of both halves in one lane, which
+// pairs from the lane that has it.  (2 x 17776 x 24 heads of 64, of which 48 channels turn: 38.9 us; 43.7 with pieces of both halves in one lane, which
 // touch parts of sectors.)
 template <bool F32, int HEADS>
 __global__ void __launch_bounds__(kThreads) rope_halves_across_kernel(const Args a) {

@@ -1,5 +1,6 @@
 """Rotary positions against the formula in 64 bits."""
 import math
+from decimal import Decimal, getcontext
 
 import pytest
 import torch
@@ -220,3 +221,25 @@ def test_on_a_side_stream_and_replayed():
         x.copy_(torch.randn((1, 4, 64, 128), device="cuda"))
         graph.replay()
         assert torch.equal(y, cn.rope(x, freq, s, Y=torch.empty_like(x)))
+
+
+TWO_PI = Decimal("6.28318530717958647692528676655900576839433879875021")
+
+
+@pytest.mark.parametrize("half", [False, True])
+def test_sine_and_cosine_at_any_position(half):
+    """fp32, against angles of 50 digits, out to positions of 2^32 with the offset.  CUDA's sine and cosine are good to a unit of 2^-24, and the rest of the angle is added with one
+    rounding, 2^-25: less than 2^-23."""
+    getcontext().prec = 50
+    freq = torch.cat((cn.rope_frequencies(6)[0], torch.tensor([0.7312345678901234, 3.0], dtype=torch.float64)))
+    pos = [0, 1, -1, 7, 100, 4097, 75599, 10 ** 6 + 3, -(10 ** 7) - 1, (1 << 27) + 1, (1 << 30) + 12345, -(1 << 30) - 999, (1 << 31) - 1, -(1 << 31)]
+    x = torch.zeros((1, 1, len(pos), 16), device="cuda")
+    x[..., slice(0, 8) if half else slice(0, 16, 2)] = 1
+    p = torch.tensor(pos, dtype=torch.int64).int().cuda()[None, :, None]
+    for offset in (0, (1 << 31) - 1, -(1 << 31)):
+        y = cn.rope(x, freq.cuda(), cn.make_rope_shape(x, None, 8, positions=p, offset=(offset, 0, 0), layout=int(half)), positions=p)[0, 0].double().cpu()
+        for n, at in enumerate(pos):
+            for i, f in enumerate(freq.tolist()):
+                angle = float((Decimal(at) + offset) * Decimal(f) % TWO_PI)
+                u, v = (y[n, i], y[n, i + 8]) if half else (y[n, 2 * i], y[n, 2 * i + 1])
+                assert abs(u - math.cos(angle)) <= 2.0 ** -23 and abs(v - math.sin(angle)) <= 2.0 ** -23, (at, offset, f)
