@@ -30,6 +30,7 @@ namespace carnator {
 std::atomic<long long> g_launches{0};
 thread_local char g_cuda_error[256] = "";
 
+// The device must be sm_100 (the kernels are built for sm_100a only).
 carnator_status check_device() {
     static thread_local int cached_dev = -1;
     static thread_local carnator_status cached = CARNATOR_OK;
@@ -80,7 +81,6 @@ carnator_status check_params(const carnator_build_params* p) {
     return CARNATOR_OK;
 }
 
-// The device must be sm_100 (the kernels are built for sm_100a only).
 float effective_scale(const carnator_shape* s) {
     return s->softmax_scale > 0.f ? s->softmax_scale : 1.0f / sqrtf(float(s->D));
 }
