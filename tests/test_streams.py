@@ -117,3 +117,27 @@ def test_memory_that_a_call_took_stays_with_its_stream(name, external, monkeypat
     for k, (a, b) in enumerate(zip(copies, want)):
         if a.dtype != torch.uint8 or (name.startswith("build") and k == 0):        # a result, not a workspace
             assert torch.equal(a.float(), b.float())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", ["block_norm_backward", "linear_backward", "linear_fp8", "rope", "sparse_attn"])
+def test_captured_on_a_stream_that_joins_the_capture(name):
+    call = _calls()[name]
+    want = _tensors(call(None))
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        side.wait_stream(torch.cuda.current_stream())
+        out = _tensors(call(side))       # drops the workspace that it made
+        with torch.cuda.stream(side):
+            kept = [t + 0 if t.dtype != torch.uint8 else None for t in out]
+        again = _tensors(call(side))
+        torch.cuda.current_stream().wait_stream(side)
+    for _ in range(3):
+        for t in (*out, *again):
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b, c, w in zip(out, kept, again, want):
+            if w.dtype != torch.uint8:
+                assert torch.equal(a, w) and torch.equal(b, w) and torch.equal(c, w)
