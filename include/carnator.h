@@ -519,12 +519,14 @@ carnator_status carnator_block_norm_backward(const void* dY, const void* dS_opt,
  *   z = sum_j x_scale[b,n,j] w_scale[m / 128, j] sum_{k in block j} x[b,n,k] W[m,k] + bias,   y = residual + gate_b act(z)
  *   X      device, [B,N,in_features]: e4m3 with x_scale, or F32 / BF16 and x_scale NULL: the call takes it to 8 bits as carnator_quantize_fp8 does
  *   W      device, e4m3 [out_features,in_features] with row stride w_stride;  w_scale  device, fp32 [ceil(out_features / 128), ceil(in_features / 128)]
- *   x_scale, w_scale   any fp32 numbers (powers of two or not), strides of `shape`
+ *   x_scale, w_scale   any fp32 numbers (powers of two or not) whose products are numbers of fp32, too (below 2^-126 they have fewer bits); strides of `shape`
  *   bias, gate, residual, Y, ws   as in carnator_linear (ws >= carnator_linear_fp8_workspace_bytes)
  * Where every scale is a power of two (those of carnator_quantize_fp8 are), the tensor cores apply them and sum up runs of k (2560 for fp32 Y, 65536 for bf16, as in carnator_linear), which are added
  * in fp32; with any other scale in the call each block's sum is taken times its scales in fp32.  The GPU finds out which, by itself.  Bias, activation, gate and residual
  * are applied to the unrounded sum and y is rounded once.  Up to 16 rows in all run on a kernel that streams W once through mma.sync; more rows on two kernels, one that
  * prepares scales and x and the product on tcgen05 with bounded waits, whose status carnator_query_status(ws) returns.
+ * Against carnator_linear: faster for one row into a large W and from some 2000 rows on; slower for tens to hundreds of rows, and for any number above 16 with scales that are no
+ * powers of two.
  * ws holds the status header and, for more than 16 rows, what the two kernels pass on (the scales' exponents and, where the call quantises X, room for it): a workspace
  * serves one call at a time.
  * Limits: those of carnator_linear.

@@ -3,11 +3,11 @@
 //
 // Scales that are powers of two (fp8_quantize.cuh makes no others) are applied by the tensor cores: kind::mxf8f6f4 takes an exponent per row and 32 k from tensor memory
 // (here the same for the four products of a block), so that an accumulator sums up all of k, or runs of 2560 of it for fp32 outputs.
-// Any other scales: an accumulator sums up one block (kind::f8f6f4, in which nothing is lost: 7 significant bits a product, 128 terms) and the epilogue warps take it
-// times the block's scale into 128 fp32 sums per thread, while the next block's products run into the other accumulator.  That costs the reading and scaling of every
-// block's sums, which bounds it: 9472 x 5120 x 5120 358 us against 205.
-// Otherwise bound by what an SM takes in (92 bytes a nanosecond) and, in long loops, by the power limit: 75600 x 5120 x 5120 in 1500 to 1580 us, 2.5 to 2.6 PFLOP/s, onto
-// an fp32 stream with a gate 1820 to 1890.
+// Any other scales: an accumulator sums up one block (kind::f8f6f4: products of two 4-bit significands are exact, a block's sum of them is cut off like any other; measured, all of
+// k = 5120, 0.8 to 1.9 2^-24) and the epilogue warps take it times the block's scale into 128 fp32 sums per thread, while the next block's products run into the other
+// accumulator.  That costs the reading and scaling of every block's sums, which bounds it: 9472 x 5120 x 5120 358 us against 205, and slower than the product in bf16.
+// Otherwise bound by what an SM takes in (92 bytes a nanosecond) and, in long loops, by the power limit: 75600 x 5120 x 5120 in 1500 to 1770 us (1850 in a loop of a second at 1357 MHz and
+// 990 W), onto an fp32 stream with a gate 1890 to 2030 (2370 at 1305 MHz).
 // A first kernel quantises x where the call does, lays the exponents out as the tensor cores read them and notes whether all scales are powers of two; the product
 // goes by its note, so that a caller does not have to say.
 //
@@ -167,7 +167,8 @@ struct Epi {
 };
 enum { kAtOnce, kEachRun, kEachBlock };  // an accumulator holds a tile's whole sum, a run of it, or that of one block without its scales
 // Its tiles; a shared one is left in shared memory.  (Three functions, so that what one way holds in registers does not cost another: in one loop, the sums of the
-// third spilled what the first needs: 75600 x 5120 x 5120 onto an fp32 stream 2889 us, now 1830.)
+// third spilled 3 KB, what the first needs among it: 75600 x 5120 x 5120 onto an fp32 stream 2889 us, apart 1830.  What is left, where sums are held beside a tile's end: 266 bytes of
+// stores and 300 of loads in the fp32 kernels, 120 and 104 in the bf16 ones.)
 template <bool kF32, int kMode>
 __device__ __forceinline__ void epilogue_warp(const Args8& args, const Epi& c) {
     const TcArgs& a = args.t;
